@@ -45,6 +45,18 @@
  *   bitsmoe_moe_decode_topk_noalloc  the same, allocating nothing   (device)
  *   bitsmoe_moe_decode_in     y = sum_j g_j C^_{e_j}^T Phi^T x      (device)
  *
+ * An MoE layer around the experts, with the experts' weights in microscaled
+ * 4-bit floats (MX4), for serving and for training what is not quantized:
+ *   bitsmoe_route             top-k experts, weights, expert order, losses (device)
+ *   bitsmoe_route_grad        gradient of the router's logits               (device)
+ *   bitsmoe_mx4_quantize      rows to MX4, and bitsmoe_mx4_dequantize back  (device)
+ *   bitsmoe_mx4_product       y_s = W_e(s) x_s, bf16 tokens                 (device)
+ *   bitsmoe_mx4_product_q     the same with the tokens in MX4               (device)
+ *   bitsmoe_mx4_product_grad  dx_s = W_e(s)^T dy_s                          (device)
+ *   bitsmoe_combine           y_t = sum_j w_tj z_{slot(t,j)}                (device)
+ *   bitsmoe_combine_grad      its gradients                                 (device)
+ * No call of these waits for the stream or reads anything back to the host.
+ *
  * Conventions shared by every call:
  *  - Pointers named *_dev are device memory on the current HIP device;
  *    *_host are host memory.  The caller allocates and owns every input and
@@ -549,6 +561,155 @@ bitsmoe_status bitsmoe_unpack(const uint64_t* codes_dev, const uint16_t* params_
                               const uint8_t* bits_dev, const int64_t* word_offsets_dev,
                               int64_t total_words, int64_t units, int64_t d, int group,
                               float* Chat_dev, void* stream);
+
+/* Largest k of bitsmoe_route and bitsmoe_combine. */
+#define BITSMOE_ROUTE_MAX_K 64
+
+/*
+ * The router of an MoE layer.  A row t of logits counts if valid_dev is NULL
+ * or valid_dev[t] is nonzero, and a logit of it is above -inf.  For those
+ *     lse_t = log sum_e exp(l_te),  p_te = exp(l_te - lse_t),
+ * the row's k slots are its k largest logits (ties: the lowest index; -inf is
+ * never taken, such a slot has expert -1 and weight 0) with weights p_te, or
+ * p_te / (sum over the row's slots) with renorm.  Slots of rows that do not
+ * count have expert -1 and weight 0, and lse = -inf.  A row that counts and
+ * holds a NaN or +inf has experts -1 and NaN for its weights, lse and both
+ * losses.
+ *   experts_dev  [T][k] int32;  weights_dev [T][k] fp32
+ *   counts_dev   [E + 1] int32: the slots c_e of every expert, then the number
+ *                n of rows that count
+ *   offsets_dev  [E + 1] int32: exclusive sums of the counts; the slots in
+ *                expert order (each expert's in row order) are
+ *                offsets[e] .. offsets[e + 1] - 1, those without an expert
+ *                follow from offsets[E] on, T k in all
+ *   rows_dev     [T k] int32: the row of each slot in expert order
+ *   slots_dev    [T][k] int32: the place of each slot in expert order
+ *   lse_dev      [T] fp32
+ *   losses_dev   [2] fp32: balance = E / (k n^2) sum_e c_e sum_t p_te (1 where
+ *                all are used alike) and z = 1/n sum_t lse_t^2; 0 if n = 0
+ *   logits_dev   [T] rows of E entries of type lt, ld entries apart
+ * Sums are fp32 in a fixed order.  T may be 0 (counts, offsets and losses are
+ * zero).  Shape rules: 1 <= k <= min(E, BITSMOE_ROUTE_MAX_K), E <= 4096,
+ * ld >= E, T k < 2^31.  Uses the library's scratch when T > 16.
+ */
+bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt, int64_t T, int64_t E,
+                             int64_t ld, int64_t k, const uint8_t* valid_dev, int renorm,
+                             int32_t* experts_dev, float* weights_dev, int32_t* counts_dev,
+                             int32_t* offsets_dev, int32_t* rows_dev, int32_t* slots_dev,
+                             float* lse_dev, float* losses_dev, void* stream);
+
+/*
+ * Gradient of the logits from those of the weights, dweights_dev [T][k], and
+ * of the two losses, dlosses_dev [2] (either may be NULL: zero).  The choice of
+ * experts and the counts carry no gradient:
+ *     dl_te = g_b p_te (a_e - sum_f p_tf a_f) + g_z 2/n lse_t p_te + r_te,
+ * a_e = E c_e / (k n^2), with r_te = w_te (dw_te - sum_S w dw) on the row's
+ * slots S with renorm, else p_te (dw_te [e in S] - sum_S p dw).
+ *   logits .. renorm, experts, weights, counts, lse   as bitsmoe_route had and
+ *                 wrote them
+ *   dlogits_dev   [T][E] of type lt, densely packed (rows that do not count: 0)
+ * Shape rules as bitsmoe_route.
+ */
+bitsmoe_status bitsmoe_route_grad(const void* logits_dev, bitsmoe_dtype lt, int64_t T, int64_t E,
+                                  int64_t ld, int64_t k, int renorm, const int32_t* experts_dev,
+                                  const float* weights_dev, const int32_t* counts_dev,
+                                  const float* lse_dev, const float* dweights_dev,
+                                  const float* dlosses_dev, void* dlogits_dev, void* stream);
+
+/*
+ * Rows to MX4.  Each block of 32 consecutive entries of a row gets the scale
+ * 2^(s - 127), s - 127 = floor(log2 max|x|) - 2 (at least -127; 0 for a block of
+ * zeros), and each entry the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 times the
+ * scale, with its sign (ties to the even code, beyond 6 to 6).  A block with a NaN
+ * or an infinity gets s = 255 and codes 0, and stands for NaN.
+ *   X_dev       rows of cols entries of type xt, ld entries apart
+ *   codes_dev   [rows][cols/2] bytes, entry 2i in the low four bits of byte i
+ *   scales_dev  [rows][cols/32] bytes
+ * rows may be 0.  Shape rules: cols % 32 == 0, cols <= 2^30, rows * cols <=
+ * 2^40, ld >= cols, rows a multiple of 16 bytes apart.
+ */
+bitsmoe_status bitsmoe_mx4_quantize(const void* X_dev, bitsmoe_dtype xt, int64_t rows,
+                                    int64_t cols, int64_t ld, uint8_t* codes_dev,
+                                    uint8_t* scales_dev, void* stream);
+
+/* What MX4 rows stand for, exactly: Y_dev [rows][cols] of type yt. */
+bitsmoe_status bitsmoe_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev,
+                                      int64_t rows, int64_t cols, void* Y_dev, bitsmoe_dtype yt,
+                                      void* stream);
+
+/*
+ * The experts' product: for the S slots in expert order, of which expert e has
+ * offsets[e] .. offsets[e + 1] - 1,
+ *     y_s = W_e x_{rows[s]},
+ * or with glu, W_e holding N rows W^g_e and then N rows W^u_e,
+ *     y_s = silu(W^g_e x) * (W^u_e x),  silu(v) = v / (1 + exp(-v)).
+ * Slots from offsets[E] on, and those whose row is not in [0, x_rows), get 0
+ * (offsets are cut to [0, S]).  Sums are fp32; results are rounded once.
+ *   codes_dev, scales_dev   W [E][N] rows of K entries in MX4 (glu: [E][2 N])
+ *   X_dev        x_rows rows of K bf16, ldx entries apart
+ *   offsets_dev  [E + 1] int32, or NULL with E = 1: all slots are expert 0's
+ *   rows_dev     [S] int32, or NULL: slot s reads row s
+ *   Y_dev        [S] rows of N entries of type yt, ldy entries apart
+ * S may be 0.  Shape rules: K % 32 == 0, ldx >= K, ldx % 8 == 0, ldy >= N,
+ * E <= 65535, N and K <= 2^24, S < 2^31.
+ */
+bitsmoe_status bitsmoe_mx4_product(const uint8_t* codes_dev, const uint8_t* scales_dev, int64_t E,
+                                   int64_t N, int64_t K, const void* X_dev, bitsmoe_dtype xt,
+                                   int64_t x_rows, int64_t ldx, const int32_t* offsets_dev,
+                                   const int32_t* rows_dev, int64_t S, int glu, void* Y_dev,
+                                   bitsmoe_dtype yt, int64_t ldy, void* stream);
+
+/*
+ * bitsmoe_mx4_product with the tokens in MX4 as well (bitsmoe_mx4_quantize of
+ * the rows): xcodes_dev [x_rows][K/2], xscales_dev [x_rows][K/32].
+ */
+bitsmoe_status bitsmoe_mx4_product_q(const uint8_t* codes_dev, const uint8_t* scales_dev,
+                                     int64_t E, int64_t N, int64_t K, const uint8_t* xcodes_dev,
+                                     const uint8_t* xscales_dev, int64_t x_rows,
+                                     const int32_t* offsets_dev, const int32_t* rows_dev, int64_t S,
+                                     int glu, void* Y_dev, bitsmoe_dtype yt, int64_t ldy,
+                                     void* stream);
+
+/*
+ * Gradient of the tokens: dx_s = W_e^T dy_s for the same slots (those from
+ * offsets[E] on get 0).  The sum over a token's slots is bitsmoe_combine with
+ * weights NULL; the weights are held in 4 bits and have no gradient.  For a
+ * product with glu, dY is that of the 2 N values before it, and N counts them.
+ *   dY_dev  [S] rows of N bf16, lddy entries apart
+ *   dX_dev  [S] rows of K entries of type xt, ldx entries apart
+ * Shape rules as bitsmoe_mx4_product, and N % 8 == 0, lddy % 8 == 0.
+ */
+bitsmoe_status bitsmoe_mx4_product_grad(const uint8_t* codes_dev, const uint8_t* scales_dev,
+                                        int64_t E, int64_t N, int64_t K, const void* dY_dev,
+                                        bitsmoe_dtype dyt, int64_t lddy, const int32_t* offsets_dev,
+                                        int64_t S, void* dX_dev, bitsmoe_dtype xt, int64_t ldx,
+                                        void* stream);
+
+/*
+ * The experts' outputs joined: y_t = sum_j w_tj z_{slots[t][j]}, summed in slot
+ * order in fp32.  A slot outside [0, S) contributes nothing.
+ *   Z_dev        [S][d] of type zt
+ *   slots_dev    [T][k] int32 (bitsmoe_route)
+ *   weights_dev  [T][k] fp32, or NULL: all 1
+ *   Y_dev        [T][d] of type zt
+ * T and S may be 0.  Shape rules: d % 8 == 0, d <= 2^24, k <=
+ * BITSMOE_ROUTE_MAX_K, S and T < 2^31.
+ */
+bitsmoe_status bitsmoe_combine(const void* Z_dev, bitsmoe_dtype zt, int64_t S,
+                               const int32_t* slots_dev, const float* weights_dev, int64_t T,
+                               int64_t k, int64_t d, void* Y_dev, void* stream);
+
+/*
+ * Gradients of bitsmoe_combine: dz_{slots[t][j]} = w_tj dy_t and dw_tj =
+ * <dy_t, z_{slots[t][j]}> (dweights_dev [T][k] fp32, or NULL: not wanted; Z_dev is
+ * then not read).  Rows of dZ_dev [S][d] that no slot names are left as they
+ * are (bitsmoe_route names every one); a row named twice gets either value.
+ * Shape rules as bitsmoe_combine, and T < 2^24.
+ */
+bitsmoe_status bitsmoe_combine_grad(const void* Z_dev, bitsmoe_dtype zt, int64_t S,
+                                    const int32_t* slots_dev, const float* weights_dev,
+                                    const void* dY_dev, int64_t T, int64_t k, int64_t d,
+                                    void* dZ_dev, float* dweights_dev, void* stream);
 
 /* Path of a LAPACK shared library for bitsmoe_shared_basis (LP64 or ILP64
  * dsyevd; both plain and "64_"-suffixed symbol names are tried).  When never

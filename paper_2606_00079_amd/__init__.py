@@ -16,13 +16,21 @@ Steps, in order (one projection type of one MoE layer):
     b, obj = allocate(L, bits, budget)       # exact ILP (host)
     off    = pack_layout(b, d)
     codes, params = pack(C, b, off, group)
+
+An MoE layer whose experts are held in microscaled 4-bit floats (MX4):
+
+    codes, scales = mx4_quantize(W)          # once, [E][N][K/2] and [E][N][K/32]
+    r = route(logits, k)                     # experts, weights, expert order, losses
+    z = mx4_product(codes, scales, x, offsets=r.offsets, rows=r.rows)
+    y = combine(z, r.slots, r.weights)
+    (route_grad, mx4_product_grad, combine_grad: the gradients)
 """
 from __future__ import annotations
 
 import ctypes
 import glob
 import os
-from typing import Optional, Sequence, Tuple
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 import numpy as np
 
@@ -46,7 +54,10 @@ EXPORTS = [
     "bitsmoe_project_in", "bitsmoe_basis_importance", "bitsmoe_score_diag",
     "bitsmoe_gram_routed", "bitsmoe_score_routed", "bitsmoe_moe_decode",
     "bitsmoe_moe_decode_topk", "bitsmoe_shared_basis_gpu", "bitsmoe_moe_decode_in",
-    "bitsmoe_moe_decode_topk_noalloc",
+    "bitsmoe_moe_decode_topk_noalloc", "bitsmoe_route", "bitsmoe_route_grad",
+    "bitsmoe_mx4_quantize", "bitsmoe_mx4_dequantize", "bitsmoe_mx4_product",
+    "bitsmoe_mx4_product_q", "bitsmoe_mx4_product_grad", "bitsmoe_combine",
+    "bitsmoe_combine_grad",
 ]
 # Candidate widths of the surrogate table, in column order.
 SURROGATE_WIDTHS = (0, 1, 2, 3, 4, 6, 8, 16)
@@ -110,6 +121,18 @@ def lib() -> ctypes.CDLL:
     L.bitsmoe_moe_decode_topk.argtypes = [vp, vp, vp, vp, i64, i64, i64, i64, i32, vp, i64, vp,
                                           i64, i64, vp, vp, vp, vp]
     L.bitsmoe_moe_decode_topk_noalloc.argtypes = L.bitsmoe_moe_decode_topk.argtypes
+    L.bitsmoe_route.argtypes = [vp, i32, i64, i64, i64, i64, vp, i32] + [vp] * 9
+    L.bitsmoe_route_grad.argtypes = [vp, i32, i64, i64, i64, i64, i32] + [vp] * 8
+    L.bitsmoe_mx4_quantize.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp]
+    L.bitsmoe_mx4_dequantize.argtypes = [vp, vp, i64, i64, vp, i32, vp]
+    L.bitsmoe_mx4_product.argtypes = [vp, vp, i64, i64, i64, vp, i32, i64, i64, vp, vp, i64, i32,
+                                      vp, i32, i64, vp]
+    L.bitsmoe_mx4_product_q.argtypes = [vp, vp, i64, i64, i64, vp, vp, i64, vp, vp, i64, i32, vp,
+                                        i32, i64, vp]
+    L.bitsmoe_mx4_product_grad.argtypes = [vp, vp, i64, i64, i64, vp, i32, i64, vp, i64, vp, i32,
+                                           i64, vp]
+    L.bitsmoe_combine.argtypes = [vp, i32, i64, vp, vp, i64, i64, i64, vp, vp]
+    L.bitsmoe_combine_grad.argtypes = [vp, i32, i64, vp, vp, vp, i64, i64, i64, vp, vp, vp]
     L.bitsmoe_set_lapack.argtypes = [ctypes.c_char_p]
     L.bitsmoe_timing.argtypes = [i32]
     L.bitsmoe_timing_only.argtypes = [ctypes.c_char_p]
@@ -515,6 +538,235 @@ def unpack(codes, params, bits_dev, offsets_dev, units: int, d: int, group: int,
                                 _dev(offsets_dev, "offsets"), int(total_words), units, d, group,
                                 _dev(out, "Chat"), _stream()), "unpack")
     return out
+
+
+# ---------------------------------------------------------------------------
+# an MoE layer with experts in MX4
+# ---------------------------------------------------------------------------
+def _rows(t, name: str):
+    """(pointer, row stride) of a matrix whose rows may be apart."""
+    if t.is_contiguous():
+        return _dev(t, name), t.shape[-1]
+    torch = _torch()
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must have contiguous rows")
+    return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def _opt(t, name: str, dtype, shape=None):
+    """Pointer of an optional tensor of a given type and shape."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {str(dtype).replace('torch.', '')}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}")
+    return _dev(t, name)
+
+
+def _out(out, shape, dtype, device, name: str):
+    torch = _torch()
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if out.dtype != dtype or tuple(out.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)} of {str(dtype).replace('torch.', '')}")
+    return out
+
+
+class Routing(NamedTuple):
+    """What ``route`` gives for T rows and E experts."""
+    experts: object  # int32 [T][k], -1 for a slot without an expert
+    weights: object  # fp32 [T][k]
+    counts: object   # int32 [E+1]: slots of every expert, then the rows that count
+    offsets: object  # int32 [E+1]: where each expert's slots begin in expert order
+    rows: object     # int32 [T*k]: the row of each slot in expert order
+    slots: object    # int32 [T][k]: the place of each slot in expert order
+    lse: object      # fp32 [T]
+    losses: object   # fp32 [2]: balance, z
+
+
+def route(logits, k: int, valid=None, renorm: bool = True) -> Routing:
+    """Top-k experts of every row of logits [T][E] (bf16 or fp32), their softmax
+    weights, the slots in expert order, and the balance and z losses; rows with
+    valid[t] = 0 (bool or uint8) do not count."""
+    torch = _torch()
+    if logits.dim() != 2:
+        raise ValueError("logits must be [T][E]")
+    T, E = logits.shape
+    k = int(k)
+    if valid is not None and valid.dtype == torch.bool:
+        valid = valid.view(torch.uint8)
+    vp = _opt(valid, "valid", torch.uint8, (T,))
+    lp, ld = _rows(logits, "logits")
+    i32, f32, dev = torch.int32, torch.float32, logits.device
+    n = max(T * k, 0)
+    r = Routing(torch.empty((T, max(k, 0)), dtype=i32, device=dev),
+                torch.empty((T, max(k, 0)), dtype=f32, device=dev),
+                torch.empty((E + 1,), dtype=i32, device=dev), torch.empty((E + 1,), dtype=i32, device=dev),
+                torch.empty((n,), dtype=i32, device=dev), torch.empty((T, max(k, 0)), dtype=i32, device=dev),
+                torch.empty((T,), dtype=f32, device=dev), torch.empty((2,), dtype=f32, device=dev))
+    _check(lib().bitsmoe_route(lp, _dtype_code(logits, "logits"), T, E, ld, k, vp, int(renorm),
+                               *(ctypes.c_void_p(t.data_ptr()) for t in r), _stream()), "route")
+    return r
+
+
+def route_grad(logits, routing: Routing, dweights=None, dlosses=None, renorm: bool = True, out=None):
+    """Gradient of the logits from those of the weights [T][k] and of the losses
+    [2] (fp32, on the device) -> [T][E] of the logits' type."""
+    torch = _torch()
+    T, E = logits.shape
+    k = routing.experts.shape[1]
+    out = _out(out, (T, E), logits.dtype, logits.device, "out")
+    lp, ld = _rows(logits, "logits")
+    _check(lib().bitsmoe_route_grad(
+        lp, _dtype_code(logits, "logits"), T, E, ld, k, int(renorm),
+        _opt(routing.experts, "experts", torch.int32, (T, k)),
+        _opt(routing.weights, "weights", torch.float32, (T, k)),
+        _opt(routing.counts, "counts", torch.int32, (E + 1,)),
+        _opt(routing.lse, "lse", torch.float32, (T,)),
+        _opt(dweights, "dweights", torch.float32, (T, k)),
+        _opt(dlosses, "dlosses", torch.float32, (2,)), _dev(out, "out"), _stream()), "route_grad")
+    return out
+
+
+def mx4_quantize(X):
+    """Rows of X [..][cols] (bf16 or fp32) to MX4: codes uint8 [..][cols/2] and
+    scales uint8 [..][cols/32]."""
+    torch = _torch()
+    cols = X.shape[-1]
+    if cols % 32 != 0:
+        raise ValueError("cols must be a multiple of 32")
+    xp, ld = _rows(X, "X")
+    rows = X.numel() // cols if cols else 0
+    codes = torch.empty((*X.shape[:-1], cols // 2), dtype=torch.uint8, device=X.device)
+    scales = torch.empty((*X.shape[:-1], cols // 32), dtype=torch.uint8, device=X.device)
+    _check(lib().bitsmoe_mx4_quantize(xp, _dtype_code(X, "X"), rows, cols, ld, _dev(codes, "codes"),
+                                      _dev(scales, "scales"), _stream()), "mx4_quantize")
+    return codes, scales
+
+
+def _mx4(codes, scales, name: str, dims: int):
+    torch = _torch()
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
+        raise TypeError(f"{name} codes and scales must be uint8")
+    if (dims and codes.dim() != dims) or codes.shape[:-1] != scales.shape[:-1] or \
+            codes.shape[-1] != 16 * scales.shape[-1]:
+        raise ValueError(f"{name} codes must be [..][K/2] and scales [..][K/32]")
+    return _dev(codes, name + " codes"), _dev(scales, name + " scales")
+
+
+def mx4_dequantize(codes, scales, dtype=None, out=None):
+    """What MX4 rows stand for -> [..][cols] (bf16 unless ``dtype`` says fp32)."""
+    torch = _torch()
+    cp, sp = _mx4(codes, scales, "X", 0)
+    cols = 2 * codes.shape[-1]
+    dtype = dtype or torch.bfloat16
+    out = _out(out, (*codes.shape[:-1], cols), dtype, codes.device, "out")
+    rows = codes.numel() // (cols // 2) if cols else 0
+    _check(lib().bitsmoe_mx4_dequantize(cp, sp, rows, cols, _dev(out, "out"), _dtype_code(out, "out"),
+                                        _stream()), "mx4_dequantize")
+    return out
+
+
+def _experts(codes, scales, offsets, S: int, glu: bool = False):
+    torch = _torch()
+    cp, sp = _mx4(codes, scales, "W", 3)
+    E, N, K = codes.shape[0], codes.shape[1], 2 * codes.shape[2]
+    if glu:
+        if N % 2:
+            raise ValueError("glu takes as many gate as up rows")
+        N //= 2
+    return cp, sp, E, N, K, _opt(offsets, "offsets", torch.int32, (E + 1,))
+
+
+def mx4_product(codes, scales, X, offsets=None, rows=None, glu: bool = False, dtype=None, out=None):
+    """y_s = W_e x_{rows[s]} for the slots in expert order (offsets int32 [E+1],
+    rows int32 [S]; without rows slot s reads row s): W in MX4 as codes
+    [E][N][K/2] and scales [E][N][K/32], X bf16 [rows][K] -> [S][N], bf16 unless
+    ``dtype`` says fp32.  glu: W holds gate rows, then up rows, and
+    y = silu(gate) * up -> [S][N/2]."""
+    torch = _torch()
+    if X.dim() != 2:
+        raise ValueError("X must be [rows][K]")
+    S = X.shape[0] if rows is None else rows.shape[0]
+    cp, sp, E, N, K, op = _experts(codes, scales, offsets, S, glu)
+    if X.shape[1] != K:
+        raise ValueError("X and W disagree on K")
+    xp, ldx = _rows(X, "X")
+    out = _out(out, (S, N), dtype or torch.bfloat16, X.device, "out")
+    _check(lib().bitsmoe_mx4_product(cp, sp, E, N, K, xp, _dtype_code(X, "X"), X.shape[0], ldx, op,
+                                     _opt(rows, "rows", torch.int32, (S,)), S, int(glu),
+                                     _dev(out, "out"), _dtype_code(out, "out"), N, _stream()),
+           "mx4_product")
+    return out
+
+
+def mx4_product_q(codes, scales, xcodes, xscales, offsets=None, rows=None, glu: bool = False,
+                  dtype=None, out=None):
+    """mx4_product with the tokens in MX4 too (``mx4_quantize`` of X)."""
+    torch = _torch()
+    xcp, xsp = _mx4(xcodes, xscales, "X", 2)
+    S = xcodes.shape[0] if rows is None else rows.shape[0]
+    cp, sp, E, N, K, op = _experts(codes, scales, offsets, S, glu)
+    if 2 * xcodes.shape[1] != K:
+        raise ValueError("X and W disagree on K")
+    out = _out(out, (S, N), dtype or torch.bfloat16, codes.device, "out")
+    _check(lib().bitsmoe_mx4_product_q(cp, sp, E, N, K, xcp, xsp, xcodes.shape[0], op,
+                                       _opt(rows, "rows", torch.int32, (S,)), S, int(glu),
+                                       _dev(out, "out"), _dtype_code(out, "out"), N, _stream()),
+           "mx4_product_q")
+    return out
+
+
+def mx4_product_grad(codes, scales, dY, offsets=None, dtype=None, out=None):
+    """dx_s = W_e^T dy_s for the slots in expert order: dY bf16 [S][N] ->
+    [S][K], bf16 unless ``dtype`` says fp32."""
+    torch = _torch()
+    if dY.dim() != 2:
+        raise ValueError("dY must be [S][N]")
+    S = dY.shape[0]
+    cp, sp, E, N, K, op = _experts(codes, scales, offsets, S)
+    if dY.shape[1] != N:
+        raise ValueError("dY and W disagree on N")
+    yp, ldy = _rows(dY, "dY")
+    out = _out(out, (S, K), dtype or torch.bfloat16, dY.device, "out")
+    _check(lib().bitsmoe_mx4_product_grad(cp, sp, E, N, K, yp, _dtype_code(dY, "dY"), ldy, op, S,
+                                          _dev(out, "out"), _dtype_code(out, "out"), K, _stream()),
+           "mx4_product_grad")
+    return out
+
+
+def combine(Z, slots, weights=None, out=None):
+    """y_t = sum_j weights[t][j] Z[slots[t][j]] (weights None: all 1) for Z [S][d]
+    (bf16 or fp32), slots int32 [T][k], weights fp32 [T][k] -> [T][d] of Z's type."""
+    torch = _torch()
+    if Z.dim() != 2 or slots.dim() != 2:
+        raise ValueError("Z must be [S][d] and slots [T][k]")
+    (S, d), (T, k) = Z.shape, slots.shape
+    out = _out(out, (T, d), Z.dtype, Z.device, "out")
+    _check(lib().bitsmoe_combine(_dev(Z, "Z"), _dtype_code(Z, "Z"), S,
+                                 _opt(slots, "slots", torch.int32), _opt(weights, "weights", torch.float32, (T, k)),
+                                 T, k, d, _dev(out, "out"), _stream()), "combine")
+    return out
+
+
+def combine_grad(Z, slots, weights, dY):
+    """Gradients of ``combine``: (dZ [S][d], dweights fp32 [T][k]).  Every row of Z
+    is taken to be named by one slot, as ``route`` does."""
+    torch = _torch()
+    if Z.dim() != 2 or slots.dim() != 2:
+        raise ValueError("Z must be [S][d] and slots [T][k]")
+    (S, d), (T, k) = Z.shape, slots.shape
+    dZ = torch.empty_like(Z)
+    dw = torch.empty((T, k), dtype=torch.float32, device=Z.device)
+    _check(lib().bitsmoe_combine_grad(_dev(Z, "Z"), _dtype_code(Z, "Z"), S,
+                                      _opt(slots, "slots", torch.int32),
+                                      _opt(weights, "weights", torch.float32, (T, k)),
+                                      _opt(dY, "dY", Z.dtype, (T, d)), T, k, d, _dev(dZ, "dZ"),
+                                      _dev(dw, "dweights"), _stream()), "combine_grad")
+    return dZ, dw
 
 
 def timing(enable: bool, only: Optional[str] = None) -> None:

@@ -1,0 +1,134 @@
+// Rows to MX4 and back.
+//
+// The scale of a block is the power of two that puts its largest magnitude
+// into [4, 8), 2^(floor(log2 max) - 2): read off the exponent bits, so it is
+// exact.  Entries round to the nearest value of the format (ties to the even
+// code, beyond 6 to 6), which one conversion instruction does for two of
+// them.  A block of zeros has scale byte 0.  Both directions are bound by
+// memory: eight entries a lane, four lanes a block.
+#include <cstdint>
+#include <string>
+
+#include "internal.hpp"
+#include "mx4.hpp"
+
+namespace bitsmoe {
+namespace {
+
+constexpr int kThreads = 256;
+
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void mx4_quantize_kernel(const void* x, int64_t rows, int pieces, int64_t ld,
+                                                                uint32_t* codes, uint8_t* scales) {
+  const int64_t n = rows * pieces;  // pieces of eight entries
+  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < n; i += int64_t(gridDim.x) * kThreads) {
+    const int64_t r = i / pieces;
+    const int64_t at = r * ld + (i - r * pieces) * 8;
+    float v[8];
+    if constexpr (BF16) {
+      const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(x) + at);
+      const uint32_t d[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        v[2 * q] = __uint_as_float(d[q] << 16);
+        v[2 * q + 1] = __uint_as_float(d[q] & 0xFFFF0000u);
+      }
+    } else {
+      const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(x) + at);
+      const f32x4 a = p[0], b = p[1];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        v[q] = a[q];
+        v[4 + q] = b[q];
+      }
+    }
+    // largest magnitude as bits (a NaN's and an infinity's lie above every number's)
+    uint32_t top = 0;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) top = max(top, __float_as_uint(v[q]) & 0x7FFFFFFFu);
+    top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 1, 64)));
+    top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 2, 64)));
+    const bool lost = top >= 0x7F800000u;
+    // exponent byte of 2^(floor(log2 max) - 2), not below 0 (subnormals and numbers near them)
+    const int e = static_cast<int>(top >> 23) - 2;
+    const uint32_t s = lost ? 255u : e > 0 ? static_cast<uint32_t>(e) : 0u;
+    const float scale = mx4_scale(s);
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], scale, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], scale, 3);
+    codes[i] = lost ? 0u : w;
+    if ((threadIdx.x & 3) == 0) scales[i / 4] = static_cast<uint8_t>(s);
+  }
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void mx4_dequantize_kernel(const uint32_t* codes, const uint8_t* scales,
+                                                                  int64_t n, void* y) {
+  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < n; i += int64_t(gridDim.x) * kThreads) {
+    const uint32_t w = codes[i];
+    const float scale = mx4_scale(scales[i / 4]);
+    if constexpr (BF16) {
+      static_cast<bf16x8*>(y)[i] = mx4_bf16(w, scale);
+    } else {
+      const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0);
+      const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
+      const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2);
+      const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
+      static_cast<f32x4*>(y)[2 * i] = f32x4{a[0], a[1], b[0], b[1]};
+      static_cast<f32x4*>(y)[2 * i + 1] = f32x4{c[0], c[1], d[0], d[1]};
+    }
+  }
+}
+
+unsigned grid_for(int64_t n) {
+  const int64_t b = (n + kThreads - 1) / kThreads;
+  return static_cast<unsigned>(b < (1 << 20) ? b : (1 << 20));
+}
+
+bitsmoe_status check(const char* who, bitsmoe_dtype t, int64_t rows, int64_t cols) {
+  if (rows < 0 || cols <= 0) return fail(BITSMOE_ERR_ARG, std::string(who) + ": non-positive size");
+  if (t != BITSMOE_F32 && t != BITSMOE_BF16)
+    return fail(BITSMOE_ERR_DTYPE, std::string(who) + ": rows must be fp32 or bf16");
+  if (cols % kMx4Block != 0 || cols > (int64_t(1) << 30) || rows > (int64_t(1) << 40) / cols)
+    return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": needs cols % 32 == 0, cols <= 2^30, rows * cols <= 2^40");
+  return BITSMOE_OK;
+}
+
+}  // namespace
+}  // namespace bitsmoe
+
+using namespace bitsmoe;
+
+extern "C" bitsmoe_status bitsmoe_mx4_quantize(const void* X_dev, bitsmoe_dtype xt, int64_t rows, int64_t cols,
+                                               int64_t ld, uint8_t* codes_dev, uint8_t* scales_dev, void* stream) {
+  if (bitsmoe_status st = check("mx4_quantize", xt, rows, cols)) return st;
+  if (ld < cols || ld * (xt == BITSMOE_BF16 ? 2 : 4) % 16 != 0 || ld > (int64_t(1) << 40))
+    return fail(BITSMOE_ERR_SHAPE, "mx4_quantize: needs ld >= cols and rows 16 bytes apart or a multiple of that");
+  if (rows == 0) return ok();
+  if (!X_dev || !codes_dev || !scales_dev) return fail(BITSMOE_ERR_ARG, "mx4_quantize: null pointer");
+  if (!aligned16({X_dev, codes_dev, scales_dev}))
+    return fail(BITSMOE_ERR_ARG, "mx4_quantize: device pointers must be 16-byte aligned");
+  const int64_t n = rows * (cols / 8);
+  auto* fn = xt == BITSMOE_BF16 ? mx4_quantize_kernel<true> : mx4_quantize_kernel<false>;
+  fn<<<grid_for(n), kThreads, 0, static_cast<hipStream_t>(stream)>>>(
+      X_dev, rows, static_cast<int>(cols / 8), ld, reinterpret_cast<uint32_t*>(codes_dev), scales_dev);
+  BITSMOE_LAUNCH_CHECK("mx4_quantize_kernel");
+  return ok();
+}
+
+extern "C" bitsmoe_status bitsmoe_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev, int64_t rows,
+                                                 int64_t cols, void* Y_dev, bitsmoe_dtype yt, void* stream) {
+  if (bitsmoe_status st = check("mx4_dequantize", yt, rows, cols)) return st;
+  if (rows == 0) return ok();
+  if (!codes_dev || !scales_dev || !Y_dev) return fail(BITSMOE_ERR_ARG, "mx4_dequantize: null pointer");
+  if (!aligned16({codes_dev, scales_dev, Y_dev}))
+    return fail(BITSMOE_ERR_ARG, "mx4_dequantize: device pointers must be 16-byte aligned");
+  const int64_t n = rows * (cols / 8);
+  auto* fn = yt == BITSMOE_BF16 ? mx4_dequantize_kernel<true> : mx4_dequantize_kernel<false>;
+  fn<<<grid_for(n), kThreads, 0, static_cast<hipStream_t>(stream)>>>(reinterpret_cast<const uint32_t*>(codes_dev),
+                                                                     scales_dev, n, Y_dev);
+  BITSMOE_LAUNCH_CHECK("mx4_dequantize_kernel");
+  return ok();
+}

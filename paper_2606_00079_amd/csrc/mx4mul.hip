@@ -1,0 +1,314 @@
+// Products with expert weights held in MX4.
+//
+//     y_s = W_e(s) x_row(s)            (mx4_product: bf16 tokens; _q: MX4 tokens)
+//     y_s = silu(g) u, [g; u] = W_e(s) x_row(s)        (the same with glu)
+//     dx_s = W_e(s)^T dy_s             (mx4_product_grad)
+//
+// for S slots in expert order, expert e's being offsets[e] .. offsets[e+1].
+#include <cstdint>
+#include <string>
+
+#include "internal.hpp"
+#include "mx4.hpp"
+
+namespace bitsmoe {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct MulArgs {
+  const uint8_t* codes;   // [E][N or 2N][K/2]
+  const uint8_t* scales;  // [E][..][K/32]
+  int E;
+  int64_t N, K;
+  const uint16_t* x;       // bf16 rows (product: tokens; grad: dy)
+  const uint8_t* xcodes;   // or MX4 rows
+  const uint8_t* xscales;
+  int64_t x_rows, ldx;
+  const int32_t* offsets;
+  const int32_t* rows;
+  int64_t S;
+  void* y;
+  int64_t ldy;
+  int yf32;
+};
+
+// The slots of one workgroup: `lo` .. `hi` of expert e, at most `tile` of
+// them.  Experts' runs are cut into tiles from their first slot on, tile g of
+// all is looked for; e = E holds the slots of no expert, whose results are
+// zero.  Every wave looks by itself, 64 experts at a time.
+struct Tile {
+  int e, lo, hi;
+};
+__device__ __forceinline__ bool find_tile(const int32_t* offsets, int E, int64_t S, int64_t g, int tile, Tile* out) {
+  const int s = static_cast<int>(S), lane = threadIdx.x & 63;
+  int64_t before = 0;
+  for (int base = 0; base <= E; base += 64) {
+    const int e = base + lane;
+    int lo = 0, hi = 0;
+    if (e <= E) {
+      lo = offsets ? min(max(offsets[e], 0), s) : (e == 0 ? 0 : s);
+      hi = e < E && offsets ? min(max(offsets[e + 1], lo), s) : s;
+    }
+    const int tiles = (hi - lo + tile - 1) / tile;
+    int inc = tiles;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(inc, o, 64);
+      if (lane >= o) inc += u;
+    }
+    const uint64_t hit = __ballot(before + inc > g);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      const int first = static_cast<int>(g - before) - (__shfl(inc, l, 64) - __shfl(tiles, l, 64));
+      out->e = base + l;
+      out->lo = __shfl(lo, l, 64) + first * tile;
+      out->hi = min(__shfl(hi, l, 64), out->lo + tile);
+      return true;
+    }
+    before += __shfl(inc, 63, 64);
+  }
+  return false;
+}
+
+__device__ __forceinline__ float silu(float g) { return g / (1.0f + expf(-g)); }
+
+// Four consecutive results n .. n + 3 of slot s.
+__device__ __forceinline__ void store4(const MulArgs& a, int64_t s, int64_t n, int64_t N, bool wide, f32x4 v) {
+  if (a.yf32) {
+    float* p = static_cast<float*>(a.y) + s * a.ldy + n;
+    if (wide && n + 4 <= N) {
+      *reinterpret_cast<f32x4*>(p) = v;
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i < N) p[i] = v[i];
+  } else {
+    uint16_t* p = static_cast<uint16_t*>(a.y) + s * a.ldy + n;
+    uint16_t h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v[i]));
+    if (wide && n + 4 <= N) {
+      *reinterpret_cast<uint2*>(p) = make_uint2(h[0] | (uint32_t(h[1]) << 16), h[2] | (uint32_t(h[3]) << 16));
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i < N) p[i] = h[i];
+  }
+}
+
+// 16 outputs x 16 slots a workgroup.  The four waves share out K in segments
+// of 128: lane l holds 32 codes of row l % 16 (block l / 16 of the segment),
+// which one load fetches with their scale, and the same entries of slot l % 16.
+template <bool MX, bool GLU>
+__global__ __launch_bounds__(kThreads) void mx4_rows_kernel(MulArgs a) {
+  constexpr int H = GLU ? 2 : 1;
+  __shared__ f32x4 part[kThreads / 64][H][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
+  const int64_t ntiles = (a.N + 15) / 16;
+  const int64_t g = blockIdx.x / ntiles, n0 = (blockIdx.x - g * ntiles) * 16;
+  Tile t;
+  if (!find_tile(a.offsets, a.E, a.S, g, 16, &t)) return;
+  f32x4 acc[H];
+#pragma unroll
+  for (int h = 0; h < H; ++h) acc[h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (t.e < a.E) {
+    const int64_t n = min(n0 + r, a.N - 1);
+    const int64_t slot = t.lo + r;
+    const int64_t row = slot < t.hi ? (a.rows ? static_cast<int64_t>(a.rows[slot]) : slot) : -1;
+    const bool have = row >= 0 && row < a.x_rows;
+    const int64_t kb = a.K / 32;
+    const int64_t wrow = static_cast<int64_t>(t.e) * (a.N * H) + n;
+    for (int64_t seg = wave; seg * 4 < kb; seg += kThreads / 64) {
+      const int64_t b = seg * 4 + q;  // this lane's block
+      uint4 xc = make_uint4(0, 0, 0, 0);
+      uint4 xv[4] = {xc, xc, xc, xc};
+      int xs = 127;
+      if (b < kb && have) {
+        if constexpr (MX) {
+          xc = *reinterpret_cast<const uint4*>(a.xcodes + (row * kb + b) * 16);
+          xs = a.xscales[row * kb + b];
+        } else {
+          const uint4* p = reinterpret_cast<const uint4*>(a.x + row * a.ldx + b * 32);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) xv[i] = p[i];
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        uint4 c = make_uint4(0, 0, 0, 0);
+        int s = 127;
+        if (b < kb) {
+          const int64_t at = (wrow + h * a.N) * kb + b;
+          c = *reinterpret_cast<const uint4*>(a.codes + at * 16);
+          s = a.scales[at];
+        }
+        if constexpr (MX) {
+          const i32x8 A = {(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0};
+          const i32x8 B = {(int)xc.x, (int)xc.y, (int)xc.z, (int)xc.w, 0, 0, 0, 0};
+          acc[h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, acc[h], 4, 4, 0, s, 0, xs);
+        } else {
+          const float scale = mx4_scale(s);
+          const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mx4_bf16(w[i], scale), __builtin_bit_cast(bf16x8, xv[i]),
+                                                             acc[h], 0, 0, 0);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < H; ++h) part[wave][h][lane] = acc[h];
+  __syncthreads();
+  if (wave != 0) return;
+#pragma unroll
+  for (int h = 0; h < H; ++h)
+#pragma unroll
+    for (int w = 1; w < kThreads / 64; ++w) acc[h] += part[w][h][lane];
+  if constexpr (GLU) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[0][i] = silu(acc[0][i]) * acc[1][i];
+  }
+  const int64_t slot = t.lo + r, n = n0 + 4 * q;  // (a lane holds four outputs of one slot)
+  const bool wide = a.ldy % 4 == 0;
+  if (slot < t.hi && n < a.N) store4(a, slot, n, a.N, wide, acc[0]);
+}
+
+// dx: 64 columns x 16 slots a workgroup, 16 columns a wave.  The weights' tile
+// (32 rows x 64 columns) is widened to bf16 and transposed in LDS.
+__global__ __launch_bounds__(kThreads) void mx4_grad_kernel(MulArgs a) {
+  constexpr int KT = 64, LD = 40;  // (LD: rows 80 bytes apart)
+  __shared__ __align__(16) uint16_t wt[KT * LD];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, q = lane >> 4;
+  const int64_t ktiles = (a.K + KT - 1) / KT;
+  const int64_t g = blockIdx.x / ktiles, k0 = (blockIdx.x - g * ktiles) * KT;
+  Tile t;
+  if (!find_tile(a.offsets, a.E, a.S, g, 16, &t)) return;
+  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  const int64_t slot = t.lo + r;
+  if (t.e < a.E) {
+    const int64_t kb = a.K / 32;
+    const int wr = tid >> 3, wc = tid & 7;  // this thread's row and word of the tile
+    for (int64_t n0 = 0; n0 < a.N; n0 += 32) {
+      uint32_t w = 0;
+      float scale = 1.0f;
+      if (n0 + wr < a.N && k0 + 8 * wc < a.K) {
+        const int64_t row = static_cast<int64_t>(t.e) * a.N + n0 + wr;
+        w = *reinterpret_cast<const uint32_t*>(a.codes + row * kb * 16 + k0 / 2 + 4 * wc);
+        scale = mx4_scale(a.scales[row * kb + (k0 + 8 * wc) / 32]);
+      }
+      const uint4 v4 = mx4_bf16_words(w, scale);
+      const uint32_t v[4] = {v4.x, v4.y, v4.z, v4.w};
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) wt[(8 * wc + i) * LD + wr] = static_cast<uint16_t>(v[i / 2] >> (16 * (i & 1)));
+      __syncthreads();
+      uint4 xv = make_uint4(0, 0, 0, 0);
+      const int64_t n = n0 + 8 * q;
+      if (slot < t.hi && n < a.N) xv = *reinterpret_cast<const uint4*>(a.x + slot * a.ldx + n);
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+          *reinterpret_cast<const bf16x8*>(&wt[(16 * wave + r) * LD + 8 * q]), __builtin_bit_cast(bf16x8, xv), acc,
+          0, 0, 0);
+    }
+  }
+  const int64_t k = k0 + 16 * wave + 4 * q;
+  if (slot < t.hi && k < a.K) store4(a, slot, k, a.K, a.ldy % 4 == 0, acc);
+}
+
+bitsmoe_status check(const char* who, const MulArgs& a, bitsmoe_dtype yt, int64_t wide) {
+  const std::string w(who);
+  if (a.E <= 0 || a.N <= 0 || a.K <= 0 || a.S < 0 || a.x_rows < 0)
+    return fail(BITSMOE_ERR_ARG, w + ": non-positive size");
+  if (yt != BITSMOE_F32 && yt != BITSMOE_BF16) return fail(BITSMOE_ERR_DTYPE, w + ": results are fp32 or bf16");
+  if (a.K % kMx4Block != 0 || a.K > (1 << 24) || a.N > (1 << 24) || a.E > 65535 || a.S > 0x7FFFFFF0 ||
+      a.x_rows > 0x7FFFFFFF)
+    return fail(BITSMOE_ERR_SHAPE, w + ": needs K % 32 == 0, K and N <= 2^24, E <= 65535, S and rows < 2^31");
+  if (a.ldy < wide || a.ldy > (int64_t(1) << 32))
+    return fail(BITSMOE_ERR_SHAPE, w + ": the results' row stride is too small or too large");
+  if (!a.offsets && a.E != 1) return fail(BITSMOE_ERR_ARG, w + ": no offsets, and more than one expert");
+  if (a.S > 0 && (!a.codes || !a.scales || !a.y)) return fail(BITSMOE_ERR_ARG, w + ": null pointer");
+  if (!a.rows && a.x_rows < a.S) return fail(BITSMOE_ERR_SHAPE, w + ": fewer rows than slots");
+  if (!aligned16({a.codes, a.scales, a.x, a.xcodes, a.xscales, a.offsets, a.rows, a.y}))
+    return fail(BITSMOE_ERR_ARG, w + ": device pointers must be 16-byte aligned");
+  return BITSMOE_OK;
+}
+
+// Workgroups for tiles of `tile` slots and `per` workgroups each.
+bool grid_of(const MulArgs& a, int64_t tile, int64_t per, unsigned* grid) {
+  const int64_t tiles = a.S / tile + (a.E + 1 < a.S ? a.E + 1 : a.S);
+  if (tiles > ((int64_t(1) << 24) - 1) / per) return false;
+  *grid = static_cast<unsigned>(tiles * per);
+  return true;
+}
+
+bitsmoe_status product(const char* who, const MulArgs& a, bool glu, hipStream_t s) {
+  unsigned grid;
+  if (!grid_of(a, 16, (a.N + 15) / 16, &grid))
+    return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": too many slots and outputs for one call");
+  auto* fn = a.xcodes ? (glu ? mx4_rows_kernel<true, true> : mx4_rows_kernel<true, false>)
+                      : (glu ? mx4_rows_kernel<false, true> : mx4_rows_kernel<false, false>);
+  fn<<<grid, kThreads, 0, s>>>(a);
+  BITSMOE_LAUNCH_CHECK("mx4_rows_kernel");
+  return ok();
+}
+
+}  // namespace
+}  // namespace bitsmoe
+
+using namespace bitsmoe;
+
+extern "C" bitsmoe_status bitsmoe_mx4_product(const uint8_t* codes_dev, const uint8_t* scales_dev, int64_t E,
+                                              int64_t N, int64_t K, const void* X_dev, bitsmoe_dtype xt,
+                                              int64_t x_rows, int64_t ldx, const int32_t* offsets_dev,
+                                              const int32_t* rows_dev, int64_t S, int glu, void* Y_dev,
+                                              bitsmoe_dtype yt, int64_t ldy, void* stream) {
+  MulArgs a{codes_dev, scales_dev, static_cast<int>(E < 0x7FFFFFFF ? E : 0x7FFFFFFF), N, K,
+            static_cast<const uint16_t*>(X_dev), nullptr, nullptr, x_rows, ldx, offsets_dev, rows_dev, S,
+            Y_dev, ldy, yt == BITSMOE_F32};
+  if (bitsmoe_status st = check("mx4_product", a, yt, N)) return st;
+  if (xt != BITSMOE_BF16) return fail(BITSMOE_ERR_DTYPE, "mx4_product: tokens must be bf16");
+  if (ldx < K || ldx % 8 != 0 || ldx > (int64_t(1) << 32))
+    return fail(BITSMOE_ERR_SHAPE, "mx4_product: needs ldx >= K and ldx % 8 == 0");
+  if (S == 0) return ok();
+  if (x_rows > 0 && !X_dev) return fail(BITSMOE_ERR_ARG, "mx4_product: null pointer");
+  return product("mx4_product", a, glu != 0, static_cast<hipStream_t>(stream));
+}
+
+extern "C" bitsmoe_status bitsmoe_mx4_product_q(const uint8_t* codes_dev, const uint8_t* scales_dev, int64_t E,
+                                                int64_t N, int64_t K, const uint8_t* xcodes_dev,
+                                                const uint8_t* xscales_dev, int64_t x_rows,
+                                                const int32_t* offsets_dev, const int32_t* rows_dev, int64_t S,
+                                                int glu, void* Y_dev, bitsmoe_dtype yt, int64_t ldy,
+                                                void* stream) {
+  MulArgs a{codes_dev, scales_dev, static_cast<int>(E < 0x7FFFFFFF ? E : 0x7FFFFFFF), N, K,
+            nullptr, xcodes_dev, xscales_dev, x_rows, 0, offsets_dev, rows_dev, S,
+            Y_dev, ldy, yt == BITSMOE_F32};
+  if (bitsmoe_status st = check("mx4_product_q", a, yt, N)) return st;
+  if (S == 0) return ok();
+  if (!xcodes_dev || !xscales_dev) return fail(BITSMOE_ERR_ARG, "mx4_product_q: null pointer");
+  return product("mx4_product_q", a, glu != 0, static_cast<hipStream_t>(stream));
+}
+
+extern "C" bitsmoe_status bitsmoe_mx4_product_grad(const uint8_t* codes_dev, const uint8_t* scales_dev, int64_t E,
+                                                   int64_t N, int64_t K, const void* dY_dev, bitsmoe_dtype dyt,
+                                                   int64_t lddy, const int32_t* offsets_dev, int64_t S,
+                                                   void* dX_dev, bitsmoe_dtype xt, int64_t ldx, void* stream) {
+  MulArgs a{codes_dev, scales_dev, static_cast<int>(E < 0x7FFFFFFF ? E : 0x7FFFFFFF), N, K,
+            static_cast<const uint16_t*>(dY_dev), nullptr, nullptr, S, lddy, offsets_dev, nullptr, S,
+            dX_dev, ldx, xt == BITSMOE_F32};
+  if (bitsmoe_status st = check("mx4_product_grad", a, xt, K)) return st;
+  if (dyt != BITSMOE_BF16) return fail(BITSMOE_ERR_DTYPE, "mx4_product_grad: dY must be bf16");
+  if (N % 8 != 0 || lddy < N || lddy % 8 != 0 || lddy > (int64_t(1) << 32))
+    return fail(BITSMOE_ERR_SHAPE, "mx4_product_grad: needs N % 8 == 0, lddy >= N and lddy % 8 == 0");
+  if (S == 0) return ok();
+  if (!dY_dev) return fail(BITSMOE_ERR_ARG, "mx4_product_grad: null pointer");
+  unsigned grid;
+  if (!grid_of(a, 16, (K + 63) / 64, &grid))
+    return fail(BITSMOE_ERR_SHAPE, "mx4_product_grad: too many slots and columns for one call");
+  mx4_grad_kernel<<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
+  BITSMOE_LAUNCH_CHECK("mx4_grad_kernel");
+  return ok();
+}

@@ -1,0 +1,640 @@
+// The router of an MoE layer: softmax, the k largest experts of every token,
+// their weights, the slots in expert order, and the losses that keep the
+// experts evenly used; and the gradient of its logits.
+//
+// Forward, for a counted row t (valid, with a logit above -inf):
+//     p_te = exp(l_te - lse_t),  S_t = the k largest logits (ties: lowest e),
+//     w_tj = p_tj / sum_{S_t} p  (or p_tj as it is),
+//     c_e = number of slots of e,  P_e = sum_t p_te,  n = counted rows,
+//     balance = E / (k n^2) sum_e c_e P_e,   z = 1/n sum_t lse_t^2.
+// Backward, with a_e = E c_e / (k n^2) (the counts carry no gradient):
+//     dl_te = gb p_te (a_e - sum_f p_tf a_f) + 2 gz / n lse_t p_te + gate term.
+//
+// A row lies on LPT lanes, V consecutive logits a lane (V = 8 up to 512
+// experts), so that up to 64 rows share a wave and every reduction is a few
+// lane exchanges.  Workgroups take runs of consecutive rows: a first launch
+// writes each run's expert counts and probability sums, a second one adds the
+// runs before its own (integers, or fp32 in the order of the runs: results do
+// not depend on timing) and places the slots.  A single run does both in one
+// launch.
+#include <cstdint>
+#include <string>
+
+#include "common.hpp"
+#include "internal.hpp"
+
+namespace bitsmoe {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxExperts = 4096;
+constexpr int kMaxRuns = 256;       // workgroups of the first launch, unless a run gets too long
+constexpr int kMinRun = 16;         // rows of the shortest run
+constexpr int kMaxRunSlots = 16384;  // slots of the longest (its list is held in LDS)
+
+// fp32 as an unsigned integer of the same order, and back; 0 is below -inf.
+__device__ __forceinline__ uint32_t order_bits(float f) {
+  const uint32_t u = __float_as_uint(f + 0.0f);  // (-0 counts as 0)
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+__device__ __forceinline__ float order_value(uint32_t o) {
+  return __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
+}
+
+template <int LPT, typename F>
+__device__ __forceinline__ float row_reduce(float v, F f) {
+#pragma unroll
+  for (int o = 1; o < LPT; o <<= 1) v = f(v, __shfl_xor(v, o, 64));
+  return v;
+}
+template <int LPT>
+__device__ __forceinline__ float row_sum(float v) {
+  return row_reduce<LPT>(v, [](float a, float b) { return a + b; });
+}
+template <int LPT>
+__device__ __forceinline__ uint64_t row_max(uint64_t v) {
+#pragma unroll
+  for (int o = 1; o < LPT; o <<= 1) {
+    const uint64_t w = __shfl_xor(static_cast<unsigned long long>(v), o, 64);
+    v = w > v ? w : v;
+  }
+  return v;
+}
+
+// The V logits first .. first + V - 1 of a row (experts past E: -inf).
+template <bool BF16, int V>
+__device__ __forceinline__ void load_logits(const void* row, int first, int E, bool wide, float* x) {
+  if (wide && first + V <= E) {
+    if constexpr (BF16 && V % 8 == 0) {
+#pragma unroll
+      for (int q = 0; q < V / 8; ++q) {
+        const uint4 v = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(row) + first)[q];
+        const uint32_t d[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[8 * q + 2 * i] = __uint_as_float(d[i] << 16);
+          x[8 * q + 2 * i + 1] = __uint_as_float(d[i] & 0xFFFF0000u);
+        }
+      }
+      return;
+    }
+    if constexpr (!BF16) {
+#pragma unroll
+      for (int q = 0; q < V / 4; ++q) {
+        const f32x4 v = reinterpret_cast<const f32x4*>(static_cast<const float*>(row) + first)[q];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[4 * q + i] = v[i];
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int e = first + i;
+    float v = -INFINITY;
+    if (e < E)
+      v = BF16 ? bf16_to_f32(static_cast<const uint16_t*>(row)[e]) : static_cast<const float*>(row)[e];
+    x[i] = v;
+  }
+}
+
+struct RouteArgs {
+  const void* logits;
+  int64_t ld;
+  int64_t T;
+  int E, k, renorm, wide;
+  int run, runs;  // rows of a run, and how many runs
+  const uint8_t* valid;
+  int32_t* experts;
+  float* weights;
+  int32_t* counts;   // [E + 1]: slots of every expert, then the counted rows
+  int32_t* offsets;  // [E + 1]
+  int32_t* rows;
+  int32_t* slots;
+  float* lse;
+  float* losses;
+  // of every run: slots of every expert and of none [E + 1], probability sums [E], z and counted rows
+  int32_t* run_counts;
+  float* run_probs;
+  float* run_z;
+  int32_t* run_n;
+};
+
+// Exclusive sums over v[0 .. n) in LDS (n <= kMaxExperts + 1), in place;
+// `tmp` holds kThreads values.  Ends with a barrier.
+__device__ __forceinline__ void exclusive_scan(int32_t* v, int n, int32_t* tmp) {
+  const int per = (n + kThreads - 1) / kThreads, tid = threadIdx.x;
+  const int lo = min(n, tid * per), hi = min(n, lo + per);
+  int s = 0;
+  for (int i = lo; i < hi; ++i) s += v[i];
+  int inc = s;  // inclusive over the wave
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(inc, o, 64);
+    if ((tid & 63) >= o) inc += u;
+  }
+  if ((tid & 63) == 63) tmp[tid >> 6] = inc;
+  __syncthreads();
+  int base = inc - s;
+  for (int w = 0; w < (tid >> 6); ++w) base += tmp[w];
+  for (int i = lo; i < hi; ++i) {
+    const int c = v[i];
+    v[i] = base;
+    base += c;
+  }
+  __syncthreads();
+}
+
+// Places the slots of a run: next[e] is where the run's first slot of expert
+// e goes (e = E: no expert), list[i] the expert of its slot i.  One thread
+// per expert walks the list, so equal experts keep their order.
+__device__ __forceinline__ void place_slots(const RouteArgs& a, const int32_t* next,
+                                            const uint16_t* list, int64_t slot0, int n) {
+  for (int e = threadIdx.x; e <= a.E; e += kThreads) {
+    int pos = next[e];
+    for (int i0 = 0; i0 < n; i0 += 8) {
+      const uint4 v = *reinterpret_cast<const uint4*>(list + i0);
+      const uint32_t d[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int f = (d[i / 2] >> (16 * (i & 1))) & 0xFFFF;
+        if (f == e) {  // (the list is filled up with values above E)
+          const int64_t s = slot0 + i0 + i;
+          a.rows[pos] = static_cast<int32_t>(s / a.k);
+          a.slots[s] = pos++;
+        }
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ void write_losses(const RouteArgs& a, float balance, float z, int rows) {
+  const float n = static_cast<float>(rows);
+  a.losses[0] = rows > 0 ? balance * (static_cast<float>(a.E) / (static_cast<float>(a.k) * n * n)) : 0.0f;
+  a.losses[1] = rows > 0 ? z / n : 0.0f;
+  a.counts[a.E] = rows;
+}
+
+// Sum over the workgroup in a fixed order, valid in thread 0.
+template <typename T>
+__device__ __forceinline__ T block_sum(T v, void* lds) {
+  T* tmp = static_cast<T*>(lds);
+  v = wave_sum(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
+  __syncthreads();
+  T s = 0;
+  for (int w = 0; w < kThreads / 64; ++w) s += tmp[w];
+  return s;
+}
+
+__host__ __device__ inline int list_len(int n) { return (n + 7) & ~7; }
+
+// First launch: the rows of one run.
+template <bool BF16, int V, int LPT>
+__global__ __launch_bounds__(kThreads) void route_rows_kernel(RouteArgs a) {
+  constexpr int G = kThreads / LPT;  // rows at a time
+  extern __shared__ __align__(16) char smem[];
+  float* probs = reinterpret_cast<float*>(smem);                  // [G][LPT * V]
+  int32_t* cnt = reinterpret_cast<int32_t*>(probs + kThreads * V);  // [E + 1]
+  float* chosen = reinterpret_cast<float*>(cnt + a.E + 1);        // [G][k]
+  float* tmp = chosen + G * a.k;                                  // [kThreads]
+  uint16_t* list = reinterpret_cast<uint16_t*>(
+      (reinterpret_cast<uintptr_t>(tmp + kThreads) + 15) & ~uintptr_t(15));  // one run only
+  const int tid = threadIdx.x, lane = tid % LPT, grp = tid / LPT;
+  const bool one = a.runs == 1;
+  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * a.run;
+  const int nrows = static_cast<int>(min(static_cast<int64_t>(a.run), a.T - t0));
+  for (int e = tid; e <= a.E; e += kThreads) cnt[e] = 0;
+  if (one)
+    for (int i = nrows * a.k + tid; i < list_len(nrows * a.k); i += kThreads) list[i] = 0xFFFF;
+  __syncthreads();
+  const int first = lane * V;
+  float sum[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) sum[i] = 0.0f;
+  float zsum = 0.0f;
+  int nsum = 0;
+  for (int r = grp; r < nrows; r += G) {
+    const int64_t t = t0 + r;
+    const char* row = static_cast<const char*>(a.logits) + t * a.ld * (BF16 ? 2 : 4);
+    float x[V];
+    load_logits<BF16, V>(row, first, a.E, a.wide != 0, x);
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < V; ++i) m = fmaxf(m, x[i]);
+    m = row_reduce<LPT>(m, [](float p, float q) { return fmaxf(p, q); });
+    m = m == -INFINITY ? 0.0f : m;
+    float ex[V], total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      ex[i] = expf(x[i] - m);  // (NaN for a NaN, and in a row with an infinity)
+      total += ex[i];
+    }
+    total = row_sum<LPT>(total);
+    const bool broken = !(total == total);
+    const bool live = (a.valid == nullptr || a.valid[t] != 0) && (broken || total > 0.0f);
+    const float inv = 1.0f / total;
+    const float lse = live ? m + logf(total) : -INFINITY;
+    if (live) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) sum[i] += ex[i] * inv;
+      ++nsum;
+      zsum += lse * lse;
+    }
+    if (lane == 0) a.lse[t] = lse;
+    // the k largest, one after another: logit and 2^32 - 1 - index in one key
+    uint64_t key[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      key[i] = live && !broken && x[i] > -INFINITY
+                   ? (static_cast<uint64_t>(order_bits(x[i])) << 32) | (0xFFFFFFFFu - (first + i))
+                   : 0;
+    float total_w = 0.0f;
+    for (int j = 0; j < a.k; ++j) {
+      uint64_t best = key[0];
+#pragma unroll
+      for (int i = 1; i < V; ++i) best = key[i] > best ? key[i] : best;
+      best = row_max<LPT>(best);
+      int e = -1;
+      float p = 0.0f;
+      if (best != 0) {
+        e = static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(best));
+        p = expf(order_value(static_cast<uint32_t>(best >> 32)) - m) * inv;
+#pragma unroll
+        for (int i = 0; i < V; ++i) key[i] = key[i] == best ? 0 : key[i];
+      }
+      if (live && broken) p = __uint_as_float(0x7FC00000u);
+      total_w += p;
+      if (lane == j % LPT) {
+        a.experts[t * a.k + j] = e;
+        chosen[grp * a.k + j] = p;
+        const int bucket = e < 0 ? a.E : e;
+        atomicAdd(&cnt[bucket], 1);
+        if (one) list[r * a.k + j] = static_cast<uint16_t>(bucket);
+      }
+    }
+    const float scale = a.renorm && total_w != 0.0f ? 1.0f / total_w : 1.0f;
+    for (int j = lane; j < a.k; j += LPT)  // (a lane reads what it wrote itself)
+      a.weights[t * a.k + j] = chosen[grp * a.k + j] * scale;
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) probs[grp * LPT * V + first + i] = sum[i];
+  // z and n of the run: from one lane of every row, the rows in a fixed order
+  const float z = block_sum(lane == 0 ? zsum : 0.0f, tmp);
+  const int n = block_sum(lane == 0 ? nsum : 0, tmp);
+  __syncthreads();
+  if (!one) {
+    for (int e = tid; e <= a.E; e += kThreads) a.run_counts[int64_t(blockIdx.x) * (a.E + 1) + e] = cnt[e];
+    for (int e = tid; e < a.E; e += kThreads) {
+      float s = 0.0f;
+      for (int g = 0; g < G; ++g) s += probs[g * LPT * V + e];
+      a.run_probs[int64_t(blockIdx.x) * a.E + e] = s;
+    }
+    if (tid == 0) {
+      a.run_z[blockIdx.x] = z;
+      a.run_n[blockIdx.x] = n;
+    }
+    return;
+  }
+  float balance = 0.0f;
+  for (int e = tid; e < a.E; e += kThreads) {
+    float s = 0.0f;
+    for (int g = 0; g < G; ++g) s += probs[g * LPT * V + e];
+    balance += s * static_cast<float>(cnt[e]);
+    a.counts[e] = cnt[e];
+  }
+  balance = block_sum(balance, tmp);
+  if (tid == 0) write_losses(a, balance, z, n);
+  __syncthreads();
+  exclusive_scan(cnt, a.E + 1, reinterpret_cast<int32_t*>(tmp));
+  for (int e = tid; e <= a.E; e += kThreads) a.offsets[e] = cnt[e];
+  place_slots(a, cnt, list, 0, nrows * a.k);
+}
+
+// Second launch: workgroup b < runs places the slots of run b; the last one
+// writes the counts and losses.
+__global__ __launch_bounds__(kThreads) void route_place_kernel(RouteArgs a) {
+  extern __shared__ __align__(16) char smem[];
+  int32_t* total = reinterpret_cast<int32_t*>(smem);  // [E + 1]
+  int32_t* before = total + a.E + 1;                  // [E + 1]
+  int32_t* tmp = before + a.E + 1;                    // [kThreads]
+  uint16_t* list = reinterpret_cast<uint16_t*>(
+      (reinterpret_cast<uintptr_t>(tmp + kThreads) + 15) & ~uintptr_t(15));
+  const int tid = threadIdx.x, b = blockIdx.x;
+  const bool last = b == a.runs;
+  float balance = 0.0f;
+  for (int e = tid; e <= a.E; e += kThreads) {
+    int sum = 0, mine = 0;
+    for (int q = 0; q < a.runs; ++q) {
+      const int c = a.run_counts[int64_t(q) * (a.E + 1) + e];
+      if (q == b) mine = sum;
+      sum += c;
+    }
+    total[e] = sum;
+    before[e] = mine;
+    if (last && e < a.E) {
+      float p = 0.0f;
+      for (int q = 0; q < a.runs; ++q) p += a.run_probs[int64_t(q) * a.E + e];
+      balance += p * static_cast<float>(sum);
+      a.counts[e] = sum;
+    }
+  }
+  if (last) {
+    float z = 0.0f;
+    int n = 0;
+    for (int q = tid; q < a.runs; q += kThreads) {
+      z += a.run_z[q];
+      n += a.run_n[q];
+    }
+    balance = block_sum(balance, tmp);
+    z = block_sum(z, tmp);
+    n = block_sum(n, tmp);
+    if (tid == 0) write_losses(a, balance, z, n);
+    __syncthreads();
+    exclusive_scan(total, a.E + 1, tmp);
+    for (int e = tid; e <= a.E; e += kThreads) a.offsets[e] = total[e];
+    return;
+  }
+  const int64_t slot0 = static_cast<int64_t>(b) * a.run * a.k;
+  const int n = static_cast<int>(min(static_cast<int64_t>(a.run), a.T - static_cast<int64_t>(b) * a.run)) * a.k;
+  for (int i = tid; i < list_len(n); i += kThreads) {
+    const int e = i < n ? a.experts[slot0 + i] : 0xFFFF;
+    list[i] = static_cast<uint16_t>(e < 0 ? a.E : e);
+  }
+  __syncthreads();
+  exclusive_scan(total, a.E + 1, tmp);
+  for (int e = tid; e <= a.E; e += kThreads) before[e] += total[e];
+  __syncthreads();
+  place_slots(a, before, list, slot0, n);
+}
+
+// No rows at all.
+__global__ void route_none_kernel(int E, int32_t* counts, int32_t* offsets, float* losses) {
+  for (int e = threadIdx.x; e <= E; e += blockDim.x) counts[e] = offsets[e] = 0;
+  if (threadIdx.x < 2) losses[threadIdx.x] = 0.0f;
+}
+
+struct GradArgs {
+  const void* logits;
+  int64_t ld, T;
+  int E, k, renorm, wide;
+  const int32_t* experts;
+  const float* weights;
+  const int32_t* counts;
+  const float* lse;
+  const float* dweights;
+  const float* dlosses;
+  void* dlogits;
+};
+
+template <bool BF16, int V, int LPT>
+__global__ __launch_bounds__(kThreads) void route_grad_kernel(GradArgs a) {
+  constexpr int G = kThreads / LPT;
+  const int lane = threadIdx.x % LPT, grp = threadIdx.x / LPT, first = lane * V;
+  const float n = static_cast<float>(a.counts[a.E]);
+  const float gb = a.dlosses && n > 0.0f ? a.dlosses[0] * (static_cast<float>(a.E) / (static_cast<float>(a.k) * n * n)) : 0.0f;
+  const float gz = a.dlosses && n > 0.0f ? a.dlosses[1] * 2.0f / n : 0.0f;
+  float share[V];  // gb E c_e / (k n^2)
+#pragma unroll
+  for (int i = 0; i < V; ++i) share[i] = first + i < a.E ? gb * static_cast<float>(a.counts[first + i]) : 0.0f;
+  for (int64_t t = static_cast<int64_t>(blockIdx.x) * G + grp; t < a.T;
+       t += static_cast<int64_t>(gridDim.x) * G) {
+    const float lse = a.lse[t];
+    float d[V];
+    if (lse == -INFINITY) {  // a row that does not count
+#pragma unroll
+      for (int i = 0; i < V; ++i) d[i] = 0.0f;
+    } else {
+      // p anew from the row: from lse alone a large lse would cost it its digits
+      float p[V], m = -INFINITY, total = 0.0f, s = 0.0f;
+      load_logits<BF16, V>(static_cast<const char*>(a.logits) + t * a.ld * (BF16 ? 2 : 4), first, a.E,
+                           a.wide != 0, p);
+#pragma unroll
+      for (int i = 0; i < V; ++i) m = fmaxf(m, p[i]);
+      m = row_reduce<LPT>(m, [](float u, float v) { return fmaxf(u, v); });
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        p[i] = expf(p[i] - m);
+        total += p[i];
+      }
+      const float inv = 1.0f / row_sum<LPT>(total);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        p[i] *= inv;
+        s += p[i] * share[i];
+      }
+      s = row_sum<LPT>(s);
+      // the gates: sum of weight x gradient, then each slot's own term
+      float wd = 0.0f;
+      if (a.dweights)
+        for (int j = lane; j < a.k; j += LPT)
+          if (a.experts[t * a.k + j] >= 0) wd += a.weights[t * a.k + j] * a.dweights[t * a.k + j];
+      wd = row_sum<LPT>(wd);
+      const float all = gz * lse - s - (a.renorm ? 0.0f : wd);
+#pragma unroll
+      for (int i = 0; i < V; ++i) d[i] = p[i] * (share[i] + all);
+      if (a.dweights) {
+        const float mean = a.renorm ? wd : 0.0f;
+        for (int j = 0; j < a.k; ++j) {
+          const int e = a.experts[t * a.k + j];
+          if (e < 0) continue;
+          const float g = a.weights[t * a.k + j] * (a.dweights[t * a.k + j] - mean);
+#pragma unroll
+          for (int i = 0; i < V; ++i) d[i] += e == first + i ? g : 0.0f;
+        }
+      }
+    }
+    if constexpr (BF16) {
+      uint16_t* out = static_cast<uint16_t*>(a.dlogits) + t * a.E + first;
+      if (V % 8 == 0 && a.E % 8 == 0 && first + V <= a.E) {
+#pragma unroll
+        for (int q = 0; q < V / 8; ++q) {
+          bf16x8 v;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = static_cast<__bf16>(d[8 * q + i]);
+          reinterpret_cast<bf16x8*>(out)[q] = v;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (first + i < a.E) out[i] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(d[i]));
+      }
+    } else {
+      float* out = static_cast<float*>(a.dlogits) + t * a.E + first;
+      if (a.E % 4 == 0 && first + V <= a.E) {
+#pragma unroll
+        for (int q = 0; q < V / 4; ++q) {
+          f32x4 v;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = d[4 * q + i];
+          reinterpret_cast<f32x4*>(out)[q] = v;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (first + i < a.E) out[i] = d[i];
+      }
+    }
+  }
+}
+
+// Calls f(V, LPT) as integral constants for rows of E logits.
+template <typename F>
+void with_layout(int64_t E, F f) {
+  using I8 = std::integral_constant<int, 8>;
+  using I64 = std::integral_constant<int, 64>;
+  if (E <= 8) f(I8(), std::integral_constant<int, 1>());
+  else if (E <= 16) f(I8(), std::integral_constant<int, 2>());
+  else if (E <= 32) f(I8(), std::integral_constant<int, 4>());
+  else if (E <= 64) f(I8(), std::integral_constant<int, 8>());
+  else if (E <= 128) f(I8(), std::integral_constant<int, 16>());
+  else if (E <= 256) f(I8(), std::integral_constant<int, 32>());
+  else if (E <= 512) f(I8(), I64());
+  else if (E <= 1024) f(std::integral_constant<int, 16>(), I64());
+  else if (E <= 2048) f(std::integral_constant<int, 32>(), I64());
+  else f(I64(), I64());
+}
+
+bitsmoe_status check(const char* who, const void* logits, bitsmoe_dtype lt, int64_t T, int64_t E, int64_t ld,
+                     int64_t k) {
+  if (T < 0 || E <= 0 || k <= 0 || (T > 0 && logits == nullptr))
+    return fail(BITSMOE_ERR_ARG, std::string(who) + ": null pointer or non-positive size");
+  if (lt != BITSMOE_F32 && lt != BITSMOE_BF16)
+    return fail(BITSMOE_ERR_DTYPE, std::string(who) + ": logits must be fp32 or bf16");
+  if (E > kMaxExperts || k > E || k > BITSMOE_ROUTE_MAX_K)
+    return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": needs E <= 4096 and k <= min(E, 64)");
+  if (ld < E || T > (int64_t(1) << 31) / k - 1 || ld > (int64_t(1) << 40))
+    return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": needs ld >= E and T * k < 2^31");
+  return BITSMOE_OK;
+}
+
+bool wide_rows(const void* p, bitsmoe_dtype lt, int64_t E, int64_t ld) {
+  const int64_t size = lt == BITSMOE_BF16 ? 2 : 4;
+  return aligned16({p}) && ld * size % 16 == 0 && E % 8 == 0;
+}
+
+}  // namespace
+}  // namespace bitsmoe
+
+using namespace bitsmoe;
+
+extern "C" bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt, int64_t T, int64_t E,
+                                        int64_t ld, int64_t k, const uint8_t* valid_dev, int renorm,
+                                        int32_t* experts_dev, float* weights_dev, int32_t* counts_dev,
+                                        int32_t* offsets_dev, int32_t* rows_dev, int32_t* slots_dev,
+                                        float* lse_dev, float* losses_dev, void* stream) {
+  if (bitsmoe_status st = check("route", logits_dev, lt, T, E, ld, k)) return st;
+  if (!counts_dev || !offsets_dev || !losses_dev ||
+      (T > 0 && (!experts_dev || !weights_dev || !rows_dev || !slots_dev || !lse_dev)))
+    return fail(BITSMOE_ERR_ARG, "route: null pointer");
+  if (!aligned16({logits_dev, experts_dev, weights_dev, counts_dev, offsets_dev, rows_dev, slots_dev, lse_dev,
+                  losses_dev}))
+    return fail(BITSMOE_ERR_ARG, "route: device pointers must be 16-byte aligned");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (T == 0) {
+    route_none_kernel<<<1, 256, 0, s>>>(static_cast<int>(E), counts_dev, offsets_dev, losses_dev);
+    BITSMOE_LAUNCH_CHECK("route_none_kernel");
+    return ok();
+  }
+  RouteArgs a{};
+  a.logits = logits_dev;
+  a.ld = ld;
+  a.T = T;
+  a.E = static_cast<int>(E);
+  a.k = static_cast<int>(k);
+  a.renorm = renorm != 0;
+  a.wide = wide_rows(logits_dev, lt, E, ld);
+  a.valid = valid_dev;
+  a.experts = experts_dev;
+  a.weights = weights_dev;
+  a.counts = counts_dev;
+  a.offsets = offsets_dev;
+  a.rows = rows_dev;
+  a.slots = slots_dev;
+  a.lse = lse_dev;
+  a.losses = losses_dev;
+  int64_t run = (T + kMaxRuns - 1) / kMaxRuns;
+  if (run < kMinRun) run = kMinRun;
+  if (run > kMaxRunSlots / k) run = kMaxRunSlots / k;
+  const int64_t runs = (T + run - 1) / run;
+  a.run = static_cast<int>(run);
+  a.runs = static_cast<int>(runs);
+  if (runs > 1) {
+    bitsmoe_status st;
+    const size_t nc = ((size_t(runs) * (E + 1) * 4) + 255) & ~size_t(255);
+    const size_t np = ((size_t(runs) * E * 4) + 255) & ~size_t(255);
+    char* p = static_cast<char*>(scratch(kScratchMisc, nc + np + size_t(runs) * 8, stream, &st));
+    if (!p) return st;
+    a.run_counts = reinterpret_cast<int32_t*>(p);
+    a.run_probs = reinterpret_cast<float*>(p + nc);
+    a.run_z = reinterpret_cast<float*>(p + nc + np);
+    a.run_n = reinterpret_cast<int32_t*>(a.run_z + runs);
+  }
+  bitsmoe_status st = BITSMOE_OK;
+  with_layout(E, [&](auto v, auto l) {
+    constexpr int V = decltype(v)::value, LPT = decltype(l)::value;
+    const size_t lds = size_t(kThreads) * V * 4 + (E + 1) * 4 + size_t(kThreads / LPT) * k * 4 + kThreads * 4 +
+                       16 + (runs == 1 ? size_t(list_len(static_cast<int>(run * k))) * 2 : 0);
+    auto* fn = lt == BITSMOE_BF16 ? route_rows_kernel<true, V, LPT> : route_rows_kernel<false, V, LPT>;
+    if (lds > 65536) {
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+      if (e != hipSuccess) {
+        st = device_error("route: shared memory", e);
+        return;
+      }
+    }
+    fn<<<static_cast<unsigned>(runs), kThreads, lds, s>>>(a);
+  });
+  if (st) return st;
+  BITSMOE_LAUNCH_CHECK("route_rows_kernel");
+  if (runs > 1) {
+    const size_t lds = size_t(2) * (E + 1) * 4 + kThreads * 4 + 16 + size_t(list_len(static_cast<int>(run * k))) * 2;
+    if (lds > 65536) {
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(route_place_kernel),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+      if (e != hipSuccess) return device_error("route: shared memory", e);
+    }
+    route_place_kernel<<<static_cast<unsigned>(runs + 1), kThreads, lds, s>>>(a);
+    BITSMOE_LAUNCH_CHECK("route_place_kernel");
+  }
+  return ok();
+}
+
+extern "C" bitsmoe_status bitsmoe_route_grad(const void* logits_dev, bitsmoe_dtype lt, int64_t T, int64_t E,
+                                             int64_t ld, int64_t k, int renorm, const int32_t* experts_dev,
+                                             const float* weights_dev, const int32_t* counts_dev,
+                                             const float* lse_dev, const float* dweights_dev,
+                                             const float* dlosses_dev, void* dlogits_dev, void* stream) {
+  if (bitsmoe_status st = check("route_grad", logits_dev, lt, T, E, ld, k)) return st;
+  if (T == 0) return ok();
+  if (!experts_dev || !weights_dev || !counts_dev || !lse_dev || !dlogits_dev)
+    return fail(BITSMOE_ERR_ARG, "route_grad: null pointer");
+  if (!aligned16({logits_dev, experts_dev, weights_dev, counts_dev, lse_dev, dweights_dev, dlosses_dev, dlogits_dev}))
+    return fail(BITSMOE_ERR_ARG, "route_grad: device pointers must be 16-byte aligned");
+  GradArgs a{};
+  a.logits = logits_dev;
+  a.ld = ld;
+  a.T = T;
+  a.E = static_cast<int>(E);
+  a.k = static_cast<int>(k);
+  a.renorm = renorm != 0;
+  a.wide = wide_rows(logits_dev, lt, E, ld);
+  a.experts = experts_dev;
+  a.weights = weights_dev;
+  a.counts = counts_dev;
+  a.lse = lse_dev;
+  a.dweights = dweights_dev;
+  a.dlosses = dlosses_dev;
+  a.dlogits = dlogits_dev;
+  with_layout(E, [&](auto v, auto l) {
+    constexpr int V = decltype(v)::value, LPT = decltype(l)::value;
+    const int64_t groups = (T + kThreads / LPT - 1) / (kThreads / LPT);
+    const unsigned grid = static_cast<unsigned>(groups < 8192 ? groups : 8192);
+    auto* fn = lt == BITSMOE_BF16 ? route_grad_kernel<true, V, LPT> : route_grad_kernel<false, V, LPT>;
+    fn<<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
+  });
+  BITSMOE_LAUNCH_CHECK("route_grad_kernel");
+  return ok();
+}

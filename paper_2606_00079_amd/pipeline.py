@@ -15,6 +15,9 @@ calibration input, so their H is computed once.
 ``surrogate_allocation`` runs the paper's own allocation on the same spectral
 units: the closed-form surrogate costs on the device, then the ILP over the
 widths {0, 1, 2, 3, 4, 6, 8, 16} under the equivalent-bit budget.
+
+``mx4_layer`` runs an MoE layer whose experts are held in MX4, from the
+router's logits to the layer's output, and ``mx4_layer_grad`` its gradients.
 """
 from __future__ import annotations
 
@@ -24,9 +27,11 @@ from typing import Dict, List, Optional, Sequence
 
 import numpy as np
 
-from . import (SURROGATE_WIDTHS, allocate, basis_importance, gram, gram_experts, gram_experts_in,
-               gram_routed, pack, pack_layout, project, project_in, score, score_diag,
-               score_routed, shared_basis, shared_basis_gpu, surrogate, surrogate_budget)
+from . import (SURROGATE_WIDTHS, Routing, allocate, basis_importance, combine, combine_grad, gram,
+               gram_experts, gram_experts_in, gram_routed, mx4_product, mx4_product_grad,
+               mx4_product_q, mx4_quantize, pack, pack_layout, project, project_in, route,
+               route_grad, score, score_diag, score_routed, shared_basis, shared_basis_gpu,
+               surrogate, surrogate_budget)
 
 
 @dataclasses.dataclass
@@ -272,3 +277,74 @@ def surrogate_allocation(C, H, gamma: float, kappa: Sequence[float], E: int, n_o
     times["gpu_pack_ms"] = sp.ms()
     times["gpu_ms"] = times["gpu_cost_ms"] + times["gpu_pack_ms"]
     return SurrogateResult(L, st, bits_u, budget, obj, off, codes, params, times)
+
+
+# ---------------------------------------------------------------------------
+# an MoE layer with its experts in MX4
+# ---------------------------------------------------------------------------
+@dataclasses.dataclass
+class Mx4Experts:
+    """The experts' weights in MX4: gate rows, then up rows, of every expert
+    [E][2 N][K], and its down rows [E][K][N]."""
+    up_codes: object
+    up_scales: object
+    down_codes: object
+    down_scales: object
+
+
+def mx4_experts(W_gate, W_up, W_down) -> Mx4Experts:
+    """Weights [E][N][K], [E][N][K] and [E][K][N] (bf16 or fp32) to MX4, once."""
+    import torch
+    return Mx4Experts(*mx4_quantize(torch.cat((W_gate, W_up), 1)), *mx4_quantize(W_down.contiguous()))
+
+
+@dataclasses.dataclass
+class Mx4Saved:
+    """What the gradients of a layer read."""
+    routing: Routing
+    logits: object
+    up: object       # [S][2 N] bf16: the gate and up values
+    z: object        # [S][K] bf16: the experts' outputs
+    renorm: bool
+
+
+def mx4_layer(x, logits, experts: Mx4Experts, k: int, valid=None, renorm: bool = True,
+              quantize_tokens: bool = False, train: bool = False):
+    """y_t = sum_j w_tj down_e(silu(gate_e x_t) * up_e x_t) for tokens x bf16
+    [T][K] and the router's logits [T][E] -> (y bf16 [T][K], Routing), and with
+    ``train`` also what ``mx4_layer_grad`` reads.  quantize_tokens: the products
+    take their tokens in MX4 as well."""
+    import torch
+    r = route(logits, k, valid=valid, renorm=renorm)
+
+    def product(codes, scales, v, rows, glu):
+        if quantize_tokens:
+            return mx4_product_q(codes, scales, *mx4_quantize(v), offsets=r.offsets, rows=rows, glu=glu)
+        return mx4_product(codes, scales, v, offsets=r.offsets, rows=rows, glu=glu)
+
+    up = product(experts.up_codes, experts.up_scales, x, r.rows, not train)
+    if train:
+        g, u = up.float().chunk(2, dim=1)
+        h = (torch.nn.functional.silu(g) * u).to(torch.bfloat16)
+    else:
+        h = up
+    z = product(experts.down_codes, experts.down_scales, h, None, False)
+    y = combine(z, r.slots, r.weights)
+    return (y, r, Mx4Saved(r, logits, up, z, renorm)) if train else (y, r)
+
+
+def mx4_layer_grad(saved: Mx4Saved, experts: Mx4Experts, dy, dlosses=None):
+    """Gradients of the tokens (bf16 [T][K]) and of the logits from that of y
+    (bf16 [T][K]) and of the two losses (fp32 [2]); where the tokens were
+    quantized, as if they had not been."""
+    import torch
+    r = saved.routing
+    dz, dw = combine_grad(saved.z, r.slots, r.weights, dy)
+    dh = mx4_product_grad(experts.down_codes, experts.down_scales, dz, offsets=r.offsets,
+                          dtype=torch.float32)
+    g, u = saved.up.float().chunk(2, dim=1)
+    sig = torch.sigmoid(g)
+    dup = torch.cat((dh * u * sig * (1 + g * (1 - sig)), dh * g * sig), 1).to(torch.bfloat16)
+    dx = combine(mx4_product_grad(experts.up_codes, experts.up_scales, dup, offsets=r.offsets),
+                 r.slots)
+    return dx, route_grad(saved.logits, r, dweights=dw, dlosses=dlosses, renorm=saved.renorm)

@@ -1,0 +1,521 @@
+"""GPU parity of the MoE layer's operators (router, MX4, experts' products,
+joining) against the fp64 oracle.
+
+Bounds: whole numbers and MX4 codes are equal.  A sum of n fp32 terms in any
+order is within n 2^-24 of the sum of their magnitudes; 2^-23 is allowed, as a
+matrix core may cut instead of round.  A bf16 result is rounded once, 2^-8 of
+it at most (2^-9, and the fp32 error may move it over a rounding point).
+exp and log are taken to be within 2^-21.
+"""
+import numpy as np
+import pytest
+
+from conftest import gpu_available
+from oracle import mx4 as omx4
+from oracle import route as oroute
+
+pytestmark = pytest.mark.gpu
+
+if not gpu_available():  # pragma: no cover
+    pytest.skip("no GPU", allow_module_level=True)
+
+import torch  # noqa: E402
+
+import paper_2606_00079_amd as bm  # noqa: E402
+from paper_2606_00079_amd import pipeline  # noqa: E402
+
+DEV = "cuda:0"
+U = 2.0 ** -23
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def np64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def dev(a, dtype=None):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV, dtype)
+
+
+def within(got, want, bound, what):
+    got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
+    assert got.shape == want.shape, what
+    want = np.where(np.abs(want) >= 2.0 ** 128, np.copysign(np.inf, want), want)  # past fp32 and bf16
+    assert (np.isnan(got) == np.isnan(want)).all(), what
+    inf = np.isinf(want)
+    assert (got[inf] == want[inf]).all(), what
+    ok = np.isfinite(want)
+    off = np.abs(got[ok] - want[ok]) - np.broadcast_to(bound, want.shape)[ok]
+    assert not (off > 0).any(), (what, float(off.max()), int((off > 0).sum()))
+
+
+# ------------------------------------------------------------------- MX4
+def rows_for(kind, rows, cols, g):
+    x = g.standard_normal((rows, cols)) * np.exp(2 * g.standard_normal((rows, 1)))
+    if kind == "edges":  # every rounding point of the format, both signs, over many scales
+        pts = np.array([0, .25, .5, .75, 1, 1.25, 1.5, 1.75, 2, 2.5, 3, 3.5, 4, 5, 6, 6.5, 7, 7.75])
+        x = g.choice(pts, (rows, cols)) * g.choice([-1, 1], (rows, cols))
+        x *= 2.0 ** g.integers(-133, 120, (rows, cols // 32)).repeat(32, 1)
+    elif kind == "special":
+        at = g.random((rows, cols))
+        x[at < 0.01], x[(at > 0.01) & (at < 0.015)], x[(at > 0.015) & (at < 0.02)] = np.nan, np.inf, -np.inf
+        x[:, :32] = 0.0
+        x[rows // 2] = -0.0
+        x[0, 32:] = 1e-42
+        x[-1] = 3e38
+    return x
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["normal", "edges", "special"])
+@pytest.mark.parametrize("rows,cols", [(1, 32), (1, 2048), (3, 96), (257, 160), (64, 1024)])
+def test_mx4_is_exact(dtype, kind, rows, cols):
+    g = np.random.default_rng([rows, cols, len(kind)])
+    X = dev(rows_for(kind, rows, cols, g).astype(np.float32)).to(DT[dtype])
+    codes, scales = bm.mx4_quantize(X)
+    want = omx4.quantize(np64(X))
+    assert (scales.cpu().numpy() == want[1]).all()
+    assert (codes.cpu().numpy() == want[0]).all()
+    for out in ("bf16", "f32"):
+        got = bm.mx4_dequantize(codes, scales, dtype=DT[out])
+        assert got.dtype == DT[out]
+        within(np64(got), omx4.dequantize(*want), 0.0, out)
+
+
+def test_mx4_strided_rows_and_none():
+    g = np.random.default_rng(0)
+    big = dev(g.standard_normal((9, 256)).astype(np.float32))
+    part = big[:, 32:128]
+    want = omx4.quantize(np64(part))
+    codes, scales = bm.mx4_quantize(part)
+    assert (codes.cpu().numpy() == want[0]).all() and (scales.cpu().numpy() == want[1]).all()
+    codes, scales = bm.mx4_quantize(big[:0])
+    assert codes.shape == (0, 128) and bm.mx4_dequantize(codes, scales).shape == (0, 256)
+
+
+def test_every_code_with_every_scale():
+    codes = torch.arange(256, dtype=torch.uint8, device=DEV).repeat(256, 1)
+    scales = torch.arange(256, dtype=torch.uint8, device=DEV)[:, None].repeat(1, 16)
+    want = omx4.dequantize(codes.cpu().numpy(), scales.cpu().numpy())
+    within(np64(bm.mx4_dequantize(codes, scales, dtype=torch.float32)), want, 0.0, "f32")
+    within(np64(bm.mx4_dequantize(codes, scales)), want, 0.0, "bf16")
+
+
+# ----------------------------------------------------------------- router
+def logits_for(kind, T, E, g):
+    x = 2 * g.standard_normal((T, E))
+    if kind == "ties":
+        x = g.integers(-2, 3, (T, E)).astype(float)
+    elif kind == "masked":
+        x[g.random((T, E)) < 0.5] = -np.inf
+        x[T // 2] = -np.inf
+        x[-1, 1:] = -np.inf
+    elif kind == "broken":
+        x[T // 3, E // 2] = np.nan
+        x[T // 2, 0] = np.inf
+    elif kind == "large":
+        x = 3e4 * x
+        x[0] = -3.0e38
+    return x
+
+
+def check_route(x, k, valid, renorm, dw, dl, what):
+    """Everything of the router against the oracle; x is on the device."""
+    T, E = x.shape
+    want = oroute.route(np64(x), k, None if valid is None else valid.cpu().numpy(), renorm)
+    r = bm.route(x, k, valid=valid, renorm=renorm)
+    for name in ("experts", "counts", "offsets", "rows", "slots"):
+        got = getattr(r, name).cpu().numpy()
+        assert got.dtype == np.int32 and (got == want[name]).all(), (what, name)
+    e1 = (E + 64) * U
+    top = np.abs(np.where(np.isfinite(want["lse"]), want["lse"], 0))
+    # a softmax's entry carries the rounding of its logit's distance to the largest: |x - m| 2^-24
+    finite = np.where(np.isfinite(np64(x)), np64(x), 0)
+    spread = (finite.max(1) - finite.min(1))[:, None]
+    e2 = e1 + U * np.minimum(spread, 128)  # (beyond, the entry is 0 in fp32)
+    within(np64(r.lse), want["lse"], e1 * (1 + top), (what, "lse"))
+    within(np64(r.weights), want["weights"], e2 * np.abs(want["weights"]) + 2.0 ** -126, (what, "weights"))
+    e3 = float((e2.max() if T else 0) + (T + 300) * U)
+    within(np64(r.losses), want["losses"], 2 * e3 * np.abs(want["losses"]) + 1e-30, (what, "losses"))
+    for a, b in ((dw, dl), (None, dl), (dw, None)):
+        got = bm.route_grad(x, r, None if a is None else dev(a, torch.float32),
+                            None if b is None else dev(b, torch.float32), renorm)
+        d = oroute.route_grad(np64(x), want, a, b, renorm)
+        # the magnitudes that are added and subtracted for an entry
+        n = max(1, want["counts"][E])
+        share = E * want["counts"][:E].max() / (k * n * n)
+        size = np.zeros((T, 1))
+        if b is not None:
+            size = size + 2 * abs(b[0]) * share + 2 * abs(b[1]) / n * top[:, None]
+        if a is not None:
+            size = size + 2 * np.abs(np.nan_to_num(want["weights"]) * a).sum(1, keepdims=True)
+            size = size + np.abs(a).max() * np.nan_to_num(want["weights"]).max(1, keepdims=True)
+        bound = 4 * (e2 + U * np.minimum(top[:, None], 2.0 ** 20)) * size + (2.0 ** -8 * np.abs(d) if x.dtype == torch.bfloat16 else 0)
+        within(np64(got), d, bound + 1e-37, (what, "dlogits"))
+    return r
+
+
+@pytest.mark.parametrize("E,k", [(1, 1), (4, 2), (8, 8), (9, 3), (16, 2), (33, 5), (60, 4), (128, 8), (130, 6),
+                                 (256, 8), (300, 7), (512, 8), (1000, 9), (2049, 3), (4096, 64)])
+@pytest.mark.parametrize("T", [1, 7, 16, 17, 150])
+def test_route(E, k, T):
+    g = np.random.default_rng([E, k, T])
+    for dtype in ("bf16", "f32"):
+        x = dev(logits_for("normal", T, E, g).astype(np.float32)).to(DT[dtype])
+        check_route(x, k, None, bool((E + T) % 2), g.standard_normal((T, k)), np.array([0.5, 0.25]), (dtype,))
+
+
+@pytest.mark.parametrize("kind", ["ties", "masked", "broken", "large"])
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("T,E,k", [(5, 8, 3), (40, 60, 4), (37, 256, 8)])
+def test_route_rows_that_go_wrong(kind, renorm, T, E, k):
+    g = np.random.default_rng([T, E, k, len(kind)])
+    x = dev(logits_for(kind, T, E, g).astype(np.float32))
+    if kind == "ties":
+        x = x.to(torch.bfloat16)
+    valid = dev(g.random(T) < 0.7) if kind == "masked" else None
+    check_route(x, k, valid, renorm, g.standard_normal((T, k)), np.array([0.5, 0.25]), kind)
+
+
+def test_route_with_no_row_that_counts_and_with_none():
+    x = torch.randn(20, 16, device=DEV)
+    r = bm.route(x, 2, valid=torch.zeros(20, dtype=torch.bool, device=DEV))
+    assert (r.experts == -1).all() and (r.counts == 0).all() and (r.losses == 0).all()
+    assert (r.offsets == 0).all() and r.slots.flatten().tolist() == list(range(40))
+    assert (bm.route_grad(x, r, torch.ones(20, 2, device=DEV), torch.ones(2, device=DEV)) == 0).all()
+    r = bm.route(x[:0], 2)
+    assert (r.counts == 0).all() and (r.offsets == 0).all() and (r.losses == 0).all()
+    assert bm.route_grad(x[:0], r).shape == (0, 16)
+
+
+def test_route_strided_logits_and_a_long_batch():
+    g = np.random.default_rng(9)
+    wide = dev(g.standard_normal((5000, 72)).astype(np.float32))
+    for x in (wide[:, :64], wide[:, :61], wide[::2, 8:40]):
+        check_route(x, 6, dev(g.random(len(x)) < 0.9), True, g.standard_normal((len(x), 6)), np.array([1.0, 0.1]),
+                    tuple(x.shape))
+
+
+def test_route_twice_gives_the_same_bits():
+    x = torch.randn(9000, 96, device=DEV)
+    a, b = bm.route(x, 4), bm.route(x, 4)
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+# --------------------------------------------------------------- products
+def experts_case(E, N, K, S, g, empty=0.3, tail=0):
+    """Weights in MX4, and offsets of S slots over E experts, some without any,
+    the last `tail` slots without an expert."""
+    W = g.standard_normal((E, N, K)) * np.exp(0.5 * g.standard_normal((E, N, 1))) / np.sqrt(K)
+    codes, scales = omx4.quantize(W)
+    load = np.exp(g.standard_normal(E)) * (g.random(E) >= empty)
+    if not load.any():
+        load[-1] = 1
+    n = g.multinomial(S - tail, load / load.sum())
+    return codes, scales, omx4.dequantize(codes, scales), np.r_[0, np.cumsum(n)].astype(np.int32)
+
+
+def product_bound(W, X, offsets, rows, S, glu, out):
+    """Bound of the oracle's product: the sum of magnitudes times the terms."""
+    K = W.shape[2]
+    size = omx4.product(np.abs(W), np.abs(X), offsets, rows, S) * (K + 16) * U
+    y = omx4.product(W, X, offsets, rows, S)
+    if glu:
+        N = W.shape[1] // 2
+        eg, eu, g, u = size[:, :N], size[:, N:], y[:, :N], y[:, N:]
+        want = omx4.silu(g) * u
+        size = 1.1 * eg * (np.abs(u) + eu) + np.abs(omx4.silu(g)) * eu + np.abs(want) * 2.0 ** -20
+    else:
+        want = y
+    return want, size + (2.0 ** -8 * np.abs(want) if out == "bf16" else 0) + 1e-38
+
+
+SHAPES = [
+    # E, N, K, S, tail
+    (1, 16, 32, 1, 0), (1, 1, 32, 5, 0), (2, 33, 64, 7, 2), (4, 100, 160, 40, 0), (8, 64, 96, 3, 0),
+    (130, 24, 32, 300, 11), (3, 130, 288, 150, 0), (2, 264, 544, 401, 5), (5, 520, 128, 700, 0),
+    (1, 300, 1056, 129, 0), (2, 257, 320, 257, 1),
+]
+
+
+@pytest.mark.parametrize("form", ["bf16", "mx4"])
+@pytest.mark.parametrize("glu", [False, True])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_product(form, glu, shape):
+    E, N, K, S, tail = shape
+    g = np.random.default_rng([*shape, glu])
+    codes, scales, W, off = experts_case(E, N * (2 if glu else 1), K, S, g, tail=tail)
+    T = max(1, S // 2)
+    X = dev(g.standard_normal((T, K)).astype(np.float32)).to(torch.bfloat16)
+    rows = g.integers(0, T, S).astype(np.int32)
+    rows[::7] = T + 3  # (no such row: zero)
+    rows[3::11] = -1
+    XS = dev(g.standard_normal((S, K)).astype(np.float32)).to(torch.bfloat16)
+    for x, rw, out in ((X, rows, "f32"), (X, rows, "bf16"), (XS, None, "f32")):
+        kw = {"offsets": dev(off), "rows": None if rw is None else dev(rw), "glu": glu, "dtype": DT[out]}
+        if form == "mx4":
+            q = bm.mx4_quantize(x)
+            got = bm.mx4_product_q(dev(codes), dev(scales), *q, **kw)
+            x64 = omx4.dequantize(q[0].cpu().numpy(), q[1].cpu().numpy())
+        else:
+            got, x64 = bm.mx4_product(dev(codes), dev(scales), x, **kw), np64(x)
+        want, bound = product_bound(W, x64, off, rw, S, glu, out)
+        within(np64(got), want, bound, (form, glu, shape, out))
+        assert (got[off[-1]:] == 0).all()
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_product_grad(shape):
+    E, N, K, S, tail = shape
+    N = -(-N // 8) * 8
+    g = np.random.default_rng([*shape, 7])
+    codes, scales, W, off = experts_case(E, N, K, S, g, tail=tail)
+    dY = dev(g.standard_normal((S, N)).astype(np.float32)).to(torch.bfloat16)
+    for out in ("f32", "bf16"):
+        got = bm.mx4_product_grad(dev(codes), dev(scales), dY, offsets=dev(off), dtype=DT[out])
+        want = omx4.product_grad(W, np64(dY), off)
+        size = omx4.product_grad(np.abs(W), np.abs(np64(dY)), off) * (N + 16) * U
+        within(np64(got), want, size + (2.0 ** -8 * np.abs(want) if out == "bf16" else 0) + 1e-38, (shape, out))
+        assert (got[off[-1]:] == 0).all()
+
+
+def test_product_gradient_against_differences():
+    # the product is linear: <dy, f(x + h) - f(x)> = <dx, h>
+    g = np.random.default_rng(11)
+    codes, scales, W, off = experts_case(3, 96, 128, 50, g)
+    dY = torch.randn(50, 96, device=DEV).to(torch.bfloat16)
+    X, H = (torch.randint(-8, 9, (50, 128), device=DEV).to(torch.bfloat16) for _ in range(2))  # (X + H is exact)
+    f = lambda x: bm.mx4_product(dev(codes), dev(scales), x, offsets=dev(off), dtype=torch.float32).double()  # noqa: E731
+    dx = bm.mx4_product_grad(dev(codes), dev(scales), dY, offsets=dev(off), dtype=torch.float32).double()
+    got = ((f(X + H) - f(X)) * dY.double()).sum(1)
+    want = (dx * H.double()).sum(1)
+    size = omx4.product(np.abs(W), np.abs(np64(X)) + np.abs(np64(H)) + 8, off) * np.abs(np64(dY))
+    assert (np.abs(np64(got - want)) <= 4 * 150 * U * size.sum(1) + 1e-38).all()
+
+
+def test_products_of_strided_rows_scales_and_blocks_that_are_lost():
+    g = np.random.default_rng(12)
+    codes, scales, W, off = experts_case(2, 48, 128, 30, g, empty=0)
+    scales[0, 3, 1], scales[1, 5, 0], scales[1, 6, :] = 255, 0, 1  # lost; 2^-127; all but 0
+    W = omx4.dequantize(codes, scales)
+    wide = torch.randn(30, 192, device=DEV).to(torch.bfloat16)
+    x = wide[:, 64:]
+    got = bm.mx4_product(dev(codes), dev(scales), x, offsets=dev(off), dtype=torch.float32)
+    want, bound = product_bound(W, np64(x), off, None, 30, False, "f32")
+    # a weight below 2^-126 may count as 0 in a matrix core's sum
+    small = omx4.product((np.abs(W) < 2.0 ** -126) * np.nan_to_num(np.abs(W)), np.abs(np64(x)), off)
+    within(np64(got), want, np.nan_to_num(bound) + small, "strided")
+    back = bm.mx4_product_grad(dev(codes), dev(scales), wide[:, :48], offsets=dev(off), dtype=torch.float32)
+    want = omx4.product_grad(W, np64(wide[:, :48]), off)
+    size = omx4.product_grad(np.nan_to_num(np.abs(W)), np.abs(np64(wide[:, :48])), off)
+    within(np64(back), want, size * 64 * U + 1e-36, "strided grad")
+
+
+def test_product_with_offsets_that_are_no_offsets():
+    """Cut to [0, S]; nothing is read or written outside."""
+    g = np.random.default_rng(13)
+    codes, scales, W, _ = experts_case(3, 32, 64, 20, g)
+    X = torch.randn(20, 64, device=DEV).to(torch.bfloat16)
+    off = np.array([-5, 4, 4, 90], np.int32)
+    got = bm.mx4_product(dev(codes), dev(scales), X, offsets=dev(off), dtype=torch.float32)
+    want, bound = product_bound(W, np64(X), np.array([0, 4, 4, 20]), None, 20, False, "f32")
+    within(np64(got), want, bound, "cut")
+
+
+def test_products_of_no_slots_and_one_expert_without_offsets():
+    g = np.random.default_rng(14)
+    codes, scales, W, _ = experts_case(1, 40, 96, 9, g)
+    X = torch.randn(9, 96, device=DEV).to(torch.bfloat16)
+    got = bm.mx4_product(dev(codes), dev(scales), X, dtype=torch.float32)
+    want, bound = product_bound(W, np64(X), None, None, 9, False, "f32")
+    within(np64(got), want, bound, "dense")
+    assert bm.mx4_product(dev(codes), dev(scales), X[:0]).shape == (0, 40)
+    assert bm.mx4_product_grad(dev(codes), dev(scales), got[:0].to(torch.bfloat16)).shape == (0, 96)
+    none = torch.zeros(0, dtype=torch.int32, device=DEV)
+    assert bm.mx4_product(dev(codes), dev(scales), X, rows=none).shape == (0, 40)
+
+
+def test_product_past_32_bits():
+    """Codes of more than 2^32 bytes and rows past 2^31 entries."""
+    E, N, K = 320, 2048, 16384
+    codes = torch.zeros((E, N, K // 2), dtype=torch.uint8, device=DEV)
+    scales = torch.full((E, N, K // 32), 120, dtype=torch.uint8, device=DEV)
+    assert codes.numel() > 1 << 32
+    g = np.random.default_rng(15)
+    part = g.integers(0, 256, (N, K // 2), dtype=np.uint8)
+    ps = g.integers(115, 121, (N, K // 32), dtype=np.uint8)
+    codes[E - 1], scales[E - 1] = dev(part), dev(ps)
+    rows = (1 << 17) + 5
+    X = torch.zeros((rows, K), dtype=torch.bfloat16, device=DEV)
+    X[-3:] = torch.randn(3, K, device=DEV).to(torch.bfloat16)
+    off = np.zeros(E + 1, np.int32)
+    off[E] = 3
+    at = np.arange(rows - 3, rows, dtype=np.int32)
+    got = bm.mx4_product(codes, scales, X, offsets=dev(off), rows=dev(at), dtype=torch.float32)
+    W, x = omx4.dequantize(part, ps), np64(X[-3:])
+    within(np64(got), x @ W.T, np.abs(x) @ np.abs(W).T * (K + 16) * U, "far")
+    dY = torch.randn(3, N, device=DEV).to(torch.bfloat16)
+    back = bm.mx4_product_grad(codes, scales, dY, offsets=dev(off), dtype=torch.float32)
+    d = np64(dY)
+    within(np64(back), d @ W, np.abs(d) @ np.abs(W) * (N + 16) * U, "far grad")
+
+
+# ---------------------------------------------------------------- joining
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,k,d", [(1, 1, 8), (1, 8, 2048), (3, 2, 40), (130, 5, 264), (33, 64, 72), (9, 3, 8200)])
+def test_combine(dtype, T, k, d):
+    g = np.random.default_rng([T, k, d])
+    S = T * k
+    Z = dev(g.standard_normal((S, d)).astype(np.float32)).to(DT[dtype])
+    slots = g.permutation(S).astype(np.int32).reshape(T, k)
+    w = g.standard_normal((T, k)).astype(np.float32)
+    dY = dev(g.standard_normal((T, d)).astype(np.float32)).to(DT[dtype])
+    r = 2.0 ** -8 if dtype == "bf16" else 0
+    for ww in (w, None):
+        want = oroute.combine(np64(Z), slots, ww)
+        size = oroute.combine(np.abs(np64(Z)), slots, None if ww is None else np.abs(ww)) * (k + 2) * U
+        got = bm.combine(Z, dev(slots), None if ww is None else dev(ww))
+        assert got.dtype == DT[dtype]
+        within(np64(got), want, size + r * np.abs(want), "y")
+        dz, dw = bm.combine_grad(Z, dev(slots), None if ww is None else dev(ww), dY)
+        wz, wdw = oroute.combine_grad(np64(Z), slots, ww, np64(dY))
+        within(np64(dz), wz, (U + r) * np.abs(wz), "dz")
+        mags = oroute.combine_grad(np.abs(np64(Z)), slots, ww, np.abs(np64(dY)))[1]
+        within(np64(dw), wdw, mags * (d + 16) * U, "dw")
+
+
+def test_combine_of_slots_that_do_not_exist():
+    Z = torch.randn(6, 16, device=DEV)
+    slots = torch.tensor([[0, 6], [-1, 5], [2, -7], [1 << 30, -1]], dtype=torch.int32, device=DEV)
+    w = torch.rand(4, 2, device=DEV)
+    y = bm.combine(Z, slots, w)
+    within(np64(y), oroute.combine(np64(Z), slots.cpu().numpy(), np64(w)), 1e-6, "y")
+    dz, dw = bm.combine_grad(Z, slots, w, torch.ones(4, 16, device=DEV))
+    assert (dw[0, 1] == 0) and (dw[3] == 0).all() and torch.equal(dz[5], w[1, 1].expand(16))
+    assert bm.combine(Z[:0], slots, w).abs().max() == 0
+    assert bm.combine(Z, slots[:0]).shape == (0, 16)
+
+
+def test_combine_past_32_bits():
+    S, d = (1 << 18) + 2, 8448
+    Z = torch.zeros((S, d), dtype=torch.bfloat16, device=DEV)
+    Z[-2:] = torch.randn(2, d, device=DEV).to(torch.bfloat16)
+    slots = torch.tensor([[S - 2, S - 1]], dtype=torch.int32, device=DEV)
+    w = torch.tensor([[0.25, 0.5]], device=DEV)
+    want = 0.25 * np64(Z[-2]) + 0.5 * np64(Z[-1])
+    within(np64(bm.combine(Z, slots, w))[0], want, 2.0 ** -7 * np.abs(want) + 1e-6, "far")
+
+
+# --------------------------------------------------------------- together
+def layer_case(T, E, k, N, K, seed):
+    g = np.random.default_rng(seed)
+    ws = [dev((g.standard_normal(s) / np.sqrt(s[2])).astype(np.float32)).to(torch.bfloat16)
+          for s in ((E, N, K), (E, N, K), (E, K, N))]
+    x = dev(g.standard_normal((T, K)).astype(np.float32)).to(torch.bfloat16)
+    logits = dev(g.standard_normal((T, E)).astype(np.float32))
+    valid = dev(g.random(T) < 0.8)
+    return pipeline.mx4_experts(*ws), x, logits, valid
+
+
+def oracle_layer(ex, x, logits, k, valid):
+    r = oroute.route(np64(logits), k, valid.cpu().numpy())
+    up = omx4.dequantize(ex.up_codes.cpu().numpy(), ex.up_scales.cpu().numpy())
+    down = omx4.dequantize(ex.down_codes.cpu().numpy(), ex.down_scales.cpu().numpy())
+    h = omx4.product(up, np64(x), r["offsets"], r["rows"], glu=True)
+    z = omx4.product(down, h, r["offsets"])
+    return oroute.combine(z, r["slots"], r["weights"]), r, up, down, z
+
+
+@pytest.mark.parametrize("T,E,k,N,K", [(1, 8, 2, 64, 96), (50, 12, 3, 96, 160)])
+def test_layer_and_its_gradients(T, E, k, N, K):
+    ex, x, logits, valid = layer_case(T, E, k, N, K, 21)
+    valid[0] = True
+    y, r = pipeline.mx4_layer(x, logits, ex, k, valid=valid)
+    want, wr, up, down, z = oracle_layer(ex, x, logits, k, valid)
+    assert (r.experts.cpu().numpy() == wr["experts"]).all()
+    rel = lambda a, b: np.linalg.norm(np64(a) - b) / max(np.linalg.norm(b), 1e-30)  # noqa: E731
+    # three roundings to bf16 (h, z, y), 2^-9 each at most: 2^-7 of the norm
+    assert rel(y, want) < 2.0 ** -7
+    # MX4 tokens: an entry is off by a quarter of itself at most, and a sum's errors partly cancel
+    yq, _ = pipeline.mx4_layer(x, logits, ex, k, valid=valid, quantize_tokens=True)
+    assert rel(yq, want) < 0.5
+    yt, _, saved = pipeline.mx4_layer(x, logits, ex, k, valid=valid, train=True)
+    assert rel(yt, want) < 2.0 ** -7
+    dy = torch.randn(T, K, device=DEV).to(torch.bfloat16)
+    dl = np.array([0.3, 0.1])
+    dx, dlogits = pipeline.mx4_layer_grad(saved, ex, dy, dlosses=dev(dl, torch.float32))
+    dz, dw = oroute.combine_grad(z, wr["slots"], wr["weights"], np64(dy))
+    dh = omx4.product_grad(down, dz, wr["offsets"])
+    gu = omx4.product(up, np64(x), wr["offsets"], wr["rows"])
+    gg, uu = gu[:, :N], gu[:, N:]
+    sig = 1 / (1 + np.exp(-gg))
+    dgu = np.concatenate((dh * uu * sig * (1 + gg * (1 - sig)), dh * gg * sig), 1)
+    assert rel(dx, oroute.combine(omx4.product_grad(up, dgu, wr["offsets"]), wr["slots"])) < 2.0 ** -6
+    assert rel(dlogits, oroute.route_grad(np64(logits), wr, dw, dl)) < 2.0 ** -6
+
+
+def test_layer_on_another_stream_and_in_a_graph():
+    ex, x, logits, valid = layer_case(24, 10, 2, 64, 128, 22)
+    want, _ = pipeline.mx4_layer(x, logits, ex, 2, valid=valid)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got, _ = pipeline.mx4_layer(x, logits, ex, 2, valid=valid)
+    side.synchronize()
+    assert torch.equal(got, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, _ = pipeline.mx4_layer(x, logits, ex, 2, valid=valid)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    for _ in range(4):
+        x.copy_(torch.randn(x.shape, generator=g, device=DEV))
+        logits.copy_(torch.randn(logits.shape, generator=g, device=DEV))
+        graph.replay()
+        eager, _ = pipeline.mx4_layer(x, logits, ex, 2, valid=valid)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)
+
+
+# --------------------------------------------------------------- refusals
+def test_refusals():
+    x = torch.randn(4, 64, device=DEV)
+    h = x.to(torch.bfloat16)
+    codes, scales = bm.mx4_quantize(torch.randn(2, 16, 64, device=DEV))
+    off = torch.tensor([0, 2, 4], dtype=torch.int32, device=DEV)
+
+    def refused(code, f, *a, **kw):
+        with pytest.raises((bm.BitsmoeError, ValueError, TypeError)) as e:
+            f(*a, **kw)
+        if code:
+            assert isinstance(e.value, bm.BitsmoeError) and e.value.code == code, e.value
+
+    refused("ERR_SHAPE", bm.route, x, 65)                        # k > E
+    refused("ERR_ARG", bm.route, x, 0)
+    refused("ERR_SHAPE", bm.route, torch.zeros(2, 5000, device=DEV), 2)
+    refused(None, bm.route, x.half(), 2)
+    refused(None, bm.route, x, 2, valid=torch.ones(5, dtype=torch.bool, device=DEV))
+    refused(None, bm.route, x.t(), 2)
+    refused("ERR_ARG", bm.route, x[:, 1:], 2)                    # not 16-byte aligned
+    refused(None, bm.mx4_quantize, x[:, :40])                    # not whole blocks
+    refused(None, bm.mx4_quantize, x.double())
+    refused("ERR_SHAPE", bm.mx4_quantize, torch.zeros(3, 34, device=DEV)[:, :32])  # rows 136 bytes apart
+    refused(None, bm.mx4_dequantize, codes, scales[:1])
+    refused(None, bm.mx4_dequantize, codes, scales, dtype=torch.float16)
+    refused("ERR_DTYPE", bm.mx4_product, codes, scales, x, offsets=off)
+    refused("ERR_ARG", bm.mx4_product, codes, scales, h)         # two experts, no offsets
+    refused(None, bm.mx4_product, codes, scales, h[:, :32], offsets=off)
+    refused(None, bm.mx4_product, codes, scales, h, offsets=off[:2])
+    refused(None, bm.mx4_product, codes, scales, h, offsets=off.long())
+    refused(None, bm.mx4_product, codes[:, :15].contiguous(), scales[:, :15].contiguous(), h, offsets=off, glu=True)
+    refused(None, bm.mx4_product_q, codes, scales, codes[0, :, :16].contiguous(), scales[0, :, :1].contiguous(),
+            offsets=off)
+    refused("ERR_SHAPE", bm.mx4_product, codes, scales, torch.zeros(4, 68, device=DEV).to(torch.bfloat16)[:, :64],
+            offsets=off)                                         # rows 136 bytes apart
+    refused(None, bm.mx4_product_grad, codes, scales, h, offsets=off)   # N is 16, not 64
+    c9, s9 = codes[:, :9].contiguous(), scales[:, :9].contiguous()
+    refused("ERR_SHAPE", bm.mx4_product_grad, c9, s9, torch.zeros(4, 9, device=DEV).to(torch.bfloat16), offsets=off)
+    refused("ERR_SHAPE", bm.combine, torch.zeros(4, 12, device=DEV), off[None, :2].contiguous())
+    refused(None, bm.combine, x, off[None, :2].long())
+    refused(None, bm.combine, x, off[None, :2].contiguous(), torch.ones(1, 3, device=DEV))
+    refused(None, bm.combine_grad, x, off[None, :2].contiguous(), None, h[:1])
