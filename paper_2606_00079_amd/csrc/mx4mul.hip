@@ -177,6 +177,275 @@ __global__ __launch_bounds__(kThreads) void mx4_rows_kernel(MulArgs a) {
   if (slot < t.hi && n < a.N) store4(a, slot, n, a.N, wide, acc[0]);
 }
 
+// ---------------------------------------------------------------------------
+// Large tiles: TM slots x 256 outputs a workgroup of eight waves.
+//
+// K advances KS entries at a time through kStages LDS stages that direct
+// global->LDS loads fill (16 bytes a lane for codes and tokens, one byte a lane,
+// widened to a word, for scales): codes stay four bits wide up to the registers.
+// Wave (wm, wn) of 2 x 4 owns TM/2 slots x 64 outputs as 32 x 32 accumulators,
+// the weights on the matrix core's row side, so that a lane holds runs of four
+// outputs of one slot.  With bf16 tokens a wave widens each fragment of codes
+// once (exact) and uses it for its TM/64 blocks of slots; with MX4 tokens the
+// scaled matrix-core form takes codes and scales as they lie.
+// ---------------------------------------------------------------------------
+constexpr int kTileThreads = 512, kWaves = 8, kTN = 256;
+
+template <bool MX, int TM_>
+struct Shape {
+  static constexpr int TM = TM_;
+  static constexpr int KS = MX ? 128 : 64;   // entries of K a step
+  static constexpr int XB = MX ? 64 : 128;   // bytes of a token's row in a stage
+  static constexpr int WB = KS / 2;          // bytes of a weight row in a stage
+  static constexpr int SC = KS / 32;         // scales of a row in a stage (a word each)
+  static constexpr int kX = 0, kW = TM * XB, kWS = kW + kTN * WB, kXS = kWS + kTN * SC * 4;
+  static constexpr int kStage = kXS + (MX ? TM * SC * 4 : 0);
+  static constexpr int kFit = 163840 / kStage;
+  static constexpr int kStages = kFit < 5 ? kFit : 5;
+  // direct loads of a wave for a stage
+  static constexpr int LX = TM * XB / 1024 / kWaves, LW = kTN * WB / 1024 / kWaves;
+  static constexpr int LWS = kTN * SC / 64 / kWaves, LXS = MX ? TM * SC / 64 / kWaves : 0;
+  static constexpr int kLoads = LX + LW + LWS + LXS;
+  static constexpr int MB = TM / 64, NB = 2;
+  static_assert(kStages >= 3 && (kStages - 2) * kLoads < 64);
+};
+
+// What lanes past the end of a row read: zeros, and scales of 1.
+__device__ const uint8_t kPad[32] __attribute__((aligned(16))) = {
+    0,   0,   0,   0,   0,   0,   0,   0,   0,   0,   0,   0,   0,   0,   0,   0,
+    127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127};
+
+// One wave-wide direct load: lane l's 16 bytes (or byte) at p go to lds + 16 l
+// (lds + 4 l, as a word).  `lds` is wave-uniform.  The compiler does not track
+// it: callers wait by count (wait_loads) and synchronize before the data is read.
+__device__ __forceinline__ void load_lds16(const void* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p),
+               "s"(__builtin_amdgcn_readfirstlane(lds))
+               : "memory");
+}
+__device__ __forceinline__ void load_lds1(const void* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_ubyte %0, off" ::"v"(p),
+               "s"(__builtin_amdgcn_readfirstlane(lds))
+               : "memory");
+}
+// Waits until at most N of this wave's loads, and none of its LDS reads, are
+// under way, and for the workgroup.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// Slot of 16-byte chunk c of row r in a stage whose rows have `chunks` of them:
+// sixteen rows read at the same chunk (what the LDS serves together) then lie in
+// different banks.
+template <int chunks>
+__device__ __forceinline__ int chunk_slot(int r, int c) {
+  return c ^ ((r / (16 / chunks)) & (chunks - 1));
+}
+
+template <bool MX, bool GLU, int TM>
+__global__ __launch_bounds__(kTileThreads) void mx4_tile_kernel(MulArgs a) {
+  using H = Shape<MX, TM>;
+  extern __shared__ __align__(16) char smem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int TNO = GLU ? kTN / 2 : kTN;  // results a tile has of a slot
+  const int64_t ntiles = (a.N + TNO - 1) / TNO;
+  const int64_t g = blockIdx.x / ntiles, n0 = (blockIdx.x - g * ntiles) * TNO;
+  Tile t;
+  if (!find_tile(a.offsets, a.E, a.S, g, TM, &t)) return;
+  const int wm = wave >> 2, wn = wave & 3, r32 = lane & 31, half = lane >> 5;
+  f32x16 acc[H::NB][H::MB];
+#pragma unroll
+  for (int i = 0; i < H::NB; ++i)
+#pragma unroll
+    for (int j = 0; j < H::MB; ++j)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.0f;
+
+  if (t.e < a.E) {
+    const int64_t kb = a.K / 32;
+    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
+    // this lane's addresses in the first stage, and how far along K it is there
+    auto token = [&](int r) {  // row of X of the tile's slot r (slots past the tile: its last; no such row: row 0)
+      const int64_t s = min(t.lo + r, t.hi - 1);
+      const int64_t row = a.rows ? static_cast<int64_t>(a.rows[s]) : s;
+      return row >= 0 && row < a.x_rows ? row : int64_t(0);
+    };
+    auto weight = [&](int r) {  // row of W of the tile's output row r
+      int64_t n;
+      if constexpr (GLU) {
+        n = min(n0 + (r >> 6) * 32 + (r & 31), a.N - 1) + ((r >> 5) & 1) * a.N;
+        return static_cast<int64_t>(t.e) * 2 * a.N + n;
+      } else {
+        n = min(n0 + r, a.N - 1);
+        return static_cast<int64_t>(t.e) * a.N + n;
+      }
+    };
+    const char *px[H::LX], *pw[H::LW], *pws[H::LWS], *pxs[MX ? H::LXS : 1];
+    int kx[H::LX], kw[H::LW], kws, kxs = 0;
+    constexpr int XC = H::XB / 16, WC = H::WB / 16;
+#pragma unroll
+    for (int q = 0; q < H::LX; ++q) {
+      const int r = (wave + kWaves * q) * (64 / XC) + lane / XC;
+      const int c = chunk_slot<XC>(r, lane % XC);
+      kx[q] = c * (MX ? 32 : 8);
+      px[q] = MX ? reinterpret_cast<const char*>(a.xcodes + token(r) * kb * 16 + c * 16)
+                 : reinterpret_cast<const char*>(a.x + token(r) * a.ldx + c * 8);
+    }
+#pragma unroll
+    for (int q = 0; q < H::LW; ++q) {
+      const int r = (wave + kWaves * q) * (64 / WC) + lane / WC;
+      const int c = chunk_slot<WC>(r, lane % WC);
+      kw[q] = c * 32;
+      pw[q] = reinterpret_cast<const char*>(a.codes + weight(r) * kb * 16 + c * 16);
+    }
+#pragma unroll
+    for (int q = 0; q < H::LWS; ++q)
+      pws[q] = reinterpret_cast<const char*>(
+          a.scales + weight((wave + kWaves * q) * (64 / H::SC) + lane / H::SC) * kb + lane % H::SC);
+    kws = (lane % H::SC) * 32;
+    if constexpr (MX) {
+#pragma unroll
+      for (int q = 0; q < H::LXS; ++q)
+        pxs[q] = reinterpret_cast<const char*>(
+            a.xscales + token((wave + kWaves * q) * (64 / H::SC) + lane / H::SC) * kb + lane % H::SC);
+      kxs = kws;
+    }
+    const int nk = static_cast<int>((a.K + H::KS - 1) / H::KS);
+    const int last = static_cast<int>(a.K - static_cast<int64_t>(nk - 1) * H::KS);  // entries of the last step
+    int issued = 0, to = 0;
+    auto issue = [&]() {  // the next stage's loads
+      const uint32_t s = lds0 + to * H::kStage;
+      if (issued == nk - 1 && last < H::KS) {
+#pragma unroll
+        for (int q = 0; q < H::LX; ++q) px[q] = kx[q] < last ? px[q] : reinterpret_cast<const char*>(kPad);
+#pragma unroll
+        for (int q = 0; q < H::LW; ++q) pw[q] = kw[q] < last ? pw[q] : reinterpret_cast<const char*>(kPad);
+#pragma unroll
+        for (int q = 0; q < H::LWS; ++q) pws[q] = kws < last ? pws[q] : reinterpret_cast<const char*>(kPad + 16);
+        if constexpr (MX) {
+#pragma unroll
+          for (int q = 0; q < H::LXS; ++q) pxs[q] = kxs < last ? pxs[q] : reinterpret_cast<const char*>(kPad + 16);
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < H::LX; ++q) {
+        load_lds16(px[q], s + H::kX + (wave + kWaves * q) * 1024);
+        px[q] += H::XB;
+      }
+#pragma unroll
+      for (int q = 0; q < H::LW; ++q) {
+        load_lds16(pw[q], s + H::kW + (wave + kWaves * q) * 1024);
+        pw[q] += H::WB;
+      }
+#pragma unroll
+      for (int q = 0; q < H::LWS; ++q) {
+        load_lds1(pws[q], s + H::kWS + (wave + kWaves * q) * 256);
+        pws[q] += H::SC;
+      }
+      if constexpr (MX) {
+#pragma unroll
+        for (int q = 0; q < H::LXS; ++q) {
+          load_lds1(pxs[q], s + H::kXS + (wave + kWaves * q) * 256);
+          pxs[q] += H::SC;
+        }
+      }
+      ++issued;
+      to = to + 1 == H::kStages ? 0 : to + 1;
+    };
+    for (int i = 0; i < H::kStages - 1 && i < nk; ++i) issue();
+    int from = 0;
+    const int wrow = wn * 64 + r32, xrow = wm * (TM / 2) + r32;
+    for (int i = 0; i < nk; ++i) {
+      // stage i has landed once all loads but those of the kStages - 2 stages after it have
+      if (issued - 1 - i >= H::kStages - 2)
+        wait_loads<(H::kStages - 2) * H::kLoads>();
+      else
+        wait_loads<0>();
+      // every wave is past stage i - 1 here: its buffer is free
+      if (issued < nk) issue();
+      const char* s = smem + from * H::kStage;
+      from = from + 1 == H::kStages ? 0 : from + 1;
+      if constexpr (MX) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {  // 64 entries: chunk 2u + half of a row
+          i32x8 wf[H::NB], xf[H::MB];
+          int ws[H::NB], xs[H::MB];
+#pragma unroll
+          for (int n = 0; n < H::NB; ++n) {
+            const int r = wrow + 32 * n;
+            const uint4 v = *reinterpret_cast<const uint4*>(s + H::kW + r * H::WB + chunk_slot<4>(r, 2 * u + half) * 16);
+            wf[n] = i32x8{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0};
+            ws[n] = *reinterpret_cast<const int*>(s + H::kWS + (r * H::SC + 2 * u + half) * 4);
+          }
+#pragma unroll
+          for (int m = 0; m < H::MB; ++m) {
+            const int r = xrow + 32 * m;
+            const uint4 v = *reinterpret_cast<const uint4*>(s + H::kX + r * H::XB + chunk_slot<4>(r, 2 * u + half) * 16);
+            xf[m] = i32x8{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0};
+            xs[m] = *reinterpret_cast<const int*>(s + H::kXS + (r * H::SC + 2 * u + half) * 4);
+          }
+#pragma unroll
+          for (int n = 0; n < H::NB; ++n)
+#pragma unroll
+            for (int m = 0; m < H::MB; ++m)
+              acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[n], xf[m], acc[n][m], 4, 4, 0, ws[n], 0,
+                                                                          xs[m]);
+        }
+      } else {
+        uint32_t wc[H::NB][4];
+        float sc[H::NB];
+#pragma unroll
+        for (int n = 0; n < H::NB; ++n) {
+          const int r = wrow + 32 * n;
+          const uint4 v = *reinterpret_cast<const uint4*>(s + H::kW + r * H::WB + chunk_slot<2>(r, half) * 16);
+          wc[n][0] = v.x, wc[n][1] = v.y, wc[n][2] = v.z, wc[n][3] = v.w;
+          sc[n] = mx4_scale(*reinterpret_cast<const uint32_t*>(s + H::kWS + (r * H::SC + half) * 4));
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {  // entries 32 half + 8 j + 0 .. 7 of the step
+          bf16x8 xf[H::MB];
+#pragma unroll
+          for (int m = 0; m < H::MB; ++m) {
+            const int r = xrow + 32 * m;
+            xf[m] = *reinterpret_cast<const bf16x8*>(s + H::kX + r * H::XB + chunk_slot<8>(r, 4 * half + j) * 16);
+          }
+#pragma unroll
+          for (int n = 0; n < H::NB; ++n) {
+            const bf16x8 wf = mx4_bf16(wc[n][j], sc[n]);
+#pragma unroll
+            for (int m = 0; m < H::MB; ++m)
+              acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf, xf[m], acc[n][m], 0, 0, 0);
+          }
+        }
+      }
+    }
+  }
+
+  const bool wide = a.ldy % 4 == 0;
+#pragma unroll
+  for (int m = 0; m < H::MB; ++m) {
+    const int64_t slot = t.lo + wm * (TM / 2) + 32 * m + r32;
+    if (slot >= t.hi) continue;
+    bool have = true;
+    if (t.e < a.E && a.rows) have = a.rows[slot] >= 0 && a.rows[slot] < a.x_rows;
+#pragma unroll
+    for (int n = 0; n < (GLU ? 1 : H::NB); ++n)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[i] = acc[n][m][4 * q + i];
+          if constexpr (GLU) v[i] = silu(v[i]) * acc[1][m][4 * q + i];
+          v[i] = have ? v[i] : 0.0f;
+        }
+        const int64_t at = n0 + wn * (GLU ? 32 : 64) + 32 * n + 8 * q + 4 * half;
+        if (at < a.N) store4(a, slot, at, a.N, wide, v);
+      }
+  }
+}
+
 // dx: 64 columns x 16 slots a workgroup, 16 columns a wave.  The weights' tile
 // (32 rows x 64 columns) is widened to bf16 and transposed in LDS.
 __global__ __launch_bounds__(kThreads) void mx4_grad_kernel(MulArgs a) {
@@ -244,12 +513,37 @@ bool grid_of(const MulArgs& a, int64_t tile, int64_t per, unsigned* grid) {
   return true;
 }
 
+// Large tiles pay from about this many slots an expert on.
+constexpr int64_t kTileSlots = 32;
+
+template <bool MX, bool GLU, int TM>
+bitsmoe_status tile_product(const char* who, const MulArgs& a, hipStream_t s) {
+  using H = Shape<MX, TM>;
+  constexpr int TNO = GLU ? kTN / 2 : kTN;
+  unsigned grid;
+  if (!grid_of(a, TM, (a.N + TNO - 1) / TNO, &grid))
+    return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": too many slots and outputs for one call");
+  constexpr int lds = H::kStages * H::kStage;
+  auto* fn = mx4_tile_kernel<MX, GLU, TM>;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return device_error("mx4_product: shared memory", e);
+  fn<<<grid, kTileThreads, lds, s>>>(a);
+  BITSMOE_LAUNCH_CHECK("mx4_tile_kernel");
+  return ok();
+}
+
 bitsmoe_status product(const char* who, const MulArgs& a, bool glu, hipStream_t s) {
+  const bool mx = a.xcodes != nullptr;
+  if (a.S >= kTileSlots * a.E && a.x_rows > 0) {
+    if (mx) return glu ? tile_product<true, true, 128>(who, a, s) : tile_product<true, false, 128>(who, a, s);
+    return glu ? tile_product<false, true, 128>(who, a, s) : tile_product<false, false, 128>(who, a, s);
+  }
   unsigned grid;
   if (!grid_of(a, 16, (a.N + 15) / 16, &grid))
     return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": too many slots and outputs for one call");
-  auto* fn = a.xcodes ? (glu ? mx4_rows_kernel<true, true> : mx4_rows_kernel<true, false>)
-                      : (glu ? mx4_rows_kernel<false, true> : mx4_rows_kernel<false, false>);
+  auto* fn = mx ? (glu ? mx4_rows_kernel<true, true> : mx4_rows_kernel<true, false>)
+                : (glu ? mx4_rows_kernel<false, true> : mx4_rows_kernel<false, false>);
   fn<<<grid, kThreads, 0, s>>>(a);
   BITSMOE_LAUNCH_CHECK("mx4_rows_kernel");
   return ok();
