@@ -487,6 +487,160 @@ __global__ __launch_bounds__(kThreads) void mx4_grad_kernel(MulArgs a) {
   if (slot < t.hi && k < a.K) store4(a, slot, k, a.K, a.ldy % 4 == 0, acc);
 }
 
+// ---------------------------------------------------------------------------
+// dx in large tiles: 128 slots x 256 columns a workgroup of eight waves, n
+// advancing 64 rows of W a step.  The sum runs over W's rows, along which its
+// scales change, so the codes of a step (64 rows x 256 columns, loaded as the
+// forward form loads them) are widened to bf16 once by the whole workgroup, one
+// block of 32 a thread, into an LDS tile that the transposing LDS read takes
+// the fragments from.  Two such tiles: the next step is widened while this one
+// is multiplied.
+// ---------------------------------------------------------------------------
+struct GradShape {
+  static constexpr int TM = 128, KT = 256, NS = 64;  // slots, columns, rows of W a step
+  static constexpr int kX = 0, kW = TM * NS * 2, kWS = kW + NS * KT / 2, kStage = kWS + NS * (KT / 32) * 4;
+  static constexpr int kStages = 3;
+  static constexpr int kTile = NS * KT * 2;
+  static constexpr int kBytes = kStages * kStage + 2 * kTile;
+  static constexpr int LX = 2, kLoads = LX + 2;
+  static constexpr int MB = 2, NB = 2;
+};
+static_assert(GradShape::kBytes <= 163840);
+
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+__device__ __forceinline__ s16x4 read_transposed(const char* p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (__attribute__((address_space(3))) s16x4*)(reinterpret_cast<uintptr_t>(p)));
+}
+
+__global__ __launch_bounds__(kTileThreads) void mx4_grad_tile_kernel(MulArgs a) {
+  using H = GradShape;
+  extern __shared__ __align__(16) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t ktiles = (a.K + H::KT - 1) / H::KT;
+  const int64_t g = blockIdx.x / ktiles, k0 = (blockIdx.x - g * ktiles) * H::KT;
+  Tile t;
+  if (!find_tile(a.offsets, a.E, a.S, g, H::TM, &t)) return;
+  const int wm = wave >> 2, wn = wave & 3, r32 = lane & 31, half = lane >> 5;
+  f32x16 acc[H::NB][H::MB];
+#pragma unroll
+  for (int i = 0; i < H::NB; ++i)
+#pragma unroll
+    for (int j = 0; j < H::MB; ++j)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.0f;
+
+  if (t.e < a.E) {
+    const int64_t kb = a.K / 32;
+    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
+    char* wide = smem + H::kStages * H::kStage;
+    const char *px[H::LX], *pw, *ps;
+    int nx[H::LX];
+#pragma unroll
+    for (int q = 0; q < H::LX; ++q) {
+      const int r = (wave + kWaves * q) * 8 + lane / 8, c = chunk_slot<8>(r, lane % 8);
+      nx[q] = 8 * c;
+      px[q] = reinterpret_cast<const char*>(a.x + min(t.lo + r, t.hi - 1) * a.ldx + 8 * c);
+    }
+    // codes and scales of row wave * 8 + lane / 8 of a step, block lane % 8 of the tile
+    const int wr = wave * 8 + lane / 8;
+    const int64_t block = min(k0 / 32 + lane % 8, kb - 1);
+    pw = reinterpret_cast<const char*>(a.codes + ((static_cast<int64_t>(t.e) * a.N + wr) * kb + block) * 16);
+    ps = reinterpret_cast<const char*>(a.scales + (static_cast<int64_t>(t.e) * a.N + wr) * kb + block);
+    const int64_t wstep = H::NS * kb * 16, sstep = H::NS * kb;
+    const int nk = static_cast<int>((a.N + H::NS - 1) / H::NS);
+    const int last = static_cast<int>(a.N - static_cast<int64_t>(nk - 1) * H::NS);
+    int issued = 0, to = 0;
+    auto issue = [&]() {
+      const uint32_t s = lds0 + to * H::kStage;
+      if (issued == nk - 1 && last < H::NS) {
+#pragma unroll
+        for (int q = 0; q < H::LX; ++q) px[q] = nx[q] < last ? px[q] : reinterpret_cast<const char*>(kPad);
+        pw = wr < last ? pw : reinterpret_cast<const char*>(kPad);
+        ps = wr < last ? ps : reinterpret_cast<const char*>(kPad + 16);
+      }
+#pragma unroll
+      for (int q = 0; q < H::LX; ++q) {
+        load_lds16(px[q], s + H::kX + (wave + kWaves * q) * 1024);
+        px[q] += H::NS * 2;
+      }
+      load_lds16(pw, s + H::kW + wave * 1024);
+      load_lds1(ps, s + H::kWS + wave * 256);
+      pw += wstep;
+      ps += sstep;
+      ++issued;
+      to = to + 1 == H::kStages ? 0 : to + 1;
+    };
+    // this thread's block of stage `s`, widened into row wr of tile `w`
+    auto widen = [&](const char* s, char* w) {
+      const uint4 c = *reinterpret_cast<const uint4*>(s + H::kW + tid * 16);
+      const float scale = mx4_scale(*reinterpret_cast<const uint32_t*>(s + H::kWS + tid * 4));
+      const uint32_t d[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)  // 16-byte chunk 4 (lane % 8) + i of the row
+        *reinterpret_cast<uint4*>(w + wr * (H::KT * 2) + ((4 * (lane % 8) + i) ^ (4 * (wr & 3))) * 16) =
+            mx4_bf16_words(d[i], scale);
+    };
+    for (int i = 0; i < H::kStages - 1 && i < nk; ++i) issue();
+    if (issued > 1)
+      wait_loads<H::kLoads>();
+    else
+      wait_loads<0>();
+    widen(smem, wide);
+    const int xrow = wm * (H::TM / 2) + r32;
+    int from = 0;
+    for (int i = 0; i < nk; ++i) {
+      // step i + 1 has landed, step i is widened, and every wave is past step i - 1
+      wait_loads<0>();
+      if (issued < nk) issue();
+      const char* s = smem + from * H::kStage;
+      from = from + 1 == H::kStages ? 0 : from + 1;
+      if (i + 1 < nk) widen(smem + from * H::kStage, wide + ((i + 1) & 1) * H::kTile);
+      const char* w = wide + (i & 1) * H::kTile;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {  // 16 rows of W
+        bf16x8 xf[H::MB];
+#pragma unroll
+        for (int m = 0; m < H::MB; ++m) {
+          const int r = xrow + 32 * m;
+          xf[m] = *reinterpret_cast<const bf16x8*>(s + H::kX + r * (H::NS * 2) + chunk_slot<8>(r, 2 * j + half) * 16);
+        }
+#pragma unroll
+        for (int n = 0; n < H::NB; ++n) {
+          // rows 16 j + 8 half + 4 q + (lane % 16) / 4, column 16 ((lane / 16) % 2) + 4 (lane % 4) of the block
+          const int col = wn * 64 + 32 * n + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+          s16x4 h[2];
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const int r = 16 * j + 8 * half + 4 * q + ((lane & 15) >> 2);
+            h[q] = read_transposed(w + r * (H::KT * 2) + (((col >> 3) ^ (4 * (r & 3))) << 4) + (col & 7) * 2);
+          }
+          const bf16x8 wf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+          for (int m = 0; m < H::MB; ++m)
+            acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf, xf[m], acc[n][m], 0, 0, 0);
+        }
+      }
+    }
+  }
+  const bool aligned = a.ldy % 4 == 0;
+#pragma unroll
+  for (int m = 0; m < H::MB; ++m) {
+    const int64_t slot = t.lo + wm * (H::TM / 2) + 32 * m + r32;
+    if (slot >= t.hi) continue;
+#pragma unroll
+    for (int n = 0; n < H::NB; ++n)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = acc[n][m][4 * q + i];
+        const int64_t at = k0 + wn * 64 + 32 * n + 8 * q + 4 * half;
+        if (at < a.K) store4(a, slot, at, a.K, aligned, v);
+      }
+  }
+}
+
 bitsmoe_status check(const char* who, const MulArgs& a, bitsmoe_dtype yt, int64_t wide) {
   const std::string w(who);
   if (a.E <= 0 || a.N <= 0 || a.K <= 0 || a.S < 0 || a.x_rows < 0)
@@ -600,6 +754,16 @@ extern "C" bitsmoe_status bitsmoe_mx4_product_grad(const uint8_t* codes_dev, con
   if (S == 0) return ok();
   if (!dY_dev) return fail(BITSMOE_ERR_ARG, "mx4_product_grad: null pointer");
   unsigned grid;
+  if (S >= kTileSlots * E) {
+    if (!grid_of(a, GradShape::TM, (K + GradShape::KT - 1) / GradShape::KT, &grid))
+      return fail(BITSMOE_ERR_SHAPE, "mx4_product_grad: too many slots and columns for one call");
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(mx4_grad_tile_kernel),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, GradShape::kBytes);
+    if (e != hipSuccess) return device_error("mx4_product_grad: shared memory", e);
+    mx4_grad_tile_kernel<<<grid, kTileThreads, GradShape::kBytes, static_cast<hipStream_t>(stream)>>>(a);
+    BITSMOE_LAUNCH_CHECK("mx4_grad_tile_kernel");
+    return ok();
+  }
   if (!grid_of(a, 16, (K + 63) / 64, &grid))
     return fail(BITSMOE_ERR_SHAPE, "mx4_product_grad: too many slots and columns for one call");
   mx4_grad_kernel<<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
