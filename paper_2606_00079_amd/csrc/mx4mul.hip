@@ -33,42 +33,76 @@ struct MulArgs {
   int yf32;
 };
 
-// The slots of one workgroup: `lo` .. `hi` of expert e, at most `tile` of
-// them.  Experts' runs are cut into tiles from their first slot on, tile g of
-// all is looked for; e = E holds the slots of no expert, whose results are
-// zero.  Every wave looks by itself, 64 experts at a time.
+// Inclusive sums over the wave (a step inside a row of 16 lanes shifts by 1, 2,
+// 4, 8; then a row's last lane is added to the next row, and lane 31 to the
+// upper half).
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+  return v;
+}
+__device__ __forceinline__ int lane_value(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
+
+// The slots of one workgroup, `lo` .. `hi` of expert e, and its column tile.
+// Each expert's slots are cut into tiles of `tile` from its first on; e = E
+// holds the slots of no expert, whose results are zero.
+//
+// Workgroup ids go to the eight XCDs in turn; each XCD gets a contiguous range of
+// the tiles that exist (ids past them find none), ordered by expert, and there
+// up to eight slot tiles of a column tile in a row: the workgroups that run on
+// an XCD at a time share weights and tokens in its L2.  Every wave looks by
+// itself: a lane sums up a run of experts, the waves' sums tell the run, and a
+// second pass of one expert a lane the expert.
 struct Tile {
-  int e, lo, hi;
+  int e, lo, hi, col;
 };
-__device__ __forceinline__ bool find_tile(const int32_t* offsets, int E, int64_t S, int64_t g, int tile, Tile* out) {
+__device__ __forceinline__ int slots_of(const int32_t* offsets, int E, int S, int e, int* lo) {
+  *lo = offsets ? min(max(offsets[e], 0), S) : (e == 0 ? 0 : S);
+  return (e < E && offsets ? min(max(offsets[e + 1], *lo), S) : S) - *lo;
+}
+__device__ __forceinline__ bool find_tile(const int32_t* offsets, int E, int64_t S, int cols, int tile, Tile* out) {
   const int s = static_cast<int>(S), lane = threadIdx.x & 63;
-  int64_t before = 0;
-  for (int base = 0; base <= E; base += 64) {
-    const int e = base + lane;
-    int lo = 0, hi = 0;
-    if (e <= E) {
-      lo = offsets ? min(max(offsets[e], 0), s) : (e == 0 ? 0 : s);
-      hi = e < E && offsets ? min(max(offsets[e + 1], lo), s) : s;
-    }
-    const int tiles = (hi - lo + tile - 1) / tile;
-    int inc = tiles;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int u = __shfl_up(inc, o, 64);
-      if (lane >= o) inc += u;
-    }
-    const uint64_t hit = __ballot(before + inc > g);
-    if (hit) {
-      const int l = __builtin_ctzll(hit);
-      const int first = static_cast<int>(g - before) - (__shfl(inc, l, 64) - __shfl(tiles, l, 64));
-      out->e = base + l;
-      out->lo = __shfl(lo, l, 64) + first * tile;
-      out->hi = min(__shfl(hi, l, 64), out->lo + tile);
+  const int per = E / 64 + 1;  // experts a lane, of E + 1
+  int lo, tiles = 0;
+  for (int i = 0; i < per; ++i) {
+    const int e = lane * per + i;
+    if (e <= E) tiles += (slots_of(offsets, E, s, e, &lo) + tile - 1) / tile;
+  }
+  int sum = wave_scan(tiles);
+  const int64_t n = static_cast<int64_t>(lane_value(sum, 63)) * cols, id = blockIdx.x;
+  if (id >= n) return false;
+  const int64_t x = id & 7, q = n >> 3, rem = n & 7;
+  const int64_t l = x * q + (x < rem ? x : rem) + (id >> 3);
+  const int g = static_cast<int>(l / cols);
+  const int run = __builtin_ctzll(__ballot(sum > g));
+  int base = run ? lane_value(sum, run - 1) : 0;
+  int e = run * per;
+  for (;; e += 64) {  // (one pass up to 4095 experts)
+    const int f = e + lane;
+    const int have = f <= E && f < (run + 1) * per ? slots_of(offsets, E, s, f, &lo) : 0;
+    tiles = (have + tile - 1) / tile;
+    sum = base + wave_scan(tiles);
+    const uint64_t hit = __ballot(sum > g);
+    if (hit || e + 64 >= (run + 1) * per) {
+      const int at = hit ? __builtin_ctzll(hit) : 63;
+      const int m = lane_value(tiles, at), first = lane_value(lo, at), count = lane_value(have, at);
+      const int64_t in = l - static_cast<int64_t>(lane_value(sum, at) - m) * cols;
+      const int group = static_cast<int>(in / (8 * static_cast<int64_t>(cols)));
+      const int rest = static_cast<int>(in - group * 8 * static_cast<int64_t>(cols));
+      const int high = min(8, m - 8 * group);
+      const int row = 8 * group + rest % high;
+      out->e = e + at;
+      out->col = rest / high;
+      out->lo = first + row * tile;
+      out->hi = min(first + count, out->lo + tile);
       return true;
     }
-    before += __shfl(inc, 63, 64);
+    base = lane_value(sum, 63);
   }
-  return false;
 }
 
 __device__ __forceinline__ float silu(float g) { return g / (1.0f + expf(-g)); }
@@ -107,10 +141,9 @@ __global__ __launch_bounds__(kThreads) void mx4_rows_kernel(MulArgs a) {
   constexpr int H = GLU ? 2 : 1;
   __shared__ f32x4 part[kThreads / 64][H][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
-  const int64_t ntiles = (a.N + 15) / 16;
-  const int64_t g = blockIdx.x / ntiles, n0 = (blockIdx.x - g * ntiles) * 16;
   Tile t;
-  if (!find_tile(a.offsets, a.E, a.S, g, 16, &t)) return;
+  if (!find_tile(a.offsets, a.E, a.S, static_cast<int>((a.N + 15) / 16), 16, &t)) return;
+  const int64_t n0 = static_cast<int64_t>(t.col) * 16;
   f32x4 acc[H];
 #pragma unroll
   for (int h = 0; h < H; ++h) acc[h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -249,10 +282,9 @@ __global__ __launch_bounds__(kTileThreads) void mx4_tile_kernel(MulArgs a) {
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   constexpr int TNO = GLU ? kTN / 2 : kTN;  // results a tile has of a slot
-  const int64_t ntiles = (a.N + TNO - 1) / TNO;
-  const int64_t g = blockIdx.x / ntiles, n0 = (blockIdx.x - g * ntiles) * TNO;
   Tile t;
-  if (!find_tile(a.offsets, a.E, a.S, g, TM, &t)) return;
+  if (!find_tile(a.offsets, a.E, a.S, static_cast<int>((a.N + TNO - 1) / TNO), TM, &t)) return;
+  const int64_t n0 = static_cast<int64_t>(t.col) * TNO;
   const int wm = wave >> 2, wn = wave & 3, r32 = lane & 31, half = lane >> 5;
   f32x16 acc[H::NB][H::MB];
 #pragma unroll
@@ -452,10 +484,9 @@ __global__ __launch_bounds__(kThreads) void mx4_grad_kernel(MulArgs a) {
   constexpr int KT = 64, LD = 40;  // (LD: rows 80 bytes apart)
   __shared__ __align__(16) uint16_t wt[KT * LD];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, q = lane >> 4;
-  const int64_t ktiles = (a.K + KT - 1) / KT;
-  const int64_t g = blockIdx.x / ktiles, k0 = (blockIdx.x - g * ktiles) * KT;
   Tile t;
-  if (!find_tile(a.offsets, a.E, a.S, g, 16, &t)) return;
+  if (!find_tile(a.offsets, a.E, a.S, static_cast<int>((a.K + KT - 1) / KT), 16, &t)) return;
+  const int64_t k0 = static_cast<int64_t>(t.col) * KT;
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
   const int64_t slot = t.lo + r;
   if (t.e < a.E) {
@@ -517,10 +548,9 @@ __global__ __launch_bounds__(kTileThreads) void mx4_grad_tile_kernel(MulArgs a) 
   using H = GradShape;
   extern __shared__ __align__(16) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int64_t ktiles = (a.K + H::KT - 1) / H::KT;
-  const int64_t g = blockIdx.x / ktiles, k0 = (blockIdx.x - g * ktiles) * H::KT;
   Tile t;
-  if (!find_tile(a.offsets, a.E, a.S, g, H::TM, &t)) return;
+  if (!find_tile(a.offsets, a.E, a.S, static_cast<int>((a.K + H::KT - 1) / H::KT), H::TM, &t)) return;
+  const int64_t k0 = static_cast<int64_t>(t.col) * H::KT;
   const int wm = wave >> 2, wn = wave & 3, r32 = lane & 31, half = lane >> 5;
   f32x16 acc[H::NB][H::MB];
 #pragma unroll
