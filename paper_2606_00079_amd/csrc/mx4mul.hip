@@ -227,20 +227,19 @@ constexpr int kTileThreads = 512, kWaves = 8, kTN = 256;
 template <bool MX, int TM_>
 struct Shape {
   static constexpr int TM = TM_;
-  static constexpr int KS = MX ? 128 : 64;   // entries of K a step
-  static constexpr int XB = MX ? 64 : 128;   // bytes of a token's row in a stage
-  static constexpr int WB = KS / 2;          // bytes of a weight row in a stage
-  static constexpr int SC = KS / 32;         // scales of a row in a stage (a word each)
+  static constexpr int KS = MX ? 256 : 128;      // entries of K a step
+  static constexpr int XB = MX ? KS / 2 : 2 * KS;  // bytes of a token's row in a stage
+  static constexpr int WB = KS / 2;              // bytes of a weight row in a stage
+  static constexpr int SC = KS / 32;             // scales of a row in a stage (a word each)
   static constexpr int kX = 0, kW = TM * XB, kWS = kW + kTN * WB, kXS = kWS + kTN * SC * 4;
   static constexpr int kStage = kXS + (MX ? TM * SC * 4 : 0);
-  static constexpr int kFit = 163840 / kStage;
-  static constexpr int kStages = kFit < 5 ? kFit : 5;
+  static constexpr int kStages = 163840 / kStage;
   // direct loads of a wave for a stage
   static constexpr int LX = TM * XB / 1024 / kWaves, LW = kTN * WB / 1024 / kWaves;
   static constexpr int LWS = kTN * SC / 64 / kWaves, LXS = MX ? TM * SC / 64 / kWaves : 0;
   static constexpr int kLoads = LX + LW + LWS + LXS;
   static constexpr int MB = TM / 64, NB = 2;
-  static_assert(kStages >= 3 && (kStages - 2) * kLoads < 64);
+  static_assert(kStages >= 2 && (kStages - 1) * kLoads < 64);
 };
 
 // What lanes past the end of a row read: zeros, and scales of 1.
@@ -276,8 +275,82 @@ __device__ __forceinline__ int chunk_slot(int r, int c) {
   return c ^ ((r / (16 / chunks)) & (chunks - 1));
 }
 
+// Place of scale c of row r among the SC words of its row: as above, for words
+// that two half-waves read at neighbouring places.
+template <int SC>
+__device__ __forceinline__ int scale_slot(int r, int c) {
+  return c ^ (2 * ((r * SC / 64) & (SC / 2 - 1)));
+}
+
+// The operand fragments of a quarter of a step (32 entries of K with bf16
+// tokens, 64 with MX4 ones): read from a stage while the quarter before is
+// multiplied.
+template <bool MX, int TM>
+struct Frags {
+  using H = Shape<MX, TM>;
+  uint4 w[H::NB];  // bf16 tokens: two words of each in use
+  uint4 x[H::MB][MX ? 1 : 2];
+  int ws[H::NB], xs[MX ? H::MB : 1];
+  // quarter u of the stage at s; wrow, xrow: this lane's first rows
+  template <int u>
+  __device__ __forceinline__ void read(const char* s, int wrow, int xrow, int half) {
+    const int c = 2 * (MX ? u : u / 2) + half;  // this lane's block of 32 in the step
+    constexpr int WC = H::WB / 16, XC = H::XB / 16;
+#pragma unroll
+    for (int n = 0; n < H::NB; ++n) {
+      const int r = wrow + 32 * n;
+      const char* at = s + H::kW + r * H::WB + chunk_slot<WC>(r, c) * 16;
+      if constexpr (MX) {
+        w[n] = *reinterpret_cast<const uint4*>(at);
+      } else {
+        const uint2 v = *reinterpret_cast<const uint2*>(at + 8 * (u % 2));
+        w[n].x = v.x;
+        w[n].y = v.y;
+      }
+      ws[n] = *reinterpret_cast<const int*>(s + H::kWS + (r * H::SC + scale_slot<H::SC>(r, c)) * 4);
+    }
+#pragma unroll
+    for (int m = 0; m < H::MB; ++m) {
+      const int r = xrow + 32 * m;
+      const char* row = s + H::kX + r * H::XB;
+      if constexpr (MX) {
+        x[m][0] = *reinterpret_cast<const uint4*>(row + chunk_slot<XC>(r, c) * 16);
+        xs[m] = *reinterpret_cast<const int*>(s + H::kXS + (r * H::SC + scale_slot<H::SC>(r, c)) * 4);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          x[m][j] = *reinterpret_cast<const uint4*>(row + chunk_slot<XC>(r, 4 * c + 2 * (u % 2) + j) * 16);
+      }
+    }
+  }
+  __device__ __forceinline__ void multiply(f32x16 (&acc)[H::NB][H::MB]) const {
+    if constexpr (MX) {
+#pragma unroll
+      for (int n = 0; n < H::NB; ++n)
+#pragma unroll
+        for (int m = 0; m < H::MB; ++m)
+          acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(codes(w[n]), codes(x[m][0]), acc[n][m], 4, 4, 0,
+                                                                      ws[n], 0, xs[m]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int n = 0; n < H::NB; ++n) {
+          const bf16x8 wf = mx4_bf16(j ? w[n].y : w[n].x, mx4_scale(ws[n]));
+#pragma unroll
+          for (int m = 0; m < H::MB; ++m)
+            acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf, __builtin_bit_cast(bf16x8, x[m][j]), acc[n][m], 0,
+                                                                0, 0);
+        }
+    }
+  }
+  __device__ __forceinline__ static i32x8 codes(uint4 v) {
+    return i32x8{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0};
+  }
+};
+
 template <bool MX, bool GLU, int TM>
-__global__ __launch_bounds__(kTileThreads) void mx4_tile_kernel(MulArgs a) {
+__global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(MulArgs a) {
   using H = Shape<MX, TM>;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -314,7 +387,7 @@ __global__ __launch_bounds__(kTileThreads) void mx4_tile_kernel(MulArgs a) {
       }
     };
     const char *px[H::LX], *pw[H::LW], *pws[H::LWS], *pxs[MX ? H::LXS : 1];
-    int kx[H::LX], kw[H::LW], kws, kxs = 0;
+    int kx[H::LX], kw[H::LW], kws[H::LWS], kxs[MX ? H::LXS : 1];
     constexpr int XC = H::XB / 16, WC = H::WB / 16;
 #pragma unroll
     for (int q = 0; q < H::LX; ++q) {
@@ -332,16 +405,18 @@ __global__ __launch_bounds__(kTileThreads) void mx4_tile_kernel(MulArgs a) {
       pw[q] = reinterpret_cast<const char*>(a.codes + weight(r) * kb * 16 + c * 16);
     }
 #pragma unroll
-    for (int q = 0; q < H::LWS; ++q)
-      pws[q] = reinterpret_cast<const char*>(
-          a.scales + weight((wave + kWaves * q) * (64 / H::SC) + lane / H::SC) * kb + lane % H::SC);
-    kws = (lane % H::SC) * 32;
+    for (int q = 0; q < H::LWS; ++q) {
+      const int r = (wave + kWaves * q) * (64 / H::SC) + lane / H::SC, c = scale_slot<H::SC>(r, lane % H::SC);
+      kws[q] = c * 32;
+      pws[q] = reinterpret_cast<const char*>(a.scales + weight(r) * kb + c);
+    }
     if constexpr (MX) {
 #pragma unroll
-      for (int q = 0; q < H::LXS; ++q)
-        pxs[q] = reinterpret_cast<const char*>(
-            a.xscales + token((wave + kWaves * q) * (64 / H::SC) + lane / H::SC) * kb + lane % H::SC);
-      kxs = kws;
+      for (int q = 0; q < H::LXS; ++q) {
+        const int r = (wave + kWaves * q) * (64 / H::SC) + lane / H::SC, c = scale_slot<H::SC>(r, lane % H::SC);
+        kxs[q] = c * 32;
+        pxs[q] = reinterpret_cast<const char*>(a.xscales + token(r) * kb + c);
+      }
     }
     const int nk = static_cast<int>((a.K + H::KS - 1) / H::KS);
     const int last = static_cast<int>(a.K - static_cast<int64_t>(nk - 1) * H::KS);  // entries of the last step
@@ -354,10 +429,10 @@ __global__ __launch_bounds__(kTileThreads) void mx4_tile_kernel(MulArgs a) {
 #pragma unroll
         for (int q = 0; q < H::LW; ++q) pw[q] = kw[q] < last ? pw[q] : reinterpret_cast<const char*>(kPad);
 #pragma unroll
-        for (int q = 0; q < H::LWS; ++q) pws[q] = kws < last ? pws[q] : reinterpret_cast<const char*>(kPad + 16);
+        for (int q = 0; q < H::LWS; ++q) pws[q] = kws[q] < last ? pws[q] : reinterpret_cast<const char*>(kPad + 16);
         if constexpr (MX) {
 #pragma unroll
-          for (int q = 0; q < H::LXS; ++q) pxs[q] = kxs < last ? pxs[q] : reinterpret_cast<const char*>(kPad + 16);
+          for (int q = 0; q < H::LXS; ++q) pxs[q] = kxs[q] < last ? pxs[q] : reinterpret_cast<const char*>(kPad + 16);
         }
       }
 #pragma unroll
@@ -385,73 +460,46 @@ __global__ __launch_bounds__(kTileThreads) void mx4_tile_kernel(MulArgs a) {
       ++issued;
       to = to + 1 == H::kStages ? 0 : to + 1;
     };
-    for (int i = 0; i < H::kStages - 1 && i < nk; ++i) issue();
-    int from = 0;
+    for (int i = 0; i < H::kStages && i < nk; ++i) issue();
     const int wrow = wn * 64 + r32, xrow = wm * (TM / 2) + r32;
-    for (int i = 0; i < nk; ++i) {
-      // stage i has landed once all loads but those of the kStages - 2 stages after it have
-      if (issued - 1 - i >= H::kStages - 2)
+    // a stage has landed once all loads but those of the stages after it have
+    if (nk >= H::kStages)
+      wait_loads<(H::kStages - 1) * H::kLoads>();
+    else
+      wait_loads<0>();
+    Frags<MX, TM> p, q;
+    p.template read<0>(smem, wrow, xrow, half);
+    const char* s = smem;
+    auto quarters = [&]() {  // the first three quarters of the stage at s, and the last one's fragments
+      q.template read<1>(s, wrow, xrow, half);
+      __builtin_amdgcn_sched_barrier(0);
+      p.multiply(acc);
+      __builtin_amdgcn_sched_barrier(0);
+      p.template read<2>(s, wrow, xrow, half);
+      __builtin_amdgcn_sched_barrier(0);
+      q.multiply(acc);
+      __builtin_amdgcn_sched_barrier(0);
+      q.template read<3>(s, wrow, xrow, half);
+      __builtin_amdgcn_sched_barrier(0);
+      p.multiply(acc);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    for (int i = 0; i < nk - 1; ++i) {
+      quarters();
+      // stage i + 1 has landed, and every wave has read all of stage i: its buffer is free
+      if (issued - 2 - i >= H::kStages - 2)
         wait_loads<(H::kStages - 2) * H::kLoads>();
       else
         wait_loads<0>();
-      // every wave is past stage i - 1 here: its buffer is free
       if (issued < nk) issue();
-      const char* s = smem + from * H::kStage;
-      from = from + 1 == H::kStages ? 0 : from + 1;
-      if constexpr (MX) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {  // 64 entries: chunk 2u + half of a row
-          i32x8 wf[H::NB], xf[H::MB];
-          int ws[H::NB], xs[H::MB];
-#pragma unroll
-          for (int n = 0; n < H::NB; ++n) {
-            const int r = wrow + 32 * n;
-            const uint4 v = *reinterpret_cast<const uint4*>(s + H::kW + r * H::WB + chunk_slot<4>(r, 2 * u + half) * 16);
-            wf[n] = i32x8{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0};
-            ws[n] = *reinterpret_cast<const int*>(s + H::kWS + (r * H::SC + 2 * u + half) * 4);
-          }
-#pragma unroll
-          for (int m = 0; m < H::MB; ++m) {
-            const int r = xrow + 32 * m;
-            const uint4 v = *reinterpret_cast<const uint4*>(s + H::kX + r * H::XB + chunk_slot<4>(r, 2 * u + half) * 16);
-            xf[m] = i32x8{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0};
-            xs[m] = *reinterpret_cast<const int*>(s + H::kXS + (r * H::SC + 2 * u + half) * 4);
-          }
-#pragma unroll
-          for (int n = 0; n < H::NB; ++n)
-#pragma unroll
-            for (int m = 0; m < H::MB; ++m)
-              acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[n], xf[m], acc[n][m], 4, 4, 0, ws[n], 0,
-                                                                          xs[m]);
-        }
-      } else {
-        uint32_t wc[H::NB][4];
-        float sc[H::NB];
-#pragma unroll
-        for (int n = 0; n < H::NB; ++n) {
-          const int r = wrow + 32 * n;
-          const uint4 v = *reinterpret_cast<const uint4*>(s + H::kW + r * H::WB + chunk_slot<2>(r, half) * 16);
-          wc[n][0] = v.x, wc[n][1] = v.y, wc[n][2] = v.z, wc[n][3] = v.w;
-          sc[n] = mx4_scale(*reinterpret_cast<const uint32_t*>(s + H::kWS + (r * H::SC + half) * 4));
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {  // entries 32 half + 8 j + 0 .. 7 of the step
-          bf16x8 xf[H::MB];
-#pragma unroll
-          for (int m = 0; m < H::MB; ++m) {
-            const int r = xrow + 32 * m;
-            xf[m] = *reinterpret_cast<const bf16x8*>(s + H::kX + r * H::XB + chunk_slot<8>(r, 4 * half + j) * 16);
-          }
-#pragma unroll
-          for (int n = 0; n < H::NB; ++n) {
-            const bf16x8 wf = mx4_bf16(wc[n][j], sc[n]);
-#pragma unroll
-            for (int m = 0; m < H::MB; ++m)
-              acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf, xf[m], acc[n][m], 0, 0, 0);
-          }
-        }
-      }
+      s = s + H::kStage == smem + H::kStages * H::kStage ? smem : s + H::kStage;
+      p.template read<0>(s, wrow, xrow, half);
+      __builtin_amdgcn_sched_barrier(0);
+      q.multiply(acc);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    quarters();
+    q.multiply(acc);
   }
 
   const bool wide = a.ldy % 4 == 0;
