@@ -105,6 +105,68 @@ __device__ __forceinline__ bool find_tile(const int32_t* offsets, int E, int64_t
   }
 }
 
+// The same order of tiles for a workgroup that stays and takes one tile after
+// another (without those of e = E): it goes on from expert to expert with
+// scalar loads, which do not touch the count of its vector loads.
+struct Walk {
+  const __attribute__((address_space(4))) int32_t* offsets;
+  int E, S, cols, tile;
+  int64_t l, end, step;       // this workgroup's tile, the end of its XCD's range
+  int e, before, first, count;  // expert, tiles before it, its first slot and their number
+  __device__ __forceinline__ int tiles() const { return (count + tile - 1) / tile; }
+  __device__ __forceinline__ void load() {
+    first = offsets ? min(max(offsets[e], 0), S) : 0;
+    count = (offsets ? min(max(offsets[e + 1], first), S) : S) - first;
+  }
+  // to the expert of tile l; false if there is none
+  __device__ __forceinline__ bool find() {
+    if (l >= end) return false;
+    const int g = static_cast<int>(l / cols);
+    while (g >= before + tiles()) {
+      before += tiles();
+      ++e;
+      load();
+    }
+    return true;
+  }
+  __device__ __forceinline__ void get(Tile* out) const {
+    const int64_t in = l - static_cast<int64_t>(before) * cols;
+    const int group = static_cast<int>(in / (8 * static_cast<int64_t>(cols)));
+    const int rest = static_cast<int>(in - group * 8 * static_cast<int64_t>(cols));
+    const int high = min(8, tiles() - 8 * group), row = 8 * group + rest % high;
+    out->e = e;
+    out->col = rest / high;
+    out->lo = first + row * tile;
+    out->hi = min(first + count, out->lo + tile);
+  }
+  // The first tile of this workgroup; *none: where the slots of no expert begin.
+  __device__ __forceinline__ bool start(const int32_t* off, int E_, int64_t S_, int cols_, int tile_, int* none) {
+    offsets = (const __attribute__((address_space(4))) int32_t*)reinterpret_cast<uintptr_t>(off);
+    E = E_, S = static_cast<int>(S_), cols = cols_, tile = tile_;
+    const int lane = threadIdx.x & 63, per = (E + 63) / 64;
+    int lo, sum = 0;
+    for (int i = 0; i < per; ++i) {
+      const int f = lane * per + i;
+      if (f < E) sum += (slots_of(off, E, S, f, &lo) + tile - 1) / tile;
+    }
+    const int own = sum;
+    sum = wave_scan(sum);
+    *none = offsets ? min(max(offsets[E], 0), S) : S;
+    const int64_t n = static_cast<int64_t>(lane_value(sum, 63)) * cols;
+    const int64_t x = blockIdx.x & 7, q = n >> 3, rem = n & 7;
+    const int64_t begin = x * q + (x < rem ? x : rem);
+    end = begin + q + (x < rem ? 1 : 0);
+    step = gridDim.x >> 3;
+    l = begin + (blockIdx.x >> 3);
+    if (l >= end) return false;
+    const int run = __builtin_ctzll(__ballot(sum > static_cast<int>(l / cols)));
+    before = lane_value(sum, run) - lane_value(own, run);
+    e = run * per;
+    load();
+    return find();
+  }
+};
+
 __device__ __forceinline__ float silu(float g) { return g / (1.0f + expf(-g)); }
 
 // Four consecutive results n .. n + 3 of slot s.
@@ -353,124 +415,193 @@ template <bool MX, bool GLU, int TM>
 __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(MulArgs a) {
   using H = Shape<MX, TM>;
   extern __shared__ __align__(16) char smem[];
+  // rows of X of the slots of three tiles: the one multiplied, the next, and one before
+  int32_t* const rowbuf = reinterpret_cast<int32_t*>(smem + H::kStages * H::kStage);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   constexpr int TNO = GLU ? kTN / 2 : kTN;  // results a tile has of a slot
-  Tile t;
-  if (!find_tile(a.offsets, a.E, a.S, static_cast<int>((a.N + TNO - 1) / TNO), TM, &t)) return;
-  const int64_t n0 = static_cast<int64_t>(t.col) * TNO;
   const int wm = wave >> 2, wn = wave & 3, r32 = lane & 31, half = lane >> 5;
-  f32x16 acc[H::NB][H::MB];
-#pragma unroll
-  for (int i = 0; i < H::NB; ++i)
-#pragma unroll
-    for (int j = 0; j < H::MB; ++j)
-#pragma unroll
-      for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.0f;
+  const int64_t kb = a.K / 32;
+  const int nk = static_cast<int>((a.K + H::KS - 1) / H::KS);
+  const int last = static_cast<int>(a.K - static_cast<int64_t>(nk - 1) * H::KS);  // entries of the last step
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
 
-  if (t.e < a.E) {
-    const int64_t kb = a.K / 32;
-    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
-    // this lane's addresses in the first stage, and how far along K it is there
-    auto token = [&](int r) {  // row of X of the tile's slot r (slots past the tile: its last; no such row: row 0)
-      const int64_t s = min(t.lo + r, t.hi - 1);
-      const int64_t row = a.rows ? static_cast<int64_t>(a.rows[s]) : s;
-      return row >= 0 && row < a.x_rows ? row : int64_t(0);
+  int none;
+  Walk walk;
+  Tile cur, next;
+  bool more = walk.start(a.offsets, a.E, a.S, static_cast<int>((a.N + TNO - 1) / TNO), TM, &none);
+  // slots of no expert: zeros
+  for (int64_t s = none + static_cast<int64_t>(blockIdx.x); s < a.S; s += gridDim.x)
+    for (int64_t n = threadIdx.x; n < a.N; n += kTileThreads) {
+      if (a.yf32)
+        static_cast<float*>(a.y)[s * a.ldy + n] = 0.0f;
+      else
+        static_cast<uint16_t*>(a.y)[s * a.ldy + n] = 0;
+    }
+  if (!more) return;
+  walk.get(&cur);
+
+  // Direct loads.  They run through the stages of one tile after another, a
+  // ring of kStages ahead of the multiplication and at most into the tile after
+  // the one multiplied, so that a tile's results are stored while the next
+  // one's first stages are on their way.
+  constexpr int XC = H::XB / 16, WC = H::WB / 16;
+  const char *px[H::LX], *pw[H::LW], *pws[H::LWS], *pxs[MX ? H::LXS : 1];
+  auto row_of = [&](int q, int per) { return (wave + kWaves * q) * per + lane / (64 / per); };
+  auto load_rows = [&](const Tile& t, int buf) {  // the rows of a tile's slots (past its end: its last)
+    if (a.rows && wave < TM / 64) {
+      const int32_t* p = a.rows + min(t.lo + wave * 64 + lane, t.hi - 1);
+      asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" ::"v"(p),
+                   "s"(__builtin_amdgcn_readfirstlane(lds0 + H::kStages * H::kStage + (buf * TM + wave * 64) * 4))
+                   : "memory");
+    }
+  };
+  auto aim = [&](const Tile& t, int buf) {  // the loads' addresses in the first stage of a tile
+    auto token = [&](int r) {  // (a row that does not exist: row 0, its results are replaced)
+      if (!a.rows) return static_cast<int64_t>(min(t.lo + r, t.hi - 1));
+      const int row = rowbuf[buf * TM + r];
+      return static_cast<int64_t>(row >= 0 && row < a.x_rows ? row : 0);
     };
-    auto weight = [&](int r) {  // row of W of the tile's output row r
-      int64_t n;
-      if constexpr (GLU) {
-        n = min(n0 + (r >> 6) * 32 + (r & 31), a.N - 1) + ((r >> 5) & 1) * a.N;
-        return static_cast<int64_t>(t.e) * 2 * a.N + n;
-      } else {
-        n = min(n0 + r, a.N - 1);
-        return static_cast<int64_t>(t.e) * a.N + n;
-      }
+    const int64_t n0 = static_cast<int64_t>(t.col) * TNO;
+    auto weight = [&](int r) {
+      if constexpr (GLU)  // 32 gate rows, then the 32 up rows of the same outputs
+        return static_cast<int64_t>(t.e) * 2 * a.N + min(n0 + (r >> 6) * 32 + (r & 31), a.N - 1) +
+               ((r >> 5) & 1) * a.N;
+      else
+        return static_cast<int64_t>(t.e) * a.N + min(n0 + r, a.N - 1);
     };
-    const char *px[H::LX], *pw[H::LW], *pws[H::LWS], *pxs[MX ? H::LXS : 1];
-    int kx[H::LX], kw[H::LW], kws[H::LWS], kxs[MX ? H::LXS : 1];
-    constexpr int XC = H::XB / 16, WC = H::WB / 16;
 #pragma unroll
     for (int q = 0; q < H::LX; ++q) {
-      const int r = (wave + kWaves * q) * (64 / XC) + lane / XC;
-      const int c = chunk_slot<XC>(r, lane % XC);
-      kx[q] = c * (MX ? 32 : 8);
+      const int r = row_of(q, 64 / XC), c = chunk_slot<XC>(r, lane % XC);
       px[q] = MX ? reinterpret_cast<const char*>(a.xcodes + token(r) * kb * 16 + c * 16)
                  : reinterpret_cast<const char*>(a.x + token(r) * a.ldx + c * 8);
     }
 #pragma unroll
     for (int q = 0; q < H::LW; ++q) {
-      const int r = (wave + kWaves * q) * (64 / WC) + lane / WC;
-      const int c = chunk_slot<WC>(r, lane % WC);
-      kw[q] = c * 32;
+      const int r = row_of(q, 64 / WC), c = chunk_slot<WC>(r, lane % WC);
       pw[q] = reinterpret_cast<const char*>(a.codes + weight(r) * kb * 16 + c * 16);
     }
 #pragma unroll
     for (int q = 0; q < H::LWS; ++q) {
-      const int r = (wave + kWaves * q) * (64 / H::SC) + lane / H::SC, c = scale_slot<H::SC>(r, lane % H::SC);
-      kws[q] = c * 32;
+      const int r = row_of(q, 64 / H::SC), c = scale_slot<H::SC>(r, lane % H::SC);
       pws[q] = reinterpret_cast<const char*>(a.scales + weight(r) * kb + c);
     }
     if constexpr (MX) {
 #pragma unroll
       for (int q = 0; q < H::LXS; ++q) {
-        const int r = (wave + kWaves * q) * (64 / H::SC) + lane / H::SC, c = scale_slot<H::SC>(r, lane % H::SC);
-        kxs[q] = c * 32;
+        const int r = row_of(q, 64 / H::SC), c = scale_slot<H::SC>(r, lane % H::SC);
         pxs[q] = reinterpret_cast<const char*>(a.xscales + token(r) * kb + c);
       }
     }
-    const int nk = static_cast<int>((a.K + H::KS - 1) / H::KS);
-    const int last = static_cast<int>(a.K - static_cast<int64_t>(nk - 1) * H::KS);  // entries of the last step
-    int issued = 0, to = 0;
-    auto issue = [&]() {  // the next stage's loads
-      const uint32_t s = lds0 + to * H::kStage;
-      if (issued == nk - 1 && last < H::KS) {
+  };
+  int step = 0, to = 0, ahead = 0;  // the next stage of the tile loaded, its buffer, and stages not yet multiplied
+  auto issue = [&]() {
+    const uint32_t s = lds0 + to * H::kStage;
+    if (step == nk - 1 && last < H::KS) {  // lanes past K: zeros
+      const char *zero = reinterpret_cast<const char*>(kPad), *one = zero + 16;
 #pragma unroll
-        for (int q = 0; q < H::LX; ++q) px[q] = kx[q] < last ? px[q] : reinterpret_cast<const char*>(kPad);
+      for (int q = 0; q < H::LX; ++q)
+        px[q] = chunk_slot<XC>(row_of(q, 64 / XC), lane % XC) * (MX ? 32 : 8) < last ? px[q] : zero;
 #pragma unroll
-        for (int q = 0; q < H::LW; ++q) pw[q] = kw[q] < last ? pw[q] : reinterpret_cast<const char*>(kPad);
+      for (int q = 0; q < H::LW; ++q) pw[q] = chunk_slot<WC>(row_of(q, 64 / WC), lane % WC) * 32 < last ? pw[q] : zero;
 #pragma unroll
-        for (int q = 0; q < H::LWS; ++q) pws[q] = kws[q] < last ? pws[q] : reinterpret_cast<const char*>(kPad + 16);
-        if constexpr (MX) {
-#pragma unroll
-          for (int q = 0; q < H::LXS; ++q) pxs[q] = kxs[q] < last ? pxs[q] : reinterpret_cast<const char*>(kPad + 16);
-        }
-      }
-#pragma unroll
-      for (int q = 0; q < H::LX; ++q) {
-        load_lds16(px[q], s + H::kX + (wave + kWaves * q) * 1024);
-        px[q] += H::XB;
-      }
-#pragma unroll
-      for (int q = 0; q < H::LW; ++q) {
-        load_lds16(pw[q], s + H::kW + (wave + kWaves * q) * 1024);
-        pw[q] += H::WB;
-      }
-#pragma unroll
-      for (int q = 0; q < H::LWS; ++q) {
-        load_lds1(pws[q], s + H::kWS + (wave + kWaves * q) * 256);
-        pws[q] += H::SC;
-      }
+      for (int q = 0; q < H::LWS; ++q)
+        pws[q] = scale_slot<H::SC>(row_of(q, 64 / H::SC), lane % H::SC) * 32 < last ? pws[q] : one;
       if constexpr (MX) {
 #pragma unroll
-        for (int q = 0; q < H::LXS; ++q) {
-          load_lds1(pxs[q], s + H::kXS + (wave + kWaves * q) * 256);
-          pxs[q] += H::SC;
-        }
+        for (int q = 0; q < H::LXS; ++q)
+          pxs[q] = scale_slot<H::SC>(row_of(q, 64 / H::SC), lane % H::SC) * 32 < last ? pxs[q] : one;
       }
-      ++issued;
-      to = to + 1 == H::kStages ? 0 : to + 1;
-    };
-    for (int i = 0; i < H::kStages && i < nk; ++i) issue();
-    const int wrow = wn * 64 + r32, xrow = wm * (TM / 2) + r32;
-    // a stage has landed once all loads but those of the stages after it have
-    if (nk >= H::kStages)
+    }
+#pragma unroll
+    for (int q = 0; q < H::LX; ++q) {
+      load_lds16(px[q], s + H::kX + (wave + kWaves * q) * 1024);
+      px[q] += H::XB;
+    }
+#pragma unroll
+    for (int q = 0; q < H::LW; ++q) {
+      load_lds16(pw[q], s + H::kW + (wave + kWaves * q) * 1024);
+      pw[q] += H::WB;
+    }
+#pragma unroll
+    for (int q = 0; q < H::LWS; ++q) {
+      load_lds1(pws[q], s + H::kWS + (wave + kWaves * q) * 256);
+      pws[q] += H::SC;
+    }
+    if constexpr (MX) {
+#pragma unroll
+      for (int q = 0; q < H::LXS; ++q) {
+        load_lds1(pxs[q], s + H::kXS + (wave + kWaves * q) * 256);
+        pxs[q] += H::SC;
+      }
+    }
+    ++step;
+    ++ahead;
+    to = to + 1 == H::kStages ? 0 : to + 1;
+  };
+  // Waits for all stages but the last `after` issued, and for the workgroup.
+  auto landed = [&](int after) {
+    if (H::kStages > 2 && after >= H::kStages - 1)
       wait_loads<(H::kStages - 1) * H::kLoads>();
+    else if (after >= 1)
+      wait_loads<H::kLoads>();
     else
       wait_loads<0>();
-    Frags<MX, TM> p, q;
-    p.template read<0>(smem, wrow, xrow, half);
-    const char* s = smem;
-    auto quarters = [&]() {  // the first three quarters of the stage at s, and the last one's fragments
+  };
+  static_assert(H::kStages <= 3);
+
+  int buf = 0;                    // of rowbuf: the tile multiplied; the next one's is buf + 1
+  bool into_next = false;         // the loads have reached the next tile
+  int since = 0;                  // steps since the next tile's rows were asked for
+  auto find_next = [&]() {
+    walk.l += walk.step;
+    more = walk.find();
+    if (more) {
+      walk.get(&next);
+      load_rows(next, buf == 2 ? 0 : buf + 1);
+    }
+    into_next = false;
+    since = 0;
+  };
+  // Fills the ring as far as it goes.
+  auto refill = [&]() {
+    while (ahead < H::kStages) {
+      if (step == nk) {
+        if (!more || into_next) break;
+        // the rows have landed if the stages asked for since then fill the ring
+        if (a.rows && since < H::kStages) wait_loads<0>();
+        aim(next, buf == 2 ? 0 : buf + 1);
+        step = 0;
+        into_next = true;
+      }
+      issue();
+    }
+    ++since;
+  };
+
+  load_rows(cur, 0);
+  wait_loads<0>();
+  aim(cur, 0);
+  while (ahead < H::kStages && step < nk) issue();
+  find_next();
+  refill();
+
+  const int wrow = wn * 64 + r32, xrow = wm * (TM / 2) + r32;
+  f32x16 acc[H::NB][H::MB];
+  auto clear = [&]() {
+#pragma unroll
+    for (int i = 0; i < H::NB; ++i)
+#pragma unroll
+      for (int j = 0; j < H::MB; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+  };
+  clear();
+  Frags<MX, TM> p, q;
+  landed(ahead - 1);
+  const char* s = smem;
+  p.template read<0>(s, wrow, xrow, half);
+  for (;;) {
+    for (int i = 0; i < nk; ++i) {
       q.template read<1>(s, wrow, xrow, half);
       __builtin_amdgcn_sched_barrier(0);
       p.multiply(acc);
@@ -483,46 +614,46 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(MulArgs a) {
       __builtin_amdgcn_sched_barrier(0);
       p.multiply(acc);
       __builtin_amdgcn_sched_barrier(0);
-    };
-    for (int i = 0; i < nk - 1; ++i) {
-      quarters();
-      // stage i + 1 has landed, and every wave has read all of stage i: its buffer is free
-      if (issued - 2 - i >= H::kStages - 2)
-        wait_loads<(H::kStages - 2) * H::kLoads>();
-      else
-        wait_loads<0>();
-      if (issued < nk) issue();
+      // the next stage has landed, and every wave has read all of this one: its buffer is free
+      landed(ahead - 2);
+      --ahead;
+      refill();
       s = s + H::kStage == smem + H::kStages * H::kStage ? smem : s + H::kStage;
-      p.template read<0>(s, wrow, xrow, half);
+      p.template read<0>(s, wrow, xrow, half);  // (of the next tile after a tile's last step; unused at the end)
       __builtin_amdgcn_sched_barrier(0);
       q.multiply(acc);
       __builtin_amdgcn_sched_barrier(0);
     }
-    quarters();
-    q.multiply(acc);
-  }
-
-  const bool wide = a.ldy % 4 == 0;
+    const int64_t n0 = static_cast<int64_t>(cur.col) * TNO;
+    const bool wide = a.ldy % 4 == 0;
 #pragma unroll
-  for (int m = 0; m < H::MB; ++m) {
-    const int64_t slot = t.lo + wm * (TM / 2) + 32 * m + r32;
-    if (slot >= t.hi) continue;
-    bool have = true;
-    if (t.e < a.E && a.rows) have = a.rows[slot] >= 0 && a.rows[slot] < a.x_rows;
+    for (int m = 0; m < H::MB; ++m) {
+      const int r = wm * (TM / 2) + 32 * m + r32;
+      const int64_t slot = cur.lo + r;
+      if (slot >= cur.hi) continue;
+      bool have = true;
+      if (a.rows) have = rowbuf[buf * TM + r] >= 0 && rowbuf[buf * TM + r] < a.x_rows;
 #pragma unroll
-    for (int n = 0; n < (GLU ? 1 : H::NB); ++n)
+      for (int n = 0; n < (GLU ? 1 : H::NB); ++n)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        f32x4 v;
+        for (int e = 0; e < 4; ++e) {
+          f32x4 v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[i] = acc[n][m][4 * q + i];
-          if constexpr (GLU) v[i] = silu(v[i]) * acc[1][m][4 * q + i];
-          v[i] = have ? v[i] : 0.0f;
+          for (int i = 0; i < 4; ++i) {
+            v[i] = acc[n][m][4 * e + i];
+            if constexpr (GLU) v[i] = silu(v[i]) * acc[1][m][4 * e + i];
+            v[i] = have ? v[i] : 0.0f;
+          }
+          const int64_t at = n0 + wn * (GLU ? 32 : 64) + 32 * n + 8 * e + 4 * half;
+          if (at < a.N) store4(a, slot, at, a.N, wide, v);
         }
-        const int64_t at = n0 + wn * (GLU ? 32 : 64) + 32 * n + 8 * q + 4 * half;
-        if (at < a.N) store4(a, slot, at, a.N, wide, v);
-      }
+    }
+    if (!more) return;
+    cur = next;
+    buf = buf == 2 ? 0 : buf + 1;
+    clear();
+    find_next();
+    refill();
   }
 }
 
@@ -755,7 +886,10 @@ bitsmoe_status tile_product(const char* who, const MulArgs& a, hipStream_t s) {
   unsigned grid;
   if (!grid_of(a, TM, (a.N + TNO - 1) / TNO, &grid))
     return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": too many slots and outputs for one call");
-  constexpr int lds = H::kStages * H::kStage;
+  grid = static_cast<unsigned>(device_cus());  // one workgroup a compute unit, a multiple of the XCDs
+  grid = grid < 8 ? 8 : grid / 8 * 8;
+  constexpr int lds = H::kStages * H::kStage + 3 * TM * 4;
+  static_assert(lds <= 163840);
   auto* fn = mx4_tile_kernel<MX, GLU, TM>;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, lds);
