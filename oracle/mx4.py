@@ -55,10 +55,10 @@ def product(W, X, offsets=None, rows=None, S=None, glu=False):
     offsets = np.array([0, S]) if offsets is None else offsets
     Y = np.zeros((S, W.shape[1]))
     for e in range(E):
-        for s in range(max(0, offsets[e]), min(S, offsets[e + 1])):
-            r = s if rows is None else rows[s]
-            if 0 <= r < len(X):
-                Y[s] = W[e] @ X[r]
+        slots = np.arange(max(0, offsets[e]), min(S, offsets[e + 1]))
+        r = slots if rows is None else rows[slots]
+        there = (r >= 0) & (r < len(X))
+        Y[slots[there]] = X[r[there]] @ W[e].T
     if glu:
         N = W.shape[1] // 2
         Y = silu(Y[:, :N]) * Y[:, N:]

@@ -167,7 +167,12 @@ struct Walk {
   }
 };
 
-__device__ __forceinline__ float silu(float g) { return g / (1.0f + expf(-g)); }
+// v / (1 + exp(-v)) by the hardware's exponential and reciprocal (an ulp each;
+// the exponent's own rounding adds |v| 2^-24): a fifth of the instructions of
+// the library's exponential and an exact division.
+__device__ __forceinline__ float silu(float v) {
+  return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.44269504088896341f));
+}
 
 // Four consecutive results n .. n + 3 of slot s.
 __device__ __forceinline__ void store4(const MulArgs& a, int64_t s, int64_t n, int64_t N, bool wide, f32x4 v) {
@@ -192,6 +197,41 @@ __device__ __forceinline__ void store4(const MulArgs& a, int64_t s, int64_t n, i
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (n + i < N) p[i] = h[i];
+  }
+}
+
+// A lane's part of the 32 results n .. n + 31 of slot s: v[i] is that of
+// n + 8 (i / 4) + 4 half + i % 4, as a 32 x 32 accumulator lies.
+__device__ __forceinline__ void store32(const MulArgs& a, int64_t s, int64_t n, int half, bool whole,
+                                        const float (&v)[16]) {
+  if (!whole) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int64_t at = n + 8 * e + 4 * half;
+      if (at < a.N) store4(a, s, at, a.N, a.ldy % 4 == 0, f32x4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]});
+    }
+  } else if (a.yf32) {
+    float* p = static_cast<float*>(a.y) + s * a.ldy + n + 4 * half;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      *reinterpret_cast<f32x4*>(p + 8 * e) = f32x4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
+  } else {
+    // the two half-waves exchange words, so that each has eight results in a row
+    uint16_t* p = static_cast<uint16_t*>(a.y) + s * a.ldy + n + 8 * half;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      uint32_t w[2][2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const bf16x2 b = {static_cast<__bf16>(v[8 * e + 4 * i + 2 * h]), static_cast<__bf16>(v[8 * e + 4 * i + 2 * h + 1])};
+          w[i][h] = __builtin_bit_cast(uint32_t, b);
+        }
+      const auto x = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
+      const auto y = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+      *reinterpret_cast<uint4*>(p + 16 * e) = make_uint4(x[0], y[0], x[1], y[1]);
+    }
   }
 }
 
@@ -273,35 +313,50 @@ __global__ __launch_bounds__(kThreads) void mx4_rows_kernel(MulArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Large tiles: TM slots x 256 outputs a workgroup of eight waves.
+// Large tiles: 128 slots x 256 outputs a workgroup of eight waves.
 //
-// K advances KS entries at a time through kStages LDS stages that direct
-// global->LDS loads fill (16 bytes a lane for codes and tokens, one byte a lane,
-// widened to a word, for scales): codes stay four bits wide up to the registers.
-// Wave (wm, wn) of 2 x 4 owns TM/2 slots x 64 outputs as 32 x 32 accumulators,
+// Wave (wm, wn) of 2 x 4 owns 64 slots x 64 outputs as 32 x 32 accumulators,
 // the weights on the matrix core's row side, so that a lane holds runs of four
-// outputs of one slot.  With bf16 tokens a wave widens each fragment of codes
-// once (exact) and uses it for its TM/64 blocks of slots; with MX4 tokens the
-// scaled matrix-core form takes codes and scales as they lie.
+// outputs of one slot.  With bf16 tokens a wave widens each fragment of codes in
+// registers (exact; two conversions a matrix-core op) and uses it for its two
+// blocks of slots; with MX4 tokens the scaled matrix-core form takes codes and
+// scales as they lie.
+//
+// Direct global->LDS loads fill rings of stages: weights 256 entries of K at a
+// time and tokens 64 (bf16) or 256 (MX4), so that a row of either is a whole
+// cache line of 128 bytes; two loads in flight that share a line make the
+// second wait for the first's data.  For the same reason scales, 1/32 of a
+// byte an entry, come 512 entries at a time (16 bytes a row) where rows of
+// scales are a multiple of that (AL: K % 512 == 0), else a byte a lane with
+// each stage of weights.  A step that finds its stage read by every wave refills
+// the ring at once.
+//
+// A workgroup stays on its compute unit and takes tile after tile; the loads run
+// on into the next tile, so its first stages are there when the results of one
+// have been stored.
 // ---------------------------------------------------------------------------
-constexpr int kTileThreads = 512, kWaves = 8, kTN = 256;
+constexpr int kTileThreads = 512, kWaves = 8, kTM = 128, kTN = 256, kLds = 163840;
 
-template <bool MX, int TM_>
+template <bool MX_, bool AL_>
 struct Shape {
-  static constexpr int TM = TM_;
-  static constexpr int KS = MX ? 256 : 128;      // entries of K a step
-  static constexpr int XB = MX ? KS / 2 : 2 * KS;  // bytes of a token's row in a stage
-  static constexpr int WB = KS / 2;              // bytes of a weight row in a stage
-  static constexpr int SC = KS / 32;             // scales of a row in a stage (a word each)
-  static constexpr int kX = 0, kW = TM * XB, kWS = kW + kTN * WB, kXS = kWS + kTN * SC * 4;
-  static constexpr int kStage = kXS + (MX ? TM * SC * 4 : 0);
-  static constexpr int kStages = 163840 / kStage;
+  static constexpr bool MX = MX_, AL = AL_;
+  static constexpr int WK = 256, XK = MX ? 256 : 64;  // entries of K in a stage of weights, of tokens
+  static constexpr int kXStage = kTM * 128, kWStage = kTN * 128;
+  // scales: of a stage of weights, a word each; or of 512 entries, a byte each
+  static constexpr int kWS = AL ? 0 : kTN * 8 * 4, kXS = AL || !MX ? 0 : kTM * 8 * 4;
+  static constexpr int kChunk = AL ? (kTN + (MX ? kTM : 0)) * 16 : 0;
+  static constexpr int NX = MX ? (AL ? 3 : 2) : (AL ? 5 : 4), NW = MX ? NX : 2;
+  // LDS: the token ring, the weight ring (codes, then scales), two chunks of scales, rows of X of three tiles
+  static constexpr int oW = NX * kXStage, kWRing = kWStage + kWS + kXS, oC = oW + NW * kWRing;
+  static constexpr int oRows = oC + 2 * kChunk, kBytes = oRows + 3 * kTM * 4;
+  static_assert(kBytes <= kLds);
   // direct loads of a wave for a stage
-  static constexpr int LX = TM * XB / 1024 / kWaves, LW = kTN * WB / 1024 / kWaves;
-  static constexpr int LWS = kTN * SC / 64 / kWaves, LXS = MX ? TM * SC / 64 / kWaves : 0;
-  static constexpr int kLoads = LX + LW + LWS + LXS;
-  static constexpr int MB = TM / 64, NB = 2;
-  static_assert(kStages >= 2 && (kStages - 1) * kLoads < 64);
+  static constexpr int LX = kXStage / 1024 / kWaves, LW = kWStage / 1024 / kWaves;
+  static constexpr int LWS = kWS / 256 / kWaves, LXS = kXS / 256 / kWaves;
+  static constexpr int kWLoads = LW + LWS + LXS;
+  static constexpr int MB = 2, NB = 2;
+  // stages of weights a tile has at least, so that the rings never reach past the next tile
+  static constexpr int kLeast = MX ? (AL ? 4 : 2) : 2;
 };
 
 // What lanes past the end of a row read: zeros, and scales of 1.
@@ -309,11 +364,17 @@ __device__ const uint8_t kPad[32] __attribute__((aligned(16))) = {
     0,   0,   0,   0,   0,   0,   0,   0,   0,   0,   0,   0,   0,   0,   0,   0,
     127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127, 127};
 
-// One wave-wide direct load: lane l's 16 bytes (or byte) at p go to lds + 16 l
-// (lds + 4 l, as a word).  `lds` is wave-uniform.  The compiler does not track
-// it: callers wait by count (wait_loads) and synchronize before the data is read.
+// One wave-wide direct load: lane l's 16 bytes (word, byte) at p go to lds + 16 l
+// (lds + 4 l, a byte as a word).  `lds` is wave-uniform.  The compiler does not
+// track it: callers wait by count (wait_loads) and synchronize before the data
+// is read.
 __device__ __forceinline__ void load_lds16(const void* p, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p),
+               "s"(__builtin_amdgcn_readfirstlane(lds))
+               : "memory");
+}
+__device__ __forceinline__ void load_lds4(const void* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" ::"v"(p),
                "s"(__builtin_amdgcn_readfirstlane(lds))
                : "memory");
 }
@@ -326,109 +387,111 @@ __device__ __forceinline__ void load_lds1(const void* p, uint32_t lds) {
 // under way, and for the workgroup.
 template <int N>
 __device__ __forceinline__ void wait_loads() {
+  static_assert(N < 64);
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// Slot of 16-byte chunk c of row r in a stage whose rows have `chunks` of them:
-// sixteen rows read at the same chunk (what the LDS serves together) then lie in
-// different banks.
-template <int chunks>
-__device__ __forceinline__ int chunk_slot(int r, int c) {
-  return c ^ ((r / (16 / chunks)) & (chunks - 1));
-}
+// Place of 16-byte chunk c of row r in a stage of 128-byte rows: sixteen rows
+// read at the same chunk (what the LDS serves together) then lie in different
+// banks.
+__device__ __forceinline__ int chunk_slot(int r, int c) { return c ^ ((r >> 1) & 7); }
+// Place of scale c of row r among the eight words of its row.
+__device__ __forceinline__ int scale_slot(int r, int c) { return c ^ (2 * ((r >> 3) & 3)); }
 
-// Place of scale c of row r among the SC words of its row: as above, for words
-// that two half-waves read at neighbouring places.
-template <int SC>
-__device__ __forceinline__ int scale_slot(int r, int c) {
-  return c ^ (2 * ((r * SC / 64) & (SC / 2 - 1)));
-}
-
-// The operand fragments of a quarter of a step (32 entries of K with bf16
-// tokens, 64 with MX4 ones): read from a stage while the quarter before is
-// multiplied.
-template <bool MX, int TM>
+// The operand fragments of a part of a stage (32 entries of K with bf16 tokens,
+// 64 with MX4 ones): read while the part before is multiplied.
+template <class H>
 struct Frags {
-  using H = Shape<MX, TM>;
   uint4 w[H::NB];  // bf16 tokens: two words of each in use
-  uint4 x[H::MB][MX ? 1 : 2];
-  int ws[H::NB], xs[MX ? H::MB : 1];
-  // quarter u of the stage at s; wrow, xrow: this lane's first rows
-  template <int u>
-  __device__ __forceinline__ void read(const char* s, int wrow, int xrow, int half) {
-    const int c = 2 * (MX ? u : u / 2) + half;  // this lane's block of 32 in the step
-    constexpr int WC = H::WB / 16, XC = H::XB / 16;
+  uint4 x[H::MB][H::MX ? 1 : 2];
+  int ws[H::NB], xs[H::MX ? H::MB : 1];
+  // Part u of the stages at xst and wst, g being the token stage's place in the
+  // weights' (0 with MX4 tokens); sc: this stage's scales of row 0 (AL).
+  __device__ __forceinline__ void read(const char* xst, const char* wst, const char* sc, int g, int u, int wrow,
+                                       int xrow, int half) {
+    const int c = 2 * (H::MX ? u : g) + half;  // this lane's block of 32 in the weights' stage
 #pragma unroll
     for (int n = 0; n < H::NB; ++n) {
       const int r = wrow + 32 * n;
-      const char* at = s + H::kW + r * H::WB + chunk_slot<WC>(r, c) * 16;
-      if constexpr (MX) {
+      const char* at = wst + r * 128 + chunk_slot(r, c) * 16;
+      if constexpr (H::MX) {
         w[n] = *reinterpret_cast<const uint4*>(at);
       } else {
-        const uint2 v = *reinterpret_cast<const uint2*>(at + 8 * (u % 2));
+        const uint2 v = *reinterpret_cast<const uint2*>(at + 8 * u);
         w[n].x = v.x;
         w[n].y = v.y;
       }
-      ws[n] = *reinterpret_cast<const int*>(s + H::kWS + (r * H::SC + scale_slot<H::SC>(r, c)) * 4);
+      if constexpr (H::AL)
+        ws[n] = *reinterpret_cast<const uint8_t*>(sc + r * 16 + c);
+      else
+        ws[n] = *reinterpret_cast<const int*>(wst + H::kWStage + (r * 8 + scale_slot(r, c)) * 4);
     }
 #pragma unroll
     for (int m = 0; m < H::MB; ++m) {
       const int r = xrow + 32 * m;
-      const char* row = s + H::kX + r * H::XB;
-      if constexpr (MX) {
-        x[m][0] = *reinterpret_cast<const uint4*>(row + chunk_slot<XC>(r, c) * 16);
-        xs[m] = *reinterpret_cast<const int*>(s + H::kXS + (r * H::SC + scale_slot<H::SC>(r, c)) * 4);
+      const char* row = xst + r * 128;
+      if constexpr (H::MX) {
+        x[m][0] = *reinterpret_cast<const uint4*>(row + chunk_slot(r, c) * 16);
+        if constexpr (H::AL)
+          xs[m] = *reinterpret_cast<const uint8_t*>(sc + (kTN + r) * 16 + c);
+        else
+          xs[m] = *reinterpret_cast<const int*>(wst + H::kWStage + H::kWS + (r * 8 + scale_slot(r, c)) * 4);
       } else {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
-          x[m][j] = *reinterpret_cast<const uint4*>(row + chunk_slot<XC>(r, 4 * c + 2 * (u % 2) + j) * 16);
+          x[m][j] = *reinterpret_cast<const uint4*>(row + chunk_slot(r, 4 * half + 2 * u + j) * 16);
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
   }
-  __device__ __forceinline__ void multiply(f32x16 (&acc)[H::NB][H::MB]) const {
-    if constexpr (MX) {
+  // live: whether any of the wave's slots exist (not in the last tile of an expert)
+  __device__ __forceinline__ void multiply(f32x16 (&acc)[H::NB][H::MB], bool live) const {
+    if (live) {
+      if constexpr (H::MX) {
 #pragma unroll
-      for (int n = 0; n < H::NB; ++n)
-#pragma unroll
-        for (int m = 0; m < H::MB; ++m)
-          acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(codes(w[n]), codes(x[m][0]), acc[n][m], 4, 4, 0,
-                                                                      ws[n], 0, xs[m]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int n = 0; n < H::NB; ++n) {
-          const bf16x8 wf = mx4_bf16(j ? w[n].y : w[n].x, mx4_scale(ws[n]));
+        for (int n = 0; n < H::NB; ++n)
 #pragma unroll
           for (int m = 0; m < H::MB; ++m)
-            acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf, __builtin_bit_cast(bf16x8, x[m][j]), acc[n][m], 0,
-                                                                0, 0);
-        }
+            acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(codes(w[n]), codes(x[m][0]), acc[n][m], 4, 4,
+                                                                        0, ws[n], 0, xs[m]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int n = 0; n < H::NB; ++n) {
+            const bf16x8 wf = mx4_bf16(j ? w[n].y : w[n].x, mx4_scale(ws[n]));
+#pragma unroll
+            for (int m = 0; m < H::MB; ++m)
+              acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf, __builtin_bit_cast(bf16x8, x[m][j]), acc[n][m],
+                                                                  0, 0, 0);
+          }
+      }
     }
+    __builtin_amdgcn_sched_barrier(0);
   }
   __device__ __forceinline__ static i32x8 codes(uint4 v) {
     return i32x8{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0};
   }
 };
 
-template <bool MX, bool GLU, int TM>
+template <bool MX, bool AL, bool GLU>
 __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(MulArgs a) {
-  using H = Shape<MX, TM>;
+  using H = Shape<MX, AL>;
   extern __shared__ __align__(16) char smem[];
-  // rows of X of the slots of three tiles: the one multiplied, the next, and one before
-  int32_t* const rowbuf = reinterpret_cast<int32_t*>(smem + H::kStages * H::kStage);
+  int32_t* const rowbuf = reinterpret_cast<int32_t*>(smem + H::oRows);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   constexpr int TNO = GLU ? kTN / 2 : kTN;  // results a tile has of a slot
   const int wm = wave >> 2, wn = wave & 3, r32 = lane & 31, half = lane >> 5;
-  const int64_t kb = a.K / 32;
-  const int nk = static_cast<int>((a.K + H::KS - 1) / H::KS);
-  const int last = static_cast<int>(a.K - static_cast<int64_t>(nk - 1) * H::KS);  // entries of the last step
+  const int K = static_cast<int>(a.K), kb = K / 32;
+  const int nb = max((K + H::WK - 1) / H::WK, H::kLeast);  // stages of weights of a tile
+  const int nx = nb * (H::WK / H::XK);                     // and of tokens
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
+  const char *const zero = reinterpret_cast<const char*>(kPad), *const one = zero + 16;
 
   int none;
   Walk walk;
   Tile cur, next;
-  bool more = walk.start(a.offsets, a.E, a.S, static_cast<int>((a.N + TNO - 1) / TNO), TM, &none);
+  bool more = walk.start(a.offsets, a.E, a.S, static_cast<int>((a.N + TNO - 1) / TNO), kTM, &none);
   // slots of no expert: zeros
   for (int64_t s = none + static_cast<int64_t>(blockIdx.x); s < a.S; s += gridDim.x)
     for (int64_t n = threadIdx.x; n < a.N; n += kTileThreads) {
@@ -440,152 +503,171 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(MulArgs a) {
   if (!more) return;
   walk.get(&cur);
 
-  // Direct loads.  They run through the stages of one tile after another, a
-  // ring of kStages ahead of the multiplication and at most into the tile after
-  // the one multiplied, so that a tile's results are stored while the next
-  // one's first stages are on their way.
-  constexpr int XC = H::XB / 16, WC = H::WB / 16;
-  const char *px[H::LX], *pw[H::LW], *pws[H::LWS], *pxs[MX ? H::LXS : 1];
-  auto row_of = [&](int q, int per) { return (wave + kWaves * q) * per + lane / (64 / per); };
+  // ---- where the loads come from: 8 lanes a row of tokens or weights, and of scales by bytes
+  const char *px[H::LX], *pw[H::LW], *pws[AL ? 1 : H::LWS], *pxs[H::LXS ? H::LXS : 1], *pc = nullptr;
+  auto row_of = [&](int q) { return (wave + kWaves * q) * 8 + lane / 8; };
   auto load_rows = [&](const Tile& t, int buf) {  // the rows of a tile's slots (past its end: its last)
-    if (a.rows && wave < TM / 64) {
-      const int32_t* p = a.rows + min(t.lo + wave * 64 + lane, t.hi - 1);
-      asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" ::"v"(p),
-                   "s"(__builtin_amdgcn_readfirstlane(lds0 + H::kStages * H::kStage + (buf * TM + wave * 64) * 4))
-                   : "memory");
-    }
+    if (a.rows && wave < kTM / 64)
+      load_lds4(a.rows + min(t.lo + wave * 64 + lane, t.hi - 1), lds0 + H::oRows + (buf * kTM + wave * 64) * 4);
   };
-  auto aim = [&](const Tile& t, int buf) {  // the loads' addresses in the first stage of a tile
-    auto token = [&](int r) {  // (a row that does not exist: row 0, its results are replaced)
-      if (!a.rows) return static_cast<int64_t>(min(t.lo + r, t.hi - 1));
-      const int row = rowbuf[buf * TM + r];
-      return static_cast<int64_t>(row >= 0 && row < a.x_rows ? row : 0);
-    };
+  auto token = [&](const Tile& t, int buf, int r) {  // (a row that does not exist: row 0, its results are replaced)
+    if (!a.rows) return static_cast<int64_t>(min(t.lo + r, t.hi - 1));
+    const int row = rowbuf[buf * kTM + r];
+    return static_cast<int64_t>(row >= 0 && row < a.x_rows ? row : 0);
+  };
+  auto weight = [&](const Tile& t, int r) {
     const int64_t n0 = static_cast<int64_t>(t.col) * TNO;
-    auto weight = [&](int r) {
-      if constexpr (GLU)  // 32 gate rows, then the 32 up rows of the same outputs
-        return static_cast<int64_t>(t.e) * 2 * a.N + min(n0 + (r >> 6) * 32 + (r & 31), a.N - 1) +
-               ((r >> 5) & 1) * a.N;
-      else
-        return static_cast<int64_t>(t.e) * a.N + min(n0 + r, a.N - 1);
-    };
-#pragma unroll
-    for (int q = 0; q < H::LX; ++q) {
-      const int r = row_of(q, 64 / XC), c = chunk_slot<XC>(r, lane % XC);
-      px[q] = MX ? reinterpret_cast<const char*>(a.xcodes + token(r) * kb * 16 + c * 16)
-                 : reinterpret_cast<const char*>(a.x + token(r) * a.ldx + c * 8);
-    }
-#pragma unroll
-    for (int q = 0; q < H::LW; ++q) {
-      const int r = row_of(q, 64 / WC), c = chunk_slot<WC>(r, lane % WC);
-      pw[q] = reinterpret_cast<const char*>(a.codes + weight(r) * kb * 16 + c * 16);
-    }
-#pragma unroll
-    for (int q = 0; q < H::LWS; ++q) {
-      const int r = row_of(q, 64 / H::SC), c = scale_slot<H::SC>(r, lane % H::SC);
-      pws[q] = reinterpret_cast<const char*>(a.scales + weight(r) * kb + c);
-    }
-    if constexpr (MX) {
-#pragma unroll
-      for (int q = 0; q < H::LXS; ++q) {
-        const int r = row_of(q, 64 / H::SC), c = scale_slot<H::SC>(r, lane % H::SC);
-        pxs[q] = reinterpret_cast<const char*>(a.xscales + token(r) * kb + c);
-      }
-    }
-  };
-  int step = 0, to = 0, ahead = 0;  // the next stage of the tile loaded, its buffer, and stages not yet multiplied
-  auto issue = [&]() {
-    const uint32_t s = lds0 + to * H::kStage;
-    if (step == nk - 1 && last < H::KS) {  // lanes past K: zeros
-      const char *zero = reinterpret_cast<const char*>(kPad), *one = zero + 16;
-#pragma unroll
-      for (int q = 0; q < H::LX; ++q)
-        px[q] = chunk_slot<XC>(row_of(q, 64 / XC), lane % XC) * (MX ? 32 : 8) < last ? px[q] : zero;
-#pragma unroll
-      for (int q = 0; q < H::LW; ++q) pw[q] = chunk_slot<WC>(row_of(q, 64 / WC), lane % WC) * 32 < last ? pw[q] : zero;
-#pragma unroll
-      for (int q = 0; q < H::LWS; ++q)
-        pws[q] = scale_slot<H::SC>(row_of(q, 64 / H::SC), lane % H::SC) * 32 < last ? pws[q] : one;
-      if constexpr (MX) {
-#pragma unroll
-        for (int q = 0; q < H::LXS; ++q)
-          pxs[q] = scale_slot<H::SC>(row_of(q, 64 / H::SC), lane % H::SC) * 32 < last ? pxs[q] : one;
-      }
-    }
-#pragma unroll
-    for (int q = 0; q < H::LX; ++q) {
-      load_lds16(px[q], s + H::kX + (wave + kWaves * q) * 1024);
-      px[q] += H::XB;
-    }
-#pragma unroll
-    for (int q = 0; q < H::LW; ++q) {
-      load_lds16(pw[q], s + H::kW + (wave + kWaves * q) * 1024);
-      pw[q] += H::WB;
-    }
-#pragma unroll
-    for (int q = 0; q < H::LWS; ++q) {
-      load_lds1(pws[q], s + H::kWS + (wave + kWaves * q) * 256);
-      pws[q] += H::SC;
-    }
-    if constexpr (MX) {
-#pragma unroll
-      for (int q = 0; q < H::LXS; ++q) {
-        load_lds1(pxs[q], s + H::kXS + (wave + kWaves * q) * 256);
-        pxs[q] += H::SC;
-      }
-    }
-    ++step;
-    ++ahead;
-    to = to + 1 == H::kStages ? 0 : to + 1;
-  };
-  // Waits for all stages but the last `after` issued, and for the workgroup.
-  auto landed = [&](int after) {
-    if (H::kStages > 2 && after >= H::kStages - 1)
-      wait_loads<(H::kStages - 1) * H::kLoads>();
-    else if (after >= 1)
-      wait_loads<H::kLoads>();
+    if constexpr (GLU)  // 32 gate rows, then the 32 up rows of the same outputs
+      return static_cast<int64_t>(t.e) * 2 * a.N + min(n0 + (r >> 6) * 32 + (r & 31), a.N - 1) + ((r >> 5) & 1) * a.N;
     else
-      wait_loads<0>();
+      return static_cast<int64_t>(t.e) * a.N + min(n0 + r, a.N - 1);
   };
-  static_assert(H::kStages <= 3);
+  auto aim_x = [&](const Tile& t, int buf) {
+#pragma unroll
+    for (int q = 0; q < H::LX; ++q) {
+      const int r = row_of(q), c = chunk_slot(r, lane & 7);
+      const int64_t row = token(t, buf, r);
+      px[q] = MX ? reinterpret_cast<const char*>(a.xcodes + row * kb * 16 + c * 16)
+                 : reinterpret_cast<const char*>(a.x + row * a.ldx + c * 8);
+    }
+    if constexpr (!AL) {
+#pragma unroll
+      for (int q = 0; q < H::LXS; ++q) {
+        const int r = row_of(q);
+        pxs[q] = reinterpret_cast<const char*>(a.xscales + token(t, buf, r) * kb + scale_slot(r, lane & 7));
+      }
+    } else if (MX && wave >= 4 && wave < 6) {
+      pc = reinterpret_cast<const char*>(a.xscales + token(t, buf, (wave - 4) * 64 + lane) * kb);
+    }
+  };
+  auto aim_w = [&](const Tile& t) {
+#pragma unroll
+    for (int q = 0; q < H::LW; ++q) {
+      const int r = row_of(q);
+      pw[q] = reinterpret_cast<const char*>(a.codes + weight(t, r) * kb * 16 + chunk_slot(r, lane & 7) * 16);
+    }
+    if constexpr (!AL) {
+#pragma unroll
+      for (int q = 0; q < H::LWS; ++q) {
+        const int r = row_of(q);
+        pws[q] = reinterpret_cast<const char*>(a.scales + weight(t, r) * kb + scale_slot(r, lane & 7));
+      }
+    } else if (wave < 4) {
+      pc = reinterpret_cast<const char*>(a.scales + weight(t, wave * 64 + lane) * kb);
+    }
+  };
 
-  int buf = 0;                    // of rowbuf: the tile multiplied; the next one's is buf + 1
-  bool into_next = false;         // the loads have reached the next tile
-  int since = 0;                  // steps since the next tile's rows were asked for
+  // ---- the loads of the next stage of tokens and of weights
+  int xstep = 0, xto = 0, wstep = 0, wto = 0, cto = 0;
+  auto issue_x = [&]() {
+    const int rem = K - xstep * H::XK;  // entries from this stage on
+#pragma unroll
+    for (int q = 0; q < H::LX; ++q) {
+      const char* p = px[q];
+      if (rem < H::XK) {
+        asm volatile("");  // (a branch, not three selects at every step)
+        p = chunk_slot(row_of(q), lane & 7) * (MX ? 32 : 8) < rem ? p : zero;
+      }
+      load_lds16(p, lds0 + xto * H::kXStage + (wave + kWaves * q) * 1024);
+      px[q] += 128;
+    }
+    ++xstep;
+    xto = xto + 1 == H::NX ? 0 : xto + 1;
+  };
+  auto issue_w = [&]() {
+    const int rem = K - wstep * H::WK;
+    const uint32_t s = lds0 + H::oW + wto * H::kWRing;
+    if constexpr (AL) {
+      if ((wstep & 1) == 0) {  // the scales of 512 entries
+        if (wave < (MX ? 6 : 4)) {
+          load_lds16(rem > 0 ? pc : one, lds0 + H::oC + cto * H::kChunk + wave * 1024);
+          pc += 16;
+        }
+        cto ^= 1;
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < H::LW; ++q) {
+      const char* p = pw[q];
+      if (rem < H::WK) p = chunk_slot(row_of(q), lane & 7) * 32 < rem ? p : zero;
+      load_lds16(p, s + (wave + kWaves * q) * 1024);
+      pw[q] += 128;
+    }
+    if constexpr (!AL) {
+#pragma unroll
+      for (int q = 0; q < H::LWS; ++q) {
+        const char* p = pws[q];
+        if (rem < H::WK) p = scale_slot(row_of(q), lane & 7) * 32 < rem ? p : one;
+        load_lds1(p, s + H::kWStage + (wave + kWaves * q) * 256);
+        pws[q] += 8;
+      }
+#pragma unroll
+      for (int q = 0; q < H::LXS; ++q) {
+        const char* p = pxs[q];
+        if (rem < H::WK) p = scale_slot(row_of(q), lane & 7) * 32 < rem ? p : one;
+        load_lds1(p, s + H::kWStage + H::kWS + (wave + kWaves * q) * 256);
+        pxs[q] += 8;
+      }
+    }
+    ++wstep;
+    wto = wto + 1 == H::NW ? 0 : wto + 1;
+  };
+
+  // ---- going on into the next tile
+  int buf = 0;    // of rowbuf: the tile multiplied; the next one's is the one after
+  int since = 0;  // steps since the next tile's rows were asked for
+  bool xdry = false, wdry = false;  // loads of tokens, of weights are left out: there is no next tile
+  auto after = [&](int b) { return b == 2 ? 0 : b + 1; };
   auto find_next = [&]() {
     walk.l += walk.step;
     more = walk.find();
     if (more) {
       walk.get(&next);
-      load_rows(next, buf == 2 ? 0 : buf + 1);
+      load_rows(next, after(buf));
     }
-    into_next = false;
     since = 0;
   };
-  // Fills the ring as far as it goes.
-  auto refill = [&]() {
-    while (ahead < H::kStages) {
-      if (step == nk) {
-        if (!more || into_next) break;
-        // the rows have landed if the stages asked for since then fill the ring
-        if (a.rows && since < H::kStages) wait_loads<0>();
-        aim(next, buf == 2 ? 0 : buf + 1);
-        step = 0;
-        into_next = true;
-      }
-      issue();
-    }
-    ++since;
+  auto next_x = [&]() {  // whether there is a stage of tokens to load
+    if (xstep < nx) return true;
+    if (!more) return false;
+    // the next tile's rows have landed if the tokens asked for since then fill the ring
+    if (a.rows && since < H::NX) wait_loads<0>();
+    aim_x(next, after(buf));
+    xstep = 0;
+    return true;
+  };
+  auto next_w = [&]() {
+    if (wstep < nb) return true;
+    if (!more) return false;
+    aim_w(next);
+    wstep = 0;
+    return true;
   };
 
   load_rows(cur, 0);
   wait_loads<0>();
-  aim(cur, 0);
-  while (ahead < H::kStages && step < nk) issue();
+  aim_x(cur, 0);
+  aim_w(cur);
+  // the order of the main loop, which the counts of its waits go by
+  issue_w();
+  if constexpr (MX) {
+    issue_x();
+#pragma unroll
+    for (int i = 1; i < H::NW; ++i) {
+      issue_w();
+      issue_x();
+    }
+    wait_loads<(H::NW - 1) * (H::kWLoads + H::LX)>();
+  } else {
+#pragma unroll
+    for (int i = 0; i < H::NX - 1; ++i) issue_x();
+    issue_w();
+    issue_x();
+    wait_loads<(H::NX - 1) * H::LX + H::kWLoads>();
+  }
   find_next();
-  refill();
 
-  const int wrow = wn * 64 + r32, xrow = wm * (TM / 2) + r32;
+  const int wrow = wn * 64 + r32, xrow = wm * (kTM / 2) + r32;
   f32x16 acc[H::NB][H::MB];
   auto clear = [&]() {
 #pragma unroll
@@ -596,64 +678,106 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(MulArgs a) {
         for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
   };
   clear();
-  Frags<MX, TM> p, q;
-  landed(ahead - 1);
-  const char* s = smem;
-  p.template read<0>(s, wrow, xrow, half);
+  const char *xst = smem, *wst = smem + H::oW, *sc = smem + H::oC;
+  auto advance_x = [&]() { xst = xst + H::kXStage == smem + H::oW ? smem : xst + H::kXStage; };
+  int chunk = 0;
+  auto advance_w = [&](int b) {  // to stage b of its tile
+    wst = wst + H::kWRing == smem + H::oC ? smem + H::oW : wst + H::kWRing;
+    if constexpr (AL) {
+      if ((b & 1) == 0) chunk ^= 1;
+      sc = smem + H::oC + chunk * H::kChunk + (b & 1) * 8;
+    }
+  };
+  Frags<H> p, q;
+  bool live = cur.lo + wm * (kTM / 2) < cur.hi;
+  p.read(xst, wst, sc, 0, 0, wrow, xrow, half);
   for (;;) {
-    for (int i = 0; i < nk; ++i) {
-      q.template read<1>(s, wrow, xrow, half);
-      __builtin_amdgcn_sched_barrier(0);
-      p.multiply(acc);
-      __builtin_amdgcn_sched_barrier(0);
-      p.template read<2>(s, wrow, xrow, half);
-      __builtin_amdgcn_sched_barrier(0);
-      q.multiply(acc);
-      __builtin_amdgcn_sched_barrier(0);
-      q.template read<3>(s, wrow, xrow, half);
-      __builtin_amdgcn_sched_barrier(0);
-      p.multiply(acc);
-      __builtin_amdgcn_sched_barrier(0);
-      // the next stage has landed, and every wave has read all of this one: its buffer is free
-      landed(ahead - 2);
-      --ahead;
-      refill();
-      s = s + H::kStage == smem + H::kStages * H::kStage ? smem : s + H::kStage;
-      p.template read<0>(s, wrow, xrow, half);  // (of the next tile after a tile's last step; unused at the end)
-      __builtin_amdgcn_sched_barrier(0);
-      q.multiply(acc);
-      __builtin_amdgcn_sched_barrier(0);
+    for (int b = 0; b < nb; ++b) {
+      if constexpr (MX) {
+        q.read(xst, wst, sc, 0, 1, wrow, xrow, half);
+        p.multiply(acc, live);
+        p.read(xst, wst, sc, 0, 2, wrow, xrow, half);
+        q.multiply(acc, live);
+        q.read(xst, wst, sc, 0, 3, wrow, xrow, half);
+        p.multiply(acc, live);
+        // the next stage has landed (but for the NW - 2 after it), and every wave has read this one
+        if (xdry)
+          wait_loads<0>();
+        else
+          wait_loads<(H::NW - 2) * (H::kWLoads + H::LX)>();
+        ++since;
+        if (next_x() && next_w()) {
+          issue_w();
+          issue_x();
+        } else {
+          xdry = true;
+        }
+        advance_x();
+        advance_w(b + 1 == nb ? 0 : b + 1);
+        p.read(xst, wst, sc, 0, 0, wrow, xrow, half);  // (unused after the last tile)
+        q.multiply(acc, live);
+      } else {
+        auto step = [&](auto gg) {  // stage of tokens 4 b + g
+          constexpr int g = decltype(gg)::value;
+          q.read(xst, wst, sc, g, 1, wrow, xrow, half);
+          p.multiply(acc, live);
+          // The next stage has landed: later than its loads are those of NX - 2 stages of tokens, and of a stage
+          // of weights if the last step of a stage of weights is among the steps they were issued in.
+          if (xdry)
+            wait_loads<0>();
+          else if (wdry)
+            wait_loads<(H::NX - 2) * H::LX>();
+          else
+            wait_loads<(H::NX - 2) * H::LX + (g <= H::NX - 3 ? H::kWLoads : 0)>();
+          ++since;
+          if constexpr (g == 3) {
+            if (next_w())
+              issue_w();
+            else
+              wdry = true;
+          }
+          if (next_x())
+            issue_x();
+          else
+            xdry = true;
+          advance_x();
+          if constexpr (g == 3) advance_w(b + 1 == nb ? 0 : b + 1);
+          p.read(xst, wst, sc, (g + 1) & 3, 0, wrow, xrow, half);  // (unused after the last tile)
+          q.multiply(acc, live);
+        };
+        step(std::integral_constant<int, 0>());
+        step(std::integral_constant<int, 1>());
+        step(std::integral_constant<int, 2>());
+        step(std::integral_constant<int, 3>());
+      }
     }
     const int64_t n0 = static_cast<int64_t>(cur.col) * TNO;
-    const bool wide = a.ldy % 4 == 0;
+    const bool whole = n0 + TNO <= a.N && a.ldy % 8 == 0;
 #pragma unroll
     for (int m = 0; m < H::MB; ++m) {
-      const int r = wm * (TM / 2) + 32 * m + r32;
+      const int r = wm * (kTM / 2) + 32 * m + r32;
       const int64_t slot = cur.lo + r;
       if (slot >= cur.hi) continue;
       bool have = true;
-      if (a.rows) have = rowbuf[buf * TM + r] >= 0 && rowbuf[buf * TM + r] < a.x_rows;
+      if (a.rows) have = rowbuf[buf * kTM + r] >= 0 && rowbuf[buf * kTM + r] < a.x_rows;
 #pragma unroll
-      for (int n = 0; n < (GLU ? 1 : H::NB); ++n)
+      for (int n = 0; n < (GLU ? 1 : H::NB); ++n) {
+        float v[16];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          f32x4 v;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            v[i] = acc[n][m][4 * e + i];
-            if constexpr (GLU) v[i] = silu(v[i]) * acc[1][m][4 * e + i];
-            v[i] = have ? v[i] : 0.0f;
-          }
-          const int64_t at = n0 + wn * (GLU ? 32 : 64) + 32 * n + 8 * e + 4 * half;
-          if (at < a.N) store4(a, slot, at, a.N, wide, v);
+        for (int i = 0; i < 16; ++i) {
+          v[i] = acc[n][m][i];
+          if constexpr (GLU) v[i] = silu(v[i]) * acc[1][m][i];
+          v[i] = have ? v[i] : 0.0f;
         }
+        store32(a, slot, n0 + wn * (GLU ? 32 : 64) + 32 * n, half, whole, v);
+      }
     }
     if (!more) return;
     cur = next;
-    buf = buf == 2 ? 0 : buf + 1;
+    buf = after(buf);
+    live = cur.lo + wm * (kTM / 2) < cur.hi;
     clear();
     find_next();
-    refill();
   }
 }
 
@@ -747,7 +871,7 @@ __global__ __launch_bounds__(kTileThreads) void mx4_grad_tile_kernel(MulArgs a) 
     int nx[H::LX];
 #pragma unroll
     for (int q = 0; q < H::LX; ++q) {
-      const int r = (wave + kWaves * q) * 8 + lane / 8, c = chunk_slot<8>(r, lane % 8);
+      const int r = (wave + kWaves * q) * 8 + lane / 8, c = chunk_slot(r, lane % 8);
       nx[q] = 8 * c;
       px[q] = reinterpret_cast<const char*>(a.x + min(t.lo + r, t.hi - 1) * a.ldx + 8 * c);
     }
@@ -812,7 +936,7 @@ __global__ __launch_bounds__(kTileThreads) void mx4_grad_tile_kernel(MulArgs a) 
 #pragma unroll
         for (int m = 0; m < H::MB; ++m) {
           const int r = xrow + 32 * m;
-          xf[m] = *reinterpret_cast<const bf16x8*>(s + H::kX + r * (H::NS * 2) + chunk_slot<8>(r, 2 * j + half) * 16);
+          xf[m] = *reinterpret_cast<const bf16x8*>(s + H::kX + r * (H::NS * 2) + chunk_slot(r, 2 * j + half) * 16);
         }
 #pragma unroll
         for (int n = 0; n < H::NB; ++n) {
@@ -879,18 +1003,13 @@ bool grid_of(const MulArgs& a, int64_t tile, int64_t per, unsigned* grid) {
 // Large tiles pay from about this many slots an expert on.
 constexpr int64_t kTileSlots = 32;
 
-template <bool MX, bool GLU, int TM>
-bitsmoe_status tile_product(const char* who, const MulArgs& a, hipStream_t s) {
-  using H = Shape<MX, TM>;
-  constexpr int TNO = GLU ? kTN / 2 : kTN;
-  unsigned grid;
-  if (!grid_of(a, TM, (a.N + TNO - 1) / TNO, &grid))
-    return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": too many slots and outputs for one call");
-  grid = static_cast<unsigned>(device_cus());  // one workgroup a compute unit, a multiple of the XCDs
-  grid = grid < 8 ? 8 : grid / 8 * 8;
-  constexpr int lds = H::kStages * H::kStage + 3 * TM * 4;
-  static_assert(lds <= 163840);
-  auto* fn = mx4_tile_kernel<MX, GLU, TM>;
+template <bool MX, bool AL, bool GLU>
+bitsmoe_status tile_product(const MulArgs& a, hipStream_t s) {
+  // one workgroup a compute unit, as many on every XCD
+  const int cus = device_cus();
+  const unsigned grid = static_cast<unsigned>(cus < 8 ? 8 : cus / 8 * 8);
+  constexpr int lds = Shape<MX, AL>::kBytes;
+  auto* fn = mx4_tile_kernel<MX, AL, GLU>;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return device_error("mx4_product: shared memory", e);
@@ -902,8 +1021,12 @@ bitsmoe_status tile_product(const char* who, const MulArgs& a, hipStream_t s) {
 bitsmoe_status product(const char* who, const MulArgs& a, bool glu, hipStream_t s) {
   const bool mx = a.xcodes != nullptr;
   if (a.S >= kTileSlots * a.E && a.x_rows > 0) {
-    if (mx) return glu ? tile_product<true, true, 128>(who, a, s) : tile_product<true, false, 128>(who, a, s);
-    return glu ? tile_product<false, true, 128>(who, a, s) : tile_product<false, false, 128>(who, a, s);
+    // (with MX4 tokens four stages of weights a tile at least, so that a chunk of scales outlives its two)
+    const bool al = a.K % 512 == 0 && (!mx || a.K >= 1024);
+    if (mx && al) return glu ? tile_product<true, true, true>(a, s) : tile_product<true, true, false>(a, s);
+    if (mx) return glu ? tile_product<true, false, true>(a, s) : tile_product<true, false, false>(a, s);
+    if (al) return glu ? tile_product<false, true, true>(a, s) : tile_product<false, true, false>(a, s);
+    return glu ? tile_product<false, false, true>(a, s) : tile_product<false, false, false>(a, s);
   }
   unsigned grid;
   if (!grid_of(a, 16, (a.N + 15) / 16, &grid))
