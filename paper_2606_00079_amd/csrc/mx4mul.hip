@@ -398,29 +398,20 @@ __device__ __forceinline__ int chunk_slot(int r, int c) { return c ^ ((r >> 1) &
 // Place of scale c of row r among the eight words of its row.
 __device__ __forceinline__ int scale_slot(int r, int c) { return c ^ (2 * ((r >> 3) & 3)); }
 
-// The operand fragments of a part of a stage (32 entries of K with bf16 tokens,
-// 64 with MX4 ones): read while the part before is multiplied.
+// MX4 tokens: the operand fragments of 64 entries of K, a quarter of a stage,
+// read while the quarter before is multiplied.
 template <class H>
 struct Frags {
-  uint4 w[H::NB];  // bf16 tokens: two words of each in use
-  uint4 x[H::MB][H::MX ? 1 : 2];
-  int ws[H::NB], xs[H::MX ? H::MB : 1];
-  // Part u of the stages at xst and wst, g being the token stage's place in the
-  // weights' (0 with MX4 tokens); sc: this stage's scales of row 0 (AL).
-  __device__ __forceinline__ void read(const char* xst, const char* wst, const char* sc, int g, int u, int wrow,
-                                       int xrow, int half) {
-    const int c = 2 * (H::MX ? u : g) + half;  // this lane's block of 32 in the weights' stage
+  uint4 w[H::NB], x[H::MB];
+  int ws[H::NB], xs[H::MB];
+  // Quarter u of the stages at xst and wst; sc: this stage's scales of row 0 (AL).
+  __device__ __forceinline__ void read(const char* xst, const char* wst, const char* sc, int u, int wrow, int xrow,
+                                       int half) {
+    const int c = 2 * u + half;  // this lane's block of 32
 #pragma unroll
     for (int n = 0; n < H::NB; ++n) {
       const int r = wrow + 32 * n;
-      const char* at = wst + r * 128 + chunk_slot(r, c) * 16;
-      if constexpr (H::MX) {
-        w[n] = *reinterpret_cast<const uint4*>(at);
-      } else {
-        const uint2 v = *reinterpret_cast<const uint2*>(at + 8 * u);
-        w[n].x = v.x;
-        w[n].y = v.y;
-      }
+      w[n] = *reinterpret_cast<const uint4*>(wst + r * 128 + chunk_slot(r, c) * 16);
       if constexpr (H::AL)
         ws[n] = *reinterpret_cast<const uint8_t*>(sc + r * 16 + c);
       else
@@ -429,48 +420,71 @@ struct Frags {
 #pragma unroll
     for (int m = 0; m < H::MB; ++m) {
       const int r = xrow + 32 * m;
-      const char* row = xst + r * 128;
-      if constexpr (H::MX) {
-        x[m][0] = *reinterpret_cast<const uint4*>(row + chunk_slot(r, c) * 16);
-        if constexpr (H::AL)
-          xs[m] = *reinterpret_cast<const uint8_t*>(sc + (kTN + r) * 16 + c);
-        else
-          xs[m] = *reinterpret_cast<const int*>(wst + H::kWStage + H::kWS + (r * 8 + scale_slot(r, c)) * 4);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          x[m][j] = *reinterpret_cast<const uint4*>(row + chunk_slot(r, 4 * half + 2 * u + j) * 16);
-      }
+      x[m] = *reinterpret_cast<const uint4*>(xst + r * 128 + chunk_slot(r, c) * 16);
+      if constexpr (H::AL)
+        xs[m] = *reinterpret_cast<const uint8_t*>(sc + (kTN + r) * 16 + c);
+      else
+        xs[m] = *reinterpret_cast<const int*>(wst + H::kWStage + H::kWS + (r * 8 + scale_slot(r, c)) * 4);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
-  // live: whether any of the wave's slots exist (not in the last tile of an expert)
-  __device__ __forceinline__ void multiply(f32x16 (&acc)[H::NB][H::MB], bool live) const {
-    if (live) {
-      if constexpr (H::MX) {
+  __device__ __forceinline__ void multiply(f32x16 (&acc)[H::NB][H::MB]) const {
 #pragma unroll
-        for (int n = 0; n < H::NB; ++n)
+    for (int n = 0; n < H::NB; ++n)
 #pragma unroll
-          for (int m = 0; m < H::MB; ++m)
-            acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(codes(w[n]), codes(x[m][0]), acc[n][m], 4, 4,
-                                                                        0, ws[n], 0, xs[m]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int n = 0; n < H::NB; ++n) {
-            const bf16x8 wf = mx4_bf16(j ? w[n].y : w[n].x, mx4_scale(ws[n]));
-#pragma unroll
-            for (int m = 0; m < H::MB; ++m)
-              acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf, __builtin_bit_cast(bf16x8, x[m][j]), acc[n][m],
-                                                                  0, 0, 0);
-          }
-      }
-    }
+      for (int m = 0; m < H::MB; ++m)
+        acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(codes(w[n]), codes(x[m]), acc[n][m], 4, 4, 0, ws[n],
+                                                                    0, xs[m]);
     __builtin_amdgcn_sched_barrier(0);
   }
   __device__ __forceinline__ static i32x8 codes(uint4 v) {
     return i32x8{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0};
+  }
+};
+
+// bf16 tokens: half a stage of tokens at a time (32 entries of K).  A half goes
+// through three phases: its codes and scales are read; they are widened and its
+// tokens read; it is multiplied.  The phases of three halves run together, one
+// read and two conversions behind each matrix-core op: both waves of a SIMD
+// leave a barrier together, so what stands before or after the ops would leave
+// the matrix cores idle in both.
+template <class H>
+struct Codes {
+  uint2 w[H::NB];
+  int s[H::NB];
+  // row n's part of half u of stage g of tokens, in the weights' stage at wst
+  __device__ __forceinline__ void read(int n, const char* wst, const char* sc, int g, int u, int wrow, int half) {
+    const int c = 2 * g + half, r = wrow + 32 * n;
+    w[n] = *reinterpret_cast<const uint2*>(wst + r * 128 + chunk_slot(r, c) * 16 + 8 * u);
+    if constexpr (H::AL)
+      s[n] = *reinterpret_cast<const uint8_t*>(sc + r * 16 + c);
+    else
+      s[n] = *reinterpret_cast<const int*>(wst + H::kWStage + (r * 8 + scale_slot(r, c)) * 4);
+  }
+};
+template <class H>
+struct Wide {
+  uint4 w[2][H::NB];
+  // words 2 i and 2 i + 1 of entry group j of row n, (j, n, i) the digits of k = 0 .. 7
+  __device__ __forceinline__ void convert(int k, const Codes<H>& c) {
+    const int j = k >> 2, n = (k >> 1) & 1;
+    const uint32_t v = j ? c.w[n].y : c.w[n].x;
+    const float s = mx4_scale(c.s[n]);
+    if ((k & 1) == 0) {
+      w[j][n].x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, s, 0));
+      w[j][n].y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, s, 1));
+    } else {
+      w[j][n].z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, s, 2));
+      w[j][n].w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, s, 3));
+    }
+  }
+};
+template <class H>
+struct Tokens {
+  uint4 x[H::MB][2];
+  __device__ __forceinline__ void read(int m, int j, const char* xst, int u, int xrow, int half) {
+    const int r = xrow + 32 * m;
+    x[m][j] = *reinterpret_cast<const uint4*>(xst + r * 128 + chunk_slot(r, 4 * half + 2 * u + j) * 16);
   }
 };
 
@@ -688,18 +702,46 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(MulArgs a) {
       sc = smem + H::oC + chunk * H::kChunk + (b & 1) * 8;
     }
   };
+  // MX4 tokens
   Frags<H> p, q;
-  bool live = cur.lo + wm * (kTM / 2) < cur.hi;
-  p.read(xst, wst, sc, 0, 0, wrow, xrow, half);
+  // bf16 tokens: halves 0 and 1 of a stage
+  Codes<H> c0, c1;
+  Wide<H> w0, w1;
+  Tokens<H> x0, x1;
+  // Multiplies a half by (w, x), widens the next (c to wn), and reads that one's tokens and the codes after those.
+  auto work = [&](const Wide<H>& w, const Tokens<H>& x, const Codes<H>& c, Wide<H>& wnext, auto reads) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int j = k >> 2, n = (k >> 1) & 1, m = k & 1;
+      acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w.w[j][n]),
+                                                          __builtin_bit_cast(bf16x8, x.x[m][j]), acc[n][m], 0, 0, 0);
+      reads(k);
+      wnext.convert(k, c);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  if constexpr (MX) {
+    p.read(xst, wst, sc, 0, wrow, xrow, half);
+  } else {
+#pragma unroll
+    for (int n = 0; n < H::NB; ++n) {
+      c0.read(n, wst, sc, 0, 0, wrow, half);
+      c1.read(n, wst, sc, 0, 1, wrow, half);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x0.read(k & 1, k >> 1, xst, 0, xrow, half);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w0.convert(k, c0);
+  }
   for (;;) {
     for (int b = 0; b < nb; ++b) {
       if constexpr (MX) {
-        q.read(xst, wst, sc, 0, 1, wrow, xrow, half);
-        p.multiply(acc, live);
-        p.read(xst, wst, sc, 0, 2, wrow, xrow, half);
-        q.multiply(acc, live);
-        q.read(xst, wst, sc, 0, 3, wrow, xrow, half);
-        p.multiply(acc, live);
+        q.read(xst, wst, sc, 1, wrow, xrow, half);
+        p.multiply(acc);
+        p.read(xst, wst, sc, 2, wrow, xrow, half);
+        q.multiply(acc);
+        q.read(xst, wst, sc, 3, wrow, xrow, half);
+        p.multiply(acc);
         // the next stage has landed (but for the NW - 2 after it), and every wave has read this one
         if (xdry)
           wait_loads<0>();
@@ -714,23 +756,30 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(MulArgs a) {
         }
         advance_x();
         advance_w(b + 1 == nb ? 0 : b + 1);
-        p.read(xst, wst, sc, 0, 0, wrow, xrow, half);  // (unused after the last tile)
-        q.multiply(acc, live);
+        p.read(xst, wst, sc, 0, wrow, xrow, half);  // (unused after the last tile)
+        q.multiply(acc);
       } else {
         auto step = [&](auto gg) {  // stage of tokens 4 b + g
           constexpr int g = decltype(gg)::value;
-          q.read(xst, wst, sc, g, 1, wrow, xrow, half);
-          p.multiply(acc, live);
-          // The next stage has landed: later than its loads are those of NX - 2 stages of tokens, and of a stage
-          // of weights if the last step of a stage of weights is among the steps they were issued in.
+          // codes are read a stage of tokens ahead
+          if constexpr (g == 3) advance_w(b + 1 == nb ? 0 : b + 1);
+          work(w0, x0, c1, w1, [&](int k) {
+            if (k < 4)
+              x1.read(k & 1, k >> 1, xst, 1, xrow, half);
+            else if (k < 6)
+              c0.read(k - 4, wst, sc, (g + 1) & 3, 0, wrow, half);
+          });
+          // The next stage of tokens has landed, and before the last step of a stage of weights the next one too:
+          // later than those loads are those of NX - 2 stages of tokens, and of a stage of weights if the last step
+          // of a stage of weights is among the steps they were issued in.
           if (xdry)
             wait_loads<0>();
           else if (wdry)
             wait_loads<(H::NX - 2) * H::LX>();
           else
-            wait_loads<(H::NX - 2) * H::LX + (g <= H::NX - 3 ? H::kWLoads : 0)>();
+            wait_loads<(H::NX - 2) * H::LX + (g < 2 && g <= H::NX - 3 ? H::kWLoads : 0)>();
           ++since;
-          if constexpr (g == 3) {
+          if constexpr (g == 3) {  // (every wave has read the codes before: their buffer is free)
             if (next_w())
               issue_w();
             else
@@ -741,9 +790,12 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(MulArgs a) {
           else
             xdry = true;
           advance_x();
-          if constexpr (g == 3) advance_w(b + 1 == nb ? 0 : b + 1);
-          p.read(xst, wst, sc, (g + 1) & 3, 0, wrow, xrow, half);  // (unused after the last tile)
-          q.multiply(acc, live);
+          work(w1, x1, c0, w0, [&](int k) {  // (what is read after the last tile is not used)
+            if (k < 4)
+              x0.read(k & 1, k >> 1, xst, 0, xrow, half);
+            else if (k < 6)
+              c1.read(k - 4, wst, sc, (g + 1) & 3, 1, wrow, half);
+          });
         };
         step(std::integral_constant<int, 0>());
         step(std::integral_constant<int, 1>());
@@ -775,7 +827,6 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(MulArgs a) {
     if (!more) return;
     cur = next;
     buf = after(buf);
-    live = cur.lo + wm * (kTM / 2) < cur.hi;
     clear();
     find_next();
   }
