@@ -20,8 +20,7 @@ constexpr int kMx4Block = 32;
 __device__ __forceinline__ float mx4_scale(uint32_t s) { return __uint_as_float(s << 23); }
 
 // The eight entries of a word of codes as bf16.  Exact: a value has two
-// significant bits and lies in bf16's range (down to its subnormals).  In
-// words: single elements taken out of the conversions' results came out wrong.
+// significant bits and lies in bf16's range (down to its subnormals).
 __device__ __forceinline__ uint4 mx4_bf16_words(uint32_t w, float scale) {
   return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),

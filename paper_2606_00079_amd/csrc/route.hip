@@ -13,10 +13,10 @@
 // A row lies on LPT lanes, V consecutive logits a lane (V = 8 up to 512
 // experts), so that up to 64 rows share a wave and every reduction is a few
 // lane exchanges.  Workgroups take runs of consecutive rows: a first launch
-// writes each run's expert counts and probability sums, a second one adds the
-// runs before its own (integers, or fp32 in the order of the runs: results do
-// not depend on timing) and places the slots.  A single run does both in one
-// launch.
+// writes each run's expert counts and probability sums, a second one sums them
+// up over the runs (integers, and fp32 in the order of the runs: results do not
+// depend on timing), and a third places the slots.  A single run does it all in
+// one launch.
 #include <cstdint>
 #include <string>
 
@@ -26,7 +26,8 @@
 namespace bitsmoe {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 1024;      // of a workgroup with eight logits a lane (256 with more)
+constexpr int kGradThreads = 256;
 constexpr int kMaxExperts = 4096;
 constexpr int kMaxRuns = 256;       // workgroups of the first launch, unless a run gets too long
 constexpr int kMinRun = 16;         // rows of the shortest run
@@ -41,24 +42,56 @@ __device__ __forceinline__ float order_value(uint32_t o) {
   return __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
 }
 
-template <int LPT, typename F>
-__device__ __forceinline__ float row_reduce(float v, F f) {
-#pragma unroll
-  for (int o = 1; o < LPT; o <<= 1) v = f(v, __shfl_xor(v, o, 64));
+// A row's lanes exchange values inside the VALU: by lane permutations within
+// sixteen lanes (neighbour, pair, then mirrored halves, whose lanes already
+// agree), and by swapping rows of lanes beyond.
+template <int LPT, typename T, typename F>
+__device__ __forceinline__ T row_reduce(T v, F f) {
+  static_assert(sizeof(T) == 4);
+  auto dpp = [&](auto ctrl) {
+    const int x = __builtin_bit_cast(int, v);
+    v = f(v, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(x, x, decltype(ctrl)::value, 0xF, 0xF, false)));
+  };
+  if constexpr (LPT > 1) dpp(std::integral_constant<int, 0xB1>());
+  if constexpr (LPT > 2) dpp(std::integral_constant<int, 0x4E>());
+  if constexpr (LPT > 4) dpp(std::integral_constant<int, 0x141>());
+  if constexpr (LPT > 8) dpp(std::integral_constant<int, 0x140>());
+  if constexpr (LPT > 16) {
+    const uint32_t x = __builtin_bit_cast(uint32_t, v);
+    const auto s = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    const uint32_t p = s[0], q = s[1];  // (a bit cast of a vector's element takes the first)
+    v = f(__builtin_bit_cast(T, p), __builtin_bit_cast(T, q));
+  }
+  if constexpr (LPT > 32) {
+    const uint32_t x = __builtin_bit_cast(uint32_t, v);
+    const auto s = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    const uint32_t p = s[0], q = s[1];  // (a bit cast of a vector's element takes the first)
+    v = f(__builtin_bit_cast(T, p), __builtin_bit_cast(T, q));
+  }
   return v;
 }
+// exp(d) for d <= 0 (or NaN) by the hardware's 2^t, with what t = d / ln 2 loses
+// to rounding put back: a third of the library function's instructions.
+__device__ __forceinline__ float exp_neg(float d) {
+  d = d < -150.0f ? -150.0f : d;  // (0 in fp32; -inf would give a NaN below)
+  const float t = d * 1.44269504088896341f;
+  const float e = __builtin_amdgcn_exp2f(t);
+  // log2(e) = 1.44269502162933349609375 + 1.925963033500e-8
+  const float r = fmaf(d, 1.925963033500e-8f, fmaf(d, 1.44269504088896341f, -t));
+  return fmaf(e, r * 0.693147180559945309f, e);
+}
+
 template <int LPT>
 __device__ __forceinline__ float row_sum(float v) {
   return row_reduce<LPT>(v, [](float a, float b) { return a + b; });
 }
 template <int LPT>
-__device__ __forceinline__ uint64_t row_max(uint64_t v) {
-#pragma unroll
-  for (int o = 1; o < LPT; o <<= 1) {
-    const uint64_t w = __shfl_xor(static_cast<unsigned long long>(v), o, 64);
-    v = w > v ? w : v;
-  }
-  return v;
+__device__ __forceinline__ float row_max(float v) {
+  return row_reduce<LPT>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int LPT>
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+  return row_reduce<LPT>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
 
 // The V logits first .. first + V - 1 of a row (experts past E: -inf).
@@ -113,17 +146,18 @@ struct RouteArgs {
   int32_t* slots;
   float* lse;
   float* losses;
-  // of every run: slots of every expert and of none [E + 1], probability sums [E], z and counted rows
+  // of every run: slots of every expert [E], probability sums [E], z and counted rows
   int32_t* run_counts;
   float* run_probs;
   float* run_z;
   int32_t* run_n;
 };
 
-// Exclusive sums over v[0 .. n) in LDS (n <= kMaxExperts + 1), in place;
-// `tmp` holds kThreads values.  Ends with a barrier.
+// Exclusive sums over v[0 .. n) in LDS (n <= kMaxExperts + 1), in place, by NT
+// threads; `tmp` holds a value a wave.  Ends with a barrier.
+template <int NT>
 __device__ __forceinline__ void exclusive_scan(int32_t* v, int n, int32_t* tmp) {
-  const int per = (n + kThreads - 1) / kThreads, tid = threadIdx.x;
+  const int per = (n + NT - 1) / NT, tid = threadIdx.x;
   const int lo = min(n, tid * per), hi = min(n, lo + per);
   int s = 0;
   for (int i = lo; i < hi; ++i) s += v[i];
@@ -145,26 +179,55 @@ __device__ __forceinline__ void exclusive_scan(int32_t* v, int n, int32_t* tmp) 
   __syncthreads();
 }
 
-// Places the slots of a run: next[e] is where the run's first slot of expert
-// e goes (e = E: no expert), list[i] the expert of its slot i.  One thread
-// per expert walks the list, so equal experts keep their order.
-__device__ __forceinline__ void place_slots(const RouteArgs& a, const int32_t* next,
-                                            const uint16_t* list, int64_t slot0, int n) {
-  for (int e = threadIdx.x; e <= a.E; e += kThreads) {
-    int pos = next[e];
-    for (int i0 = 0; i0 < n; i0 += 8) {
+// Threads that share out what is done for an expert: a power of two, for E
+// experts side by side.
+template <int NT>
+__device__ __forceinline__ int shares_log2(int E) {
+  int parts = 0;
+  while (parts < 5 && (E << (parts + 1)) <= NT) ++parts;
+  return parts;
+}
+
+// Places the slots of a run of rows from row0 on: next[e] is where the run's
+// first slot of expert e goes (e = E: no expert), list[i] the expert of its slot
+// i (filled up with 0xFFFF to a multiple of eight).  A thread walks a share of
+// the list for one expert, once to count and once to place, so equal experts
+// keep their order.  part: [NT].
+template <int NT>
+__device__ __forceinline__ void place_slots(const RouteArgs& a, const int32_t* next, const uint16_t* list,
+                                            int64_t row0, int n, int32_t* part) {
+  const int log = shares_log2<NT>(a.E + 1), parts = 1 << log, wide = NT >> log;
+  const int col = threadIdx.x & (wide - 1), s = threadIdx.x >> (__builtin_ctz(NT) - log);
+  const int each = (((n + parts - 1) >> log) + 7) & ~7, lo = min(n, s * each), hi = min(n, lo + each);
+  const uint64_t inv = (uint64_t(1) << 32) / a.k + 1;  // i / k = i inv / 2^32 for i < 2^16, k <= 64
+  for (int e0 = 0; e0 <= a.E; e0 += wide) {
+    const int e = e0 + col;
+    int count = 0;
+    for (int i0 = lo; i0 < hi; i0 += 8) {
       const uint4 v = *reinterpret_cast<const uint4*>(list + i0);
       const uint32_t d[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int f = (d[i / 2] >> (16 * (i & 1))) & 0xFFFF;
-        if (f == e) {  // (the list is filled up with values above E)
-          const int64_t s = slot0 + i0 + i;
-          a.rows[pos] = static_cast<int32_t>(s / a.k);
-          a.slots[s] = pos++;
+      for (int i = 0; i < 4; ++i) count += ((d[i] & 0xFFFF) == static_cast<uint32_t>(e)) + ((d[i] >> 16) == static_cast<uint32_t>(e));
+    }
+    part[threadIdx.x] = count;
+    __syncthreads();
+    if (e <= a.E && count > 0) {
+      int pos = next[e];
+      for (int u = 0; u < s; ++u) pos += part[u * wide + col];
+      for (int i0 = lo; i0 < hi; i0 += 8) {
+        const uint4 v = *reinterpret_cast<const uint4*>(list + i0);
+        const uint32_t d[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t f = (d[i / 2] >> (16 * (i & 1))) & 0xFFFF;
+          if (f == static_cast<uint32_t>(e)) {
+            a.rows[pos] = static_cast<int32_t>(row0) + static_cast<int>((static_cast<uint32_t>(i0 + i) * inv) >> 32);
+            a.slots[row0 * a.k + i0 + i] = pos++;
+          }
         }
       }
     }
+    __syncthreads();
   }
 }
 
@@ -176,7 +239,7 @@ __device__ __forceinline__ void write_losses(const RouteArgs& a, float balance, 
 }
 
 // Sum over the workgroup in a fixed order, valid in thread 0.
-template <typename T>
+template <int NT, typename T>
 __device__ __forceinline__ T block_sum(T v, void* lds) {
   T* tmp = static_cast<T*>(lds);
   v = wave_sum(v);
@@ -184,30 +247,30 @@ __device__ __forceinline__ T block_sum(T v, void* lds) {
   if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = v;
   __syncthreads();
   T s = 0;
-  for (int w = 0; w < kThreads / 64; ++w) s += tmp[w];
+  for (int w = 0; w < NT / 64; ++w) s += tmp[w];
   return s;
 }
 
 __host__ __device__ inline int list_len(int n) { return (n + 7) & ~7; }
 
 // First launch: the rows of one run.
-template <bool BF16, int V, int LPT>
-__global__ __launch_bounds__(kThreads) void route_rows_kernel(RouteArgs a) {
-  constexpr int G = kThreads / LPT;  // rows at a time
+template <bool BF16, int V, int LPT, int NT>
+__global__ __launch_bounds__(NT) void route_rows_kernel(RouteArgs a) {
+  constexpr int G = NT / LPT;  // rows at a time
   extern __shared__ __align__(16) char smem[];
   float* probs = reinterpret_cast<float*>(smem);                  // [G][LPT * V]
-  int32_t* cnt = reinterpret_cast<int32_t*>(probs + kThreads * V);  // [E + 1]
+  int32_t* cnt = reinterpret_cast<int32_t*>(probs + NT * V);  // [E + 1]
   float* chosen = reinterpret_cast<float*>(cnt + a.E + 1);        // [G][k]
   float* tmp = chosen + G * a.k;                                  // [kThreads]
   uint16_t* list = reinterpret_cast<uint16_t*>(
-      (reinterpret_cast<uintptr_t>(tmp + kThreads) + 15) & ~uintptr_t(15));  // one run only
+      (reinterpret_cast<uintptr_t>(tmp + NT) + 15) & ~uintptr_t(15));  // one run only
   const int tid = threadIdx.x, lane = tid % LPT, grp = tid / LPT;
   const bool one = a.runs == 1;
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * a.run;
   const int nrows = static_cast<int>(min(static_cast<int64_t>(a.run), a.T - t0));
-  for (int e = tid; e <= a.E; e += kThreads) cnt[e] = 0;
+  for (int e = tid; e <= a.E; e += NT) cnt[e] = 0;
   if (one)
-    for (int i = nrows * a.k + tid; i < list_len(nrows * a.k); i += kThreads) list[i] = 0xFFFF;
+    for (int i = nrows * a.k + tid; i < list_len(nrows * a.k); i += NT) list[i] = 0xFFFF;
   __syncthreads();
   const int first = lane * V;
   float sum[V];
@@ -223,12 +286,12 @@ __global__ __launch_bounds__(kThreads) void route_rows_kernel(RouteArgs a) {
     float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < V; ++i) m = fmaxf(m, x[i]);
-    m = row_reduce<LPT>(m, [](float p, float q) { return fmaxf(p, q); });
+    m = row_max<LPT>(m);
     m = m == -INFINITY ? 0.0f : m;
     float ex[V], total = 0.0f;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      ex[i] = expf(x[i] - m);  // (NaN for a NaN, and in a row with an infinity)
+      ex[i] = exp_neg(x[i] - m);  // (NaN for a NaN, and in a row with an infinity)
       total += ex[i];
     }
     total = row_sum<LPT>(total);
@@ -243,50 +306,55 @@ __global__ __launch_bounds__(kThreads) void route_rows_kernel(RouteArgs a) {
       zsum += lse * lse;
     }
     if (lane == 0) a.lse[t] = lse;
-    // the k largest, one after another: logit and 2^32 - 1 - index in one key
-    uint64_t key[V];
+    // The k largest, one after another: the largest logit over the row's lanes, and of the lanes that have it the
+    // lowest one, whose logits have the lowest indices.
+    uint32_t key[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      key[i] = live && !broken && x[i] > -INFINITY
-                   ? (static_cast<uint64_t>(order_bits(x[i])) << 32) | (0xFFFFFFFFu - (first + i))
-                   : 0;
-    float total_w = 0.0f;
+    for (int i = 0; i < V; ++i) key[i] = live && !broken && x[i] > -INFINITY ? order_bits(x[i]) : 0;
     for (int j = 0; j < a.k; ++j) {
-      uint64_t best = key[0];
+      uint32_t mine = key[0];
 #pragma unroll
-      for (int i = 1; i < V; ++i) best = key[i] > best ? key[i] : best;
-      best = row_max<LPT>(best);
-      int e = -1;
-      float p = 0.0f;
-      if (best != 0) {
-        e = static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(best));
-        p = expf(order_value(static_cast<uint32_t>(best >> 32)) - m) * inv;
+      for (int i = 1; i < V; ++i) mine = key[i] > mine ? key[i] : mine;
+      const uint32_t best = row_max<LPT>(mine);
+      const uint64_t have = __ballot(mine == best) >> ((threadIdx.x & 63) / LPT * LPT);
+      const bool winner = lane == (LPT == 64 ? __builtin_ctzll(have) : __builtin_ctz(static_cast<uint32_t>(have)));
+      if (winner) {
+        int e = -1;
+        if (best != 0) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) key[i] = key[i] == best ? 0 : key[i];
-      }
-      if (live && broken) p = __uint_as_float(0x7FC00000u);
-      total_w += p;
-      if (lane == j % LPT) {
+          for (int i = V - 1; i >= 0; --i) e = key[i] == best ? first + i : e;
+#pragma unroll
+          for (int i = 0; i < V; ++i) key[i] = first + i == e ? 0 : key[i];
+        }
         a.experts[t * a.k + j] = e;
-        chosen[grp * a.k + j] = p;
+        chosen[grp * a.k + j] = best != 0 ? order_value(best) : -INFINITY;
         const int bucket = e < 0 ? a.E : e;
         atomicAdd(&cnt[bucket], 1);
         if (one) list[r * a.k + j] = static_cast<uint16_t>(bucket);
       }
     }
+    // their weights, a slot a lane (the row's lanes are of one wave, which wrote what is read here)
+    __builtin_amdgcn_wave_barrier();
+    float total_w = 0.0f;
+    for (int j = lane; j < a.k; j += LPT) {
+      float p = exp_neg(chosen[grp * a.k + j] - m) * inv;
+      p = live && broken ? __uint_as_float(0x7FC00000u) : live ? p : 0.0f;
+      chosen[grp * a.k + j] = p;
+      total_w += p;
+    }
+    total_w = row_sum<LPT>(total_w);
     const float scale = a.renorm && total_w != 0.0f ? 1.0f / total_w : 1.0f;
-    for (int j = lane; j < a.k; j += LPT)  // (a lane reads what it wrote itself)
-      a.weights[t * a.k + j] = chosen[grp * a.k + j] * scale;
+    for (int j = lane; j < a.k; j += LPT) a.weights[t * a.k + j] = chosen[grp * a.k + j] * scale;
   }
 #pragma unroll
   for (int i = 0; i < V; ++i) probs[grp * LPT * V + first + i] = sum[i];
   // z and n of the run: from one lane of every row, the rows in a fixed order
-  const float z = block_sum(lane == 0 ? zsum : 0.0f, tmp);
-  const int n = block_sum(lane == 0 ? nsum : 0, tmp);
+  const float z = block_sum<NT>(lane == 0 ? zsum : 0.0f, tmp);
+  const int n = block_sum<NT>(lane == 0 ? nsum : 0, tmp);
   __syncthreads();
   if (!one) {
-    for (int e = tid; e <= a.E; e += kThreads) a.run_counts[int64_t(blockIdx.x) * (a.E + 1) + e] = cnt[e];
-    for (int e = tid; e < a.E; e += kThreads) {
+    for (int e = tid; e < a.E; e += NT) a.run_counts[int64_t(blockIdx.x) * a.E + e] = cnt[e];
+    for (int e = tid; e < a.E; e += NT) {
       float s = 0.0f;
       for (int g = 0; g < G; ++g) s += probs[g * LPT * V + e];
       a.run_probs[int64_t(blockIdx.x) * a.E + e] = s;
@@ -298,75 +366,117 @@ __global__ __launch_bounds__(kThreads) void route_rows_kernel(RouteArgs a) {
     return;
   }
   float balance = 0.0f;
-  for (int e = tid; e < a.E; e += kThreads) {
+  for (int e = tid; e < a.E; e += NT) {
     float s = 0.0f;
     for (int g = 0; g < G; ++g) s += probs[g * LPT * V + e];
     balance += s * static_cast<float>(cnt[e]);
     a.counts[e] = cnt[e];
   }
-  balance = block_sum(balance, tmp);
+  balance = block_sum<NT>(balance, tmp);
   if (tid == 0) write_losses(a, balance, z, n);
   __syncthreads();
-  exclusive_scan(cnt, a.E + 1, reinterpret_cast<int32_t*>(tmp));
-  for (int e = tid; e <= a.E; e += kThreads) a.offsets[e] = cnt[e];
-  place_slots(a, cnt, list, 0, nrows * a.k);
+  exclusive_scan<NT>(cnt, a.E + 1, reinterpret_cast<int32_t*>(tmp));
+  for (int e = tid; e <= a.E; e += NT) a.offsets[e] = cnt[e];
+  place_slots<NT>(a, cnt, list, 0, nrows * a.k, reinterpret_cast<int32_t*>(tmp));
 }
 
-// Second launch: workgroup b < runs places the slots of run b; the last one
-// writes the counts and losses.
+// Second launch: 32 experts a workgroup, 32 threads an expert.  Every run's
+// count becomes the sum of those before it; the totals follow the last run's.
+// With few instructions on purpose, as are the others: a launch this short is
+// bound by fetching them.
+__global__ __launch_bounds__(1024) void route_sum_kernel(RouteArgs a) {
+  __shared__ int32_t part[32][33];
+  __shared__ float ppart[32][33];
+  const int col = threadIdx.x & 31, s = threadIdx.x >> 5, e = blockIdx.x * 32 + col;
+  const int each = (a.runs + 31) / 32, lo = min(a.runs, s * each), hi = min(a.runs, lo + each);
+  int sum = 0;
+  float p = 0.0f;
+  if (e < a.E) {
+    const int32_t* c = a.run_counts + static_cast<int64_t>(lo) * a.E + e;
+    const float* f = a.run_probs + static_cast<int64_t>(lo) * a.E + e;
+#pragma unroll 8
+    for (int q = lo; q < hi; ++q) {
+      sum += *c;
+      p += *f;
+      c += a.E;
+      f += a.E;
+    }
+  }
+  part[s][col] = sum;
+  ppart[s][col] = p;
+  __syncthreads();
+  if (e >= a.E) return;
+  int before = 0;
+  for (int u = 0; u < s; ++u) before += part[u][col];
+  int32_t* c = a.run_counts + static_cast<int64_t>(lo) * a.E + e;
+#pragma unroll 8
+  for (int q = lo; q < hi; ++q) {
+    const int v = *c;
+    *c = before;
+    before += v;
+    c += a.E;
+  }
+  if (s == 31) {
+    a.run_counts[static_cast<int64_t>(a.runs) * a.E + e] = before;
+    a.counts[e] = before;
+  }
+  if (s == 0) {
+    for (int u = 1; u < 32; ++u) p += ppart[u][col];
+    a.run_probs[static_cast<int64_t>(a.runs) * a.E + e] = p;
+  }
+}
+
+// Third launch: workgroup b < runs places the slots of run b; the last one
+// writes the offsets and losses.
 __global__ __launch_bounds__(kThreads) void route_place_kernel(RouteArgs a) {
   extern __shared__ __align__(16) char smem[];
-  int32_t* total = reinterpret_cast<int32_t*>(smem);  // [E + 1]
-  int32_t* before = total + a.E + 1;                  // [E + 1]
-  int32_t* tmp = before + a.E + 1;                    // [kThreads]
-  uint16_t* list = reinterpret_cast<uint16_t*>(
-      (reinterpret_cast<uintptr_t>(tmp + kThreads) + 15) & ~uintptr_t(15));
+  int32_t* next = reinterpret_cast<int32_t*>(smem);  // [E + 1]
+  int32_t* tmp = next + a.E + 1;                     // [kThreads / 64]
+  int32_t* part = tmp + kThreads / 64;               // [kThreads]
+  uint16_t* list = reinterpret_cast<uint16_t*>((reinterpret_cast<uintptr_t>(part + kThreads) + 15) & ~uintptr_t(15));
   const int tid = threadIdx.x, b = blockIdx.x;
   const bool last = b == a.runs;
-  float balance = 0.0f;
-  for (int e = tid; e <= a.E; e += kThreads) {
-    int sum = 0, mine = 0;
-    for (int q = 0; q < a.runs; ++q) {
-      const int c = a.run_counts[int64_t(q) * (a.E + 1) + e];
-      if (q == b) mine = sum;
-      sum += c;
-    }
-    total[e] = sum;
-    before[e] = mine;
-    if (last && e < a.E) {
-      float p = 0.0f;
-      for (int q = 0; q < a.runs; ++q) p += a.run_probs[int64_t(q) * a.E + e];
-      balance += p * static_cast<float>(sum);
-      a.counts[e] = sum;
-    }
-  }
-  if (last) {
-    float z = 0.0f;
-    int n = 0;
-    for (int q = tid; q < a.runs; q += kThreads) {
-      z += a.run_z[q];
-      n += a.run_n[q];
-    }
-    balance = block_sum(balance, tmp);
-    z = block_sum(z, tmp);
-    n = block_sum(n, tmp);
-    if (tid == 0) write_losses(a, balance, z, n);
-    __syncthreads();
-    exclusive_scan(total, a.E + 1, tmp);
-    for (int e = tid; e <= a.E; e += kThreads) a.offsets[e] = total[e];
-    return;
-  }
-  const int64_t slot0 = static_cast<int64_t>(b) * a.run * a.k;
-  const int n = static_cast<int>(min(static_cast<int64_t>(a.run), a.T - static_cast<int64_t>(b) * a.run)) * a.k;
+  const int64_t row0 = static_cast<int64_t>(b) * a.run;
+  const int n = last ? 0 : static_cast<int>(min(static_cast<int64_t>(a.run), a.T - row0)) * a.k;
   for (int i = tid; i < list_len(n); i += kThreads) {
-    const int e = i < n ? a.experts[slot0 + i] : 0xFFFF;
+    const int e = i < n ? a.experts[row0 * a.k + i] : 0xFFFF;
     list[i] = static_cast<uint16_t>(e < 0 ? a.E : e);
   }
+  const int32_t* total = a.run_counts + static_cast<int64_t>(a.runs) * a.E;
+  for (int e = tid; e < a.E; e += kThreads) next[e] = total[e];
+  if (tid == 0) next[a.E] = 0;
   __syncthreads();
-  exclusive_scan(total, a.E + 1, tmp);
-  for (int e = tid; e <= a.E; e += kThreads) before[e] += total[e];
+  if (last) {
+    float balance = 0.0f, z = 0.0f;
+    int rows = 0;
+    for (int e = tid; e < a.E; e += kThreads)
+      balance += static_cast<float>(next[e]) * a.run_probs[static_cast<int64_t>(a.runs) * a.E + e];
+    for (int q = tid; q < a.runs; q += kThreads) {
+      z += a.run_z[q];
+      rows += a.run_n[q];
+    }
+    balance = block_sum<kThreads>(balance, tmp);
+    z = block_sum<kThreads>(z, tmp);
+    rows = block_sum<kThreads>(rows, tmp);
+    if (tid == 0) write_losses(a, balance, z, rows);
+    __syncthreads();
+  }
+  exclusive_scan<kThreads>(next, a.E + 1, tmp);
+  if (last) {
+    for (int e = tid; e <= a.E; e += kThreads) a.offsets[e] = next[e];
+    return;
+  }
+  // the slots of the runs before: of every expert, and (what those leave) of none
+  int taken = 0;
+  for (int e = tid; e < a.E; e += kThreads) {
+    const int c = a.run_counts[static_cast<int64_t>(b) * a.E + e];
+    next[e] += c;
+    taken += c;
+  }
+  taken = block_sum<kThreads>(taken, tmp);
+  if (tid == 0) next[a.E] += static_cast<int32_t>(row0 * a.k - taken);
   __syncthreads();
-  place_slots(a, before, list, slot0, n);
+  place_slots<kThreads>(a, next, list, row0, n, part);
 }
 
 // No rows at all.
@@ -389,8 +499,8 @@ struct GradArgs {
 };
 
 template <bool BF16, int V, int LPT>
-__global__ __launch_bounds__(kThreads) void route_grad_kernel(GradArgs a) {
-  constexpr int G = kThreads / LPT;
+__global__ __launch_bounds__(kGradThreads) void route_grad_kernel(GradArgs a) {
+  constexpr int G = kGradThreads / LPT;
   const int lane = threadIdx.x % LPT, grp = threadIdx.x / LPT, first = lane * V;
   const float n = static_cast<float>(a.counts[a.E]);
   const float gb = a.dlosses && n > 0.0f ? a.dlosses[0] * (static_cast<float>(a.E) / (static_cast<float>(a.k) * n * n)) : 0.0f;
@@ -412,10 +522,10 @@ __global__ __launch_bounds__(kThreads) void route_grad_kernel(GradArgs a) {
                            a.wide != 0, p);
 #pragma unroll
       for (int i = 0; i < V; ++i) m = fmaxf(m, p[i]);
-      m = row_reduce<LPT>(m, [](float u, float v) { return fmaxf(u, v); });
+      m = row_max<LPT>(m);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        p[i] = expf(p[i] - m);
+        p[i] = exp_neg(p[i] - m);
         total += p[i];
       }
       const float inv = 1.0f / row_sum<LPT>(total);
@@ -562,8 +672,7 @@ extern "C" bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt
   a.runs = static_cast<int>(runs);
   if (runs > 1) {
     bitsmoe_status st;
-    const size_t nc = ((size_t(runs) * (E + 1) * 4) + 255) & ~size_t(255);
-    const size_t np = ((size_t(runs) * E * 4) + 255) & ~size_t(255);
+    const size_t nc = ((size_t(runs + 1) * E * 4) + 255) & ~size_t(255), np = nc;  // (the totals after the last run)
     char* p = static_cast<char*>(scratch(kScratchMisc, nc + np + size_t(runs) * 8, stream, &st));
     if (!p) return st;
     a.run_counts = reinterpret_cast<int32_t*>(p);
@@ -574,9 +683,13 @@ extern "C" bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt
   bitsmoe_status st = BITSMOE_OK;
   with_layout(E, [&](auto v, auto l) {
     constexpr int V = decltype(v)::value, LPT = decltype(l)::value;
-    const size_t lds = size_t(kThreads) * V * 4 + (E + 1) * 4 + size_t(kThreads / LPT) * k * 4 + kThreads * 4 +
-                       16 + (runs == 1 ? size_t(list_len(static_cast<int>(run * k))) * 2 : 0);
-    auto* fn = lt == BITSMOE_BF16 ? route_rows_kernel<true, V, LPT> : route_rows_kernel<false, V, LPT>;
+    constexpr int MANY = V == 8 ? kThreads : 256;
+    const int nt = runs == 1 ? 256 : MANY;  // few rows: a workgroup that is launched sooner
+    const size_t lds = size_t(nt) * V * 4 + (E + 1) * 4 + size_t(nt / LPT) * k * 4 + nt * 4 + 16 +
+                       (runs == 1 ? size_t(list_len(static_cast<int>(run * k))) * 2 : 0);
+    auto* fn = lt == BITSMOE_BF16
+                   ? (runs == 1 ? route_rows_kernel<true, V, LPT, 256> : route_rows_kernel<true, V, LPT, MANY>)
+                   : (runs == 1 ? route_rows_kernel<false, V, LPT, 256> : route_rows_kernel<false, V, LPT, MANY>);
     if (lds > 65536) {
       const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn),
                                                hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
@@ -585,12 +698,15 @@ extern "C" bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt
         return;
       }
     }
-    fn<<<static_cast<unsigned>(runs), kThreads, lds, s>>>(a);
+    fn<<<static_cast<unsigned>(runs), nt, lds, s>>>(a);
   });
   if (st) return st;
   BITSMOE_LAUNCH_CHECK("route_rows_kernel");
   if (runs > 1) {
-    const size_t lds = size_t(2) * (E + 1) * 4 + kThreads * 4 + 16 + size_t(list_len(static_cast<int>(run * k))) * 2;
+    route_sum_kernel<<<static_cast<unsigned>((E + 31) / 32), 1024, 0, s>>>(a);
+    BITSMOE_LAUNCH_CHECK("route_sum_kernel");
+    const size_t lds = size_t(E + 1) * 4 + kThreads / 64 * 4 + kThreads * 4 + 16 +
+                       size_t(list_len(static_cast<int>(run * k))) * 2;
     if (lds > 65536) {
       const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(route_place_kernel),
                                                hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
@@ -630,10 +746,10 @@ extern "C" bitsmoe_status bitsmoe_route_grad(const void* logits_dev, bitsmoe_dty
   a.dlogits = dlogits_dev;
   with_layout(E, [&](auto v, auto l) {
     constexpr int V = decltype(v)::value, LPT = decltype(l)::value;
-    const int64_t groups = (T + kThreads / LPT - 1) / (kThreads / LPT);
+    const int64_t groups = (T + kGradThreads / LPT - 1) / (kGradThreads / LPT);
     const unsigned grid = static_cast<unsigned>(groups < 8192 ? groups : 8192);
     auto* fn = lt == BITSMOE_BF16 ? route_grad_kernel<true, V, LPT> : route_grad_kernel<false, V, LPT>;
-    fn<<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
+    fn<<<grid, kGradThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
   });
   BITSMOE_LAUNCH_CHECK("route_grad_kernel");
   return ok();
