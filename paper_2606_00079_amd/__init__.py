@@ -543,35 +543,48 @@ def unpack(codes, params, bits_dev, offsets_dev, units: int, d: int, group: int,
 # ---------------------------------------------------------------------------
 # an MoE layer with experts in MX4
 # ---------------------------------------------------------------------------
-def _rows(t, name: str):
-    """(pointer, row stride) of a matrix whose rows may be apart."""
-    if t.is_contiguous():
-        return _dev(t, name), t.shape[-1]
+# (These calls are short enough for their marshalling to count: addresses go
+# as plain ints, and the stream is asked for by its number.)
+def _place(t, name: str):
+    """(torch, the stream to run on) for calls whose first tensor is t."""
     torch = _torch()
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must have contiguous rows")
-    return ctypes.c_void_p(t.data_ptr()), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    dev = t.get_device()
+    if dev != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} must be on the current device")
+    return torch, torch._C._cuda_getCurrentRawStream(dev)
 
 
-def _opt(t, name: str, dtype, shape=None):
-    """Pointer of an optional tensor of a given type and shape."""
+def _in(t, name: str, like, dtype, shape=None):
+    """Address of a contiguous tensor (None: none) on the device of `like`."""
     if t is None:
         return None
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {str(dtype).replace('torch.', '')}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}")
-    return _dev(t, name)
+    if t.get_device() != like.get_device():
+        raise TypeError(f"{name} must be on the same CUDA (HIP) device")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
-def _out(out, shape, dtype, device, name: str):
-    torch = _torch()
+def _rows(t, name: str):
+    """(address, row stride) of a matrix whose rows may be apart."""
+    if t.is_contiguous():
+        return t.data_ptr(), t.shape[-1]
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must have contiguous rows")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def _out(out, shape, dtype, like, torch):
+    """The output tensor, new or given."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if out.dtype != dtype or tuple(out.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {list(shape)} of {str(dtype).replace('torch.', '')}")
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    _in(out, "out", like, dtype, shape)
     return out
 
 
@@ -591,94 +604,96 @@ def route(logits, k: int, valid=None, renorm: bool = True) -> Routing:
     """Top-k experts of every row of logits [T][E] (bf16 or fp32), their softmax
     weights, the slots in expert order, and the balance and z losses; rows with
     valid[t] = 0 (bool or uint8) do not count."""
-    torch = _torch()
+    torch, stream = _place(logits, "logits")
     if logits.dim() != 2:
         raise ValueError("logits must be [T][E]")
     T, E = logits.shape
     k = int(k)
-    if valid is not None and valid.dtype == torch.bool:
+    if valid is not None and valid.dtype is torch.bool:
         valid = valid.view(torch.uint8)
-    vp = _opt(valid, "valid", torch.uint8, (T,))
+    vp = _in(valid, "valid", logits, torch.uint8, (T,))
     lp, ld = _rows(logits, "logits")
-    i32, f32, dev = torch.int32, torch.float32, logits.device
-    n = max(T * k, 0)
-    r = Routing(torch.empty((T, max(k, 0)), dtype=i32, device=dev),
-                torch.empty((T, max(k, 0)), dtype=f32, device=dev),
-                torch.empty((E + 1,), dtype=i32, device=dev), torch.empty((E + 1,), dtype=i32, device=dev),
-                torch.empty((n,), dtype=i32, device=dev), torch.empty((T, max(k, 0)), dtype=i32, device=dev),
-                torch.empty((T,), dtype=f32, device=dev), torch.empty((2,), dtype=f32, device=dev))
-    _check(lib().bitsmoe_route(lp, _dtype_code(logits, "logits"), T, E, ld, k, vp, int(renorm),
-                               *(ctypes.c_void_p(t.data_ptr()) for t in r), _stream()), "route")
-    return r
+    n, w = max(T * k, 0), max(k, 0)
+    # one allocation for the whole numbers and one for the others, their parts 16 bytes aligned
+    n4, e4, t4 = (n + 3) // 4 * 4, (E + 4) // 4 * 4, (T + 3) // 4 * 4
+    ints = torch.empty((3 * n4 + 2 * e4,), dtype=torch.int32, device=logits.device)
+    floats = torch.empty((n4 + t4 + 4,), dtype=torch.float32, device=logits.device)
+    ip, fp = ints.data_ptr(), floats.data_ptr()
+    ex, co, of, ro, sl = ip, ip + 12 * n4, ip + 12 * n4 + 4 * e4, ip + 4 * n4, ip + 8 * n4
+    we, ls, lo = fp, fp + 4 * n4, fp + 4 * (n4 + t4)
+    _check(lib().bitsmoe_route(lp, _dtype_code(logits, "logits"), T, E, ld, k, vp, int(renorm), ex, we,
+                               co, of, ro, sl, ls, lo, stream), "route")
+    return Routing(ints.as_strided((T, w), (w, 1), 0), floats.as_strided((T, w), (w, 1), 0),
+                   ints.as_strided((E + 1,), (1,), 3 * n4), ints.as_strided((E + 1,), (1,), 3 * n4 + e4),
+                   ints.as_strided((n,), (1,), n4), ints.as_strided((T, w), (w, 1), 2 * n4),
+                   floats.as_strided((T,), (1,), n4), floats.as_strided((2,), (1,), n4 + t4))
 
 
 def route_grad(logits, routing: Routing, dweights=None, dlosses=None, renorm: bool = True, out=None):
     """Gradient of the logits from those of the weights [T][k] and of the losses
     [2] (fp32, on the device) -> [T][E] of the logits' type."""
-    torch = _torch()
+    torch, stream = _place(logits, "logits")
+    if logits.dim() != 2:
+        raise ValueError("logits must be [T][E]")
     T, E = logits.shape
     k = routing.experts.shape[1]
-    out = _out(out, (T, E), logits.dtype, logits.device, "out")
+    out = _out(out, (T, E), logits.dtype, logits, torch)
     lp, ld = _rows(logits, "logits")
+    i32, f32 = torch.int32, torch.float32
     _check(lib().bitsmoe_route_grad(
         lp, _dtype_code(logits, "logits"), T, E, ld, k, int(renorm),
-        _opt(routing.experts, "experts", torch.int32, (T, k)),
-        _opt(routing.weights, "weights", torch.float32, (T, k)),
-        _opt(routing.counts, "counts", torch.int32, (E + 1,)),
-        _opt(routing.lse, "lse", torch.float32, (T,)),
-        _opt(dweights, "dweights", torch.float32, (T, k)),
-        _opt(dlosses, "dlosses", torch.float32, (2,)), _dev(out, "out"), _stream()), "route_grad")
+        _in(routing.experts, "experts", logits, i32, (T, k)),
+        _in(routing.weights, "weights", logits, f32, (T, k)),
+        _in(routing.counts, "counts", logits, i32, (E + 1,)),
+        _in(routing.lse, "lse", logits, f32, (T,)),
+        _in(dweights, "dweights", logits, f32, (T, k)),
+        _in(dlosses, "dlosses", logits, f32, (2,)), out.data_ptr(), stream), "route_grad")
     return out
 
 
 def mx4_quantize(X):
     """Rows of X [..][cols] (bf16 or fp32) to MX4: codes uint8 [..][cols/2] and
     scales uint8 [..][cols/32]."""
-    torch = _torch()
-    cols = X.shape[-1]
-    if cols % 32 != 0:
+    torch, stream = _place(X, "X")
+    lead, cols = X.shape[:-1], X.shape[-1]
+    if cols % 32 != 0 or cols == 0:
         raise ValueError("cols must be a multiple of 32")
     xp, ld = _rows(X, "X")
-    rows = X.numel() // cols if cols else 0
-    codes = torch.empty((*X.shape[:-1], cols // 2), dtype=torch.uint8, device=X.device)
-    scales = torch.empty((*X.shape[:-1], cols // 32), dtype=torch.uint8, device=X.device)
-    _check(lib().bitsmoe_mx4_quantize(xp, _dtype_code(X, "X"), rows, cols, ld, _dev(codes, "codes"),
-                                      _dev(scales, "scales"), _stream()), "mx4_quantize")
+    codes = torch.empty((*lead, cols // 2), dtype=torch.uint8, device=X.device)
+    scales = torch.empty((*lead, cols // 32), dtype=torch.uint8, device=X.device)
+    _check(lib().bitsmoe_mx4_quantize(xp, _dtype_code(X, "X"), X.numel() // cols, cols, ld,
+                                      codes.data_ptr(), scales.data_ptr(), stream), "mx4_quantize")
     return codes, scales
 
 
-def _mx4(codes, scales, name: str, dims: int):
-    torch = _torch()
-    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
-        raise TypeError(f"{name} codes and scales must be uint8")
+def _mx4(codes, scales, name: str, like, torch, dims: int = 0):
+    """Addresses of MX4 rows."""
     if (dims and codes.dim() != dims) or codes.shape[:-1] != scales.shape[:-1] or \
             codes.shape[-1] != 16 * scales.shape[-1]:
-        raise ValueError(f"{name} codes must be [..][K/2] and scales [..][K/32]")
-    return _dev(codes, name + " codes"), _dev(scales, name + " scales")
+        raise ValueError(f"{name}'s codes must be [..][K/2] and its scales [..][K/32]")
+    return (_in(codes, f"{name}'s codes", like, torch.uint8),
+            _in(scales, f"{name}'s scales", like, torch.uint8))
 
 
 def mx4_dequantize(codes, scales, dtype=None, out=None):
     """What MX4 rows stand for -> [..][cols] (bf16 unless ``dtype`` says fp32)."""
-    torch = _torch()
-    cp, sp = _mx4(codes, scales, "X", 0)
+    torch, stream = _place(codes, "X's codes")
+    cp, sp = _mx4(codes, scales, "X", codes, torch)
     cols = 2 * codes.shape[-1]
-    dtype = dtype or torch.bfloat16
-    out = _out(out, (*codes.shape[:-1], cols), dtype, codes.device, "out")
-    rows = codes.numel() // (cols // 2) if cols else 0
-    _check(lib().bitsmoe_mx4_dequantize(cp, sp, rows, cols, _dev(out, "out"), _dtype_code(out, "out"),
-                                        _stream()), "mx4_dequantize")
+    out = _out(out, (*codes.shape[:-1], cols), dtype or torch.bfloat16, codes, torch)
+    _check(lib().bitsmoe_mx4_dequantize(cp, sp, codes.numel() * 2 // max(cols, 1), cols, out.data_ptr(),
+                                        _dtype_code(out, "out"), stream), "mx4_dequantize")
     return out
 
 
-def _experts(codes, scales, offsets, S: int, glu: bool = False):
-    torch = _torch()
-    cp, sp = _mx4(codes, scales, "W", 3)
+def _experts(codes, scales, offsets, like, torch, glu: bool = False):
+    cp, sp = _mx4(codes, scales, "W", like, torch, 3)
     E, N, K = codes.shape[0], codes.shape[1], 2 * codes.shape[2]
     if glu:
         if N % 2:
             raise ValueError("glu takes as many gate as up rows")
         N //= 2
-    return cp, sp, E, N, K, _opt(offsets, "offsets", torch.int32, (E + 1,))
+    return cp, sp, E, N, K, _in(offsets, "offsets", like, torch.int32, (E + 1,))
 
 
 def mx4_product(codes, scales, X, offsets=None, rows=None, glu: bool = False, dtype=None, out=None):
@@ -687,18 +702,18 @@ def mx4_product(codes, scales, X, offsets=None, rows=None, glu: bool = False, dt
     [E][N][K/2] and scales [E][N][K/32], X bf16 [rows][K] -> [S][N], bf16 unless
     ``dtype`` says fp32.  glu: W holds gate rows, then up rows, and
     y = silu(gate) * up -> [S][N/2]."""
-    torch = _torch()
+    torch, stream = _place(X, "X")
     if X.dim() != 2:
         raise ValueError("X must be [rows][K]")
     S = X.shape[0] if rows is None else rows.shape[0]
-    cp, sp, E, N, K, op = _experts(codes, scales, offsets, S, glu)
+    cp, sp, E, N, K, op = _experts(codes, scales, offsets, X, torch, glu)
     if X.shape[1] != K:
         raise ValueError("X and W disagree on K")
     xp, ldx = _rows(X, "X")
-    out = _out(out, (S, N), dtype or torch.bfloat16, X.device, "out")
+    out = _out(out, (S, N), dtype or torch.bfloat16, X, torch)
     _check(lib().bitsmoe_mx4_product(cp, sp, E, N, K, xp, _dtype_code(X, "X"), X.shape[0], ldx, op,
-                                     _opt(rows, "rows", torch.int32, (S,)), S, int(glu),
-                                     _dev(out, "out"), _dtype_code(out, "out"), N, _stream()),
+                                     _in(rows, "rows", X, torch.int32, (S,)), S, int(glu),
+                                     out.data_ptr(), _dtype_code(out, "out"), N, stream),
            "mx4_product")
     return out
 
@@ -706,16 +721,16 @@ def mx4_product(codes, scales, X, offsets=None, rows=None, glu: bool = False, dt
 def mx4_product_q(codes, scales, xcodes, xscales, offsets=None, rows=None, glu: bool = False,
                   dtype=None, out=None):
     """mx4_product with the tokens in MX4 too (``mx4_quantize`` of X)."""
-    torch = _torch()
-    xcp, xsp = _mx4(xcodes, xscales, "X", 2)
+    torch, stream = _place(xcodes, "X's codes")
+    xcp, xsp = _mx4(xcodes, xscales, "X", xcodes, torch, 2)
     S = xcodes.shape[0] if rows is None else rows.shape[0]
-    cp, sp, E, N, K, op = _experts(codes, scales, offsets, S, glu)
+    cp, sp, E, N, K, op = _experts(codes, scales, offsets, xcodes, torch, glu)
     if 2 * xcodes.shape[1] != K:
         raise ValueError("X and W disagree on K")
-    out = _out(out, (S, N), dtype or torch.bfloat16, codes.device, "out")
+    out = _out(out, (S, N), dtype or torch.bfloat16, xcodes, torch)
     _check(lib().bitsmoe_mx4_product_q(cp, sp, E, N, K, xcp, xsp, xcodes.shape[0], op,
-                                       _opt(rows, "rows", torch.int32, (S,)), S, int(glu),
-                                       _dev(out, "out"), _dtype_code(out, "out"), N, _stream()),
+                                       _in(rows, "rows", xcodes, torch.int32, (S,)), S, int(glu),
+                                       out.data_ptr(), _dtype_code(out, "out"), N, stream),
            "mx4_product_q")
     return out
 
@@ -723,17 +738,17 @@ def mx4_product_q(codes, scales, xcodes, xscales, offsets=None, rows=None, glu: 
 def mx4_product_grad(codes, scales, dY, offsets=None, dtype=None, out=None):
     """dx_s = W_e^T dy_s for the slots in expert order: dY bf16 [S][N] ->
     [S][K], bf16 unless ``dtype`` says fp32."""
-    torch = _torch()
+    torch, stream = _place(dY, "dY")
     if dY.dim() != 2:
         raise ValueError("dY must be [S][N]")
     S = dY.shape[0]
-    cp, sp, E, N, K, op = _experts(codes, scales, offsets, S)
+    cp, sp, E, N, K, op = _experts(codes, scales, offsets, dY, torch)
     if dY.shape[1] != N:
         raise ValueError("dY and W disagree on N")
     yp, ldy = _rows(dY, "dY")
-    out = _out(out, (S, K), dtype or torch.bfloat16, dY.device, "out")
+    out = _out(out, (S, K), dtype or torch.bfloat16, dY, torch)
     _check(lib().bitsmoe_mx4_product_grad(cp, sp, E, N, K, yp, _dtype_code(dY, "dY"), ldy, op, S,
-                                          _dev(out, "out"), _dtype_code(out, "out"), K, _stream()),
+                                          out.data_ptr(), _dtype_code(out, "out"), K, stream),
            "mx4_product_grad")
     return out
 
@@ -741,31 +756,32 @@ def mx4_product_grad(codes, scales, dY, offsets=None, dtype=None, out=None):
 def combine(Z, slots, weights=None, out=None):
     """y_t = sum_j weights[t][j] Z[slots[t][j]] (weights None: all 1) for Z [S][d]
     (bf16 or fp32), slots int32 [T][k], weights fp32 [T][k] -> [T][d] of Z's type."""
-    torch = _torch()
+    torch, stream = _place(Z, "Z")
     if Z.dim() != 2 or slots.dim() != 2:
         raise ValueError("Z must be [S][d] and slots [T][k]")
     (S, d), (T, k) = Z.shape, slots.shape
-    out = _out(out, (T, d), Z.dtype, Z.device, "out")
-    _check(lib().bitsmoe_combine(_dev(Z, "Z"), _dtype_code(Z, "Z"), S,
-                                 _opt(slots, "slots", torch.int32), _opt(weights, "weights", torch.float32, (T, k)),
-                                 T, k, d, _dev(out, "out"), _stream()), "combine")
+    out = _out(out, (T, d), Z.dtype, Z, torch)
+    _check(lib().bitsmoe_combine(_in(Z, "Z", Z, Z.dtype), _dtype_code(Z, "Z"), S,
+                                 _in(slots, "slots", Z, torch.int32),
+                                 _in(weights, "weights", Z, torch.float32, (T, k)), T, k, d,
+                                 out.data_ptr(), stream), "combine")
     return out
 
 
 def combine_grad(Z, slots, weights, dY):
     """Gradients of ``combine``: (dZ [S][d], dweights fp32 [T][k]).  Every row of Z
     is taken to be named by one slot, as ``route`` does."""
-    torch = _torch()
+    torch, stream = _place(Z, "Z")
     if Z.dim() != 2 or slots.dim() != 2:
         raise ValueError("Z must be [S][d] and slots [T][k]")
     (S, d), (T, k) = Z.shape, slots.shape
-    dZ = torch.empty_like(Z)
+    zp = _in(Z, "Z", Z, Z.dtype)
+    dZ = torch.empty((S, d), dtype=Z.dtype, device=Z.device)
     dw = torch.empty((T, k), dtype=torch.float32, device=Z.device)
-    _check(lib().bitsmoe_combine_grad(_dev(Z, "Z"), _dtype_code(Z, "Z"), S,
-                                      _opt(slots, "slots", torch.int32),
-                                      _opt(weights, "weights", torch.float32, (T, k)),
-                                      _opt(dY, "dY", Z.dtype, (T, d)), T, k, d, _dev(dZ, "dZ"),
-                                      _dev(dw, "dweights"), _stream()), "combine_grad")
+    _check(lib().bitsmoe_combine_grad(zp, _dtype_code(Z, "Z"), S, _in(slots, "slots", Z, torch.int32),
+                                      _in(weights, "weights", Z, torch.float32, (T, k)),
+                                      _in(dY, "dY", Z, Z.dtype, (T, d)), T, k, d, dZ.data_ptr(),
+                                      dw.data_ptr(), stream), "combine_grad")
     return dZ, dw
 
 
