@@ -24,11 +24,10 @@ def quantize(X):
     e = np.where(top > 0, np.frexp(top)[1] - 1 - 2, -127)  # frexp: top = m 2^x, m in [1/2, 1)
     e = np.maximum(e, -127)
     m = A / np.ldexp(1.0, e)[..., None]
-    # nearest grid value; of two as near, the even code
-    d = np.abs(m[..., None] - GRID)
-    near = d == d.min(-1, keepdims=True)
-    odd = np.arange(8) % 2
-    code = np.argmin(np.where(near, odd, 2), -1).astype(np.uint8)
+    # nearest grid value; half way between two (above one midpoint fewer than at or above), the even code
+    mid = (GRID[1:] + GRID[:-1]) / 2
+    low, high = np.searchsorted(mid, m, "left"), np.searchsorted(mid, m, "right")
+    code = np.where(low % 2 == 0, low, high).astype(np.uint8)
     code |= np.signbit(B).astype(np.uint8) << 3
     code = np.where(lost[..., None], 0, code).astype(np.uint8).reshape(X.shape)
     scales = np.where(lost, 255, e + 127).astype(np.uint8)

@@ -200,15 +200,15 @@ __device__ __forceinline__ void store4(const MulArgs& a, int64_t s, int64_t n, i
   }
 }
 
-// A lane's part of the 32 results n .. n + 31 of slot s: v[i] is that of
+// A lane's part of the 32 results n .. n + 31 (of N) of slot s: v[i] is that of
 // n + 8 (i / 4) + 4 half + i % 4, as a 32 x 32 accumulator lies.
-__device__ __forceinline__ void store32(const MulArgs& a, int64_t s, int64_t n, int half, bool whole,
+__device__ __forceinline__ void store32(const MulArgs& a, int64_t s, int64_t n, int half, bool whole, int64_t N,
                                         const float (&v)[16]) {
   if (!whole) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int64_t at = n + 8 * e + 4 * half;
-      if (at < a.N) store4(a, s, at, a.N, a.ldy % 4 == 0, f32x4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]});
+      if (at < N) store4(a, s, at, N, a.ldy % 4 == 0, f32x4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]});
     }
   } else if (a.yf32) {
     float* p = static_cast<float*>(a.y) + s * a.ldy + n + 4 * half;
@@ -310,6 +310,139 @@ __global__ __launch_bounds__(kThreads) void mx4_rows_kernel(MulArgs a) {
   const int64_t slot = t.lo + r, n = n0 + 4 * q;  // (a lane holds four outputs of one slot)
   const bool wide = a.ldy % 4 == 0;
   if (slot < t.hi && n < a.N) store4(a, slot, n, a.N, wide, acc[0]);
+}
+
+// 16 TB slots x 256 weight rows a workgroup, 64 rows a wave: for a few slots an
+// expert and many experts, where reading the weights is all.  The slots' tokens
+// go through LDS 1024 entries of K at a time; the weights come straight into
+// registers, a step of 128 entries (four rows' tiles, 64 bytes of a row) ahead.
+// 16-byte chunk c of a slot lies at c ^ (slot mod 16): the sixteen slots of a
+// fragment read in different banks.
+template <bool MX, bool GLU, int TB>
+__global__ __launch_bounds__(kThreads) void mx4_few_kernel(MulArgs a) {
+  constexpr int R = 4, KC = 1024, XB = MX ? KC / 2 : 2 * KC, XC = XB / 16, SL = 16 * TB;
+  constexpr int NO = GLU ? 128 : 256;  // results of a slot
+  __shared__ __align__(16) char xs[SL * XB];
+  __shared__ uint8_t ss[MX ? SL * (KC / 32) : 1];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, q = lane >> 4;
+  Tile t;
+  if (!find_tile(a.offsets, a.E, a.S, static_cast<int>((a.N + NO - 1) / NO), SL, &t)) return;
+  const int64_t n0 = static_cast<int64_t>(t.col) * NO;
+  f32x4 acc[R][TB];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int b = 0; b < TB; ++b) acc[i][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (t.e < a.E) {
+    const int kb = static_cast<int>(a.K / 32);
+    // this lane's row of each of the wave's tiles (glu: gate and up in turn), at its block of 32 in the first step
+    const uint8_t *pc[R], *ps[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      int64_t row;
+      if constexpr (GLU)
+        row = static_cast<int64_t>(t.e) * 2 * a.N + min(n0 + wave * 32 + (i >> 1) * 16 + r, a.N - 1) + (i & 1) * a.N;
+      else
+        row = static_cast<int64_t>(t.e) * a.N + min(n0 + wave * 64 + i * 16 + r, a.N - 1);
+      pc[i] = a.codes + (row * kb + q) * 16;
+      ps[i] = a.scales + row * kb + q;
+    }
+    uint4 c[R];
+    int s[R];
+    auto load = [&](int step) {
+      const int b = 4 * step + q;
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const bool in = b < kb;
+        c[i] = in ? *reinterpret_cast<const uint4*>(pc[i] + static_cast<int64_t>(step) * 64) : make_uint4(0, 0, 0, 0);
+        s[i] = in ? ps[i][4 * step] : 127;
+      }
+    };
+    const int steps = (kb + 3) / 4;
+    load(0);
+    for (int k0 = 0; k0 < steps; k0 += KC / 128) {
+      if (k0 > 0) __syncthreads();
+      for (int i = tid; i < SL * XC; i += kThreads) {
+        const int sl = i / XC, ch = i % XC;  // (powers of two)
+        const int64_t slot = t.lo + sl;
+        const int64_t row = slot < t.hi ? (a.rows ? static_cast<int64_t>(a.rows[slot]) : slot) : -1;
+        const int at = (k0 * 128 + ch * (MX ? 32 : 8)) / 32;  // block of the chunk
+        uint4 v = make_uint4(0, 0, 0, 0);
+        int sc = 127;
+        if (row >= 0 && row < a.x_rows && at < kb) {
+          if constexpr (MX) {
+            v = *reinterpret_cast<const uint4*>(a.xcodes + (row * kb + at) * 16);
+            sc = a.xscales[row * kb + at];
+          } else {
+            v = *reinterpret_cast<const uint4*>(a.x + row * a.ldx + k0 * 128 + ch * 8);
+          }
+        }
+        *reinterpret_cast<uint4*>(xs + sl * XB + ((ch ^ (sl & 15)) * 16)) = v;
+        if constexpr (MX) ss[sl * (KC / 32) + ch] = static_cast<uint8_t>(sc);
+      }
+      __syncthreads();
+      const int end = min(steps - k0, KC / 128);
+      for (int st = 0; st < end; ++st) {
+        uint4 w[R];
+        int sw[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          w[i] = c[i];
+          sw[i] = s[i];
+        }
+        if (k0 + st + 1 < steps) load(k0 + st + 1);
+        if constexpr (MX) {
+#pragma unroll
+          for (int b = 0; b < TB; ++b) {
+            const int sl = 16 * b + r, ch = 4 * st + q;
+            const uint4 v = *reinterpret_cast<const uint4*>(xs + sl * XB + ((ch ^ r) * 16));
+            const i32x8 B = {(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0};
+            const int sx = ss[sl * (KC / 32) + ch];
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+              const i32x8 A = {(int)w[i].x, (int)w[i].y, (int)w[i].z, (int)w[i].w, 0, 0, 0, 0};
+              acc[i][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, acc[i][b], 4, 4, 0, sw[i], 0, sx);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            bf16x8 xv[TB];
+#pragma unroll
+            for (int b = 0; b < TB; ++b)
+              xv[b] = *reinterpret_cast<const bf16x8*>(xs + (16 * b + r) * XB + (((16 * st + 4 * q + j) ^ r) * 16));
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+              const uint32_t d = j == 0 ? w[i].x : j == 1 ? w[i].y : j == 2 ? w[i].z : w[i].w;
+              const bf16x8 wv = mx4_bf16(d, mx4_scale(sw[i]));
+#pragma unroll
+              for (int b = 0; b < TB; ++b)
+                acc[i][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xv[b], acc[i][b], 0, 0, 0);
+            }
+          }
+        }
+      }
+    }
+  }
+  const bool wide = a.ldy % 4 == 0;
+#pragma unroll
+  for (int b = 0; b < TB; ++b) {
+    const int64_t slot = t.lo + 16 * b + r;
+    if (slot >= t.hi) continue;
+#pragma unroll
+    for (int i = 0; i < (GLU ? R / 2 : R); ++i) {
+      f32x4 v;
+      if constexpr (GLU) {
+        v = acc[2 * i][b];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = silu(v[u]) * acc[2 * i + 1][b][u];
+      } else {
+        v = acc[i][b];
+      }
+      const int64_t n = n0 + wave * (GLU ? 32 : 64) + i * 16 + 4 * q;
+      if (n < a.N) store4(a, slot, n, a.N, wide, v);
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -821,7 +954,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(MulArgs a) {
           if constexpr (GLU) v[i] = silu(v[i]) * acc[1][m][i];
           v[i] = have ? v[i] : 0.0f;
         }
-        store32(a, slot, n0 + wn * (GLU ? 32 : 64) + 32 * n, half, whole, v);
+        store32(a, slot, n0 + wn * (GLU ? 32 : 64) + 32 * n, half, whole, a.N, v);
       }
     }
     if (!more) return;
@@ -873,24 +1006,25 @@ __global__ __launch_bounds__(kThreads) void mx4_grad_kernel(MulArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// dx in large tiles: 128 slots x 256 columns a workgroup of eight waves, n
-// advancing 64 rows of W a step.  The sum runs over W's rows, along which its
-// scales change, so the codes of a step (64 rows x 256 columns, loaded as the
-// forward form loads them) are widened to bf16 once by the whole workgroup, one
-// block of 32 a thread, into an LDS tile that the transposing LDS read takes
-// the fragments from.  Two such tiles: the next step is widened while this one
-// is multiplied.
+// dx in large tiles: 128 slots x 256 columns a workgroup of eight waves, which
+// stays and takes tile after tile like the forward form.  n advances 64 rows of
+// W a step.  The sum runs over W's rows, along which its scales change, so a
+// step's codes (64 rows x 256 columns) are widened to bf16 once by the whole
+// workgroup, a block of 32 a thread, into an LDS tile that the transposing LDS
+// read takes fragments from.  Two such tiles: the next step's is made while this
+// one's is multiplied, and between the matrix-core ops go the reads of the next
+// sixteen rows' fragments and the conversions.
 // ---------------------------------------------------------------------------
 struct GradShape {
-  static constexpr int TM = 128, KT = 256, NS = 64;  // slots, columns, rows of W a step
-  static constexpr int kX = 0, kW = TM * NS * 2, kWS = kW + NS * KT / 2, kStage = kWS + NS * (KT / 32) * 4;
-  static constexpr int kStages = 3;
+  static constexpr int KT = 256, NS = 64;  // columns, rows of W a step
+  static constexpr int NX = 4, NW = 3;     // rings of dy and of codes with their scales
+  static constexpr int kXStage = kTM * NS * 2, kCodes = NS * KT / 2, kWStage = kCodes + NS * (KT / 32) * 4;
   static constexpr int kTile = NS * KT * 2;
-  static constexpr int kBytes = kStages * kStage + 2 * kTile;
-  static constexpr int LX = 2, kLoads = LX + 2;
-  static constexpr int MB = 2, NB = 2;
+  static constexpr int oW = NX * kXStage, oTile = oW + NW * kWStage, kBytes = oTile + 2 * kTile;
+  static constexpr int LX = kXStage / 1024 / kWaves, kWLoads = 2;
+  static constexpr int MB = 2, NB = 2, kLeast = NX;
+  static_assert(kBytes <= kLds);
 };
-static_assert(GradShape::kBytes <= 163840);
 
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 __device__ __forceinline__ s16x4 read_transposed(const char* p) {
@@ -898,130 +1032,230 @@ __device__ __forceinline__ s16x4 read_transposed(const char* p) {
       (__attribute__((address_space(3))) s16x4*)(reinterpret_cast<uintptr_t>(p)));
 }
 
-__global__ __launch_bounds__(kTileThreads) void mx4_grad_tile_kernel(MulArgs a) {
+__global__ __launch_bounds__(kTileThreads, 2) void mx4_grad_tile_kernel(MulArgs a) {
   using H = GradShape;
   extern __shared__ __align__(16) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  Tile t;
-  if (!find_tile(a.offsets, a.E, a.S, static_cast<int>((a.K + H::KT - 1) / H::KT), H::TM, &t)) return;
-  const int64_t k0 = static_cast<int64_t>(t.col) * H::KT;
   const int wm = wave >> 2, wn = wave & 3, r32 = lane & 31, half = lane >> 5;
-  f32x16 acc[H::NB][H::MB];
-#pragma unroll
-  for (int i = 0; i < H::NB; ++i)
-#pragma unroll
-    for (int j = 0; j < H::MB; ++j)
-#pragma unroll
-      for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.0f;
+  const int64_t kb = a.K / 32;
+  const int N = static_cast<int>(a.N), nk = max((N + H::NS - 1) / H::NS, H::kLeast);
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
+  const char *const zero = reinterpret_cast<const char*>(kPad), *const one = zero + 16;
 
-  if (t.e < a.E) {
-    const int64_t kb = a.K / 32;
-    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
-    char* wide = smem + H::kStages * H::kStage;
-    const char *px[H::LX], *pw, *ps;
-    int nx[H::LX];
+  int none;
+  Walk walk;
+  Tile cur, next;
+  bool more = walk.start(a.offsets, a.E, a.S, static_cast<int>((a.K + H::KT - 1) / H::KT), kTM, &none);
+  for (int64_t s = none + static_cast<int64_t>(blockIdx.x); s < a.S; s += gridDim.x)
+    for (int64_t k = tid; k < a.K; k += kTileThreads) {
+      if (a.yf32)
+        static_cast<float*>(a.y)[s * a.ldy + k] = 0.0f;
+      else
+        static_cast<uint16_t*>(a.y)[s * a.ldy + k] = 0;
+    }
+  if (!more) return;
+  walk.get(&cur);
+
+  // ---- loads: dy's rows 8 lanes each; codes and scales of row wr, block lane % 8 of the tile
+  const char *px[H::LX], *pw, *ps;
+  const int wr = wave * 8 + lane / 8;
+  const int64_t wstep = H::NS * kb * 16, sstep = H::NS * kb;
+  auto row_of = [&](int q) { return (wave + kWaves * q) * 8 + lane / 8; };
+  auto aim = [&](const Tile& t) {
+#pragma unroll
+    for (int q = 0; q < H::LX; ++q)
+      px[q] = reinterpret_cast<const char*>(a.x + static_cast<int64_t>(min(t.lo + row_of(q), t.hi - 1)) * a.ldx +
+                                            8 * chunk_slot(row_of(q), lane & 7));
+    const int64_t block = min(static_cast<int64_t>(t.col) * (H::KT / 32) + (lane & 7), kb - 1);
+    const int64_t row = static_cast<int64_t>(t.e) * a.N + wr;
+    pw = reinterpret_cast<const char*>(a.codes + (row * kb + block) * 16);
+    ps = reinterpret_cast<const char*>(a.scales + row * kb + block);
+  };
+  int step = 0, xto = 0, wto = 0;
+  auto issue = [&]() {
+    const int rem = N - step * H::NS;  // rows of W from this step on
+    const char *w = pw, *s = ps;
+    if (rem < H::NS) {
+      asm volatile("");  // (a branch, not selects at every step)
+      w = wr < rem ? w : zero;
+      s = wr < rem ? s : one;
+    }
+    load_lds16(w, lds0 + H::oW + wto * H::kWStage + wave * 1024);
+    load_lds1(s, lds0 + H::oW + wto * H::kWStage + H::kCodes + wave * 256);
+    pw += wstep;
+    ps += sstep;
 #pragma unroll
     for (int q = 0; q < H::LX; ++q) {
-      const int r = (wave + kWaves * q) * 8 + lane / 8, c = chunk_slot(r, lane % 8);
-      nx[q] = 8 * c;
-      px[q] = reinterpret_cast<const char*>(a.x + min(t.lo + r, t.hi - 1) * a.ldx + 8 * c);
+      const char* p = px[q];
+      if (rem < H::NS) {
+        asm volatile("");
+        p = 8 * chunk_slot(row_of(q), lane & 7) < rem ? p : zero;
+      }
+      load_lds16(p, lds0 + xto * H::kXStage + (wave + kWaves * q) * 1024);
+      px[q] += H::NS * 2;
     }
-    // codes and scales of row wave * 8 + lane / 8 of a step, block lane % 8 of the tile
-    const int wr = wave * 8 + lane / 8;
-    const int64_t block = min(k0 / 32 + lane % 8, kb - 1);
-    pw = reinterpret_cast<const char*>(a.codes + ((static_cast<int64_t>(t.e) * a.N + wr) * kb + block) * 16);
-    ps = reinterpret_cast<const char*>(a.scales + (static_cast<int64_t>(t.e) * a.N + wr) * kb + block);
-    const int64_t wstep = H::NS * kb * 16, sstep = H::NS * kb;
-    const int nk = static_cast<int>((a.N + H::NS - 1) / H::NS);
-    const int last = static_cast<int>(a.N - static_cast<int64_t>(nk - 1) * H::NS);
-    int issued = 0, to = 0;
-    auto issue = [&]() {
-      const uint32_t s = lds0 + to * H::kStage;
-      if (issued == nk - 1 && last < H::NS) {
-#pragma unroll
-        for (int q = 0; q < H::LX; ++q) px[q] = nx[q] < last ? px[q] : reinterpret_cast<const char*>(kPad);
-        pw = wr < last ? pw : reinterpret_cast<const char*>(kPad);
-        ps = wr < last ? ps : reinterpret_cast<const char*>(kPad + 16);
+    ++step;
+    xto = xto + 1 == H::NX ? 0 : xto + 1;
+    wto = wto + 1 == H::NW ? 0 : wto + 1;
+  };
+  bool dry = false;
+  auto find_next = [&]() {
+    walk.l += walk.step;
+    more = walk.find();
+    if (more) walk.get(&next);
+  };
+  auto go_on = [&]() {  // the loads of the next step, if there is one
+    if (step == nk) {
+      if (!more) {
+        dry = true;
+        return;
       }
+      aim(next);
+      step = 0;
+    }
+    issue();
+  };
+
+  // ---- a block of codes a thread, widened into row wr of a tile (chunk c of row r lies at c ^ 4 (r mod 4))
+  const char* wst = smem + H::oW;
+  auto advance_w = [&]() { wst = wst + H::kWStage == smem + H::oTile ? smem + H::oW : wst + H::kWStage; };
+  uint4 codes;
+  float scale;
+  auto take = [&]() {
+    codes = *reinterpret_cast<const uint4*>(wst + tid * 16);
+    scale = mx4_scale(*reinterpret_cast<const uint32_t*>(wst + H::kCodes + tid * 4));
+  };
+  char* const into = smem + H::oTile + wr * (H::KT * 2);
+  auto widen = [&](int i, int tile) {
+    const uint32_t d = i == 0 ? codes.x : i == 1 ? codes.y : i == 2 ? codes.z : codes.w;
+    *reinterpret_cast<uint4*>(into + tile * H::kTile + (((4 * (lane & 7) + i) ^ (4 * (wr & 3))) * 16)) =
+        mx4_bf16_words(d, scale);
+  };
+
+  // ---- fragments of sixteen rows of W
+  struct Part {
+    bf16x8 x[H::MB];
+    s16x4 w[H::NB][2];
+  };
+  const int xrow = wm * (kTM / 2) + r32;
+  // read k (0 .. 5) of part j of the step at xst, in tile `tile`
+  auto read = [&](Part& f, int k, int j, const char* xst, int tile) {
+    if (k < 2) {
+      const int r = xrow + 32 * k;
+      f.x[k] = *reinterpret_cast<const bf16x8*>(xst + r * 128 + chunk_slot(r, 2 * j + half) * 16);
+    } else {
+      // rows 16 j + 8 half + 4 q + (lane % 16) / 4, column 16 ((lane / 16) % 2) + 4 (lane % 4) of block n
+      const int n = (k - 2) >> 1, q = k & 1;
+      const int col = wn * 64 + 32 * n + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+      const int r = 16 * j + 8 * half + 4 * q + ((lane & 15) >> 2);
+      f.w[n][q] = read_transposed(smem + H::oTile + tile * H::kTile + r * (H::KT * 2) +
+                                  (((col >> 3) ^ (4 * (r & 3))) << 4) + (col & 7) * 2);
+    }
+  };
+  f32x16 acc[H::NB][H::MB];
+  auto clear = [&]() {
 #pragma unroll
-      for (int q = 0; q < H::LX; ++q) {
-        load_lds16(px[q], s + H::kX + (wave + kWaves * q) * 1024);
-        px[q] += H::NS * 2;
-      }
-      load_lds16(pw, s + H::kW + wave * 1024);
-      load_lds1(ps, s + H::kWS + wave * 256);
-      pw += wstep;
-      ps += sstep;
-      ++issued;
-      to = to + 1 == H::kStages ? 0 : to + 1;
-    };
-    // this thread's block of stage `s`, widened into row wr of tile `w`
-    auto widen = [&](const char* s, char* w) {
-      const uint4 c = *reinterpret_cast<const uint4*>(s + H::kW + tid * 16);
-      const float scale = mx4_scale(*reinterpret_cast<const uint32_t*>(s + H::kWS + tid * 4));
-      const uint32_t d[4] = {c.x, c.y, c.z, c.w};
+    for (int i = 0; i < H::NB; ++i)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)  // 16-byte chunk 4 (lane % 8) + i of the row
-        *reinterpret_cast<uint4*>(w + wr * (H::KT * 2) + ((4 * (lane % 8) + i) ^ (4 * (wr & 3))) * 16) =
-            mx4_bf16_words(d[i], scale);
-    };
-    for (int i = 0; i < H::kStages - 1 && i < nk; ++i) issue();
-    if (issued > 1)
-      wait_loads<H::kLoads>();
-    else
-      wait_loads<0>();
-    widen(smem, wide);
-    const int xrow = wm * (H::TM / 2) + r32;
-    int from = 0;
+      for (int j = 0; j < H::MB; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+  };
+  // The four ops of a part, with `between(k)` after op k.
+  auto multiply = [&](const Part& f, auto between) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int n = k >> 1, m = k & 1;
+      const bf16x8 w =
+          __builtin_bit_cast(bf16x8, __builtin_shufflevector(f.w[n][0], f.w[n][1], 0, 1, 2, 3, 4, 5, 6, 7));
+      acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, f.x[m], acc[n][m], 0, 0, 0);
+      between(k);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  aim(cur);
+  issue();
+  issue();
+  issue();
+  wait_loads<2 * (H::kWLoads + H::LX)>();
+  take();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) widen(i, 0);
+  advance_w();
+  find_next();
+  wait_loads<H::LX + H::kWLoads + H::LX>();  // (step 1's codes, too)
+  go_on();
+  clear();
+  const char* xst = smem;
+  int tile = 0;
+  Part f0, f1;
+#pragma unroll
+  for (int k = 0; k < 6; ++k) read(f0, k, 0, xst, tile);
+  for (;;) {
     for (int i = 0; i < nk; ++i) {
-      // step i + 1 has landed, step i is widened, and every wave is past step i - 1
-      wait_loads<0>();
-      if (issued < nk) issue();
-      const char* s = smem + from * H::kStage;
-      from = from + 1 == H::kStages ? 0 : from + 1;
-      if (i + 1 < nk) widen(smem + from * H::kStage, wide + ((i + 1) & 1) * H::kTile);
-      const char* w = wide + (i & 1) * H::kTile;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {  // 16 rows of W
-        bf16x8 xf[H::MB];
-#pragma unroll
-        for (int m = 0; m < H::MB; ++m) {
-          const int r = xrow + 32 * m;
-          xf[m] = *reinterpret_cast<const bf16x8*>(s + H::kX + r * (H::NS * 2) + chunk_slot(r, 2 * j + half) * 16);
+      multiply(f0, [&](int k) {
+        if (k == 0) take();
+        if (k == 0 || k == 1) read(f1, k, 1, xst, tile);
+        if (k >= 2) {
+          read(f1, 2 * k - 2, 1, xst, tile);
+          read(f1, 2 * k - 1, 1, xst, tile);
         }
-#pragma unroll
-        for (int n = 0; n < H::NB; ++n) {
-          // rows 16 j + 8 half + 4 q + (lane % 16) / 4, column 16 ((lane / 16) % 2) + 4 (lane % 4) of the block
-          const int col = wn * 64 + 32 * n + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-          s16x4 h[2];
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            const int r = 16 * j + 8 * half + 4 * q + ((lane & 15) >> 2);
-            h[q] = read_transposed(w + r * (H::KT * 2) + (((col >> 3) ^ (4 * (r & 3))) << 4) + (col & 7) * 2);
-          }
-          const bf16x8 wf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-          for (int m = 0; m < H::MB; ++m)
-            acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wf, xf[m], acc[n][m], 0, 0, 0);
+      });
+      multiply(f1, [&](int k) {
+        if (k < 2) read(f0, k, 2, xst, tile);
+        if (k >= 2) {
+          read(f0, 2 * k - 2, 2, xst, tile);
+          read(f0, 2 * k - 1, 2, xst, tile);
         }
+        if (k == 1) widen(0, tile ^ 1);
+        if (k == 3) widen(1, tile ^ 1);
+      });
+      multiply(f0, [&](int k) {
+        if (k < 2) read(f1, k, 3, xst, tile);
+        if (k >= 2) {
+          read(f1, 2 * k - 2, 3, xst, tile);
+          read(f1, 2 * k - 1, 3, xst, tile);
+        }
+        if (k == 1) widen(2, tile ^ 1);
+        if (k == 2) widen(3, tile ^ 1);
+      });
+      advance_w();
+      // The next step's tile is whole, its dy and the codes after it have landed (but for what was asked for later: dy
+      // of one step, and a step), and every wave has read all of this step.
+      if (dry)
+        wait_loads<0>();
+      else
+        wait_loads<H::LX + H::kWLoads + H::LX>();
+      go_on();
+      xst = xst + H::kXStage == smem + H::oW ? smem : xst + H::kXStage;
+      tile ^= 1;
+      multiply(f1, [&](int k) {  // (what is read after the last tile is not used)
+        if (k < 2) read(f0, k, 0, xst, tile);
+        if (k >= 2) {
+          read(f0, 2 * k - 2, 0, xst, tile);
+          read(f0, 2 * k - 1, 0, xst, tile);
+        }
+      });
+    }
+    const int64_t k0 = static_cast<int64_t>(cur.col) * H::KT;
+    const bool whole = k0 + H::KT <= a.K && a.ldy % 8 == 0;
+#pragma unroll
+    for (int m = 0; m < H::MB; ++m) {
+      const int64_t slot = cur.lo + wm * (kTM / 2) + 32 * m + r32;
+      if (slot >= cur.hi) continue;
+#pragma unroll
+      for (int n = 0; n < H::NB; ++n) {
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = acc[n][m][i];
+        store32(a, slot, k0 + wn * 64 + 32 * n, half, whole, a.K, v);
       }
     }
-  }
-  const bool aligned = a.ldy % 4 == 0;
-#pragma unroll
-  for (int m = 0; m < H::MB; ++m) {
-    const int64_t slot = t.lo + wm * (H::TM / 2) + 32 * m + r32;
-    if (slot >= t.hi) continue;
-#pragma unroll
-    for (int n = 0; n < H::NB; ++n)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        f32x4 v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = acc[n][m][4 * q + i];
-        const int64_t at = k0 + wn * 64 + 32 * n + 8 * q + 4 * half;
-        if (at < a.K) store4(a, slot, at, a.K, aligned, v);
-      }
+    if (!more) return;
+    cur = next;
+    clear();
+    find_next();
   }
 }
 
@@ -1053,18 +1287,23 @@ bool grid_of(const MulArgs& a, int64_t tile, int64_t per, unsigned* grid) {
 
 // Large tiles pay from about this many slots an expert on.
 constexpr int64_t kTileSlots = 32;
+// Below, whole rows of K a wave pay from about this many workgroups on (two a compute unit).
+constexpr int64_t kFewGroups = 512;
+
+// One workgroup a compute unit, as many on every XCD.
+unsigned tile_grid() {
+  const int cus = device_cus();
+  return static_cast<unsigned>(cus < 8 ? 8 : cus / 8 * 8);
+}
 
 template <bool MX, bool AL, bool GLU>
 bitsmoe_status tile_product(const MulArgs& a, hipStream_t s) {
-  // one workgroup a compute unit, as many on every XCD
-  const int cus = device_cus();
-  const unsigned grid = static_cast<unsigned>(cus < 8 ? 8 : cus / 8 * 8);
   constexpr int lds = Shape<MX, AL>::kBytes;
   auto* fn = mx4_tile_kernel<MX, AL, GLU>;
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return device_error("mx4_product: shared memory", e);
-  fn<<<grid, kTileThreads, lds, s>>>(a);
+  fn<<<tile_grid(), kTileThreads, lds, s>>>(a);
   BITSMOE_LAUNCH_CHECK("mx4_tile_kernel");
   return ok();
 }
@@ -1080,6 +1319,19 @@ bitsmoe_status product(const char* who, const MulArgs& a, bool glu, hipStream_t 
     return glu ? tile_product<false, false, true>(a, s) : tile_product<false, false, false>(a, s);
   }
   unsigned grid;
+  const int64_t cols = (a.N + (glu ? 127 : 255)) / (glu ? 128 : 256);
+  if ((a.S < a.E ? a.S : a.E) * cols >= kFewGroups) {
+    const bool two = a.S > 8 * a.E;
+    if (!grid_of(a, two ? 32 : 16, cols, &grid))
+      return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": too many slots and outputs for one call");
+    auto* fn = two ? (mx ? (glu ? mx4_few_kernel<true, true, 2> : mx4_few_kernel<true, false, 2>)
+                         : (glu ? mx4_few_kernel<false, true, 2> : mx4_few_kernel<false, false, 2>))
+                   : (mx ? (glu ? mx4_few_kernel<true, true, 1> : mx4_few_kernel<true, false, 1>)
+                         : (glu ? mx4_few_kernel<false, true, 1> : mx4_few_kernel<false, false, 1>));
+    fn<<<grid, kThreads, 0, s>>>(a);
+    BITSMOE_LAUNCH_CHECK("mx4_few_kernel");
+    return ok();
+  }
   if (!grid_of(a, 16, (a.N + 15) / 16, &grid))
     return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": too many slots and outputs for one call");
   auto* fn = mx ? (glu ? mx4_rows_kernel<true, true> : mx4_rows_kernel<true, false>)
@@ -1141,12 +1393,10 @@ extern "C" bitsmoe_status bitsmoe_mx4_product_grad(const uint8_t* codes_dev, con
   if (!dY_dev) return fail(BITSMOE_ERR_ARG, "mx4_product_grad: null pointer");
   unsigned grid;
   if (S >= kTileSlots * E) {
-    if (!grid_of(a, GradShape::TM, (K + GradShape::KT - 1) / GradShape::KT, &grid))
-      return fail(BITSMOE_ERR_SHAPE, "mx4_product_grad: too many slots and columns for one call");
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(mx4_grad_tile_kernel),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, GradShape::kBytes);
     if (e != hipSuccess) return device_error("mx4_product_grad: shared memory", e);
-    mx4_grad_tile_kernel<<<grid, kTileThreads, GradShape::kBytes, static_cast<hipStream_t>(stream)>>>(a);
+    mx4_grad_tile_kernel<<<tile_grid(), kTileThreads, GradShape::kBytes, static_cast<hipStream_t>(stream)>>>(a);
     BITSMOE_LAUNCH_CHECK("mx4_grad_tile_kernel");
     return ok();
   }

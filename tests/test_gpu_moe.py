@@ -204,10 +204,10 @@ def test_route_twice_gives_the_same_bits():
 
 # --------------------------------------------------------------- products
 def experts_case(E, N, K, S, g, empty=0.3, tail=0):
-    """Weights in MX4, and offsets of S slots over E experts, some without any,
-    the last `tail` slots without an expert."""
-    W = g.standard_normal((E, N, K)) * np.exp(0.5 * g.standard_normal((E, N, 1))) / np.sqrt(K)
-    codes, scales = omx4.quantize(W)
+    """Weights in MX4 (any codes, scales over a few powers of two), and offsets of S
+    slots over E experts, some without any, the last `tail` slots without an expert."""
+    codes = g.integers(0, 256, (E, N, K // 2), dtype=np.uint8)
+    scales = g.integers(118, 124, (E, N, K // 32), dtype=np.uint8)
     load = np.exp(g.standard_normal(E)) * (g.random(E) >= empty)
     if not load.any():
         load[-1] = 1
@@ -238,6 +238,8 @@ SHAPES = [
     # rows of scales that are whole 16-byte pieces, several tiles of several experts
     (3, 130, 1024, 500, 3), (2, 300, 1536, 700, 0), (8, 1040, 512, 900, 9), (70, 264, 2048, 2300, 0),
     (1, 520, 4096, 33, 0), (4, 5000, 256, 700, 40),
+    # few slots an expert, many experts
+    (130, 1030, 96, 200, 7), (300, 512, 64, 290, 0), (64, 2100, 160, 900, 5), (86, 1500, 1088, 700, 0),
 ]
 
 
