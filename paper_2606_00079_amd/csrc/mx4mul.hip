@@ -965,46 +965,6 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(MulArgs a) {
   }
 }
 
-// dx: 64 columns x 16 slots a workgroup, 16 columns a wave.  The weights' tile
-// (32 rows x 64 columns) is widened to bf16 and transposed in LDS.
-__global__ __launch_bounds__(kThreads) void mx4_grad_kernel(MulArgs a) {
-  constexpr int KT = 64, LD = 40;  // (LD: rows 80 bytes apart)
-  __shared__ __align__(16) uint16_t wt[KT * LD];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, q = lane >> 4;
-  Tile t;
-  if (!find_tile(a.offsets, a.E, a.S, static_cast<int>((a.K + KT - 1) / KT), 16, &t)) return;
-  const int64_t k0 = static_cast<int64_t>(t.col) * KT;
-  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  const int64_t slot = t.lo + r;
-  if (t.e < a.E) {
-    const int64_t kb = a.K / 32;
-    const int wr = tid >> 3, wc = tid & 7;  // this thread's row and word of the tile
-    for (int64_t n0 = 0; n0 < a.N; n0 += 32) {
-      uint32_t w = 0;
-      float scale = 1.0f;
-      if (n0 + wr < a.N && k0 + 8 * wc < a.K) {
-        const int64_t row = static_cast<int64_t>(t.e) * a.N + n0 + wr;
-        w = *reinterpret_cast<const uint32_t*>(a.codes + row * kb * 16 + k0 / 2 + 4 * wc);
-        scale = mx4_scale(a.scales[row * kb + (k0 + 8 * wc) / 32]);
-      }
-      const uint4 v4 = mx4_bf16_words(w, scale);
-      const uint32_t v[4] = {v4.x, v4.y, v4.z, v4.w};
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 8; ++i) wt[(8 * wc + i) * LD + wr] = static_cast<uint16_t>(v[i / 2] >> (16 * (i & 1)));
-      __syncthreads();
-      uint4 xv = make_uint4(0, 0, 0, 0);
-      const int64_t n = n0 + 8 * q;
-      if (slot < t.hi && n < a.N) xv = *reinterpret_cast<const uint4*>(a.x + slot * a.ldx + n);
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-          *reinterpret_cast<const bf16x8*>(&wt[(16 * wave + r) * LD + 8 * q]), __builtin_bit_cast(bf16x8, xv), acc,
-          0, 0, 0);
-    }
-  }
-  const int64_t k = k0 + 16 * wave + 4 * q;
-  if (slot < t.hi && k < a.K) store4(a, slot, k, a.K, a.ldy % 4 == 0, acc);
-}
-
 // ---------------------------------------------------------------------------
 // dx in large tiles: 128 slots x 256 columns a workgroup of eight waves, which
 // stays and takes tile after tile like the forward form.  n advances 64 rows of
@@ -1259,6 +1219,114 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_grad_tile_kernel(MulArgs 
   }
 }
 
+// dx for few slots an expert: 16 TB slots x 128 columns a workgroup.  As in the
+// large tiles the codes of 64 rows of W are widened into an LDS tile for the
+// transposing read, two tiles in turn; they come through registers, four steps
+// ahead.  With few workgroups what counts is the length of one's chain of
+// steps, so two groups of four waves take every other step, and join their sums
+// at the end.
+template <int TB>
+__global__ __launch_bounds__(kTileThreads) void mx4_grad_few_kernel(MulArgs a) {
+  constexpr int KT = 128, NS = 64, AHEAD = 4, C = KT / 64;
+  constexpr int kTile = NS * KT * 2;
+  __shared__ __align__(16) char tiles[2][2][kTile];
+  __shared__ __align__(16) char dys[2][2][16 * TB * NS * 2];  // dy of a step: 128 bytes a slot
+  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+  const int group = threadIdx.x >> 8, tid = threadIdx.x & 255, wave = tid >> 6;
+  Tile t;
+  if (!find_tile(a.offsets, a.E, a.S, static_cast<int>((a.K + KT - 1) / KT), 16 * TB, &t)) return;
+  const int64_t k0 = static_cast<int64_t>(t.col) * KT;
+  f32x4 acc[C][TB];
+#pragma unroll
+  for (int i = 0; i < C; ++i)
+#pragma unroll
+    for (int b = 0; b < TB; ++b) acc[i][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  if (t.e < a.E) {
+    const int64_t kb = a.K / 32;
+    const int N = static_cast<int>(a.N), trips = (N + 2 * NS - 1) / (2 * NS);
+    // this thread's block of a step: row wr, block tid % 4
+    const int wr = tid >> 2;
+    const int64_t block = min(k0 / 32 + (tid & 3), kb - 1), row0 = static_cast<int64_t>(t.e) * a.N + wr;
+    // and its eight entries of dy: slot tid / 8 (past the tile's end: its last), chunk tid % 8
+    const int sl = tid >> 3, ch = tid & 7;
+    const uint16_t* dy = a.x + static_cast<int64_t>(min(t.lo + min(sl, 16 * TB - 1), t.hi - 1)) * a.ldx + 8 * ch;
+    uint4 c[AHEAD], x[AHEAD];
+    int s[AHEAD];
+    auto load = [&](int u, int trip) {
+      const int n0 = (2 * trip + group) * NS;
+      c[u] = x[u] = make_uint4(0, 0, 0, 0);
+      s[u] = 127;
+      if (n0 + wr < N) {
+        c[u] = *reinterpret_cast<const uint4*>(a.codes + ((row0 + n0) * kb + block) * 16);
+        s[u] = a.scales[(row0 + n0) * kb + block];
+      }
+      if (n0 + 8 * ch < N) x[u] = *reinterpret_cast<const uint4*>(dy + n0);
+    };
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) load(u, u);
+    for (int t0 = 0; t0 < trips; t0 += AHEAD) {
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        if (t0 + u >= trips) break;
+        char* w = tiles[group][u & 1];
+        const uint32_t d[4] = {c[u].x, c[u].y, c[u].z, c[u].w};
+        const float scale = mx4_scale(s[u]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)  // 16-byte chunk 4 (tid % 4) + i of the row, at c ^ 4 (row mod 4)
+          *reinterpret_cast<uint4*>(w + wr * (KT * 2) + (((4 * (tid & 3) + i) ^ (4 * (wr & 3))) * 16)) =
+              mx4_bf16_words(d[i], scale);
+        char* g = dys[group][u & 1];
+        if (sl < 16 * TB) *reinterpret_cast<uint4*>(g + sl * 128 + chunk_slot(sl, ch) * 16) = x[u];
+        load(u, t0 + u + AHEAD);
+        __syncthreads();
+        bf16x8 y[2][TB];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int b = 0; b < TB; ++b)
+            y[h][b] = *reinterpret_cast<const bf16x8*>(g + (16 * b + r) * 128 + chunk_slot(16 * b + r, 4 * h + q) * 16);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < C; ++i) {
+            // rows 32 h + 8 q + 4 p + (lane % 16) / 4, column 4 (lane % 4) of the block of sixteen
+            const int col = wave * (16 * C) + 16 * i + 4 * (lane & 3);
+            s16x4 v[2];
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+              const int n = 32 * h + 8 * q + 4 * p + (r >> 2);
+              v[p] = read_transposed(w + n * (KT * 2) + (((col >> 3) ^ (4 * (n & 3))) << 4) + (col & 7) * 2);
+            }
+            const bf16x8 wf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+            for (int b = 0; b < TB; ++b)
+              acc[i][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, y[h][b], acc[i][b], 0, 0, 0);
+          }
+      }
+    }
+  }
+  __syncthreads();
+  f32x4* join = reinterpret_cast<f32x4*>(&tiles[0][0][0]);  // [C * TB][256]
+  static_assert(C * TB * 256 * 16 <= sizeof(tiles));
+#pragma unroll
+  for (int b = 0; b < TB; ++b)
+#pragma unroll
+    for (int i = 0; i < C; ++i)
+      if (group == 1) join[(b * C + i) * 256 + tid] = acc[i][b];
+  __syncthreads();
+  if (group == 1) return;
+#pragma unroll
+  for (int b = 0; b < TB; ++b) {
+    const int64_t slot = t.lo + 16 * b + r;
+    if (slot >= t.hi) continue;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const int64_t k = k0 + wave * (16 * C) + 16 * i + 4 * q;
+      if (k < a.K) store4(a, slot, k, a.K, a.ldy % 4 == 0, acc[i][b] + join[(b * C + i) * 256 + tid]);
+    }
+  }
+}
+
 bitsmoe_status check(const char* who, const MulArgs& a, bitsmoe_dtype yt, int64_t wide) {
   const std::string w(who);
   if (a.E <= 0 || a.N <= 0 || a.K <= 0 || a.S < 0 || a.x_rows < 0)
@@ -1400,9 +1468,10 @@ extern "C" bitsmoe_status bitsmoe_mx4_product_grad(const uint8_t* codes_dev, con
     BITSMOE_LAUNCH_CHECK("mx4_grad_tile_kernel");
     return ok();
   }
-  if (!grid_of(a, 16, (K + 63) / 64, &grid))
+  const bool two = S > 8 * E;
+  if (!grid_of(a, two ? 32 : 16, (K + 127) / 128, &grid))
     return fail(BITSMOE_ERR_SHAPE, "mx4_product_grad: too many slots and columns for one call");
-  mx4_grad_kernel<<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
-  BITSMOE_LAUNCH_CHECK("mx4_grad_kernel");
+  (two ? mx4_grad_few_kernel<2> : mx4_grad_few_kernel<1>)<<<grid, kTileThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
+  BITSMOE_LAUNCH_CHECK("mx4_grad_few_kernel");
   return ok();
 }
