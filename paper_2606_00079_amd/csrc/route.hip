@@ -31,7 +31,7 @@ constexpr int kGradThreads = 256;
 constexpr int kMaxExperts = 4096;
 constexpr int kMaxRuns = 256;       // workgroups of the first launch, unless a run gets too long
 constexpr int kMinRun = 16;         // rows of the shortest run
-constexpr int kMaxRunSlots = 16384;  // slots of the longest (its list is held in LDS)
+constexpr int kMaxRun = 128;        // and of the longest
 
 // fp32 as an unsigned integer of the same order, and back; 0 is below -inf.
 __device__ __forceinline__ uint32_t order_bits(float f) {
@@ -179,55 +179,40 @@ __device__ __forceinline__ void exclusive_scan(int32_t* v, int n, int32_t* tmp) 
   __syncthreads();
 }
 
-// Threads that share out what is done for an expert: a power of two, for E
-// experts side by side.
+// Places the slots of a run of `rows` rows from row0 on, experts[i] being the
+// expert of its slot i: next[e] is where the run's first slot of expert e goes
+// (e = E: no expert).  A slot's place among its expert's is the number of rows
+// before it that have the expert too, by a bit a row in mask [E][words]; an
+// expert is in a row once.  Slots without an expert are a row's last ones: what
+// comes before them is all slots before less those with an expert, taken
+// [rows + 1] and tmp (a value a wave).
 template <int NT>
-__device__ __forceinline__ int shares_log2(int E) {
-  int parts = 0;
-  while (parts < 5 && (E << (parts + 1)) <= NT) ++parts;
-  return parts;
-}
-
-// Places the slots of a run of rows from row0 on: next[e] is where the run's
-// first slot of expert e goes (e = E: no expert), list[i] the expert of its slot
-// i (filled up with 0xFFFF to a multiple of eight).  A thread walks a share of
-// the list for one expert, once to count and once to place, so equal experts
-// keep their order.  part: [NT].
-template <int NT>
-__device__ __forceinline__ void place_slots(const RouteArgs& a, const int32_t* next, const uint16_t* list,
-                                            int64_t row0, int n, int32_t* part) {
-  const int log = shares_log2<NT>(a.E + 1), parts = 1 << log, wide = NT >> log;
-  const int col = threadIdx.x & (wide - 1), s = threadIdx.x >> (__builtin_ctz(NT) - log);
-  const int each = (((n + parts - 1) >> log) + 7) & ~7, lo = min(n, s * each), hi = min(n, lo + each);
+__device__ __forceinline__ void place_slots(const RouteArgs& a, const int32_t* next, const int32_t* experts,
+                                            int64_t row0, int rows, uint32_t* mask, int32_t* taken, int32_t* tmp) {
+  const int words = (rows + 31) / 32, n = rows * a.k, tid = threadIdx.x;
+  for (int i = tid; i < a.E * words; i += NT) mask[i] = 0;
+  for (int i = tid; i <= rows; i += NT) taken[i] = 0;
+  __syncthreads();
   const uint64_t inv = (uint64_t(1) << 32) / a.k + 1;  // i / k = i inv / 2^32 for i < 2^16, k <= 64
-  for (int e0 = 0; e0 <= a.E; e0 += wide) {
-    const int e = e0 + col;
-    int count = 0;
-    for (int i0 = lo; i0 < hi; i0 += 8) {
-      const uint4 v = *reinterpret_cast<const uint4*>(list + i0);
-      const uint32_t d[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) count += ((d[i] & 0xFFFF) == static_cast<uint32_t>(e)) + ((d[i] >> 16) == static_cast<uint32_t>(e));
+  for (int i = tid; i < n; i += NT) {
+    const int e = experts[i], r = static_cast<int>((static_cast<uint32_t>(i) * inv) >> 32);
+    if (e < 0) continue;
+    atomicOr(&mask[e * words + (r >> 5)], 1u << (r & 31));
+    atomicAdd(&taken[r], 1);
+  }
+  __syncthreads();
+  exclusive_scan<NT>(taken, rows + 1, tmp);
+  for (int i = tid; i < n; i += NT) {
+    const int e = experts[i], r = static_cast<int>((static_cast<uint32_t>(i) * inv) >> 32);
+    int pos;
+    if (e >= 0) {
+      pos = next[e] + __popc(mask[e * words + (r >> 5)] & ((1u << (r & 31)) - 1));
+      for (int w = 0; w < (r >> 5); ++w) pos += __popc(mask[e * words + w]);
+    } else {
+      pos = next[a.E] + i - taken[r + 1];
     }
-    part[threadIdx.x] = count;
-    __syncthreads();
-    if (e <= a.E && count > 0) {
-      int pos = next[e];
-      for (int u = 0; u < s; ++u) pos += part[u * wide + col];
-      for (int i0 = lo; i0 < hi; i0 += 8) {
-        const uint4 v = *reinterpret_cast<const uint4*>(list + i0);
-        const uint32_t d[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t f = (d[i / 2] >> (16 * (i & 1))) & 0xFFFF;
-          if (f == static_cast<uint32_t>(e)) {
-            a.rows[pos] = static_cast<int32_t>(row0) + static_cast<int>((static_cast<uint32_t>(i0 + i) * inv) >> 32);
-            a.slots[row0 * a.k + i0 + i] = pos++;
-          }
-        }
-      }
-    }
-    __syncthreads();
+    a.rows[pos] = static_cast<int32_t>(row0) + r;
+    a.slots[row0 * a.k + i] = pos;
   }
 }
 
@@ -251,8 +236,6 @@ __device__ __forceinline__ T block_sum(T v, void* lds) {
   return s;
 }
 
-__host__ __device__ inline int list_len(int n) { return (n + 7) & ~7; }
-
 // First launch: the rows of one run.
 template <bool BF16, int V, int LPT, int NT>
 __global__ __launch_bounds__(NT) void route_rows_kernel(RouteArgs a) {
@@ -262,15 +245,15 @@ __global__ __launch_bounds__(NT) void route_rows_kernel(RouteArgs a) {
   int32_t* cnt = reinterpret_cast<int32_t*>(probs + NT * V);  // [E + 1]
   float* chosen = reinterpret_cast<float*>(cnt + a.E + 1);        // [G][k]
   float* tmp = chosen + G * a.k;                                  // [kThreads]
-  uint16_t* list = reinterpret_cast<uint16_t*>(
-      (reinterpret_cast<uintptr_t>(tmp + NT) + 15) & ~uintptr_t(15));  // one run only
+  // one run only: the experts of its slots, and what place_slots takes
+  int32_t* list = reinterpret_cast<int32_t*>(tmp + NT / 64);  // [run][k]
+  int32_t* taken = list + a.run * a.k;                        // [run + 1]
+  uint32_t* mask = reinterpret_cast<uint32_t*>(taken + a.run + 1);  // [E] (of at most 32 rows)
   const int tid = threadIdx.x, lane = tid % LPT, grp = tid / LPT;
   const bool one = a.runs == 1;
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * a.run;
   const int nrows = static_cast<int>(min(static_cast<int64_t>(a.run), a.T - t0));
   for (int e = tid; e <= a.E; e += NT) cnt[e] = 0;
-  if (one)
-    for (int i = nrows * a.k + tid; i < list_len(nrows * a.k); i += NT) list[i] = 0xFFFF;
   __syncthreads();
   const int first = lane * V;
   float sum[V];
@@ -330,7 +313,7 @@ __global__ __launch_bounds__(NT) void route_rows_kernel(RouteArgs a) {
         chosen[grp * a.k + j] = best != 0 ? order_value(best) : -INFINITY;
         const int bucket = e < 0 ? a.E : e;
         atomicAdd(&cnt[bucket], 1);
-        if (one) list[r * a.k + j] = static_cast<uint16_t>(bucket);
+        if (one) list[r * a.k + j] = e;
       }
     }
     // their weights, a slot a lane (the row's lanes are of one wave, which wrote what is read here)
@@ -377,7 +360,7 @@ __global__ __launch_bounds__(NT) void route_rows_kernel(RouteArgs a) {
   __syncthreads();
   exclusive_scan<NT>(cnt, a.E + 1, reinterpret_cast<int32_t*>(tmp));
   for (int e = tid; e <= a.E; e += NT) a.offsets[e] = cnt[e];
-  place_slots<NT>(a, cnt, list, 0, nrows * a.k, reinterpret_cast<int32_t*>(tmp));
+  place_slots<NT>(a, cnt, list, 0, nrows, mask, taken, reinterpret_cast<int32_t*>(tmp));
 }
 
 // Second launch: 32 experts a workgroup, 32 threads an expert.  Every run's
@@ -432,16 +415,11 @@ __global__ __launch_bounds__(kThreads) void route_place_kernel(RouteArgs a) {
   extern __shared__ __align__(16) char smem[];
   int32_t* next = reinterpret_cast<int32_t*>(smem);  // [E + 1]
   int32_t* tmp = next + a.E + 1;                     // [kThreads / 64]
-  int32_t* part = tmp + kThreads / 64;               // [kThreads]
-  uint16_t* list = reinterpret_cast<uint16_t*>((reinterpret_cast<uintptr_t>(part + kThreads) + 15) & ~uintptr_t(15));
+  int32_t* taken = tmp + kThreads / 64;              // [run + 1]
+  uint32_t* mask = reinterpret_cast<uint32_t*>(taken + a.run + 1);  // [E][words]
   const int tid = threadIdx.x, b = blockIdx.x;
   const bool last = b == a.runs;
   const int64_t row0 = static_cast<int64_t>(b) * a.run;
-  const int n = last ? 0 : static_cast<int>(min(static_cast<int64_t>(a.run), a.T - row0)) * a.k;
-  for (int i = tid; i < list_len(n); i += kThreads) {
-    const int e = i < n ? a.experts[row0 * a.k + i] : 0xFFFF;
-    list[i] = static_cast<uint16_t>(e < 0 ? a.E : e);
-  }
   const int32_t* total = a.run_counts + static_cast<int64_t>(a.runs) * a.E;
   for (int e = tid; e < a.E; e += kThreads) next[e] = total[e];
   if (tid == 0) next[a.E] = 0;
@@ -467,16 +445,16 @@ __global__ __launch_bounds__(kThreads) void route_place_kernel(RouteArgs a) {
     return;
   }
   // the slots of the runs before: of every expert, and (what those leave) of none
-  int taken = 0;
+  int before = 0;
   for (int e = tid; e < a.E; e += kThreads) {
     const int c = a.run_counts[static_cast<int64_t>(b) * a.E + e];
     next[e] += c;
-    taken += c;
+    before += c;
   }
-  taken = block_sum<kThreads>(taken, tmp);
-  if (tid == 0) next[a.E] += static_cast<int32_t>(row0 * a.k - taken);
-  __syncthreads();
-  place_slots<kThreads>(a, next, list, row0, n, part);
+  before = block_sum<kThreads>(before, tmp);
+  if (tid == 0) next[a.E] += static_cast<int32_t>(row0 * a.k - before);
+  place_slots<kThreads>(a, next, a.experts + row0 * a.k, row0,
+                        static_cast<int>(min(static_cast<int64_t>(a.run), a.T - row0)), mask, taken, tmp);
 }
 
 // No rows at all.
@@ -510,16 +488,29 @@ __global__ __launch_bounds__(kGradThreads) void route_grad_kernel(GradArgs a) {
   for (int i = 0; i < V; ++i) share[i] = first + i < a.E ? gb * static_cast<float>(a.counts[first + i]) : 0.0f;
   for (int64_t t = static_cast<int64_t>(blockIdx.x) * G + grp; t < a.T;
        t += static_cast<int64_t>(gridDim.x) * G) {
+    // (all that a row needs is asked for at once)
+    float p[V], d[V];
+    load_logits<BF16, V>(static_cast<const char*>(a.logits) + t * a.ld * (BF16 ? 2 : 4), first, a.E, a.wide != 0, p);
     const float lse = a.lse[t];
-    float d[V];
+    // a slot a lane: its expert, and weight x gradient
+    int e0 = -1;
+    float w0 = 0.0f, dw0 = 0.0f, wd = 0.0f;
+    if (a.dweights) {
+      if (lane < a.k) {
+        e0 = a.experts[t * a.k + lane];
+        w0 = a.weights[t * a.k + lane];
+        dw0 = a.dweights[t * a.k + lane];
+        wd = e0 >= 0 ? w0 * dw0 : 0.0f;
+      }
+      for (int j = lane + LPT; j < a.k; j += LPT)  // (more slots than lanes)
+        if (a.experts[t * a.k + j] >= 0) wd += a.weights[t * a.k + j] * a.dweights[t * a.k + j];
+    }
     if (lse == -INFINITY) {  // a row that does not count
 #pragma unroll
       for (int i = 0; i < V; ++i) d[i] = 0.0f;
     } else {
       // p anew from the row: from lse alone a large lse would cost it its digits
-      float p[V], m = -INFINITY, total = 0.0f, s = 0.0f;
-      load_logits<BF16, V>(static_cast<const char*>(a.logits) + t * a.ld * (BF16 ? 2 : 4), first, a.E,
-                           a.wide != 0, p);
+      float m = -INFINITY, total = 0.0f, s = 0.0f;
 #pragma unroll
       for (int i = 0; i < V; ++i) m = fmaxf(m, p[i]);
       m = row_max<LPT>(m);
@@ -535,23 +526,26 @@ __global__ __launch_bounds__(kGradThreads) void route_grad_kernel(GradArgs a) {
         s += p[i] * share[i];
       }
       s = row_sum<LPT>(s);
-      // the gates: sum of weight x gradient, then each slot's own term
-      float wd = 0.0f;
-      if (a.dweights)
-        for (int j = lane; j < a.k; j += LPT)
-          if (a.experts[t * a.k + j] >= 0) wd += a.weights[t * a.k + j] * a.dweights[t * a.k + j];
       wd = row_sum<LPT>(wd);
       const float all = gz * lse - s - (a.renorm ? 0.0f : wd);
 #pragma unroll
       for (int i = 0; i < V; ++i) d[i] = p[i] * (share[i] + all);
       if (a.dweights) {
         const float mean = a.renorm ? wd : 0.0f;
+        const float g0 = w0 * (dw0 - mean);
         for (int j = 0; j < a.k; ++j) {
-          const int e = a.experts[t * a.k + j];
-          if (e < 0) continue;
-          const float g = a.weights[t * a.k + j] * (a.dweights[t * a.k + j] - mean);
+          int e;
+          float g;
+          if (j < LPT) {
+            e = __shfl(e0, j, LPT);
+            g = __shfl(g0, j, LPT);
+          } else {
+            e = a.experts[t * a.k + j];
+            g = a.weights[t * a.k + j] * (a.dweights[t * a.k + j] - mean);
+          }
+          e -= first;
 #pragma unroll
-          for (int i = 0; i < V; ++i) d[i] += e == first + i ? g : 0.0f;
+          for (int i = 0; i < V; ++i) d[i] += e == i ? g : 0.0f;  // (e < 0: none)
         }
       }
     }
@@ -666,7 +660,7 @@ extern "C" bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt
   a.losses = losses_dev;
   int64_t run = (T + kMaxRuns - 1) / kMaxRuns;
   if (run < kMinRun) run = kMinRun;
-  if (run > kMaxRunSlots / k) run = kMaxRunSlots / k;
+  if (run > kMaxRun) run = kMaxRun;
   const int64_t runs = (T + run - 1) / run;
   a.run = static_cast<int>(run);
   a.runs = static_cast<int>(runs);
@@ -685,8 +679,8 @@ extern "C" bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt
     constexpr int V = decltype(v)::value, LPT = decltype(l)::value;
     constexpr int MANY = V == 8 ? kThreads : 256;
     const int nt = runs == 1 ? 256 : MANY;  // few rows: a workgroup that is launched sooner
-    const size_t lds = size_t(nt) * V * 4 + (E + 1) * 4 + size_t(nt / LPT) * k * 4 + nt * 4 + 16 +
-                       (runs == 1 ? size_t(list_len(static_cast<int>(run * k))) * 2 : 0);
+    const size_t lds = size_t(nt) * V * 4 + (E + 1) * 4 + size_t(nt / LPT) * k * 4 + nt / 64 * 4 +
+                       (runs == 1 ? size_t(run * k + run + 1 + E) * 4 : 0);
     auto* fn = lt == BITSMOE_BF16
                    ? (runs == 1 ? route_rows_kernel<true, V, LPT, 256> : route_rows_kernel<true, V, LPT, MANY>)
                    : (runs == 1 ? route_rows_kernel<false, V, LPT, 256> : route_rows_kernel<false, V, LPT, MANY>);
@@ -705,8 +699,7 @@ extern "C" bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt
   if (runs > 1) {
     route_sum_kernel<<<static_cast<unsigned>((E + 31) / 32), 1024, 0, s>>>(a);
     BITSMOE_LAUNCH_CHECK("route_sum_kernel");
-    const size_t lds = size_t(E + 1) * 4 + kThreads / 64 * 4 + kThreads * 4 + 16 +
-                       size_t(list_len(static_cast<int>(run * k))) * 2;
+    const size_t lds = size_t(E + 1 + kThreads / 64 + run + 1 + E * ((run + 31) / 32)) * 4;
     if (lds > 65536) {
       const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(route_place_kernel),
                                                hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
