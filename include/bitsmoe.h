@@ -590,7 +590,7 @@ bitsmoe_status bitsmoe_unpack(const uint64_t* codes_dev, const uint16_t* params_
  *   logits_dev   [T] rows of E entries of type lt, ld entries apart
  * Sums are fp32 in a fixed order.  T may be 0 (counts, offsets and losses are
  * zero).  Shape rules: 1 <= k <= min(E, BITSMOE_ROUTE_MAX_K), E <= 4096,
- * ld >= E, T k < 2^31.  Uses the library's scratch when T > 16.
+ * ld >= E, T k < 2^31.  Uses the library's scratch when T > 128 (16 where E > 512).
  */
 bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt, int64_t T, int64_t E,
                              int64_t ld, int64_t k, const uint8_t* valid_dev, int renorm,

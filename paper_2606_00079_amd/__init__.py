@@ -556,6 +556,15 @@ def _place(t, name: str):
     return torch, torch._C._cuda_getCurrentRawStream(dev)
 
 
+def _code(t, name: str, torch):
+    dt = t.dtype
+    if dt is torch.bfloat16:
+        return BF16
+    if dt is torch.float32:
+        return F32
+    raise TypeError(f"{name} must be bfloat16 or float32")
+
+
 def _in(t, name: str, like, dtype, shape=None):
     """Address of a contiguous tensor (None: none) on the device of `like`."""
     if t is None:
@@ -583,7 +592,7 @@ def _rows(t, name: str):
 def _out(out, shape, dtype, like, torch):
     """The output tensor, new or given."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
     _in(out, "out", like, dtype, shape)
     return out
 
@@ -616,12 +625,12 @@ def route(logits, k: int, valid=None, renorm: bool = True) -> Routing:
     n, w = max(T * k, 0), max(k, 0)
     # one allocation for the whole numbers and one for the others, their parts 16 bytes aligned
     n4, e4, t4 = (n + 3) // 4 * 4, (E + 4) // 4 * 4, (T + 3) // 4 * 4
-    ints = torch.empty((3 * n4 + 2 * e4,), dtype=torch.int32, device=logits.device)
-    floats = torch.empty((n4 + t4 + 4,), dtype=torch.float32, device=logits.device)
+    ints = logits.new_empty((3 * n4 + 2 * e4,), dtype=torch.int32)
+    floats = logits.new_empty((n4 + t4 + 4,), dtype=torch.float32)
     ip, fp = ints.data_ptr(), floats.data_ptr()
     ex, co, of, ro, sl = ip, ip + 12 * n4, ip + 12 * n4 + 4 * e4, ip + 4 * n4, ip + 8 * n4
     we, ls, lo = fp, fp + 4 * n4, fp + 4 * (n4 + t4)
-    _check(lib().bitsmoe_route(lp, _dtype_code(logits, "logits"), T, E, ld, k, vp, int(renorm), ex, we,
+    _check(lib().bitsmoe_route(lp, _code(logits, "logits", torch), T, E, ld, k, vp, int(renorm), ex, we,
                                co, of, ro, sl, ls, lo, stream), "route")
     return Routing(ints.as_strided((T, w), (w, 1), 0), floats.as_strided((T, w), (w, 1), 0),
                    ints.as_strided((E + 1,), (1,), 3 * n4), ints.as_strided((E + 1,), (1,), 3 * n4 + e4),
@@ -641,7 +650,7 @@ def route_grad(logits, routing: Routing, dweights=None, dlosses=None, renorm: bo
     lp, ld = _rows(logits, "logits")
     i32, f32 = torch.int32, torch.float32
     _check(lib().bitsmoe_route_grad(
-        lp, _dtype_code(logits, "logits"), T, E, ld, k, int(renorm),
+        lp, _code(logits, "logits", torch), T, E, ld, k, int(renorm),
         _in(routing.experts, "experts", logits, i32, (T, k)),
         _in(routing.weights, "weights", logits, f32, (T, k)),
         _in(routing.counts, "counts", logits, i32, (E + 1,)),
@@ -659,9 +668,9 @@ def mx4_quantize(X):
     if cols % 32 != 0 or cols == 0:
         raise ValueError("cols must be a multiple of 32")
     xp, ld = _rows(X, "X")
-    codes = torch.empty((*lead, cols // 2), dtype=torch.uint8, device=X.device)
-    scales = torch.empty((*lead, cols // 32), dtype=torch.uint8, device=X.device)
-    _check(lib().bitsmoe_mx4_quantize(xp, _dtype_code(X, "X"), X.numel() // cols, cols, ld,
+    codes = X.new_empty((*lead, cols // 2), dtype=torch.uint8)
+    scales = X.new_empty((*lead, cols // 32), dtype=torch.uint8)
+    _check(lib().bitsmoe_mx4_quantize(xp, _code(X, "X", torch), X.numel() // cols, cols, ld,
                                       codes.data_ptr(), scales.data_ptr(), stream), "mx4_quantize")
     return codes, scales
 
@@ -682,7 +691,7 @@ def mx4_dequantize(codes, scales, dtype=None, out=None):
     cols = 2 * codes.shape[-1]
     out = _out(out, (*codes.shape[:-1], cols), dtype or torch.bfloat16, codes, torch)
     _check(lib().bitsmoe_mx4_dequantize(cp, sp, codes.numel() * 2 // max(cols, 1), cols, out.data_ptr(),
-                                        _dtype_code(out, "out"), stream), "mx4_dequantize")
+                                        _code(out, "out", torch), stream), "mx4_dequantize")
     return out
 
 
@@ -711,9 +720,9 @@ def mx4_product(codes, scales, X, offsets=None, rows=None, glu: bool = False, dt
         raise ValueError("X and W disagree on K")
     xp, ldx = _rows(X, "X")
     out = _out(out, (S, N), dtype or torch.bfloat16, X, torch)
-    _check(lib().bitsmoe_mx4_product(cp, sp, E, N, K, xp, _dtype_code(X, "X"), X.shape[0], ldx, op,
+    _check(lib().bitsmoe_mx4_product(cp, sp, E, N, K, xp, _code(X, "X", torch), X.shape[0], ldx, op,
                                      _in(rows, "rows", X, torch.int32, (S,)), S, int(glu),
-                                     out.data_ptr(), _dtype_code(out, "out"), N, stream),
+                                     out.data_ptr(), _code(out, "out", torch), N, stream),
            "mx4_product")
     return out
 
@@ -730,7 +739,7 @@ def mx4_product_q(codes, scales, xcodes, xscales, offsets=None, rows=None, glu: 
     out = _out(out, (S, N), dtype or torch.bfloat16, xcodes, torch)
     _check(lib().bitsmoe_mx4_product_q(cp, sp, E, N, K, xcp, xsp, xcodes.shape[0], op,
                                        _in(rows, "rows", xcodes, torch.int32, (S,)), S, int(glu),
-                                       out.data_ptr(), _dtype_code(out, "out"), N, stream),
+                                       out.data_ptr(), _code(out, "out", torch), N, stream),
            "mx4_product_q")
     return out
 
@@ -747,8 +756,8 @@ def mx4_product_grad(codes, scales, dY, offsets=None, dtype=None, out=None):
         raise ValueError("dY and W disagree on N")
     yp, ldy = _rows(dY, "dY")
     out = _out(out, (S, K), dtype or torch.bfloat16, dY, torch)
-    _check(lib().bitsmoe_mx4_product_grad(cp, sp, E, N, K, yp, _dtype_code(dY, "dY"), ldy, op, S,
-                                          out.data_ptr(), _dtype_code(out, "out"), K, stream),
+    _check(lib().bitsmoe_mx4_product_grad(cp, sp, E, N, K, yp, _code(dY, "dY", torch), ldy, op, S,
+                                          out.data_ptr(), _code(out, "out", torch), K, stream),
            "mx4_product_grad")
     return out
 
@@ -761,7 +770,7 @@ def combine(Z, slots, weights=None, out=None):
         raise ValueError("Z must be [S][d] and slots [T][k]")
     (S, d), (T, k) = Z.shape, slots.shape
     out = _out(out, (T, d), Z.dtype, Z, torch)
-    _check(lib().bitsmoe_combine(_in(Z, "Z", Z, Z.dtype), _dtype_code(Z, "Z"), S,
+    _check(lib().bitsmoe_combine(_in(Z, "Z", Z, Z.dtype), _code(Z, "Z", torch), S,
                                  _in(slots, "slots", Z, torch.int32),
                                  _in(weights, "weights", Z, torch.float32, (T, k)), T, k, d,
                                  out.data_ptr(), stream), "combine")
@@ -776,9 +785,9 @@ def combine_grad(Z, slots, weights, dY):
         raise ValueError("Z must be [S][d] and slots [T][k]")
     (S, d), (T, k) = Z.shape, slots.shape
     zp = _in(Z, "Z", Z, Z.dtype)
-    dZ = torch.empty((S, d), dtype=Z.dtype, device=Z.device)
-    dw = torch.empty((T, k), dtype=torch.float32, device=Z.device)
-    _check(lib().bitsmoe_combine_grad(zp, _dtype_code(Z, "Z"), S, _in(slots, "slots", Z, torch.int32),
+    dZ = Z.new_empty((S, d), dtype=Z.dtype)
+    dw = Z.new_empty((T, k), dtype=torch.float32)
+    _check(lib().bitsmoe_combine_grad(zp, _code(Z, "Z", torch), S, _in(slots, "slots", Z, torch.int32),
                                       _in(weights, "weights", Z, torch.float32, (T, k)),
                                       _in(dY, "dY", Z, Z.dtype, (T, d)), T, k, d, dZ.data_ptr(),
                                       dw.data_ptr(), stream), "combine_grad")

@@ -58,6 +58,18 @@ int device_cus() {
   return n;
 }
 
+bitsmoe_status allow_lds(const void* fn, int bytes, std::atomic<uint64_t>* done) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return device_error("hipGetDevice", e);
+  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
+  if (done->load(std::memory_order_relaxed) & bit) return BITSMOE_OK;
+  e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e != hipSuccess) return device_error("hipFuncSetAttribute (shared memory)", e);
+  done->fetch_or(bit, std::memory_order_relaxed);
+  return BITSMOE_OK;
+}
+
 // ----------------------------------------------------------------------------
 // scratch
 // ----------------------------------------------------------------------------

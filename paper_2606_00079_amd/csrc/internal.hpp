@@ -1,6 +1,7 @@
 // Host-side helpers shared by the translation units of libbitsmoe.
 #pragma once
 
+#include <atomic>
 #include <cstddef>
 #include <cstdint>
 #include <initializer_list>
@@ -37,6 +38,10 @@ bitsmoe_status device_error(const char* what, int hip_err);
 // Compute units of the current device (cached per device; 256 if the query
 // fails).
 int device_cus();
+
+// Lets kernel `fn` use `bytes` of shared memory beyond the default limit, once
+// a device (*done: a bit a device below 64, for this kernel and size or less).
+bitsmoe_status allow_lds(const void* fn, int bytes, std::atomic<uint64_t>* done);
 
 // Records HIP events around a kernel launch when timing is enabled
 // (bitsmoe_timing); construct right before the launch, destroy right after.

@@ -5,8 +5,10 @@
 //     dx_s = W_e(s)^T dy_s             (mx4_product_grad)
 //
 // for S slots in expert order, expert e's being offsets[e] .. offsets[e+1].
+#include <atomic>
 #include <cstdint>
 #include <string>
+#include <type_traits>
 
 #include "internal.hpp"
 #include "mx4.hpp"
@@ -1328,20 +1330,20 @@ __global__ __launch_bounds__(kTileThreads) void mx4_grad_few_kernel(MulArgs a) {
 }
 
 bitsmoe_status check(const char* who, const MulArgs& a, bitsmoe_dtype yt, int64_t wide) {
-  const std::string w(who);
+  auto bad = [who](bitsmoe_status st, const char* what) { return fail(st, std::string(who) + what); };
   if (a.E <= 0 || a.N <= 0 || a.K <= 0 || a.S < 0 || a.x_rows < 0)
-    return fail(BITSMOE_ERR_ARG, w + ": non-positive size");
-  if (yt != BITSMOE_F32 && yt != BITSMOE_BF16) return fail(BITSMOE_ERR_DTYPE, w + ": results are fp32 or bf16");
+    return bad(BITSMOE_ERR_ARG, ": non-positive size");
+  if (yt != BITSMOE_F32 && yt != BITSMOE_BF16) return bad(BITSMOE_ERR_DTYPE, ": results are fp32 or bf16");
   if (a.K % kMx4Block != 0 || a.K > (1 << 24) || a.N > (1 << 24) || a.E > 65535 || a.S > 0x7FFFFFF0 ||
       a.x_rows > 0x7FFFFFFF)
-    return fail(BITSMOE_ERR_SHAPE, w + ": needs K % 32 == 0, K and N <= 2^24, E <= 65535, S and rows < 2^31");
+    return bad(BITSMOE_ERR_SHAPE, ": needs K % 32 == 0, K and N <= 2^24, E <= 65535, S and rows < 2^31");
   if (a.ldy < wide || a.ldy > (int64_t(1) << 32))
-    return fail(BITSMOE_ERR_SHAPE, w + ": the results' row stride is too small or too large");
-  if (!a.offsets && a.E != 1) return fail(BITSMOE_ERR_ARG, w + ": no offsets, and more than one expert");
-  if (a.S > 0 && (!a.codes || !a.scales || !a.y)) return fail(BITSMOE_ERR_ARG, w + ": null pointer");
-  if (!a.rows && a.x_rows < a.S) return fail(BITSMOE_ERR_SHAPE, w + ": fewer rows than slots");
+    return bad(BITSMOE_ERR_SHAPE, ": the results' row stride is too small or too large");
+  if (!a.offsets && a.E != 1) return bad(BITSMOE_ERR_ARG, ": no offsets, and more than one expert");
+  if (a.S > 0 && (!a.codes || !a.scales || !a.y)) return bad(BITSMOE_ERR_ARG, ": null pointer");
+  if (!a.rows && a.x_rows < a.S) return bad(BITSMOE_ERR_SHAPE, ": fewer rows than slots");
   if (!aligned16({a.codes, a.scales, a.x, a.xcodes, a.xscales, a.offsets, a.rows, a.y}))
-    return fail(BITSMOE_ERR_ARG, w + ": device pointers must be 16-byte aligned");
+    return bad(BITSMOE_ERR_ARG, ": device pointers must be 16-byte aligned");
   return BITSMOE_OK;
 }
 
@@ -1368,9 +1370,8 @@ template <bool MX, bool AL, bool GLU>
 bitsmoe_status tile_product(const MulArgs& a, hipStream_t s) {
   constexpr int lds = Shape<MX, AL>::kBytes;
   auto* fn = mx4_tile_kernel<MX, AL, GLU>;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn),
-                                           hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  if (e != hipSuccess) return device_error("mx4_product: shared memory", e);
+  static std::atomic<uint64_t> allowed{0};
+  if (bitsmoe_status st = allow_lds(reinterpret_cast<const void*>(fn), lds, &allowed)) return st;
   fn<<<tile_grid(), kTileThreads, lds, s>>>(a);
   BITSMOE_LAUNCH_CHECK("mx4_tile_kernel");
   return ok();
@@ -1461,9 +1462,9 @@ extern "C" bitsmoe_status bitsmoe_mx4_product_grad(const uint8_t* codes_dev, con
   if (!dY_dev) return fail(BITSMOE_ERR_ARG, "mx4_product_grad: null pointer");
   unsigned grid;
   if (S >= kTileSlots * E) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(mx4_grad_tile_kernel),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, GradShape::kBytes);
-    if (e != hipSuccess) return device_error("mx4_product_grad: shared memory", e);
+    static std::atomic<uint64_t> allowed{0};
+    if (bitsmoe_status st = allow_lds(reinterpret_cast<const void*>(mx4_grad_tile_kernel), GradShape::kBytes, &allowed))
+      return st;
     mx4_grad_tile_kernel<<<tile_grid(), kTileThreads, GradShape::kBytes, static_cast<hipStream_t>(stream)>>>(a);
     BITSMOE_LAUNCH_CHECK("mx4_grad_tile_kernel");
     return ok();

@@ -17,8 +17,10 @@
 // up over the runs (integers, and fp32 in the order of the runs: results do not
 // depend on timing), and a third places the slots.  A single run does it all in
 // one launch.
+#include <atomic>
 #include <cstdint>
 #include <string>
+#include <type_traits>
 
 #include "common.hpp"
 #include "internal.hpp"
@@ -32,6 +34,8 @@ constexpr int kMaxExperts = 4096;
 constexpr int kMaxRuns = 256;       // workgroups of the first launch, unless a run gets too long
 constexpr int kMinRun = 16;         // rows of the shortest run
 constexpr int kMaxRun = 128;        // and of the longest
+constexpr int kOneRun = 128;        // rows that one workgroup does alone, up to 512 experts
+constexpr int kMostLds = 163840;
 
 // fp32 as an unsigned integer of the same order, and back; 0 is below -inf.
 __device__ __forceinline__ uint32_t order_bits(float f) {
@@ -248,7 +252,7 @@ __global__ __launch_bounds__(NT) void route_rows_kernel(RouteArgs a) {
   // one run only: the experts of its slots, and what place_slots takes
   int32_t* list = reinterpret_cast<int32_t*>(tmp + NT / 64);  // [run][k]
   int32_t* taken = list + a.run * a.k;                        // [run + 1]
-  uint32_t* mask = reinterpret_cast<uint32_t*>(taken + a.run + 1);  // [E] (of at most 32 rows)
+  uint32_t* mask = reinterpret_cast<uint32_t*>(taken + a.run + 1);  // [E][words]
   const int tid = threadIdx.x, lane = tid % LPT, grp = tid / LPT;
   const bool one = a.runs == 1;
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * a.run;
@@ -661,6 +665,8 @@ extern "C" bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt
   int64_t run = (T + kMaxRuns - 1) / kMaxRuns;
   if (run < kMinRun) run = kMinRun;
   if (run > kMaxRun) run = kMaxRun;
+  // (three launches take longer than one workgroup's few rounds)
+  if (T <= kOneRun && E <= 512) run = T;
   const int64_t runs = (T + run - 1) / run;
   a.run = static_cast<int>(run);
   a.runs = static_cast<int>(runs);
@@ -678,19 +684,17 @@ extern "C" bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt
   with_layout(E, [&](auto v, auto l) {
     constexpr int V = decltype(v)::value, LPT = decltype(l)::value;
     constexpr int MANY = V == 8 ? kThreads : 256;
-    const int nt = runs == 1 ? 256 : MANY;  // few rows: a workgroup that is launched sooner
+    const bool small = T <= kMinRun;  // (a workgroup that is launched sooner)
+    const int nt = small ? 256 : MANY;
     const size_t lds = size_t(nt) * V * 4 + (E + 1) * 4 + size_t(nt / LPT) * k * 4 + nt / 64 * 4 +
-                       (runs == 1 ? size_t(run * k + run + 1 + E) * 4 : 0);
+                       (runs == 1 ? size_t(run * k + run + 1 + E * ((run + 31) / 32)) * 4 : 0);
     auto* fn = lt == BITSMOE_BF16
-                   ? (runs == 1 ? route_rows_kernel<true, V, LPT, 256> : route_rows_kernel<true, V, LPT, MANY>)
-                   : (runs == 1 ? route_rows_kernel<false, V, LPT, 256> : route_rows_kernel<false, V, LPT, MANY>);
+                   ? (small ? route_rows_kernel<true, V, LPT, 256> : route_rows_kernel<true, V, LPT, MANY>)
+                   : (small ? route_rows_kernel<false, V, LPT, 256> : route_rows_kernel<false, V, LPT, MANY>);
     if (lds > 65536) {
-      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn),
-                                               hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
-      if (e != hipSuccess) {
-        st = device_error("route: shared memory", e);
-        return;
-      }
+      static std::atomic<uint64_t> allowed[4];
+      st = allow_lds(reinterpret_cast<const void*>(fn), kMostLds, &allowed[2 * (lt == BITSMOE_BF16) + small]);
+      if (st) return;
     }
     fn<<<static_cast<unsigned>(runs), nt, lds, s>>>(a);
   });
@@ -701,9 +705,9 @@ extern "C" bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt
     BITSMOE_LAUNCH_CHECK("route_sum_kernel");
     const size_t lds = size_t(E + 1 + kThreads / 64 + run + 1 + E * ((run + 31) / 32)) * 4;
     if (lds > 65536) {
-      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(route_place_kernel),
-                                               hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
-      if (e != hipSuccess) return device_error("route: shared memory", e);
+      static std::atomic<uint64_t> allowed{0};
+      st = allow_lds(reinterpret_cast<const void*>(route_place_kernel), kMostLds, &allowed);
+      if (st) return st;
     }
     route_place_kernel<<<static_cast<unsigned>(runs + 1), kThreads, lds, s>>>(a);
     BITSMOE_LAUNCH_CHECK("route_place_kernel");
