@@ -6,6 +6,7 @@
 //
 // for S slots in expert order, expert e's being offsets[e] .. offsets[e+1].
 #include <atomic>
+#include <cmath>
 #include <cstdint>
 #include <string>
 #include <type_traits>
@@ -1350,15 +1351,58 @@ bitsmoe_status check(const char* who, const MulArgs& a, bitsmoe_dtype yt, int64_
 // Workgroups for tiles of `tile` slots and `per` workgroups each.
 bool grid_of(const MulArgs& a, int64_t tile, int64_t per, unsigned* grid) {
   const int64_t tiles = a.S / tile + (a.E + 1 < a.S ? a.E + 1 : a.S);
-  if (tiles > ((int64_t(1) << 24) - 1) / per) return false;
+  if (tiles > ((int64_t(1) << 23) - 1) / per) return false;  // (2^32 threads of 512 a workgroup)
   *grid = static_cast<unsigned>(tiles * per);
   return true;
 }
 
-// Large tiles pay from about this many slots an expert on.
-constexpr int64_t kTileSlots = 32;
-// Below, whole rows of K a wave pay from about this many workgroups on (two a compute unit).
-constexpr int64_t kFewGroups = 512;
+// Which kernel takes a call.  The counts of an expert's slots are on the device;
+// the host goes by S and E alone: about
+//     tiles(m) = max(active, S / m + active / 2),  active = E (1 - exp(-S / E))
+// tiles of m slots (as of slots that choose by chance), whose workgroups either run side by side (the length of one's
+// chain of steps counts) or fill the card (their number does).  The constants (us;
+// L entries of the sum) fit timings of all kernels at thirty shapes, E 1 .. 256,
+// 1/8 .. 4096 slots an expert, outputs 256 .. 14336, sums of 512 .. 14336 entries:
+// the choice is within a quarter of the best of them (3 % on average), and the worst of
+// them is two to ten times that (one expert, 64 slots, 1024 x 4096: 50 us in large tiles, 49 in
+// few-slot ones, 9 by rows; 4096 slots, 4096 x 4096: 150, 333, 1340).
+enum Kernel { kByRows, kFewSlots, kLargeTiles };
+
+double tiles_of(const MulArgs& a, int64_t m) {
+  const double E = static_cast<double>(a.E), active = E * (1.0 - std::exp(-static_cast<double>(a.S) / E));
+  const double t = static_cast<double>(a.S) / static_cast<double>(m) + active / 2;
+  return t > active ? t : active;
+}
+// Slots of a tile of the kernels for few.
+int64_t few_slots(const MulArgs& a) { return a.S > 8 * static_cast<int64_t>(a.E) ? 32 : 16; }
+
+// us of `groups` workgroups whose chain takes `chain`, and `each` where they fill the card.
+double side_by_side(double groups, double chain, double each) {
+  const double full = groups * each;
+  return chain > full ? chain : full;
+}
+// us of large tiles, a workgroup a compute unit
+double in_rounds(double tiles, double each) {
+  const int64_t rounds = (static_cast<int64_t>(tiles) + device_cus() - 1) / device_cus();
+  return 3.0 + static_cast<double>(rounds < 1 ? 1 : rounds) * each;
+}
+
+Kernel product_kernel(const MulArgs& a, bool mx, bool glu) {
+  const double wide = static_cast<double>(a.N) * (glu ? 2 : 1), L = static_cast<double>(a.K);
+  const double c16 = (wide + 15) / 16, c256 = (wide + 255) / 256;
+  const double rows = 6.0 + tiles_of(a, 16) * c16 * L * (mx ? 3.6e-6 : 5.2e-6);
+  const double few = 3.0 + L * side_by_side(tiles_of(a, few_slots(a)) * c256, mx ? 0.009 : 0.0115, mx ? 4e-5 : 5e-5);
+  const double large = in_rounds(tiles_of(a, kTM) * c256, L * (mx ? 0.0058 : 0.0117) + (mx ? 4.0 : 5.0));
+  if (a.x_rows > 0 && large <= rows && large <= few) return kLargeTiles;
+  return few <= rows ? kFewSlots : kByRows;
+}
+
+Kernel grad_kernel(const MulArgs& a) {
+  const double L = static_cast<double>(a.N), K = static_cast<double>(a.K);
+  const double few = 4.0 + L * side_by_side(tiles_of(a, few_slots(a)) * ((K + 127) / 128), 0.0055, 2.4e-5);
+  const double large = in_rounds(tiles_of(a, kTM) * ((K + 255) / 256), L * 0.0165 + 4.0);
+  return large <= few ? kLargeTiles : kFewSlots;
+}
 
 // One workgroup a compute unit, as many on every XCD.
 unsigned tile_grid() {
@@ -1379,7 +1423,9 @@ bitsmoe_status tile_product(const MulArgs& a, hipStream_t s) {
 
 bitsmoe_status product(const char* who, const MulArgs& a, bool glu, hipStream_t s) {
   const bool mx = a.xcodes != nullptr;
-  if (a.S >= kTileSlots * a.E && a.x_rows > 0) {
+  const Kernel kernel = product_kernel(a, mx, glu);
+  unsigned grid = 0;
+  if (kernel == kLargeTiles) {
     // (with MX4 tokens four stages of weights a tile at least, so that a chunk of scales outlives its two)
     const bool al = a.K % 512 == 0 && (!mx || a.K >= 1024);
     if (mx && al) return glu ? tile_product<true, true, true>(a, s) : tile_product<true, true, false>(a, s);
@@ -1387,11 +1433,9 @@ bitsmoe_status product(const char* who, const MulArgs& a, bool glu, hipStream_t 
     if (al) return glu ? tile_product<false, true, true>(a, s) : tile_product<false, true, false>(a, s);
     return glu ? tile_product<false, false, true>(a, s) : tile_product<false, false, false>(a, s);
   }
-  unsigned grid;
-  const int64_t cols = (a.N + (glu ? 127 : 255)) / (glu ? 128 : 256);
-  if ((a.S < a.E ? a.S : a.E) * cols >= kFewGroups) {
-    const bool two = a.S > 8 * a.E;
-    if (!grid_of(a, two ? 32 : 16, cols, &grid))
+  if (kernel == kFewSlots) {
+    const bool two = few_slots(a) == 32;
+    if (!grid_of(a, few_slots(a), (a.N + (glu ? 127 : 255)) / (glu ? 128 : 256), &grid))
       return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": too many slots and outputs for one call");
     auto* fn = two ? (mx ? (glu ? mx4_few_kernel<true, true, 2> : mx4_few_kernel<true, false, 2>)
                          : (glu ? mx4_few_kernel<false, true, 2> : mx4_few_kernel<false, false, 2>))
@@ -1460,8 +1504,7 @@ extern "C" bitsmoe_status bitsmoe_mx4_product_grad(const uint8_t* codes_dev, con
     return fail(BITSMOE_ERR_SHAPE, "mx4_product_grad: needs N % 8 == 0, lddy >= N and lddy % 8 == 0");
   if (S == 0) return ok();
   if (!dY_dev) return fail(BITSMOE_ERR_ARG, "mx4_product_grad: null pointer");
-  unsigned grid;
-  if (S >= kTileSlots * E) {
+  if (grad_kernel(a) == kLargeTiles) {
     static std::atomic<uint64_t> allowed{0};
     if (bitsmoe_status st = allow_lds(reinterpret_cast<const void*>(mx4_grad_tile_kernel), GradShape::kBytes, &allowed))
       return st;
@@ -1469,10 +1512,11 @@ extern "C" bitsmoe_status bitsmoe_mx4_product_grad(const uint8_t* codes_dev, con
     BITSMOE_LAUNCH_CHECK("mx4_grad_tile_kernel");
     return ok();
   }
-  const bool two = S > 8 * E;
-  if (!grid_of(a, two ? 32 : 16, (K + 127) / 128, &grid))
+  unsigned grid;
+  if (!grid_of(a, few_slots(a), (K + 127) / 128, &grid))
     return fail(BITSMOE_ERR_SHAPE, "mx4_product_grad: too many slots and columns for one call");
-  (two ? mx4_grad_few_kernel<2> : mx4_grad_few_kernel<1>)<<<grid, kTileThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
+  auto* fn = few_slots(a) == 32 ? mx4_grad_few_kernel<2> : mx4_grad_few_kernel<1>;
+  fn<<<grid, kTileThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
   BITSMOE_LAUNCH_CHECK("mx4_grad_few_kernel");
   return ok();
 }
