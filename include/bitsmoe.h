@@ -590,7 +590,8 @@ bitsmoe_status bitsmoe_unpack(const uint64_t* codes_dev, const uint16_t* params_
  *   logits_dev   [T] rows of E entries of type lt, ld entries apart
  * Sums are fp32 in a fixed order.  T may be 0 (counts, offsets and losses are
  * zero).  Shape rules: 1 <= k <= min(E, BITSMOE_ROUTE_MAX_K), E <= 4096,
- * ld >= E, T k < 2^31.  Uses the library's scratch when T > 128 (16 where E > 512).
+ * ld >= E, T k < 2^31.  Uses the library's scratch when T > 128 (16 where E >
+ * 512), which a first call of such a size allocates (so not under graph capture).
  */
 bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt, int64_t T, int64_t E,
                              int64_t ld, int64_t k, const uint8_t* valid_dev, int renorm,
@@ -651,7 +652,8 @@ bitsmoe_status bitsmoe_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* s
  *   rows_dev     [S] int32, or NULL: slot s reads row s
  *   Y_dev        [S] rows of N entries of type yt, ldy entries apart
  * S may be 0.  Shape rules: K % 32 == 0, ldx >= K, ldx % 8 == 0, ldy >= N,
- * E <= 65535, N and K <= 2^24, S < 2^31.
+ * E <= 65535, N and K <= 2^24, S < 2^31; where S / E is small, (S / 16 + E) times
+ * the sixteens of N below 2^23.
  */
 bitsmoe_status bitsmoe_mx4_product(const uint8_t* codes_dev, const uint8_t* scales_dev, int64_t E,
                                    int64_t N, int64_t K, const void* X_dev, bitsmoe_dtype xt,
@@ -719,7 +721,9 @@ bitsmoe_status bitsmoe_set_lapack(const char* path);
 /* Kernel timing for measurement.  While enabled, every device call records a
  * pair of HIP events on its stream around each of its main kernels, under
  * the names "gram", "gram_experts", "project", "score_dgen", "score_gemm",
- * "pack".  bitsmoe_kernel_time waits for the recorded events of `name`,
+ * "pack", and for the experts' products in MX4, by the kernel that took the
+ * call, "mx4_rows", "mx4_few", "mx4_tile", "mx4_grad_few" and "mx4_grad_tile".
+ * bitsmoe_kernel_time waits for the recorded events of `name`,
  * returns their summed duration in ms and the number of launches, and
  * forgets them.  Enabling costs two event records per kernel and no
  * synchronization; each record also holds the stream for a few microseconds

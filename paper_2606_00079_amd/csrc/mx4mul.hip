@@ -1416,6 +1416,7 @@ bitsmoe_status tile_product(const MulArgs& a, hipStream_t s) {
   auto* fn = mx4_tile_kernel<MX, AL, GLU>;
   static std::atomic<uint64_t> allowed{0};
   if (bitsmoe_status st = allow_lds(reinterpret_cast<const void*>(fn), lds, &allowed)) return st;
+  KernelTimer timer("mx4_tile", s);
   fn<<<tile_grid(), kTileThreads, lds, s>>>(a);
   BITSMOE_LAUNCH_CHECK("mx4_tile_kernel");
   return ok();
@@ -1441,6 +1442,7 @@ bitsmoe_status product(const char* who, const MulArgs& a, bool glu, hipStream_t 
                          : (glu ? mx4_few_kernel<false, true, 2> : mx4_few_kernel<false, false, 2>))
                    : (mx ? (glu ? mx4_few_kernel<true, true, 1> : mx4_few_kernel<true, false, 1>)
                          : (glu ? mx4_few_kernel<false, true, 1> : mx4_few_kernel<false, false, 1>));
+    KernelTimer timer("mx4_few", s);
     fn<<<grid, kThreads, 0, s>>>(a);
     BITSMOE_LAUNCH_CHECK("mx4_few_kernel");
     return ok();
@@ -1449,6 +1451,7 @@ bitsmoe_status product(const char* who, const MulArgs& a, bool glu, hipStream_t 
     return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": too many slots and outputs for one call");
   auto* fn = mx ? (glu ? mx4_rows_kernel<true, true> : mx4_rows_kernel<true, false>)
                 : (glu ? mx4_rows_kernel<false, true> : mx4_rows_kernel<false, false>);
+  KernelTimer timer("mx4_rows", s);
   fn<<<grid, kThreads, 0, s>>>(a);
   BITSMOE_LAUNCH_CHECK("mx4_rows_kernel");
   return ok();
@@ -1508,6 +1511,7 @@ extern "C" bitsmoe_status bitsmoe_mx4_product_grad(const uint8_t* codes_dev, con
     static std::atomic<uint64_t> allowed{0};
     if (bitsmoe_status st = allow_lds(reinterpret_cast<const void*>(mx4_grad_tile_kernel), GradShape::kBytes, &allowed))
       return st;
+    KernelTimer timer("mx4_grad_tile", stream);
     mx4_grad_tile_kernel<<<tile_grid(), kTileThreads, GradShape::kBytes, static_cast<hipStream_t>(stream)>>>(a);
     BITSMOE_LAUNCH_CHECK("mx4_grad_tile_kernel");
     return ok();
@@ -1516,6 +1520,7 @@ extern "C" bitsmoe_status bitsmoe_mx4_product_grad(const uint8_t* codes_dev, con
   if (!grid_of(a, few_slots(a), (K + 127) / 128, &grid))
     return fail(BITSMOE_ERR_SHAPE, "mx4_product_grad: too many slots and columns for one call");
   auto* fn = few_slots(a) == 32 ? mx4_grad_few_kernel<2> : mx4_grad_few_kernel<1>;
+  KernelTimer timer("mx4_grad_few", stream);
   fn<<<grid, kTileThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
   BITSMOE_LAUNCH_CHECK("mx4_grad_few_kernel");
   return ok();

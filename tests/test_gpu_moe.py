@@ -284,6 +284,90 @@ def test_product_grad(shape):
         assert (got[off[-1]:] == 0).all()
 
 
+def exact64(codes, scales, X, off, rows=None, glu=False, grad=False):
+    """(y, magnitudes) in 64 bits on the device, a loop over the experts."""
+    v = torch.tensor(omx4.GRID, dtype=torch.float64, device=DEV)
+    S = len(X) if rows is None else len(rows)
+    x = X.double() if rows is None else X.double()[rows.long()]
+    y = size = None
+    for e in range(len(off) - 1):
+        c = torch.stack((codes[e] & 15, codes[e] >> 4), -1).flatten(-2).long()
+        w = v[c & 7] * (1 - 2 * (c >> 3)) * (2.0 ** (scales[e].double() - 127)).repeat_interleave(32, -1)
+        w = w if grad else w.t().contiguous()
+        if y is None:
+            y = torch.zeros((S, w.shape[1]), dtype=torch.float64, device=DEV)
+            size = torch.zeros_like(y)
+        at = slice(int(off[e]), int(off[e + 1]))
+        y[at], size[at] = x[at] @ w, x[at].abs() @ w.abs()
+    size = size * ((x.shape[1] + 16) * U)
+    if glu:
+        N = y.shape[1] // 2
+        g, u, eg, eu = y[:, :N], y[:, N:], size[:, :N], size[:, N:]
+        s = g / (1 + torch.exp(-g))
+        y = s * u
+        size = 1.1 * eg * (u.abs() + eu) + s.abs() * eu + y.abs() * 2.0 ** -20
+    return np64(y), np64(size)
+
+
+# Each kernel of the products, at sizes that it takes (what a call costs decides): wide is N, or 2 N with glu.
+# Large tiles: several a workgroup (more tiles than compute units), K a multiple of 512 or not, odd widths, a tail.
+TAKEN = [
+    ("bf16", "mx4_rows", 6, 250, 1056, 9), ("mx4", "mx4_rows", 6, 250, 1056, 9), ("bf16", "mx4_rows", 1, 33, 4096, 3),
+    ("bf16", "mx4_few", 90, 1550, 1312, 300), ("mx4", "mx4_few", 90, 1550, 1312, 300),
+    ("bf16", "mx4_few", 40, 1550, 2080, 800), ("mx4", "mx4_few", 200, 2050, 96, 3500),
+    ("bf16", "mx4_tile", 5, 2102, 288, 9000), ("bf16", "mx4_tile", 4, 2102, 512, 9000),
+    ("bf16", "mx4_tile", 3, 1802, 1536, 9001), ("mx4", "mx4_tile", 5, 2102, 288, 9000),
+    ("mx4", "mx4_tile", 4, 2102, 512, 9000), ("mx4", "mx4_tile", 3, 1802, 1536, 9001),
+    ("bf16", "mx4_tile", 130, 1026, 800, 9000), ("mx4", "mx4_tile", 130, 1026, 1024, 9000),
+    ("grad", "mx4_grad_few", 6, 250, 1056, 9), ("grad", "mx4_grad_few", 90, 1552, 480, 1300),
+    ("grad", "mx4_grad_tile", 5, 296, 2112, 9000), ("grad", "mx4_grad_tile", 130, 800, 1056, 9001),
+    ("grad", "mx4_grad_tile", 2, 264, 4096, 9000), ("grad", "mx4_grad_tile", 1, 160, 1024, 50000),
+]
+
+
+@pytest.mark.parametrize("glu", [False, True])
+@pytest.mark.parametrize("case", TAKEN)
+def test_every_kernel_of_the_products(case, glu):
+    form, kernel, E, wide, K, S = case
+    if glu and (form == "grad" or wide % 2):
+        return  # (no such form)
+    if form == "grad":
+        wide = wide // 8 * 8
+    g = np.random.default_rng([E, wide, K, S])
+    tail = S // 50
+    load = np.exp(0.7 * g.standard_normal(E)) * (g.random(E) > 0.1)
+    load[0] += 1e-3
+    off = np.r_[0, np.cumsum(g.multinomial(S - tail, load / load.sum()))].astype(np.int32)
+    codes = torch.randint(0, 256, (E, wide, K // 2), dtype=torch.uint8, device=DEV)
+    scales = torch.randint(118, 124, (E, wide, K // 32), dtype=torch.uint8, device=DEV)
+    bm.timing(True)
+    try:
+        if form == "grad":
+            X = torch.randn(S, wide, device=DEV).to(torch.bfloat16)
+            got = bm.mx4_product_grad(codes, scales, X, offsets=dev(off), dtype=torch.float32)
+            want, size = exact64(codes, scales, X, off, grad=True)
+        else:
+            T = S // 2 + 1
+            X = torch.randn(T, K, device=DEV).to(torch.bfloat16)
+            rows = dev(g.integers(0, T, S).astype(np.int32))
+            kw = {"offsets": dev(off), "rows": rows, "glu": glu, "dtype": torch.float32}
+            if form == "mx4":
+                q = bm.mx4_quantize(X)
+                got = bm.mx4_product_q(codes, scales, *q, **kw)
+                X = bm.mx4_dequantize(*q)
+            else:
+                got = bm.mx4_product(codes, scales, X, **kw)
+            want, size = exact64(codes, scales, X, off, rows=rows, glu=glu)
+        assert bm.kernel_time(kernel)[1] == 1, kernel
+    finally:
+        bm.timing(False)
+    within(np64(got), want, size + 1e-38, case)
+    assert (got[off[-1]:] == 0).all()
+    if form == "bf16":
+        half = np64(bm.mx4_product(codes, scales, X, **{**kw, "dtype": torch.bfloat16}))
+        within(half, want, size + 2.0 ** -8 * np.abs(want) + 1e-38, case)
+
+
 def test_product_gradient_against_differences():
     # the product is linear: <dy, f(x + h) - f(x)> = <dx, h>
     g = np.random.default_rng(11)
