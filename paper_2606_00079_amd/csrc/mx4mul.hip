@@ -318,12 +318,12 @@ __global__ __launch_bounds__(kThreads) void mx4_rows_kernel(MulArgs a) {
 // 16 TB slots x 256 weight rows a workgroup, 64 rows a wave: for a few slots an
 // expert and many experts, where reading the weights is all.  The slots' tokens
 // go through LDS 1024 entries of K at a time; the weights come straight into
-// registers, a step of 128 entries (four rows' tiles, 64 bytes of a row) ahead.
+// registers, four steps of 128 entries (four rows' tiles, 64 bytes of a row) ahead.
 // 16-byte chunk c of a slot lies at c ^ (slot mod 16): the sixteen slots of a
 // fragment read in different banks.
 template <bool MX, bool GLU, int TB>
 __global__ __launch_bounds__(kThreads) void mx4_few_kernel(MulArgs a) {
-  constexpr int R = 4, KC = 1024, XB = MX ? KC / 2 : 2 * KC, XC = XB / 16, SL = 16 * TB;
+  constexpr int R = 4, AHEAD = 4, KC = 1024, XB = MX ? KC / 2 : 2 * KC, XC = XB / 16, SL = 16 * TB;
   constexpr int NO = GLU ? 128 : 256;  // results of a slot
   __shared__ __align__(16) char xs[SL * XB];
   __shared__ uint8_t ss[MX ? SL * (KC / 32) : 1];
@@ -348,21 +348,50 @@ __global__ __launch_bounds__(kThreads) void mx4_few_kernel(MulArgs a) {
       else
         row = static_cast<int64_t>(t.e) * a.N + min(n0 + wave * 64 + i * 16 + r, a.N - 1);
       pc[i] = a.codes + (row * kb + q) * 16;
-      ps[i] = a.scales + row * kb + q;
+      ps[i] = a.scales + row * kb;
     }
-    uint4 c[R];
-    int s[R];
-    auto load = [&](int step) {
-      const int b = 4 * step + q;
+    uint4 c[AHEAD][R];
+    auto load = [&](int u, int step) {
+      const bool in = 4 * step + q < kb;
 #pragma unroll
       for (int i = 0; i < R; ++i) {
-        const bool in = b < kb;
-        c[i] = in ? *reinterpret_cast<const uint4*>(pc[i] + static_cast<int64_t>(step) * 64) : make_uint4(0, 0, 0, 0);
-        s[i] = in ? ps[i][4 * step] : 127;
+        c[u][i] = make_uint4(0, 0, 0, 0);
+        if (in) c[u][i] = *reinterpret_cast<const uint4*>(pc[i] + static_cast<int64_t>(step) * 64);
+      }
+    };
+    // A row's scales sixteen at a time, the four steps': byte by byte, each would find its line still on its way.
+    uint4 s[R], snext[R];
+    auto load_scales = [&](int step) {
+      const int left = kb - 4 * step;
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        snext[i] = make_uint4(0, 0, 0, 0);
+        const uint8_t* p = ps[i] + 4 * step;
+        if (left >= 16) {
+          __builtin_memcpy(&snext[i], p, 16);
+        } else if (left > 0 && kb >= 16) {  // the row's last sixteen, those before shifted out
+          uint64_t v[2];
+          __builtin_memcpy(v, p + left - 16, 16);
+          const int out = 8 * (16 - left);
+          v[0] = out < 64 ? (v[0] >> out) | ((v[1] << 1) << (63 - out)) : v[1] >> (out - 64);
+          v[1] = out < 64 ? v[1] >> out : 0;
+          __builtin_memcpy(&snext[i], v, 16);
+        } else if (left > 0) {
+          uint32_t d[4];
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            d[w] = 0;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) d[w] |= static_cast<uint32_t>(4 * w + v < left ? p[4 * w + v] : 0) << (8 * v);
+          }
+          snext[i] = make_uint4(d[0], d[1], d[2], d[3]);
+        }
       }
     };
     const int steps = (kb + 3) / 4;
-    load(0);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) load(u, u);
+    load_scales(0);
     for (int k0 = 0; k0 < steps; k0 += KC / 128) {
       if (k0 > 0) __syncthreads();
       for (int i = tid; i < SL * XC; i += kThreads) {
@@ -385,15 +414,23 @@ __global__ __launch_bounds__(kThreads) void mx4_few_kernel(MulArgs a) {
       }
       __syncthreads();
       const int end = min(steps - k0, KC / 128);
-      for (int st = 0; st < end; ++st) {
+      for (int st0 = 0; st0 < end; st0 += AHEAD) {
+#pragma unroll
+       for (int i = 0; i < R; ++i) s[i] = snext[i];
+       load_scales(k0 + st0 + AHEAD);
+#pragma unroll
+       for (int u = 0; u < AHEAD; ++u) {
+        const int st = st0 + u;
+        if (st >= end) break;
         uint4 w[R];
         int sw[R];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-          w[i] = c[i];
-          sw[i] = s[i];
+          w[i] = c[u][i];
+          // (codes past K are 0, and so are the scales there: 2^-127 times 0)
+          sw[i] = ((u == 0 ? s[i].x : u == 1 ? s[i].y : u == 2 ? s[i].z : s[i].w) >> (8 * q)) & 255;
         }
-        if (k0 + st + 1 < steps) load(k0 + st + 1);
+        load(u, k0 + st + AHEAD);
         if constexpr (MX) {
 #pragma unroll
           for (int b = 0; b < TB; ++b) {
@@ -424,6 +461,7 @@ __global__ __launch_bounds__(kThreads) void mx4_few_kernel(MulArgs a) {
             }
           }
         }
+       }
       }
     }
   }
@@ -1363,9 +1401,9 @@ bool grid_of(const MulArgs& a, int64_t tile, int64_t per, unsigned* grid) {
 // chain of steps counts) or fill the card (their number does).  The constants (us;
 // L entries of the sum) fit timings of all kernels at thirty shapes, E 1 .. 256,
 // 1/8 .. 4096 slots an expert, outputs 256 .. 14336, sums of 512 .. 14336 entries:
-// the choice is within a quarter of the best of them (3 % on average), and the worst of
-// them is two to ten times that (one expert, 64 slots, 1024 x 4096: 50 us in large tiles, 49 in
-// few-slot ones, 9 by rows; 4096 slots, 4096 x 4096: 150, 333, 1340).
+// the choice is within 1.3 times the best of them (2 % on average), and the worst of
+// them is two to nine times that (one expert, 64 slots, 1024 x 4096: 50 us in large
+// tiles, 42 in few-slot ones, 9 by rows; 4096 slots, 4096 x 4096: 150, 266, 1340).
 enum Kernel { kByRows, kFewSlots, kLargeTiles };
 
 double tiles_of(const MulArgs& a, int64_t m) {
@@ -1388,19 +1426,21 @@ double in_rounds(double tiles, double each) {
 }
 
 Kernel product_kernel(const MulArgs& a, bool mx, bool glu) {
-  const double wide = static_cast<double>(a.N) * (glu ? 2 : 1), L = static_cast<double>(a.K);
-  const double c16 = (wide + 15) / 16, c256 = (wide + 255) / 256;
+  const int64_t wide = a.N * (glu ? 2 : 1);
+  const double L = static_cast<double>(a.K), c16 = static_cast<double>((wide + 15) / 16),
+               c256 = static_cast<double>((wide + 255) / 256);
   const double rows = 6.0 + tiles_of(a, 16) * c16 * L * (mx ? 3.6e-6 : 5.2e-6);
-  const double few = 3.0 + L * side_by_side(tiles_of(a, few_slots(a)) * c256, mx ? 0.009 : 0.0115, mx ? 4e-5 : 5e-5);
+  const double few = 4.0 + L * side_by_side(tiles_of(a, few_slots(a)) * c256, mx ? 0.006 : 0.0095, mx ? 3e-5 : 4e-5);
   const double large = in_rounds(tiles_of(a, kTM) * c256, L * (mx ? 0.0058 : 0.0117) + (mx ? 4.0 : 5.0));
   if (a.x_rows > 0 && large <= rows && large <= few) return kLargeTiles;
   return few <= rows ? kFewSlots : kByRows;
 }
 
 Kernel grad_kernel(const MulArgs& a) {
-  const double L = static_cast<double>(a.N), K = static_cast<double>(a.K);
-  const double few = 4.0 + L * side_by_side(tiles_of(a, few_slots(a)) * ((K + 127) / 128), 0.0055, 2.4e-5);
-  const double large = in_rounds(tiles_of(a, kTM) * ((K + 255) / 256), L * 0.0165 + 4.0);
+  const double L = static_cast<double>(a.N), c128 = static_cast<double>((a.K + 127) / 128),
+               c256 = static_cast<double>((a.K + 255) / 256);
+  const double few = 4.0 + L * side_by_side(tiles_of(a, few_slots(a)) * c128, 0.0055, 2.4e-5);
+  const double large = in_rounds(tiles_of(a, kTM) * c256, L * 0.0165 + 4.0);
   return large <= few ? kLargeTiles : kFewSlots;
 }
 
