@@ -416,52 +416,52 @@ __global__ __launch_bounds__(kThreads) void mx4_few_kernel(MulArgs a) {
       const int end = min(steps - k0, KC / 128);
       for (int st0 = 0; st0 < end; st0 += AHEAD) {
 #pragma unroll
-       for (int i = 0; i < R; ++i) s[i] = snext[i];
-       load_scales(k0 + st0 + AHEAD);
+        for (int i = 0; i < R; ++i) s[i] = snext[i];
+        load_scales(k0 + st0 + AHEAD);
 #pragma unroll
-       for (int u = 0; u < AHEAD; ++u) {
-        const int st = st0 + u;
-        if (st >= end) break;
-        uint4 w[R];
-        int sw[R];
+        for (int u = 0; u < AHEAD; ++u) {
+          const int st = st0 + u;
+          if (st >= end) break;
+          uint4 w[R];
+          int sw[R];
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-          w[i] = c[u][i];
-          // (codes past K are 0, and so are the scales there: 2^-127 times 0)
-          sw[i] = ((u == 0 ? s[i].x : u == 1 ? s[i].y : u == 2 ? s[i].z : s[i].w) >> (8 * q)) & 255;
-        }
-        load(u, k0 + st + AHEAD);
-        if constexpr (MX) {
-#pragma unroll
-          for (int b = 0; b < TB; ++b) {
-            const int sl = 16 * b + r, ch = 4 * st + q;
-            const uint4 v = *reinterpret_cast<const uint4*>(xs + sl * XB + ((ch ^ r) * 16));
-            const i32x8 B = {(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0};
-            const int sx = ss[sl * (KC / 32) + ch];
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-              const i32x8 A = {(int)w[i].x, (int)w[i].y, (int)w[i].z, (int)w[i].w, 0, 0, 0, 0};
-              acc[i][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, acc[i][b], 4, 4, 0, sw[i], 0, sx);
-            }
+          for (int i = 0; i < R; ++i) {
+            w[i] = c[u][i];
+            // (codes past K are 0, and so are the scales there: 2^-127 times 0)
+            sw[i] = ((u == 0 ? s[i].x : u == 1 ? s[i].y : u == 2 ? s[i].z : s[i].w) >> (8 * q)) & 255;
           }
-        } else {
+          load(u, k0 + st + AHEAD);
+          if constexpr (MX) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            bf16x8 xv[TB];
+            for (int b = 0; b < TB; ++b) {
+              const int sl = 16 * b + r, ch = 4 * st + q;
+              const uint4 v = *reinterpret_cast<const uint4*>(xs + sl * XB + ((ch ^ r) * 16));
+              const i32x8 B = {(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0};
+              const int sx = ss[sl * (KC / 32) + ch];
 #pragma unroll
-            for (int b = 0; b < TB; ++b)
-              xv[b] = *reinterpret_cast<const bf16x8*>(xs + (16 * b + r) * XB + (((16 * st + 4 * q + j) ^ r) * 16));
+              for (int i = 0; i < R; ++i) {
+                const i32x8 A = {(int)w[i].x, (int)w[i].y, (int)w[i].z, (int)w[i].w, 0, 0, 0, 0};
+                acc[i][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, acc[i][b], 4, 4, 0, sw[i], 0, sx);
+              }
+            }
+          } else {
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-              const uint32_t d = j == 0 ? w[i].x : j == 1 ? w[i].y : j == 2 ? w[i].z : w[i].w;
-              const bf16x8 wv = mx4_bf16(d, mx4_scale(sw[i]));
+            for (int j = 0; j < 4; ++j) {
+              bf16x8 xv[TB];
 #pragma unroll
               for (int b = 0; b < TB; ++b)
-                acc[i][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xv[b], acc[i][b], 0, 0, 0);
+                xv[b] = *reinterpret_cast<const bf16x8*>(xs + (16 * b + r) * XB + (((16 * st + 4 * q + j) ^ r) * 16));
+#pragma unroll
+              for (int i = 0; i < R; ++i) {
+                const uint32_t d = j == 0 ? w[i].x : j == 1 ? w[i].y : j == 2 ? w[i].z : w[i].w;
+                const bf16x8 wv = mx4_bf16(d, mx4_scale(sw[i]));
+#pragma unroll
+                for (int b = 0; b < TB; ++b)
+                  acc[i][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xv[b], acc[i][b], 0, 0, 0);
+              }
             }
           }
         }
-       }
       }
     }
   }
