@@ -228,7 +228,8 @@ __device__ __forceinline__ void store32(const MulArgs& a, int64_t s, int64_t n, 
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const bf16x2 b = {static_cast<__bf16>(v[8 * e + 4 * i + 2 * h]), static_cast<__bf16>(v[8 * e + 4 * i + 2 * h + 1])};
+          const int at = 8 * e + 4 * i + 2 * h;
+          const bf16x2 b = {static_cast<__bf16>(v[at]), static_cast<__bf16>(v[at + 1])};
           w[i][h] = __builtin_bit_cast(uint32_t, b);
         }
       const auto x = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
@@ -241,6 +242,9 @@ __device__ __forceinline__ void store32(const MulArgs& a, int64_t s, int64_t n, 
 // 16 outputs x 16 slots a workgroup.  The four waves share out K in segments
 // of 128: lane l holds 32 codes of row l % 16 (block l / 16 of the segment),
 // which one load fetches with their scale, and the same entries of slot l % 16.
+// For the fewest slots: bound by launch and one chain of loads (four segments in
+// flight a wave), so the sum is split and the workgroups are small and many.  One
+// token's 8 experts, 2 x 768 x 2048 with glu (13 MB): 9.0 us.
 template <bool MX, bool GLU>
 __global__ __launch_bounds__(kThreads) void mx4_rows_kernel(MulArgs a) {
   constexpr int H = GLU ? 2 : 1;
@@ -318,15 +322,19 @@ __global__ __launch_bounds__(kThreads) void mx4_rows_kernel(MulArgs a) {
 // 16 TB slots x 256 weight rows a workgroup, 64 rows a wave: for a few slots an
 // expert and many experts, where reading the weights is all.  The slots' tokens
 // go through LDS 1024 entries of K at a time; the weights come straight into
-// registers, four steps of 128 entries (four rows' tiles, 64 bytes of a row) ahead.
+// registers, two steps of 128 entries (four rows' tiles, 64 bytes of a row) ahead:
+// four steps ahead leave room for two waves a SIMD instead of four, and take 30 us
+// where these take 23.
 // 16-byte chunk c of a slot lies at c ^ (slot mod 16): the sixteen slots of a
-// fragment read in different banks.
+// fragment read in different banks.  Bound by the weights' bytes: 512 slots over
+// 128 experts, 2048 x 768 (110 MB), take 23 us, 4.8 TB/s.
 template <bool MX, bool GLU, int TB>
-__global__ __launch_bounds__(kThreads) void mx4_few_kernel(MulArgs a) {
-  constexpr int R = 4, AHEAD = 4, KC = 1024, XB = MX ? KC / 2 : 2 * KC, XC = XB / 16, SL = 16 * TB;
+__global__ __launch_bounds__(kThreads, TB == 1 ? 4 : 3) void mx4_few_kernel(MulArgs a) {
+  constexpr int R = 4, AHEAD = 2, KC = 1024, XB = MX ? KC / 2 : 2 * KC, XC = XB / 16, SL = 16 * TB;
   constexpr int NO = GLU ? 128 : 256;  // results of a slot
   __shared__ __align__(16) char xs[SL * XB];
   __shared__ uint8_t ss[MX ? SL * (KC / 32) : 1];
+  __shared__ __align__(16) uint32_t sw[kThreads][KC / 128];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, q = lane >> 4;
   Tile t;
   if (!find_tile(a.offsets, a.E, a.S, static_cast<int>((a.N + NO - 1) / NO), SL, &t)) return;
@@ -338,18 +346,16 @@ __global__ __launch_bounds__(kThreads) void mx4_few_kernel(MulArgs a) {
     for (int b = 0; b < TB; ++b) acc[i][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   if (t.e < a.E) {
     const int kb = static_cast<int>(a.K / 32);
-    // this lane's row of each of the wave's tiles (glu: gate and up in turn), at its block of 32 in the first step
-    const uint8_t *pc[R], *ps[R];
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      int64_t row;
+    // row r of the wave's tile i (glu: gate and up in turn)
+    auto row_of = [&](int i) {
       if constexpr (GLU)
-        row = static_cast<int64_t>(t.e) * 2 * a.N + min(n0 + wave * 32 + (i >> 1) * 16 + r, a.N - 1) + (i & 1) * a.N;
+        return static_cast<int64_t>(t.e) * 2 * a.N + min(n0 + wave * 32 + (i >> 1) * 16 + r, a.N - 1) + (i & 1) * a.N;
       else
-        row = static_cast<int64_t>(t.e) * a.N + min(n0 + wave * 64 + i * 16 + r, a.N - 1);
-      pc[i] = a.codes + (row * kb + q) * 16;
-      ps[i] = a.scales + row * kb;
-    }
+        return static_cast<int64_t>(t.e) * a.N + min(n0 + wave * 64 + i * 16 + r, a.N - 1);
+    };
+    const uint8_t* pc[R];  // at this lane's block of 32 in the first step
+#pragma unroll
+    for (int i = 0; i < R; ++i) pc[i] = a.codes + (row_of(i) * kb + q) * 16;
     uint4 c[AHEAD][R];
     auto load = [&](int u, int step) {
       const bool in = 4 * step + q < kb;
@@ -359,23 +365,25 @@ __global__ __launch_bounds__(kThreads) void mx4_few_kernel(MulArgs a) {
         if (in) c[u][i] = *reinterpret_cast<const uint4*>(pc[i] + static_cast<int64_t>(step) * 64);
       }
     };
-    // A row's scales sixteen at a time, the four steps': byte by byte, each would find its line still on its way.
-    uint4 s[R], snext[R];
-    auto load_scales = [&](int step) {
-      const int left = kb - 4 * step;
+    // The scales of a row, 32 blocks at a time by one lane (row r of tile q), go through LDS: read byte by byte as
+    // they are used, each would find its line still on its way.  Those past K are 0.
+    const uint8_t* ps = a.scales + row_of(q) * kb;
+    uint4 s[2];
+    auto load_scales = [&](int at) {
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
-        snext[i] = make_uint4(0, 0, 0, 0);
-        const uint8_t* p = ps[i] + 4 * step;
+      for (int h = 0; h < 2; ++h) {
+        const int left = kb - at - 16 * h;
+        const uint8_t* p = ps + at + 16 * h;
+        s[h] = make_uint4(0, 0, 0, 0);
         if (left >= 16) {
-          __builtin_memcpy(&snext[i], p, 16);
+          __builtin_memcpy(&s[h], p, 16);
         } else if (left > 0 && kb >= 16) {  // the row's last sixteen, those before shifted out
           uint64_t v[2];
           __builtin_memcpy(v, p + left - 16, 16);
           const int out = 8 * (16 - left);
           v[0] = out < 64 ? (v[0] >> out) | ((v[1] << 1) << (63 - out)) : v[1] >> (out - 64);
           v[1] = out < 64 ? v[1] >> out : 0;
-          __builtin_memcpy(&snext[i], v, 16);
+          __builtin_memcpy(&s[h], v, 16);
         } else if (left > 0) {
           uint32_t d[4];
 #pragma unroll
@@ -384,7 +392,7 @@ __global__ __launch_bounds__(kThreads) void mx4_few_kernel(MulArgs a) {
 #pragma unroll
             for (int v = 0; v < 4; ++v) d[w] |= static_cast<uint32_t>(4 * w + v < left ? p[4 * w + v] : 0) << (8 * v);
           }
-          snext[i] = make_uint4(d[0], d[1], d[2], d[3]);
+          s[h] = make_uint4(d[0], d[1], d[2], d[3]);
         }
       }
     };
@@ -412,23 +420,22 @@ __global__ __launch_bounds__(kThreads) void mx4_few_kernel(MulArgs a) {
         *reinterpret_cast<uint4*>(xs + sl * XB + ((ch ^ (sl & 15)) * 16)) = v;
         if constexpr (MX) ss[sl * (KC / 32) + ch] = static_cast<uint8_t>(sc);
       }
+      *reinterpret_cast<uint4*>(&sw[tid][0]) = s[0];
+      *reinterpret_cast<uint4*>(&sw[tid][4]) = s[1];
       __syncthreads();
+      load_scales(k0 * 4 + KC / 32);
       const int end = min(steps - k0, KC / 128);
       for (int st0 = 0; st0 < end; st0 += AHEAD) {
-#pragma unroll
-        for (int i = 0; i < R; ++i) s[i] = snext[i];
-        load_scales(k0 + st0 + AHEAD);
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
           const int st = st0 + u;
           if (st >= end) break;
           uint4 w[R];
-          int sw[R];
+          int scale[R];
 #pragma unroll
           for (int i = 0; i < R; ++i) {
             w[i] = c[u][i];
-            // (codes past K are 0, and so are the scales there: 2^-127 times 0)
-            sw[i] = ((u == 0 ? s[i].x : u == 1 ? s[i].y : u == 2 ? s[i].z : s[i].w) >> (8 * q)) & 255;
+            scale[i] = (sw[wave * 64 + i * 16 + r][st] >> (8 * q)) & 255;
           }
           load(u, k0 + st + AHEAD);
           if constexpr (MX) {
@@ -441,7 +448,7 @@ __global__ __launch_bounds__(kThreads) void mx4_few_kernel(MulArgs a) {
 #pragma unroll
               for (int i = 0; i < R; ++i) {
                 const i32x8 A = {(int)w[i].x, (int)w[i].y, (int)w[i].z, (int)w[i].w, 0, 0, 0, 0};
-                acc[i][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, acc[i][b], 4, 4, 0, sw[i], 0, sx);
+                acc[i][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, acc[i][b], 4, 4, 0, scale[i], 0, sx);
               }
             }
           } else {
@@ -454,7 +461,7 @@ __global__ __launch_bounds__(kThreads) void mx4_few_kernel(MulArgs a) {
 #pragma unroll
               for (int i = 0; i < R; ++i) {
                 const uint32_t d = j == 0 ? w[i].x : j == 1 ? w[i].y : j == 2 ? w[i].z : w[i].w;
-                const bf16x8 wv = mx4_bf16(d, mx4_scale(sw[i]));
+                const bf16x8 wv = mx4_bf16(d, mx4_scale(scale[i]));
 #pragma unroll
                 for (int b = 0; b < TB; ++b)
                   acc[i][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, xv[b], acc[i][b], 0, 0, 0);
@@ -508,6 +515,13 @@ __global__ __launch_bounds__(kThreads) void mx4_few_kernel(MulArgs a) {
 // A workgroup stays on its compute unit and takes tile after tile; the loads run
 // on into the next tile, so its first stages are there when the results of one
 // have been stored.
+//
+// Bound by the matrix cores, whose clock gives way under load (about 1.3 PFLOP/s
+// bf16 without a pause), and by the tiles that an expert's last slots do not fill.
+// bf16, 32768 slots over 128 experts, 2 x 768 x 2048 with glu: 254 us, 0.81
+// PFLOP/s (1.0 with what pads the tiles).  MX4, 32768 slots over 256 experts, 2048
+// x 7168: 600 us, 1.6 PFLOP/s (2.4 padded) and 3.6 TB/s; half of its time
+// goes with the weights' bytes, which every XCD's share reads once.
 // ---------------------------------------------------------------------------
 constexpr int kTileThreads = 512, kWaves = 8, kTM = 128, kTN = 256, kLds = 163840;
 
@@ -1014,7 +1028,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(MulArgs a) {
 // workgroup, a block of 32 a thread, into an LDS tile that the transposing LDS
 // read takes fragments from.  Two such tiles: the next step's is made while this
 // one's is multiplied, and between the matrix-core ops go the reads of the next
-// sixteen rows' fragments and the conversions.
+// sixteen rows' fragments and the conversions.  32768 slots over 128 experts, 2048
+// x 768: 168 us, 0.61 PFLOP/s (0.77 with what pads the tiles), bound by the matrix
+// cores' clock and, at half of their time, by the LDS (fragments used twice).
 // ---------------------------------------------------------------------------
 struct GradShape {
   static constexpr int KT = 256, NS = 64;  // columns, rows of W a step
@@ -1265,7 +1281,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_grad_tile_kernel(MulArgs 
 // transposing read, two tiles in turn; they come through registers, four steps
 // ahead.  With few workgroups what counts is the length of one's chain of
 // steps, so two groups of four waves take every other step, and join their sums
-// at the end.
+// at the end.  194 slots over 8 experts, 1024 x 4096: 17 us, launch and eight steps
+// of load, widen, barrier and multiply; the bytes alone would take 5.
 template <int TB>
 __global__ __launch_bounds__(kTileThreads) void mx4_grad_few_kernel(MulArgs a) {
   constexpr int KT = 128, NS = 64, AHEAD = 4, C = KT / 64;
@@ -1401,7 +1418,7 @@ bool grid_of(const MulArgs& a, int64_t tile, int64_t per, unsigned* grid) {
 // chain of steps counts) or fill the card (their number does).  The constants (us;
 // L entries of the sum) fit timings of all kernels at thirty shapes, E 1 .. 256,
 // 1/8 .. 4096 slots an expert, outputs 256 .. 14336, sums of 512 .. 14336 entries:
-// the choice is within 1.3 times the best of them (2 % on average), and the worst of
+// the choice is within 1.3 times the best of them (1 % on average), and the worst of
 // them is two to nine times that (one expert, 64 slots, 1024 x 4096: 50 us in large
 // tiles, 42 in few-slot ones, 9 by rows; 4096 slots, 4096 x 4096: 150, 266, 1340).
 enum Kernel { kByRows, kFewSlots, kLargeTiles };
