@@ -20,7 +20,7 @@
 //
 // The largest calls are bound by the logits' bytes and a row's chain of lane
 // exchanges, the others by their launches: 16384 rows of 256 fp32 logits, k = 8
-// (17 MB), take 17 us (rows), 5 (sums), 6 (places) and 18 for the gradient (34 MB);
+// (17 MB), take 17 us (rows), 5 (sums), 6 (places) and 16 for the gradient (34 MB);
 // one row of 128, 7.8 us in its one launch, the chain of k rounds, barriers and
 // placement.
 #include <atomic>
@@ -487,13 +487,26 @@ struct GradArgs {
   void* dlogits;
 };
 
-// A row on LPT lanes as in the forward form; a row's slots lie on its lanes too, so
-// the gate term needs no more loads.  Read and written once, 1.9 TB/s at 16384
-// rows of 256 fp32 logits.
+// LDS operations of this wave before it are done, for its other lanes too.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// A row on LPT lanes as in the forward form; a row's slots lie on its lanes too, and
+// their gate terms reach the lanes of their experts through LDS (by shuffles and
+// compares the kernel took 18 us, with it 15.6).  Read and written once: 16384 rows
+// of 256 fp32 logits (34 MB) at 2.2 TB/s, bound by the instructions of a row's
+// exponentials and sums and by its chain of loads.
 template <bool BF16, int V, int LPT>
 __global__ __launch_bounds__(kGradThreads) void route_grad_kernel(GradArgs a) {
   constexpr int G = kGradThreads / LPT;
+  __shared__ __align__(16) float gates[kGradThreads * V];  // a row's gate terms by expert; zero between rows
   const int lane = threadIdx.x % LPT, grp = threadIdx.x / LPT, first = lane * V;
+  float* gate = gates + grp * (LPT * V);
+#pragma unroll
+  for (int i = 0; i < V; ++i) gate[first + i] = 0.0f;
   const float n = static_cast<float>(a.counts[a.E]);
   const float gb =
       a.dlosses && n > 0.0f ? a.dlosses[0] * (static_cast<float>(a.E) / (static_cast<float>(a.k) * n * n)) : 0.0f;
@@ -547,21 +560,18 @@ __global__ __launch_bounds__(kGradThreads) void route_grad_kernel(GradArgs a) {
       for (int i = 0; i < V; ++i) d[i] = p[i] * (share[i] + all);
       if (a.dweights) {
         const float mean = a.renorm ? wd : 0.0f;
-        const float g0 = w0 * (dw0 - mean);
-        for (int j = 0; j < a.k; ++j) {
-          int e;
-          float g;
-          if (j < LPT) {
-            e = __shfl(e0, j, LPT);
-            g = __shfl(g0, j, LPT);
-          } else {
-            e = a.experts[t * a.k + j];
-            g = a.weights[t * a.k + j] * (a.dweights[t * a.k + j] - mean);
-          }
-          e -= first;
+        auto put = [&](int e, float g) {
+          if (e >= 0 && e < a.E) atomicAdd(gate + e, g);  // (one slot an expert)
+        };
+        if (lane < a.k) put(e0, w0 * (dw0 - mean));
+        for (int j = lane + LPT; j < a.k; j += LPT)
+          put(a.experts[t * a.k + j], a.weights[t * a.k + j] * (a.dweights[t * a.k + j] - mean));
+        wave_fence();  // (a row's lanes are of one wave)
 #pragma unroll
-          for (int i = 0; i < V; ++i) d[i] += e == i ? g : 0.0f;  // (e < 0: none)
-        }
+        for (int i = 0; i < V; ++i) d[i] += gate[first + i];
+#pragma unroll
+        for (int i = 0; i < V; ++i) gate[first + i] = 0.0f;
+        wave_fence();
       }
     }
     if constexpr (BF16) {
