@@ -645,7 +645,8 @@ bitsmoe_status bitsmoe_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* s
  * or with glu, W_e holding N rows W^g_e and then N rows W^u_e,
  *     y_s = silu(W^g_e x) * (W^u_e x),  silu(v) = v / (1 + exp(-v)).
  * Slots from offsets[E] on, and those whose row is not in [0, x_rows), get 0
- * (offsets are cut to [0, S]).  Sums are fp32; results are rounded once.
+ * whatever W holds (offsets are cut to [0, S]).  Sums are fp32; results are
+ * rounded once.
  *   codes_dev, scales_dev   W [E][N] rows of K entries in MX4 (glu: [E][2 N])
  *   X_dev        x_rows rows of K bf16, ldx entries apart
  *   offsets_dev  [E + 1] int32, or NULL with E = 1: all slots are expert 0's

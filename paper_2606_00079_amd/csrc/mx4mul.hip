@@ -256,11 +256,12 @@ __global__ __launch_bounds__(kThreads) void mx4_rows_kernel(MulArgs a) {
   f32x4 acc[H];
 #pragma unroll
   for (int h = 0; h < H; ++h) acc[h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  bool have = false;  // the row of this lane's slot exists
   if (t.e < a.E) {
     const int64_t n = min(n0 + r, a.N - 1);
     const int64_t slot = t.lo + r;
     const int64_t row = slot < t.hi ? (a.rows ? static_cast<int64_t>(a.rows[slot]) : slot) : -1;
-    const bool have = row >= 0 && row < a.x_rows;
+    have = row >= 0 && row < a.x_rows;
     const int64_t kb = a.K / 32;
     const int64_t wrow = static_cast<int64_t>(t.e) * (a.N * H) + n;
     for (int64_t seg = wave; seg * 4 < kb; seg += kThreads / 64) {
@@ -314,6 +315,7 @@ __global__ __launch_bounds__(kThreads) void mx4_rows_kernel(MulArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[0][i] = silu(acc[0][i]) * acc[1][i];
   }
+  if (!have) acc[0] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};  // (zeros times a lost block of weights are NaN)
   const int64_t slot = t.lo + r, n = n0 + 4 * q;  // (a lane holds four outputs of one slot)
   const bool wide = a.ldy % 4 == 0;
   if (slot < t.hi && n < a.N) store4(a, slot, n, a.N, wide, acc[0]);
@@ -344,7 +346,10 @@ __global__ __launch_bounds__(kThreads, TB == 1 ? 4 : 3) void mx4_few_kernel(MulA
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int b = 0; b < TB; ++b) acc[i][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  uint64_t there = 0;  // bit i: the row of slot i exists (a wave's mask: neither vector registers nor LDS to spare)
   if (t.e < a.E) {
+    const int mine = t.lo + (lane & (SL - 1));
+    const int row_of_mine = mine >= t.hi ? -1 : a.rows ? a.rows[mine] : mine;
     const int kb = static_cast<int>(a.K / 32);
     // row r of the wave's tile i (glu: gate and up in turn)
     auto row_of = [&](int i) {
@@ -420,6 +425,7 @@ __global__ __launch_bounds__(kThreads, TB == 1 ? 4 : 3) void mx4_few_kernel(MulA
         *reinterpret_cast<uint4*>(xs + sl * XB + ((ch ^ (sl & 15)) * 16)) = v;
         if constexpr (MX) ss[sl * (KC / 32) + ch] = static_cast<uint8_t>(sc);
       }
+      if (k0 == 0) there = __ballot(row_of_mine >= 0 && row_of_mine < a.x_rows);
       *reinterpret_cast<uint4*>(&sw[tid][0]) = s[0];
       *reinterpret_cast<uint4*>(&sw[tid][4]) = s[1];
       __syncthreads();
@@ -477,6 +483,7 @@ __global__ __launch_bounds__(kThreads, TB == 1 ? 4 : 3) void mx4_few_kernel(MulA
   for (int b = 0; b < TB; ++b) {
     const int64_t slot = t.lo + 16 * b + r;
     if (slot >= t.hi) continue;
+    const bool have = there >> (16 * b + r) & 1;
 #pragma unroll
     for (int i = 0; i < (GLU ? R / 2 : R); ++i) {
       f32x4 v;
@@ -487,6 +494,7 @@ __global__ __launch_bounds__(kThreads, TB == 1 ? 4 : 3) void mx4_few_kernel(MulA
       } else {
         v = acc[i][b];
       }
+      if (!have) v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};  // (zeros times a lost block of weights are NaN)
       const int64_t n = n0 + wave * (GLU ? 32 : 64) + i * 16 + 4 * q;
       if (n < a.N) store4(a, slot, n, a.N, wide, v);
     }

@@ -1,0 +1,132 @@
+"""GPU tests of the MoE layer's operators where they are easiest to get wrong:
+lost blocks beside rows that do not exist, strides, slots of no expert, every
+store of every kernel, calls that overlap or are captured.
+
+Bounds as in test_gpu_moe: a sum of n fp32 terms is within n 2^-23 of the sum of
+their magnitudes, a bf16 result is rounded once (2^-8 of it at most).
+"""
+import numpy as np
+import pytest
+
+from conftest import gpu_available
+from oracle import mx4 as omx4
+
+pytestmark = pytest.mark.gpu
+
+if not gpu_available():  # pragma: no cover
+    pytest.skip("no GPU", allow_module_level=True)
+
+import torch  # noqa: E402
+
+import paper_2606_00079_amd as bm  # noqa: E402
+
+DEV = "cuda:0"
+U = 2.0 ** -23
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def within(got, want, bound, what):
+    """NaN exactly where `want` is, and no farther from it than `bound`."""
+    got = got.double()
+    assert torch.equal(got.isnan(), want.isnan()), what
+    off = ((got - want).abs() - bound)[~want.isnan()]
+    assert not (off > 0).any(), (what, float(off.max()), int((off > 0).sum()))
+
+
+def weights(E, N, K, g, lost=0):
+    """Weights in MX4, any codes, scales over a few powers of two; `lost` blocks of
+    every expert stand for NaN."""
+    codes = torch.randint(0, 256, (E, N, K // 2), dtype=torch.uint8, device=DEV)
+    scales = g.integers(118, 124, (E, N, K // 32), dtype=np.uint8)
+    for e in range(E):
+        scales[e, g.integers(0, N, lost), g.integers(0, K // 32, lost)] = 255
+    return codes, torch.from_numpy(scales).to(DEV)
+
+
+def values(codes, scales):
+    v = torch.tensor(omx4.GRID, dtype=torch.float64, device=DEV)
+    c = torch.stack((codes & 15, codes >> 4), -1).flatten(-2).long()
+    s = torch.where(scales == 255, torch.nan, 2.0 ** (scales.double() - 127))
+    return v[c & 7] * (1 - 2 * (c >> 3)) * s.repeat_interleave(32, -1)
+
+
+def offsets_of(E, S, tail, g, head=0):
+    load = np.exp(0.7 * g.standard_normal(E)) * (g.random(E) > 0.1)
+    load[0] += 1e-3
+    n = g.multinomial(S - tail - head, load / load.sum())
+    return (head + np.r_[0, np.cumsum(n)]).astype(np.int32)
+
+
+def exact(codes, scales, X, off, rows=None, glu=False, grad=False):
+    """(y, bound of an fp32 result) in 64 bits, a loop over the experts; a slot whose
+    row does not exist, or that has no expert, is 0."""
+    S = len(X) if rows is None else len(rows)
+    r = torch.arange(S, device=DEV) if rows is None else rows.long()
+    there = (r >= 0) & (r < len(X))
+    x = X.double()[torch.where(there, r, 0)]
+    width = codes.shape[2] * 2 if grad else codes.shape[1]
+    y = torch.zeros((S, width), dtype=torch.float64, device=DEV)
+    size = torch.zeros_like(y)
+    for e in range(len(off) - 1):
+        w = values(codes[e], scales[e])
+        w = w if grad else w.t().contiguous()
+        at = slice(int(off[e]), int(off[e + 1]))
+        y[at], size[at] = x[at] @ w, x[at].abs() @ w.abs()
+    size = size * ((x.shape[1] + 16) * U)
+    if glu:
+        N = y.shape[1] // 2
+        g, u, eg, eu = y[:, :N], y[:, N:], size[:, :N], size[:, N:]
+        s = g / (1 + torch.exp(-g))
+        y = s * u
+        size = 1.1 * eg * (u.abs() + eu) + s.abs() * eu + y.abs() * 2.0 ** -20
+    y[~there], size[~there] = 0, 0
+    return y, size + 1e-38
+
+
+def product(form, codes, scales, X, **kw):
+    """The result, and the tokens as the product saw them."""
+    if form == "mx4":
+        q = bm.mx4_quantize(X)
+        return bm.mx4_product_q(codes, scales, *q, **kw), bm.mx4_dequantize(*q)
+    return bm.mx4_product(codes, scales, X, **kw), X
+
+
+def taken(kernel, call):
+    """What `call` returns; it must have gone to `kernel`, in one launch."""
+    bm.timing(True)
+    try:
+        out = call()
+        assert bm.kernel_time(kernel)[1] == 1, kernel
+    finally:
+        bm.timing(False)
+    return out
+
+
+# form, kernel, E, N (2 N with glu), K, S
+FORWARD = [
+    ("bf16", "mx4_rows", 6, 250, 1056, 9), ("mx4", "mx4_rows", 6, 250, 1056, 9),
+    ("bf16", "mx4_few", 90, 1550, 1312, 300), ("mx4", "mx4_few", 90, 1550, 1312, 300),
+    ("bf16", "mx4_few", 40, 1550, 2080, 800), ("mx4", "mx4_few", 40, 1550, 2080, 800),
+    ("bf16", "mx4_tile", 5, 2048, 288, 9000), ("bf16", "mx4_tile", 4, 2048, 512, 9000),
+    ("mx4", "mx4_tile", 5, 2048, 288, 9000), ("mx4", "mx4_tile", 4, 2048, 1024, 9000),
+]
+
+
+@pytest.mark.parametrize("glu", [False, True])
+@pytest.mark.parametrize("case", FORWARD)
+def test_rows_that_do_not_exist_beside_lost_blocks(case, glu):
+    """0 for such a slot, whatever kernel takes the call: not 0 times NaN."""
+    form, kernel, E, N, K, S = case
+    g = np.random.default_rng([E, N, K, S, glu])
+    codes, scales = weights(E, N, K, g, lost=3)
+    off = offsets_of(E, S, S // 50, g)
+    T = S // 2 + 1
+    X = torch.randn(T, K, device=DEV).to(torch.bfloat16)
+    rows = g.integers(0, T, S).astype(np.int32)
+    rows[::3], rows[1::5], rows[2::7] = -1, T, T + 1000
+    rows = torch.from_numpy(rows).to(DEV)
+    got, x = taken(kernel, lambda: product(form, codes, scales, X, offsets=torch.from_numpy(off).to(DEV), rows=rows,
+                                           glu=glu, dtype=torch.float32))
+    want, bound = exact(codes, scales, x, off, rows, glu)
+    assert want.isnan().any()
+    within(got, want, bound, case)
