@@ -653,7 +653,7 @@ bitsmoe_status bitsmoe_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* s
  *   rows_dev     [S] int32, or NULL: slot s reads row s
  *   Y_dev        [S] rows of N entries of type yt, ldy entries apart
  * S may be 0.  Shape rules: K % 32 == 0, ldx >= K, ldx % 8 == 0, ldy >= N,
- * E <= 65535, N and K <= 2^24, S < 2^31; where S / E is small, (S / 16 + E) times
+ * E <= 65535, N and K <= 2^24, S < 2^31 - 256; where S / E is small, (S / 16 + E) times
  * the sixteens of N below 2^23.
  */
 bitsmoe_status bitsmoe_mx4_product(const uint8_t* codes_dev, const uint8_t* scales_dev, int64_t E,

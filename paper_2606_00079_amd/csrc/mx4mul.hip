@@ -1398,9 +1398,11 @@ bitsmoe_status check(const char* who, const MulArgs& a, bitsmoe_dtype yt, int64_
   if (a.E <= 0 || a.N <= 0 || a.K <= 0 || a.S < 0 || a.x_rows < 0)
     return bad(BITSMOE_ERR_ARG, ": non-positive size");
   if (yt != BITSMOE_F32 && yt != BITSMOE_BF16) return bad(BITSMOE_ERR_DTYPE, ": results are fp32 or bf16");
-  if (a.K % kMx4Block != 0 || a.K > (1 << 24) || a.N > (1 << 24) || a.E > 65535 || a.S > 0x7FFFFFF0 ||
+  // (slots are ints, and the end of a tile that begins at one is too)
+  if (a.K % kMx4Block != 0 || a.K > (1 << 24) || a.N > (1 << 24) || a.E > 65535 || a.S > 0x7FFFFFFF - 2 * kTM ||
       a.x_rows > 0x7FFFFFFF)
-    return bad(BITSMOE_ERR_SHAPE, ": needs K % 32 == 0, K and N <= 2^24, E <= 65535, S and rows < 2^31");
+    return bad(BITSMOE_ERR_SHAPE,
+               ": needs K % 32 == 0, K and N <= 2^24, E <= 65535, S < 2^31 - 256 and rows < 2^31");
   if (a.ldy < wide || a.ldy > (int64_t(1) << 32))
     return bad(BITSMOE_ERR_SHAPE, ": the results' row stride is too small or too large");
   if (!a.offsets && a.E != 1) return bad(BITSMOE_ERR_ARG, ": no offsets, and more than one expert");
