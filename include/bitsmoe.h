@@ -644,7 +644,8 @@ bitsmoe_status bitsmoe_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* s
  *     y_s = W_e x_{rows[s]},
  * or with glu, W_e holding N rows W^g_e and then N rows W^u_e,
  *     y_s = silu(W^g_e x) * (W^u_e x),  silu(v) = v / (1 + exp(-v)).
- * Slots from offsets[E] on, and those whose row is not in [0, x_rows), get 0
+ * Slots before offsets[0] or from offsets[E] on (those of experts that are held
+ * elsewhere, or of none), and those whose row is not in [0, x_rows), get 0
  * whatever W holds (offsets are cut to [0, S]).  Sums are fp32; results are
  * rounded once.
  *   codes_dev, scales_dev   W [E][N] rows of K entries in MX4 (glu: [E][2 N])
@@ -674,8 +675,8 @@ bitsmoe_status bitsmoe_mx4_product_q(const uint8_t* codes_dev, const uint8_t* sc
                                      void* stream);
 
 /*
- * Gradient of the tokens: dx_s = W_e^T dy_s for the same slots (those from
- * offsets[E] on get 0).  The sum over a token's slots is bitsmoe_combine with
+ * Gradient of the tokens: dx_s = W_e^T dy_s for the same slots (those before
+ * offsets[0] or from offsets[E] on get 0).  The sum over a token's slots is bitsmoe_combine with
  * weights NULL; the weights are held in 4 bits and have no gradient.  For a
  * product with glu, dY is that of the 2 N values before it, and N counts them.
  *   dY_dev  [S] rows of N bf16, lddy entries apart

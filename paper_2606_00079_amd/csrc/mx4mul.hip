@@ -52,7 +52,8 @@ __device__ __forceinline__ int lane_value(int v, int l) { return __builtin_amdgc
 
 // The slots of one workgroup, `lo` .. `hi` of expert e, and its column tile.
 // Each expert's slots are cut into tiles of `tile` from its first on; e = E
-// holds the slots of no expert, whose results are zero.
+// holds the slots of no expert past the last expert's, and e = E + 1 those
+// before the first one's: their results are zero.
 //
 // Workgroup ids go to the eight XCDs in turn; each XCD gets a contiguous range of
 // the tiles that exist (ids past them find none), ordered by expert, and there
@@ -64,16 +65,20 @@ struct Tile {
   int e, lo, hi, col;
 };
 __device__ __forceinline__ int slots_of(const int32_t* offsets, int E, int S, int e, int* lo) {
+  if (e > E) {
+    *lo = 0;
+    return offsets ? min(max(offsets[0], 0), S) : 0;
+  }
   *lo = offsets ? min(max(offsets[e], 0), S) : (e == 0 ? 0 : S);
   return (e < E && offsets ? min(max(offsets[e + 1], *lo), S) : S) - *lo;
 }
 __device__ __forceinline__ bool find_tile(const int32_t* offsets, int E, int64_t S, int cols, int tile, Tile* out) {
   const int s = static_cast<int>(S), lane = threadIdx.x & 63;
-  const int per = E / 64 + 1;  // experts a lane, of E + 1
+  const int per = (E + 1) / 64 + 1;  // experts a lane, of E + 2
   int lo, tiles = 0;
   for (int i = 0; i < per; ++i) {
     const int e = lane * per + i;
-    if (e <= E) tiles += (slots_of(offsets, E, s, e, &lo) + tile - 1) / tile;
+    if (e <= E + 1) tiles += (slots_of(offsets, E, s, e, &lo) + tile - 1) / tile;
   }
   int sum = wave_scan(tiles);
   const int64_t n = static_cast<int64_t>(lane_value(sum, 63)) * cols, id = blockIdx.x;
@@ -84,9 +89,9 @@ __device__ __forceinline__ bool find_tile(const int32_t* offsets, int E, int64_t
   const int run = __builtin_ctzll(__ballot(sum > g));
   int base = run ? lane_value(sum, run - 1) : 0;
   int e = run * per;
-  for (;; e += 64) {  // (one pass up to 4095 experts)
+  for (;; e += 64) {  // (one pass up to 4094 experts)
     const int f = e + lane;
-    const int have = f <= E && f < (run + 1) * per ? slots_of(offsets, E, s, f, &lo) : 0;
+    const int have = f <= E + 1 && f < (run + 1) * per ? slots_of(offsets, E, s, f, &lo) : 0;
     tiles = (have + tile - 1) / tile;
     sum = base + wave_scan(tiles);
     const uint64_t hit = __ballot(sum > g);
@@ -109,7 +114,7 @@ __device__ __forceinline__ bool find_tile(const int32_t* offsets, int E, int64_t
 }
 
 // The same order of tiles for a workgroup that stays and takes one tile after
-// another (without those of e = E): it goes on from expert to expert with
+// another (without those of no expert): it goes on from expert to expert with
 // scalar loads, which do not touch the count of its vector loads.
 struct Walk {
   const __attribute__((address_space(4))) int32_t* offsets;
@@ -142,8 +147,9 @@ struct Walk {
     out->lo = first + row * tile;
     out->hi = min(first + count, out->lo + tile);
   }
-  // The first tile of this workgroup; *none: where the slots of no expert begin.
-  __device__ __forceinline__ bool start(const int32_t* off, int E_, int64_t S_, int cols_, int tile_, int* none) {
+  // The first tile of this workgroup; slots below *head and from *none on have no expert.
+  __device__ __forceinline__ bool start(const int32_t* off, int E_, int64_t S_, int cols_, int tile_, int* head,
+                                        int* none) {
     offsets = (const __attribute__((address_space(4))) int32_t*)reinterpret_cast<uintptr_t>(off);
     E = E_, S = static_cast<int>(S_), cols = cols_, tile = tile_;
     const int lane = threadIdx.x & 63, per = (E + 63) / 64;
@@ -154,6 +160,7 @@ struct Walk {
     }
     const int own = sum;
     sum = wave_scan(sum);
+    *head = offsets ? min(max(offsets[0], 0), S) : 0;
     *none = offsets ? min(max(offsets[E], 0), S) : S;
     const int64_t n = static_cast<int64_t>(lane_value(sum, 63)) * cols;
     const int64_t x = blockIdx.x & 7, q = n >> 3, rem = n & 7;
@@ -698,18 +705,20 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(MulArgs a) {
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
   const char *const zero = reinterpret_cast<const char*>(kPad), *const one = zero + 16;
 
-  int none;
+  int head, none;
   Walk walk;
   Tile cur, next;
-  bool more = walk.start(a.offsets, a.E, a.S, static_cast<int>((a.N + TNO - 1) / TNO), kTM, &none);
+  bool more = walk.start(a.offsets, a.E, a.S, static_cast<int>((a.N + TNO - 1) / TNO), kTM, &head, &none);
   // slots of no expert: zeros
-  for (int64_t s = none + static_cast<int64_t>(blockIdx.x); s < a.S; s += gridDim.x)
+  for (int64_t i = blockIdx.x; i < head + (a.S - none); i += gridDim.x) {
+    const int64_t s = i < head ? i : none + (i - head);
     for (int64_t n = threadIdx.x; n < a.N; n += kTileThreads) {
       if (a.yf32)
         static_cast<float*>(a.y)[s * a.ldy + n] = 0.0f;
       else
         static_cast<uint16_t*>(a.y)[s * a.ldy + n] = 0;
     }
+  }
   if (!more) return;
   walk.get(&cur);
 
@@ -1067,17 +1076,19 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_grad_tile_kernel(MulArgs 
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
   const char *const zero = reinterpret_cast<const char*>(kPad), *const one = zero + 16;
 
-  int none;
+  int head, none;
   Walk walk;
   Tile cur, next;
-  bool more = walk.start(a.offsets, a.E, a.S, static_cast<int>((a.K + H::KT - 1) / H::KT), kTM, &none);
-  for (int64_t s = none + static_cast<int64_t>(blockIdx.x); s < a.S; s += gridDim.x)
+  bool more = walk.start(a.offsets, a.E, a.S, static_cast<int>((a.K + H::KT - 1) / H::KT), kTM, &head, &none);
+  for (int64_t i = blockIdx.x; i < head + (a.S - none); i += gridDim.x) {
+    const int64_t s = i < head ? i : none + (i - head);
     for (int64_t k = tid; k < a.K; k += kTileThreads) {
       if (a.yf32)
         static_cast<float*>(a.y)[s * a.ldy + k] = 0.0f;
       else
         static_cast<uint16_t*>(a.y)[s * a.ldy + k] = 0;
     }
+  }
   if (!more) return;
   walk.get(&cur);
 
@@ -1415,7 +1426,7 @@ bitsmoe_status check(const char* who, const MulArgs& a, bitsmoe_dtype yt, int64_
 
 // Workgroups for tiles of `tile` slots and `per` workgroups each.
 bool grid_of(const MulArgs& a, int64_t tile, int64_t per, unsigned* grid) {
-  const int64_t tiles = a.S / tile + (a.E + 1 < a.S ? a.E + 1 : a.S);
+  const int64_t tiles = a.S / tile + (a.E + 2 < a.S ? a.E + 2 : a.S);  // (every run's last one may be part)
   if (tiles > ((int64_t(1) << 23) - 1) / per) return false;  // (2^32 threads of 512 a workgroup)
   *grid = static_cast<unsigned>(tiles * per);
   return true;

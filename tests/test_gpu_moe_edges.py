@@ -130,3 +130,30 @@ def test_rows_that_do_not_exist_beside_lost_blocks(case, glu):
     want, bound = exact(codes, scales, x, off, rows, glu)
     assert want.isnan().any()
     within(got, want, bound, case)
+
+
+# form, kernel, E, N, K, S
+BACKWARD = [
+    ("grad", "mx4_grad_few", 6, 256, 1056, 9), ("grad", "mx4_grad_few", 90, 1552, 480, 1300),
+    ("grad", "mx4_grad_tile", 5, 296, 2112, 9000), ("grad", "mx4_grad_tile", 2, 264, 4096, 9000),
+]
+
+
+@pytest.mark.parametrize("case", FORWARD + BACKWARD)
+def test_slots_before_the_first_expert_and_after_the_last(case):
+    """The slots of some of the experts only: the others' are 0, not left as they were."""
+    form, kernel, E, N, K, S = case
+    g = np.random.default_rng([E, N, K, S, 5])
+    codes, scales = weights(E, N, K, g, lost=2)
+    off = offsets_of(E, S, S // 9 + 1, g, head=S // 7 + 2)
+    kw = {"offsets": torch.from_numpy(off).to(DEV), "dtype": torch.float32}
+    X = torch.randn(S, N if form == "grad" else K, device=DEV).to(torch.bfloat16)
+    if form == "grad":
+        kw["out"] = torch.full((S, K), torch.nan, device=DEV)
+        got = taken(kernel, lambda: bm.mx4_product_grad(codes, scales, X, **kw))
+    else:
+        kw["out"] = torch.full((S, N), torch.nan, device=DEV)
+        got, X = taken(kernel, lambda: product(form, codes, scales, X, **kw))
+    want, bound = exact(codes, scales, X, off, grad=form == "grad")
+    within(got, want, bound, case)
+    assert (got[:off[0]] == 0).all() and (got[off[-1]:] == 0).all()
