@@ -654,8 +654,8 @@ bitsmoe_status bitsmoe_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* s
  *   rows_dev     [S] int32, or NULL: slot s reads row s
  *   Y_dev        [S] rows of N entries of type yt, ldy entries apart
  * S may be 0.  Shape rules: K % 32 == 0, ldx >= K, ldx % 8 == 0, ldy >= N,
- * E <= 65535, N and K <= 2^24, S < 2^31 - 256; where S / E is small, (S / 16 + E) times
- * the sixteens of N below 2^23.
+ * E <= 65535, N and K <= 2^24, S < 2^31 - 256; where S <= 8 E or x_rows = 0,
+ * (S / 16 + E + 2) times the sixteens of N below 2^23.
  */
 bitsmoe_status bitsmoe_mx4_product(const uint8_t* codes_dev, const uint8_t* scales_dev, int64_t E,
                                    int64_t N, int64_t K, const void* X_dev, bitsmoe_dtype xt,
@@ -681,7 +681,8 @@ bitsmoe_status bitsmoe_mx4_product_q(const uint8_t* codes_dev, const uint8_t* sc
  * product with glu, dY is that of the 2 N values before it, and N counts them.
  *   dY_dev  [S] rows of N bf16, lddy entries apart
  *   dX_dev  [S] rows of K entries of type xt, ldx entries apart
- * Shape rules as bitsmoe_mx4_product, and N % 8 == 0, lddy % 8 == 0.
+ * Shape rules as bitsmoe_mx4_product (its last one for the sixteens of K), and
+ * N % 8 == 0, lddy % 8 == 0.
  */
 bitsmoe_status bitsmoe_mx4_product_grad(const uint8_t* codes_dev, const uint8_t* scales_dev,
                                         int64_t E, int64_t N, int64_t K, const void* dY_dev,

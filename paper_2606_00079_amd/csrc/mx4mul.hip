@@ -1500,10 +1500,22 @@ bitsmoe_status tile_product(const MulArgs& a, hipStream_t s) {
   return ok();
 }
 
+// A call with more tiles than a launch takes goes to the resident workgroups of the large tiles, unless it has few
+// slots an expert (their walk over the experts is long) or no row that they could read for a slot without one.
+bool large_instead(const MulArgs& a) { return a.S > 8 * static_cast<int64_t>(a.E) && a.x_rows > 0; }
+
 bitsmoe_status product(const char* who, const MulArgs& a, bool glu, hipStream_t s) {
   const bool mx = a.xcodes != nullptr;
-  const Kernel kernel = product_kernel(a, mx, glu);
+  Kernel kernel = product_kernel(a, mx, glu);
   unsigned grid = 0;
+  const bool fits = kernel == kLargeTiles ||
+                    (kernel == kFewSlots ? grid_of(a, few_slots(a), (a.N + (glu ? 127 : 255)) / (glu ? 128 : 256), &grid)
+                                         : grid_of(a, 16, (a.N + 15) / 16, &grid));
+  if (!fits) {
+    if (!large_instead(a))
+      return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": too many slots and outputs for one call");
+    kernel = kLargeTiles;
+  }
   if (kernel == kLargeTiles) {
     // (with MX4 tokens four stages of weights a tile at least, so that a chunk of scales outlives its two)
     const bool al = a.K % 512 == 0 && (!mx || a.K >= 1024);
@@ -1514,8 +1526,6 @@ bitsmoe_status product(const char* who, const MulArgs& a, bool glu, hipStream_t 
   }
   if (kernel == kFewSlots) {
     const bool two = few_slots(a) == 32;
-    if (!grid_of(a, few_slots(a), (a.N + (glu ? 127 : 255)) / (glu ? 128 : 256), &grid))
-      return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": too many slots and outputs for one call");
     auto* fn = two ? (mx ? (glu ? mx4_few_kernel<true, true, 2> : mx4_few_kernel<true, false, 2>)
                          : (glu ? mx4_few_kernel<false, true, 2> : mx4_few_kernel<false, false, 2>))
                    : (mx ? (glu ? mx4_few_kernel<true, true, 1> : mx4_few_kernel<true, false, 1>)
@@ -1525,8 +1535,6 @@ bitsmoe_status product(const char* who, const MulArgs& a, bool glu, hipStream_t 
     BITSMOE_LAUNCH_CHECK("mx4_few_kernel");
     return ok();
   }
-  if (!grid_of(a, 16, (a.N + 15) / 16, &grid))
-    return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": too many slots and outputs for one call");
   auto* fn = mx ? (glu ? mx4_rows_kernel<true, true> : mx4_rows_kernel<true, false>)
                 : (glu ? mx4_rows_kernel<false, true> : mx4_rows_kernel<false, false>);
   KernelTimer timer("mx4_rows", s);
@@ -1585,7 +1593,14 @@ extern "C" bitsmoe_status bitsmoe_mx4_product_grad(const uint8_t* codes_dev, con
     return fail(BITSMOE_ERR_SHAPE, "mx4_product_grad: needs N % 8 == 0, lddy >= N and lddy % 8 == 0");
   if (S == 0) return ok();
   if (!dY_dev) return fail(BITSMOE_ERR_ARG, "mx4_product_grad: null pointer");
-  if (grad_kernel(a) == kLargeTiles) {
+  unsigned grid = 0;
+  Kernel kernel = grad_kernel(a);
+  if (kernel != kLargeTiles && !grid_of(a, few_slots(a), (K + 127) / 128, &grid)) {
+    if (!large_instead(a))
+      return fail(BITSMOE_ERR_SHAPE, "mx4_product_grad: too many slots and columns for one call");
+    kernel = kLargeTiles;
+  }
+  if (kernel == kLargeTiles) {
     static std::atomic<uint64_t> allowed{0};
     if (bitsmoe_status st = allow_lds(reinterpret_cast<const void*>(mx4_grad_tile_kernel), GradShape::kBytes, &allowed))
       return st;
@@ -1594,9 +1609,6 @@ extern "C" bitsmoe_status bitsmoe_mx4_product_grad(const uint8_t* codes_dev, con
     BITSMOE_LAUNCH_CHECK("mx4_grad_tile_kernel");
     return ok();
   }
-  unsigned grid;
-  if (!grid_of(a, few_slots(a), (K + 127) / 128, &grid))
-    return fail(BITSMOE_ERR_SHAPE, "mx4_product_grad: too many slots and columns for one call");
   auto* fn = few_slots(a) == 32 ? mx4_grad_few_kernel<2> : mx4_grad_few_kernel<1>;
   KernelTimer timer("mx4_grad_few", stream);
   fn<<<grid, kTileThreads, 0, static_cast<hipStream_t>(stream)>>>(a);

@@ -157,3 +157,33 @@ def test_slots_before_the_first_expert_and_after_the_last(case):
     want, bound = exact(codes, scales, X, off, grad=form == "grad")
     within(got, want, bound, case)
     assert (got[:off[0]] == 0).all() and (got[off[-1]:] == 0).all()
+
+
+def test_more_tiles_than_a_launch_takes():
+    """The small tiles that cost least here would be more than 2^23 workgroups: the
+    resident large ones take the call instead."""
+    g = np.random.default_rng(17)
+    S, T, first = (1 << 27) + 77, 64, (1 << 26) + 3
+    codes, scales = weights(2, 1, 32, g)
+    X = torch.randn(T, 32, device=DEV).to(torch.bfloat16)
+    rows = torch.randint(0, T, (S,), dtype=torch.int32, device=DEV)
+    off = torch.tensor([0, first, S], dtype=torch.int32, device=DEV)
+    got = taken("mx4_tile", lambda: bm.mx4_product(codes, scales, X, offsets=off, rows=rows))
+    w = values(codes, scales)[:, 0]
+    table, size = X.double() @ w.t().contiguous(), X.double().abs() @ w.t().contiguous().abs()
+    for e, at in ((0, slice(0, first)), (1, slice(first, S))):
+        r = rows[at].long()
+        want = table[:, e][r]
+        within(got[at, 0], want, size[:, e][r] * 48 * U + 2.0 ** -8 * want.abs(), ("forward", e))
+    del got, rows, r, want
+    S, first = (1 << 28) + 40, (1 << 27) + 9
+    codes, scales = weights(2, 8, 32, g)
+    dY = torch.randn(1 << 20, 8, device=DEV).to(torch.bfloat16).repeat(257, 1)[:S]
+    off = torch.tensor([0, first, S], dtype=torch.int32, device=DEV)
+    got = taken("mx4_grad_tile", lambda: bm.mx4_product_grad(codes, scales, dY, offsets=off))
+    w = values(codes, scales)
+    cuts = sorted({0, first, S, *range(0, S, 1 << 24)})
+    for lo, hi in zip(cuts, cuts[1:]):
+        e, d = int(lo >= first), dY[lo:hi].double()
+        want = d @ w[e]
+        within(got[lo:hi], want, d.abs() @ w[e].abs() * 24 * U + 2.0 ** -8 * want.abs(), ("gradient", lo))
