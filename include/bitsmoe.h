@@ -48,6 +48,7 @@
  * An MoE layer around the experts, with the experts' weights in microscaled
  * 4-bit floats (MX4), for serving and for training what is not quantized:
  *   bitsmoe_route             top-k experts, weights, expert order, losses (device)
+ *   bitsmoe_route_ws          the same in a workspace of the caller's       (device)
  *   bitsmoe_route_grad        gradient of the router's logits               (device)
  *   bitsmoe_mx4_quantize      rows to MX4, and bitsmoe_mx4_dequantize back  (device)
  *   bitsmoe_mx4_product       y_s = W_e(s) x_s, bf16 tokens                 (device)
@@ -55,7 +56,9 @@
  *   bitsmoe_mx4_product_grad  dx_s = W_e(s)^T dy_s                          (device)
  *   bitsmoe_combine           y_t = sum_j w_tj z_{slot(t,j)}                (device)
  *   bitsmoe_combine_grad      its gradients                                 (device)
- * No call of these waits for the stream or reads anything back to the host.
+ * None of these reads anything back to the host, and only bitsmoe_route uses the
+ * library's scratch (and waits for the stream where that has to grow): the others
+ * may overlap on streams of their own and be captured in graphs.
  *
  * Conventions shared by every call:
  *  - Pointers named *_dev are device memory on the current HIP device;
@@ -591,13 +594,31 @@ bitsmoe_status bitsmoe_unpack(const uint64_t* codes_dev, const uint16_t* params_
  * Sums are fp32 in a fixed order.  T may be 0 (counts, offsets and losses are
  * zero).  Shape rules: 1 <= k <= min(E, BITSMOE_ROUTE_MAX_K), E <= 4096,
  * ld >= E, T k < 2^31.  Uses the library's scratch when T > 128 (16 where E >
- * 512), which a first call of such a size allocates (so not under graph capture).
+ * 512): such calls must not overlap with others that use it, and are refused
+ * under graph capture (BITSMOE_ERR_ARG).
  */
 bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt, int64_t T, int64_t E,
                              int64_t ld, int64_t k, const uint8_t* valid_dev, int renorm,
                              int32_t* experts_dev, float* weights_dev, int32_t* counts_dev,
                              int32_t* offsets_dev, int32_t* rows_dev, int32_t* slots_dev,
                              float* lse_dev, float* losses_dev, void* stream);
+
+/* Bytes of the workspace of bitsmoe_route_ws for T rows and E experts: 0 up to 16
+ * rows, and up to 128 with E <= 512. */
+int64_t bitsmoe_route_workspace(int64_t T, int64_t E);
+
+/*
+ * bitsmoe_route with the caller's workspace work_dev of work_bytes bytes (NULL
+ * where bitsmoe_route_workspace gives 0), in use until the call's work on the
+ * stream is done.  Allocates nothing and never waits: for graph capture, and for
+ * calls that overlap on different streams.
+ */
+bitsmoe_status bitsmoe_route_ws(const void* logits_dev, bitsmoe_dtype lt, int64_t T, int64_t E,
+                                int64_t ld, int64_t k, const uint8_t* valid_dev, int renorm,
+                                int32_t* experts_dev, float* weights_dev, int32_t* counts_dev,
+                                int32_t* offsets_dev, int32_t* rows_dev, int32_t* slots_dev,
+                                float* lse_dev, float* losses_dev, void* work_dev,
+                                int64_t work_bytes, void* stream);
 
 /*
  * Gradient of the logits from those of the weights, dweights_dev [T][k], and

@@ -54,7 +54,8 @@ EXPORTS = [
     "bitsmoe_project_in", "bitsmoe_basis_importance", "bitsmoe_score_diag",
     "bitsmoe_gram_routed", "bitsmoe_score_routed", "bitsmoe_moe_decode",
     "bitsmoe_moe_decode_topk", "bitsmoe_shared_basis_gpu", "bitsmoe_moe_decode_in",
-    "bitsmoe_moe_decode_topk_noalloc", "bitsmoe_route", "bitsmoe_route_grad",
+    "bitsmoe_moe_decode_topk_noalloc", "bitsmoe_route", "bitsmoe_route_ws", "bitsmoe_route_workspace",
+    "bitsmoe_route_grad",
     "bitsmoe_mx4_quantize", "bitsmoe_mx4_dequantize", "bitsmoe_mx4_product",
     "bitsmoe_mx4_product_q", "bitsmoe_mx4_product_grad", "bitsmoe_combine",
     "bitsmoe_combine_grad",
@@ -122,6 +123,8 @@ def lib() -> ctypes.CDLL:
                                           i64, i64, vp, vp, vp, vp]
     L.bitsmoe_moe_decode_topk_noalloc.argtypes = L.bitsmoe_moe_decode_topk.argtypes
     L.bitsmoe_route.argtypes = [vp, i32, i64, i64, i64, i64, vp, i32] + [vp] * 9
+    L.bitsmoe_route_ws.argtypes = [vp, i32, i64, i64, i64, i64, vp, i32] + [vp] * 9 + [i64, vp]
+    L.bitsmoe_route_workspace.argtypes = [i64, i64]
     L.bitsmoe_route_grad.argtypes = [vp, i32, i64, i64, i64, i64, i32] + [vp] * 8
     L.bitsmoe_mx4_quantize.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp]
     L.bitsmoe_mx4_dequantize.argtypes = [vp, vp, i64, i64, vp, i32, vp]
@@ -140,9 +143,10 @@ def lib() -> ctypes.CDLL:
     L.bitsmoe_last_error.restype = ctypes.c_char_p
     L.bitsmoe_version.restype = ctypes.c_char_p
     for name in EXPORTS:
-        if name not in ("bitsmoe_last_error", "bitsmoe_version", "bitsmoe_release"):
+        if name not in ("bitsmoe_last_error", "bitsmoe_version", "bitsmoe_release", "bitsmoe_route_workspace"):
             getattr(L, name).restype = ctypes.c_int
     L.bitsmoe_release.restype = None
+    L.bitsmoe_route_workspace.restype = i64
     lp = _find_lapack()
     if lp and os.environ.get("BITSMOE_LAPACK") is None:
         L.bitsmoe_set_lapack(lp.encode())
@@ -630,8 +634,12 @@ def route(logits, k: int, valid=None, renorm: bool = True) -> Routing:
     ip, fp = ints.data_ptr(), floats.data_ptr()
     ex, co, of, ro, sl = ip, ip + 12 * n4, ip + 12 * n4 + 4 * e4, ip + 4 * n4, ip + 8 * n4
     we, ls, lo = fp, fp + 4 * n4, fp + 4 * (n4 + t4)
-    _check(lib().bitsmoe_route(lp, _code(logits, "logits", torch), T, E, ld, k, vp, int(renorm), ex, we,
-                               co, of, ro, sl, ls, lo, stream), "route")
+    L = lib()
+    # (a workspace of the call's own: it may overlap with others, and a graph that it is captured in keeps it)
+    room = L.bitsmoe_route_workspace(T, E) if T > 16 else 0
+    work = logits.new_empty((room,), dtype=torch.uint8) if room else None
+    _check(L.bitsmoe_route_ws(lp, _code(logits, "logits", torch), T, E, ld, k, vp, int(renorm), ex, we, co, of,
+                              ro, sl, ls, lo, work.data_ptr() if room else None, room, stream), "route")
     return Routing(ints.as_strided((T, w), (w, 1), 0), floats.as_strided((T, w), (w, 1), 0),
                    ints.as_strided((E + 1,), (1,), 3 * n4), ints.as_strided((E + 1,), (1,), 3 * n4 + e4),
                    ints.as_strided((n,), (1,), n4), ints.as_strided((T, w), (w, 1), 2 * n4),

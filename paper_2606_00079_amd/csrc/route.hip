@@ -643,23 +643,55 @@ bool wide_rows(const void* p, bitsmoe_dtype lt, int64_t E, int64_t ld) {
   return aligned16({p}) && ld * size % 16 == 0 && E % 8 == 0;
 }
 
-}  // namespace
-}  // namespace bitsmoe
+// How a call's rows are cut into runs, and the bytes that more than one run takes for each one's sums (and the
+// totals after them).
+struct Runs {
+  int64_t run, runs;
+  size_t table, bytes;  // of counts (as of probabilities), in all
+};
+Runs runs_of(int64_t T, int64_t E) {
+  int64_t run = (T + kMaxRuns - 1) / kMaxRuns;
+  if (run < kMinRun) run = kMinRun;
+  if (run > kMaxRun) run = kMaxRun;
+  // (three launches take longer than one workgroup's few rounds)
+  if (T <= kOneRun && E <= 512) run = T;
+  Runs r{run, run > 0 ? (T + run - 1) / run : 0, 0, 0};
+  if (r.runs > 1) {
+    r.table = (size_t(r.runs + 1) * E * 4 + 255) & ~size_t(255);
+    r.bytes = 2 * r.table + size_t(r.runs) * 8;
+  }
+  return r;
+}
 
-using namespace bitsmoe;
+// Room for the runs' sums out of the library's scratch.
+void* run_scratch(size_t bytes, void* stream, bitsmoe_status* st) {
+  // A graph would keep the address, which a later, larger call of any operator that uses this scratch frees.
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  const hipError_t e = hipStreamIsCapturing(static_cast<hipStream_t>(stream), &capture);
+  if (e != hipSuccess) {
+    *st = device_error("route: hipStreamIsCapturing", e);
+    return nullptr;
+  }
+  if (capture != hipStreamCaptureStatusNone) {
+    *st = fail(BITSMOE_ERR_ARG, "route: under graph capture this many rows need bitsmoe_route_ws");
+    return nullptr;
+  }
+  return scratch(kScratchMisc, bytes, stream, st);
+}
 
-extern "C" bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt, int64_t T, int64_t E,
-                                        int64_t ld, int64_t k, const uint8_t* valid_dev, int renorm,
-                                        int32_t* experts_dev, float* weights_dev, int32_t* counts_dev,
-                                        int32_t* offsets_dev, int32_t* rows_dev, int32_t* slots_dev,
-                                        float* lse_dev, float* losses_dev, void* stream) {
-  if (bitsmoe_status st = check("route", logits_dev, lt, T, E, ld, k)) return st;
+// Both forms of the call: with a workspace, or (`own`) out of the library's scratch.
+bitsmoe_status run_route(const char* who, const void* logits_dev, bitsmoe_dtype lt, int64_t T, int64_t E, int64_t ld,
+                         int64_t k, const uint8_t* valid_dev, int renorm, int32_t* experts_dev, float* weights_dev,
+                         int32_t* counts_dev, int32_t* offsets_dev, int32_t* rows_dev, int32_t* slots_dev,
+                         float* lse_dev, float* losses_dev, bool own, void* work_dev, int64_t work_bytes,
+                         void* stream) {
+  if (bitsmoe_status st = check(who, logits_dev, lt, T, E, ld, k)) return st;
   if (!counts_dev || !offsets_dev || !losses_dev ||
       (T > 0 && (!experts_dev || !weights_dev || !rows_dev || !slots_dev || !lse_dev)))
-    return fail(BITSMOE_ERR_ARG, "route: null pointer");
+    return fail(BITSMOE_ERR_ARG, std::string(who) + ": null pointer");
   if (!aligned16({logits_dev, experts_dev, weights_dev, counts_dev, offsets_dev, rows_dev, slots_dev, lse_dev,
                   losses_dev}))
-    return fail(BITSMOE_ERR_ARG, "route: device pointers must be 16-byte aligned");
+    return fail(BITSMOE_ERR_ARG, std::string(who) + ": device pointers must be 16-byte aligned");
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (T == 0) {
     route_none_kernel<<<1, 256, 0, s>>>(static_cast<int>(E), counts_dev, offsets_dev, losses_dev);
@@ -683,22 +715,19 @@ extern "C" bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt
   a.slots = slots_dev;
   a.lse = lse_dev;
   a.losses = losses_dev;
-  int64_t run = (T + kMaxRuns - 1) / kMaxRuns;
-  if (run < kMinRun) run = kMinRun;
-  if (run > kMaxRun) run = kMaxRun;
-  // (three launches take longer than one workgroup's few rounds)
-  if (T <= kOneRun && E <= 512) run = T;
-  const int64_t runs = (T + run - 1) / run;
+  const Runs cut = runs_of(T, E);
+  const int64_t run = cut.run, runs = cut.runs;
   a.run = static_cast<int>(run);
   a.runs = static_cast<int>(runs);
   if (runs > 1) {
-    bitsmoe_status st;
-    const size_t nc = ((size_t(runs + 1) * E * 4) + 255) & ~size_t(255), np = nc;  // (the totals after the last run)
-    char* p = static_cast<char*>(scratch(kScratchMisc, nc + np + size_t(runs) * 8, stream, &st));
-    if (!p) return st;
+    bitsmoe_status st = BITSMOE_OK;
+    char* p = static_cast<char*>(own ? run_scratch(cut.bytes, stream, &st) : work_dev);
+    if (st) return st;
+    if (!own && (!p || work_bytes < static_cast<int64_t>(cut.bytes) || !aligned16({p})))
+      return fail(BITSMOE_ERR_ARG, std::string(who) + ": the workspace is missing, too small or misaligned");
     a.run_counts = reinterpret_cast<int32_t*>(p);
-    a.run_probs = reinterpret_cast<float*>(p + nc);
-    a.run_z = reinterpret_cast<float*>(p + nc + np);
+    a.run_probs = reinterpret_cast<float*>(p + cut.table);
+    a.run_z = reinterpret_cast<float*>(p + 2 * cut.table);
     a.run_n = reinterpret_cast<int32_t*>(a.run_z + runs);
   }
   bitsmoe_status st = BITSMOE_OK;
@@ -734,6 +763,34 @@ extern "C" bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt
     BITSMOE_LAUNCH_CHECK("route_place_kernel");
   }
   return ok();
+}
+
+}  // namespace
+}  // namespace bitsmoe
+
+using namespace bitsmoe;
+
+extern "C" int64_t bitsmoe_route_workspace(int64_t T, int64_t E) {
+  if (T <= 0 || T >= (int64_t(1) << 31) || E <= 0 || E > kMaxExperts) return 0;
+  return static_cast<int64_t>(runs_of(T, E).bytes);
+}
+
+extern "C" bitsmoe_status bitsmoe_route_ws(const void* logits_dev, bitsmoe_dtype lt, int64_t T, int64_t E, int64_t ld,
+                                           int64_t k, const uint8_t* valid_dev, int renorm, int32_t* experts_dev,
+                                           float* weights_dev, int32_t* counts_dev, int32_t* offsets_dev,
+                                           int32_t* rows_dev, int32_t* slots_dev, float* lse_dev, float* losses_dev,
+                                           void* work_dev, int64_t work_bytes, void* stream) {
+  return run_route("route_ws", logits_dev, lt, T, E, ld, k, valid_dev, renorm, experts_dev, weights_dev, counts_dev,
+                   offsets_dev, rows_dev, slots_dev, lse_dev, losses_dev, false, work_dev, work_bytes, stream);
+}
+
+extern "C" bitsmoe_status bitsmoe_route(const void* logits_dev, bitsmoe_dtype lt, int64_t T, int64_t E,
+                                        int64_t ld, int64_t k, const uint8_t* valid_dev, int renorm,
+                                        int32_t* experts_dev, float* weights_dev, int32_t* counts_dev,
+                                        int32_t* offsets_dev, int32_t* rows_dev, int32_t* slots_dev,
+                                        float* lse_dev, float* losses_dev, void* stream) {
+  return run_route("route", logits_dev, lt, T, E, ld, k, valid_dev, renorm, experts_dev, weights_dev, counts_dev,
+                   offsets_dev, rows_dev, slots_dev, lse_dev, losses_dev, true, nullptr, 0, stream);
 }
 
 extern "C" bitsmoe_status bitsmoe_route_grad(const void* logits_dev, bitsmoe_dtype lt, int64_t T, int64_t E,

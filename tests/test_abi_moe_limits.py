@@ -26,3 +26,28 @@ def test_products_refuse_slots_whose_tiles_would_end_past_31_bits(lib, S):
     assert lib.bitsmoe_mx4_product_q(P, P, 2, 2048, 1024, P, P, x_rows, P, P, S, 0, P, BF16, 2048, None) == SHAPE
     assert lib.bitsmoe_mx4_product_grad(P, P, 2, 512, 2048, P, BF16, 512, P, S, P, BF16, 2048, None) == SHAPE
     assert lib.bitsmoe_last_error()
+
+
+def test_route_workspace(lib):
+    """Room for the sums of more than one run of rows; none up to 16 rows, or 128 of up to 512 experts."""
+    size = lib.bitsmoe_route_workspace
+    assert size(0, 8) == size(-3, 8) == size(100, 0) == size(100, 4097) == size(1 << 31, 8) == 0
+    assert size(16, 4096) == size(128, 512) == 0
+    for T, E in [(17, 513), (129, 1), (129, 512), (4096, 128), (16384, 256), (32769, 60), (1 << 20, 4096)]:
+        run = min(max(-(-T // 256), 16), 128)
+        runs = -(-T // run)
+        assert size(T, E) >= 2 * 4 * E * (runs + 1) + 8 * runs, (T, E)
+
+
+@pytest.mark.parametrize("work,room", [(None, 1 << 30), (P, 100), (P + 4, 1 << 30)])
+def test_route_refuses_a_workspace_that_is_none(lib, work, room):
+    """Missing, too small, misaligned."""
+    assert lib.bitsmoe_route_ws(P, BF16, 300, 8, 8, 2, None, 1, P, P, P, P, P, P, P, P, work, room, None) == ARG
+    assert b"workspace" in lib.bitsmoe_last_error()
+
+
+def test_route_with_a_workspace_checks_the_rest_as_well(lib):
+    a = [P, BF16, 300, 8, 8, 2, None, 1, P, P, P, P, P, P, P, P, P, 1 << 30, None]
+    for at, value, status in [(0, None, ARG), (1, 5, DTYPE), (2, -1, ARG), (4, 7, SHAPE), (5, 9, SHAPE), (8, None, ARG),
+                              (13, P + 4, ARG)]:
+        assert lib.bitsmoe_route_ws(*a[:at], value, *a[at + 1:]) == status, at

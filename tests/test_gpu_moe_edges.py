@@ -187,3 +187,107 @@ def test_more_tiles_than_a_launch_takes():
         e, d = int(lo >= first), dY[lo:hi].double()
         want = d @ w[e]
         within(got[lo:hi], want, d.abs() @ w[e].abs() * 24 * U + 2.0 ** -8 * want.abs(), ("gradient", lo))
+
+
+# ----------------------------------------------------------------- router
+def grow_scratch():
+    """A call of another operator that needs more of the library's scratch than any before."""
+    logits = torch.randn(1 << 18, 512, device=DEV)
+    k, T, E = 1, *logits.shape
+    new = lambda n, dt: torch.empty(n, dtype=dt, device=DEV)  # noqa: E731
+    i, f = torch.int32, torch.float32
+    out = [new(T * k, i), new(T * k, f), new(E + 1, i), new(E + 1, i), new(T * k, i), new(T * k, i), new(T, f), new(2, f)]
+    st = bm.lib().bitsmoe_route(logits.data_ptr(), bm.F32, T, E, E, k, None, 1, *(t.data_ptr() for t in out),
+                                torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert st == 0
+    return out
+
+
+def equal(a, b):
+    return all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+def test_a_captured_router_of_many_rows_outlives_the_scratch():
+    g = torch.Generator(device=DEV).manual_seed(4)
+    x = torch.randn(3000, 96, generator=g, device=DEV)
+    bm.route(x, 4)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r = bm.route(x, 4)
+    for turn in range(4):
+        x.copy_(torch.randn(x.shape, generator=g, device=DEV))
+        if turn == 1:
+            grow_scratch()
+        graph.replay()
+        want = bm.route(x, 4)
+        torch.cuda.synchronize()
+        assert equal(r, want), turn
+
+
+def test_routers_of_many_rows_on_two_streams():
+    g = torch.Generator(device=DEV).manual_seed(5)
+    xs = [torch.randn(20000, 64, generator=g, device=DEV) for _ in range(2)]
+    want = [bm.route(x, 6) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    got = [[], []]
+    for _ in range(20):
+        for x, s, into in zip(xs, streams, got):
+            with torch.cuda.stream(s):
+                into.append(bm.route(x, 6))
+    torch.cuda.synchronize()
+    for w, several in zip(want, got):
+        assert all(equal(r, w) for r in several)
+
+
+def test_the_call_without_a_workspace():
+    """The same results out of the library's scratch; refused under capture, which it leaves as it was."""
+    x = torch.randn(3000, 96, device=DEV)
+    T, E, k = 3000, 96, 4
+    want = bm.route(x, k)
+    out = [torch.empty_like(t) for t in (want.experts, want.weights, want.counts, want.offsets, want.rows, want.slots,
+                                         want.lse, want.losses)]
+    args = [x.data_ptr(), bm.F32, T, E, E, k, None, 1, *(t.data_ptr() for t in out)]
+    assert bm.lib().bitsmoe_route(*args, torch.cuda.current_stream().cuda_stream) == 0
+    assert equal(out, (want.experts, want.weights, want.counts, want.offsets, want.rows, want.slots, want.lse,
+                       want.losses))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        st = bm.lib().bitsmoe_route(*args, torch.cuda.current_stream().cuda_stream)
+        text = bm.lib().bitsmoe_last_error()
+        r = bm.route(x, k)
+    assert st == 1 and b"capture" in text
+    graph.replay()
+    torch.cuda.synchronize()
+    assert equal(r, want)
+
+
+@pytest.mark.parametrize("T,E,k", [(32769, 24, 3), (70001, 8, 2)])
+def test_route_of_more_rows_than_the_longest_256_runs(T, E, k):
+    """Whole numbers against a stable sort, sums against 64 bits."""
+    g = torch.Generator(device=DEV).manual_seed(T)
+    x = torch.randn(T, E, generator=g, device=DEV)
+    valid = torch.rand(T, generator=g, device=DEV) < 0.9
+    r = bm.route(x, k, valid=valid)
+    p = torch.softmax(x.double(), 1) * valid[:, None]
+    top = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :k]  # (ties: the lowest index)
+    ex = torch.where(valid[:, None], top, -1)
+    assert torch.equal(r.experts.long(), ex)
+    w = x.double().gather(1, ex.clamp(min=0))
+    w = torch.softmax(w, 1) * valid[:, None]
+    within(r.weights, w, w * (k + 70) * U, "weights")
+    bucket = torch.where(ex < 0, E, ex).flatten()
+    order = torch.sort(bucket, stable=True).indices
+    counts = torch.bincount(bucket, minlength=E + 1)[:E]
+    n = int(valid.sum())
+    assert torch.equal(r.counts.long(), torch.cat((counts, valid.sum()[None])))
+    assert torch.equal(r.offsets[1:].long(), counts.cumsum(0)) and int(r.offsets[0]) == 0
+    assert torch.equal(r.rows.long(), order // k)
+    assert torch.equal(r.slots.flatten()[order].long(), torch.arange(T * k, device=DEV))
+    lse = torch.logsumexp(x.double(), 1)
+    z = (lse[valid] ** 2).mean()
+    balance = E / (k * n * n) * (counts * p.sum(0)).sum()
+    # a sum over the rows: at most 128 of a run, 32 parts of the runs, and as many again
+    within(r.losses, torch.stack((balance, z)), torch.stack((balance, z)) * 2000 * U, "losses")
