@@ -56,6 +56,7 @@
  *   bitsmoe_mx4_product_grad  dx_s = W_e(s)^T dy_s                          (device)
  *   bitsmoe_combine           y_t = sum_j w_tj z_{slot(t,j)}                (device)
  *   bitsmoe_combine_grad      its gradients                                 (device)
+ *   bitsmoe_combine_grad_all  the same, with 0 in the rows of no slot       (device)
  * None of these reads anything back to the host, and only bitsmoe_route uses the
  * library's scratch (and waits for the stream where that has to grow): the others
  * may overlap on streams of their own and be captured in graphs.
@@ -736,6 +737,21 @@ bitsmoe_status bitsmoe_combine_grad(const void* Z_dev, bitsmoe_dtype zt, int64_t
                                     const int32_t* slots_dev, const float* weights_dev,
                                     const void* dY_dev, int64_t T, int64_t k, int64_t d,
                                     void* dZ_dev, float* dweights_dev, void* stream);
+
+/* Most slots T k of bitsmoe_combine_grad_all without a workspace. */
+#define BITSMOE_COMBINE_SCAN 16384
+
+/*
+ * bitsmoe_combine_grad, and rows of dZ_dev that no slot names get 0, as they had
+ * no part in the sums (slots that were dropped, or are joined elsewhere).
+ *   work_dev  [S] int32, contents of no matter; NULL allowed where T k <=
+ *             BITSMOE_COMBINE_SCAN
+ */
+bitsmoe_status bitsmoe_combine_grad_all(const void* Z_dev, bitsmoe_dtype zt, int64_t S,
+                                        const int32_t* slots_dev, const float* weights_dev,
+                                        const void* dY_dev, int64_t T, int64_t k, int64_t d,
+                                        void* dZ_dev, float* dweights_dev, int32_t* work_dev,
+                                        void* stream);
 
 /* Path of a LAPACK shared library for bitsmoe_shared_basis (LP64 or ILP64
  * dsyevd; both plain and "64_"-suffixed symbol names are tried).  When never

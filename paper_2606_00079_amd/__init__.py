@@ -58,10 +58,11 @@ EXPORTS = [
     "bitsmoe_route_grad",
     "bitsmoe_mx4_quantize", "bitsmoe_mx4_dequantize", "bitsmoe_mx4_product",
     "bitsmoe_mx4_product_q", "bitsmoe_mx4_product_grad", "bitsmoe_combine",
-    "bitsmoe_combine_grad",
+    "bitsmoe_combine_grad", "bitsmoe_combine_grad_all",
 ]
 # Candidate widths of the surrogate table, in column order.
 SURROGATE_WIDTHS = (0, 1, 2, 3, 4, 6, 8, 16)
+_COMBINE_SCAN = 16384  # BITSMOE_COMBINE_SCAN
 
 
 class BitsmoeError(RuntimeError):
@@ -136,6 +137,7 @@ def lib() -> ctypes.CDLL:
                                            i64, vp]
     L.bitsmoe_combine.argtypes = [vp, i32, i64, vp, vp, i64, i64, i64, vp, vp]
     L.bitsmoe_combine_grad.argtypes = [vp, i32, i64, vp, vp, vp, i64, i64, i64, vp, vp, vp]
+    L.bitsmoe_combine_grad_all.argtypes = [vp, i32, i64, vp, vp, vp, i64, i64, i64, vp, vp, vp, vp]
     L.bitsmoe_set_lapack.argtypes = [ctypes.c_char_p]
     L.bitsmoe_timing.argtypes = [i32]
     L.bitsmoe_timing_only.argtypes = [ctypes.c_char_p]
@@ -786,8 +788,8 @@ def combine(Z, slots, weights=None, out=None):
 
 
 def combine_grad(Z, slots, weights, dY):
-    """Gradients of ``combine``: (dZ [S][d], dweights fp32 [T][k]).  Every row of Z
-    is taken to be named by one slot, as ``route`` does."""
+    """Gradients of ``combine``: (dZ [S][d], dweights fp32 [T][k]).  A row of Z that
+    no slot names has gradient 0; none may be named twice."""
     torch, stream = _place(Z, "Z")
     if Z.dim() != 2 or slots.dim() != 2:
         raise ValueError("Z must be [S][d] and slots [T][k]")
@@ -795,10 +797,11 @@ def combine_grad(Z, slots, weights, dY):
     zp = _in(Z, "Z", Z, Z.dtype)
     dZ = Z.new_empty((S, d), dtype=Z.dtype)
     dw = Z.new_empty((T, k), dtype=torch.float32)
-    _check(lib().bitsmoe_combine_grad(zp, _code(Z, "Z", torch), S, _in(slots, "slots", Z, torch.int32),
-                                      _in(weights, "weights", Z, torch.float32, (T, k)),
-                                      _in(dY, "dY", Z, Z.dtype, (T, d)), T, k, d, dZ.data_ptr(),
-                                      dw.data_ptr(), stream), "combine_grad")
+    work = Z.new_empty((S,), dtype=torch.int32) if T * k > _COMBINE_SCAN else None
+    _check(lib().bitsmoe_combine_grad_all(zp, _code(Z, "Z", torch), S, _in(slots, "slots", Z, torch.int32),
+                                          _in(weights, "weights", Z, torch.float32, (T, k)),
+                                          _in(dY, "dY", Z, Z.dtype, (T, d)), T, k, d, dZ.data_ptr(), dw.data_ptr(),
+                                          None if work is None else work.data_ptr(), stream), "combine_grad")
     return dZ, dw
 
 

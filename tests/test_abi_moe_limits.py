@@ -51,3 +51,23 @@ def test_route_with_a_workspace_checks_the_rest_as_well(lib):
     for at, value, status in [(0, None, ARG), (1, 5, DTYPE), (2, -1, ARG), (4, 7, SHAPE), (5, 9, SHAPE), (8, None, ARG),
                               (13, P + 4, ARG)]:
         assert lib.bitsmoe_route_ws(*a[:at], value, *a[at + 1:]) == status, at
+
+
+ALL = dict(Z=P, zt=BF16, S=4, slots=P, weights=P, dY=P, T=2, k=2, d=64, dZ=P, dweights=P, work=None, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (ARG, {"Z": None}), (ARG, {"slots": None}), (ARG, {"dY": None}), (ARG, {"dZ": None}), (ARG, {"T": 0, "dZ": None}),
+    (ARG, {"T": 8193}),  # more than 16384 slots, and no workspace
+    (ARG, {"T": 8193, "work": P + 4}), (DTYPE, {"zt": 7}), (SHAPE, {"d": 12}), (SHAPE, {"k": 65}),
+    (SHAPE, {"T": 1 << 24, "work": P}),
+])
+def test_combine_grad_all(lib, status, change):
+    assert lib.bitsmoe_combine_grad_all(*{**ALL, **change}.values()) == status, change
+    assert lib.bitsmoe_last_error()
+
+
+def test_combine_grad_all_of_nothing(lib):
+    n = None
+    assert lib.bitsmoe_combine_grad_all(n, BF16, 0, n, n, n, 0, 2, 64, n, n, n, n) == OK
+    assert lib.bitsmoe_last_error() == b""

@@ -10,6 +10,7 @@ import pytest
 
 from conftest import gpu_available
 from oracle import mx4 as omx4
+from oracle import route as oroute
 
 pytestmark = pytest.mark.gpu
 
@@ -291,3 +292,48 @@ def test_route_of_more_rows_than_the_longest_256_runs(T, E, k):
     balance = E / (k * n * n) * (counts * p.sum(0)).sum()
     # a sum over the rows: at most 128 of a run, 32 parts of the runs, and as many again
     within(r.losses, torch.stack((balance, z)), torch.stack((balance, z)) * 2000 * U, "losses")
+
+
+# ---------------------------------------------------------------- joining
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,k,S,d", [(1, 1, 3000, 8), (4, 2, 6, 16), (300, 8, 2400, 72), (300, 8, 7000, 40), (512, 8, 100, 64),
+                                     (0, 2, 37, 64), (700, 6, 4200, 264), (16384, 1, 20000, 24),
+                                     (2049, 8, 17000, 40), (16385, 1, 1200000, 8), (900, 8, 5, 8),
+                                     (66000, 1, 33, 8)])
+def test_gradient_of_rows_that_no_slot_names(T, k, S, d, dtype):
+    """0, whatever the memory held, for few slots and for many."""
+    g = np.random.default_rng([T, k, S, d])
+    n = T * k
+    at = np.r_[g.permutation(S), -1 - g.integers(0, 9, max(n, 1)), S + g.integers(0, 9, max(n, 1))][:max(2 * n, S)]
+    slots = g.permutation(at)[:n].reshape(T, k).astype(np.int32)  # (a row once at most; some name none)
+    Z = torch.randn(S, d, device=DEV).to(DT[dtype])
+    dY = torch.randn(T, d, device=DEV).to(DT[dtype])
+    w = torch.randn(T, k, device=DEV)
+    want, wdw = oroute.combine_grad(Z.double().cpu().numpy(), slots, w.double().cpu().numpy(), dY.double().cpu().numpy())
+    mags = oroute.combine_grad(Z.double().abs().cpu().numpy(), slots, w.double().cpu().numpy(),
+                               dY.double().abs().cpu().numpy())[1]
+    want, wdw, mags = (torch.from_numpy(x).to(DEV) for x in (want, wdw, mags))
+    unnamed = torch.ones(S, dtype=torch.bool, device=DEV)
+    unnamed[torch.from_numpy(slots[(slots >= 0) & (slots < S)].astype(np.int64)).to(DEV)] = False
+    slots = torch.from_numpy(slots).to(DEV)
+    bound = want.abs() * (U + (2.0 ** -8 if dtype == "bf16" else 0))
+    p = lambda t: t.data_ptr() if t is not None and t.numel() else None  # noqa: E731
+    # what the workspace holds does not matter: nothing of use, places of slots, places of slots that name the row
+    works = [torch.full((S,), -1, device=DEV), torch.randint(0, max(n, 1), (S,), device=DEV),
+             torch.arange(S, device=DEV) % max(n, 1), torch.full((S,), 0x7FFFFFFF, device=DEV)]
+    if n <= 16384:
+        works.append(None)
+    for work in works:
+        work = None if work is None else work.to(torch.int32)
+        dz, dw = torch.full((S, d), torch.nan, device=DEV).to(DT[dtype]), torch.full((T, k), torch.nan, device=DEV)
+        st = bm.lib().bitsmoe_combine_grad_all(p(Z), bm.BF16 if dtype == "bf16" else bm.F32, S, p(slots), p(w), p(dY), T,
+                                               k, d, p(dz), p(dw), p(work), torch.cuda.current_stream().cuda_stream)
+        assert st == 0, bm.lib().bitsmoe_last_error()
+        within(dz, want, bound, "dz")
+        assert (dz[unnamed] == 0).all()
+        within(dw, wdw, mags * (d + 16) * U, "dw")
+    junk = torch.full((S, d), torch.nan, device=DEV).to(DT[dtype])
+    del junk  # (its memory is what a new tensor of this size gets)
+    dz, dw = bm.combine_grad(Z, slots, w, dY)
+    within(dz, want, bound, "dz of the binding")
+    within(dw, wdw, mags * (d + 16) * U, "dw of the binding")
