@@ -303,7 +303,7 @@ class Mx4Saved:
     """What the gradients of a layer read."""
     routing: Routing
     logits: object
-    up: object       # [S][2 N] bf16: the gate and up values
+    up: object       # [S][2 N] fp32: the gate and up values, not rounded
     z: object        # [S][K] bf16: the experts' outputs
     renorm: bool
 
@@ -317,14 +317,15 @@ def mx4_layer(x, logits, experts: Mx4Experts, k: int, valid=None, renorm: bool =
     import torch
     r = route(logits, k, valid=valid, renorm=renorm)
 
-    def product(codes, scales, v, rows, glu):
+    def product(codes, scales, v, rows, glu, dtype=None):
         if quantize_tokens:
-            return mx4_product_q(codes, scales, *mx4_quantize(v), offsets=r.offsets, rows=rows, glu=glu)
-        return mx4_product(codes, scales, v, offsets=r.offsets, rows=rows, glu=glu)
+            return mx4_product_q(codes, scales, *mx4_quantize(v), offsets=r.offsets, rows=rows, glu=glu, dtype=dtype)
+        return mx4_product(codes, scales, v, offsets=r.offsets, rows=rows, glu=glu, dtype=dtype)
 
-    up = product(experts.up_codes, experts.up_scales, x, r.rows, not train)
+    # (in training gate and up are kept, and stay fp32 up to silu(g) u as they do within the product with glu)
+    up = product(experts.up_codes, experts.up_scales, x, r.rows, not train, torch.float32 if train else None)
     if train:
-        g, u = up.float().chunk(2, dim=1)
+        g, u = up.chunk(2, dim=1)
         h = (torch.nn.functional.silu(g) * u).to(torch.bfloat16)
     else:
         h = up
@@ -342,7 +343,7 @@ def mx4_layer_grad(saved: Mx4Saved, experts: Mx4Experts, dy, dlosses=None):
     dz, dw = combine_grad(saved.z, r.slots, r.weights, dy)
     dh = mx4_product_grad(experts.down_codes, experts.down_scales, dz, offsets=r.offsets,
                           dtype=torch.float32)
-    g, u = saved.up.float().chunk(2, dim=1)
+    g, u = saved.up.chunk(2, dim=1)
     sig = torch.sigmoid(g)
     dup = torch.cat((dh * u * sig * (1 + g * (1 - sig)), dh * g * sig), 1).to(torch.bfloat16)
     dx = combine(mx4_product_grad(experts.up_codes, experts.up_scales, dup, offsets=r.offsets),

@@ -20,6 +20,7 @@ if not gpu_available():  # pragma: no cover
 import torch  # noqa: E402
 
 import paper_2606_00079_amd as bm  # noqa: E402
+from paper_2606_00079_amd import pipeline  # noqa: E402
 
 DEV = "cuda:0"
 U = 2.0 ** -23
@@ -337,3 +338,29 @@ def test_gradient_of_rows_that_no_slot_names(T, k, S, d, dtype):
     dz, dw = bm.combine_grad(Z, slots, w, dY)
     within(dz, want, bound, "dz of the binding")
     within(dw, wdw, mags * (d + 16) * U, "dw of the binding")
+
+
+# --------------------------------------------------------------- together
+def experts_of(E, N, K, **ones):
+    """Experts whose weights are 0 but for the entries given: {(e, row, column): value}."""
+    w = {"gate": torch.zeros(E, N, K), "up": torch.zeros(E, N, K), "down": torch.zeros(E, K, N)}
+    for name, at in ones.items():
+        for i, v in at.items():
+            w[name][i] = v
+    return pipeline.mx4_experts(*(w[n].to(DEV) for n in ("gate", "up", "down")))
+
+
+def test_training_and_serving_give_one_answer():
+    """Gate and up are not rounded before silu(g) u: 257 x 257 = 66049 is 66048 in bf16; of 257 rounded first, 65536."""
+    ex = experts_of(1, 32, 32, gate={(0, 0, 0): 1, (0, 0, 1): 1}, up={(0, 0, 0): 1, (0, 0, 1): 1}, down={(0, 5, 0): 1})
+    x = torch.zeros(3, 32, device=DEV)
+    x[:, 0], x[:, 1] = 256, 1
+    logits = torch.zeros(3, 1, device=DEV)
+    for quantize in (False, True):
+        if quantize:
+            x[:, 0], x[:, 1] = 4, 0.5  # (both in the format, with one scale) 4.5 x 4.5 silu's sigma: not exact
+        y, _ = pipeline.mx4_layer(x.to(torch.bfloat16), logits, ex, 1, quantize_tokens=quantize)
+        yt, _, saved = pipeline.mx4_layer(x.to(torch.bfloat16), logits, ex, 1, quantize_tokens=quantize, train=True)
+        assert torch.equal(y, yt)
+        if not quantize:
+            assert (y[:, 5] == 66048).all() and (saved.up[:, 0] == 257).all()
