@@ -345,7 +345,9 @@ def mx4_layer_grad(saved: Mx4Saved, experts: Mx4Experts, dy, dlosses=None):
                           dtype=torch.float32)
     g, u = saved.up.chunk(2, dim=1)
     sig = torch.sigmoid(g)
+    # (bf16 is what the matrix cores take: dz and this are rounded once each, as their operands)
     dup = torch.cat((dh * u * sig * (1 + g * (1 - sig)), dh * g * sig), 1).to(torch.bfloat16)
-    dx = combine(mx4_product_grad(experts.up_codes, experts.up_scales, dup, offsets=r.offsets),
-                 r.slots)
+    # (a token's slots are summed up before the one rounding)
+    dx = combine(mx4_product_grad(experts.up_codes, experts.up_scales, dup, offsets=r.offsets,
+                                  dtype=torch.float32), r.slots).to(torch.bfloat16)
     return dx, route_grad(saved.logits, r, dweights=dw, dlosses=dlosses, renorm=saved.renorm)

@@ -364,3 +364,17 @@ def test_training_and_serving_give_one_answer():
         assert torch.equal(y, yt)
         if not quantize:
             assert (y[:, 5] == 66048).all() and (saved.up[:, 0] == 257).all()
+
+
+def test_gradient_of_a_token_is_rounded_after_its_slots_are_summed():
+    """One expert's part of dx is 256 + 1, the other's -256: 1, where 257 rounded first would leave 0."""
+    # gate = 64 (its sigmoid is 1 in fp32), up = 0: d(up) = 64 dh, d(gate) = 0
+    ex = experts_of(2, 32, 32, gate={(0, 0, 1): 1, (0, 1, 1): 1, (1, 0, 1): 1}, up={(0, 0, 0): 1, (0, 1, 0): 1, (1, 0, 0): 1},
+                    down={(0, 0, 0): 1, (0, 1, 1): 1, (1, 0, 0): -1})
+    x = torch.zeros(1, 32, device=DEV)
+    x[0, 1] = 64
+    _, _, saved = pipeline.mx4_layer(x.to(torch.bfloat16), torch.zeros(1, 2, device=DEV), ex, 2, train=True)
+    dy = torch.zeros(1, 32, device=DEV)
+    dy[0, 0], dy[0, 1] = 8, 2.0 ** -5  # (both weights are 1/2)
+    dx, _ = pipeline.mx4_layer_grad(saved, ex, dy.to(torch.bfloat16))
+    assert dx.dtype == torch.bfloat16 and dx[0, 0] == 1 and (dx[0, 1:] == 0).all()
