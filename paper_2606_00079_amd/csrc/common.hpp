@@ -36,6 +36,17 @@ __device__ __forceinline__ double f16_bits_to_f64(uint16_t b) {
   return static_cast<double>(static_cast<float>(__builtin_bit_cast(_Float16, b)));
 }
 
+// exp(d) for -150 <= d <= 88 (or NaN) by the hardware's 2^t, with what t = d / ln 2
+// loses to rounding (|d| 2^-24 of the result) put back: a third of the library
+// function's instructions.
+__device__ __forceinline__ float exp_hw(float d) {
+  const float t = d * 1.44269504088896341f;
+  const float e = __builtin_amdgcn_exp2f(t);
+  // log2(e) = 1.44269502162933349609375 + 1.92596299e-8, each as fp32 holds it
+  const float r = fmaf(d, 1.92596299e-8f, fmaf(d, 1.44269504088896341f, -t));
+  return fmaf(e, r * 0.693147180559945309f, e);
+}
+
 // Returns v unchanged but opaque to the optimizer: computations that depend
 // on the result cannot be hoisted above this point (used so that epilogue
 // address arithmetic is not moved before a long loop and kept live there).

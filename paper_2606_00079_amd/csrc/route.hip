@@ -80,15 +80,9 @@ __device__ __forceinline__ T row_reduce(T v, F f) {
   }
   return v;
 }
-// exp(d) for d <= 0 (or NaN) by the hardware's 2^t, with what t = d / ln 2 loses
-// to rounding put back: a third of the library function's instructions.
+// exp(d) for d <= 0 (or NaN).
 __device__ __forceinline__ float exp_neg(float d) {
-  d = d < -150.0f ? -150.0f : d;  // (0 in fp32; -inf would give a NaN below)
-  const float t = d * 1.44269504088896341f;
-  const float e = __builtin_amdgcn_exp2f(t);
-  // log2(e) = 1.44269502162933349609375 + 1.925963033500e-8
-  const float r = fmaf(d, 1.925963033500e-8f, fmaf(d, 1.44269504088896341f, -t));
-  return fmaf(e, r * 0.693147180559945309f, e);
+  return exp_hw(d < -150.0f ? -150.0f : d);  // (0 in fp32; -inf would give a NaN)
 }
 
 template <int LPT>

@@ -191,6 +191,35 @@ def test_more_tiles_than_a_launch_takes():
         within(got[lo:hi], want, d.abs() @ w[e].abs() * 24 * U + 2.0 ** -8 * want.abs(), ("gradient", lo))
 
 
+def gated(kernel, tokens, times=1):
+    """silu(times x) of every x of tokens as the product with glu gives it (times 1 or 6), in fp32."""
+    E, N, K, S = {"mx4_rows": (6, 16, 1056, 9), "mx4_few": (90, 776, 1312, 300), "mx4_tile": (4, 1024, 1024, 9000)}[kernel]
+    out = []
+    for part in tokens.split(S):
+        codes = torch.zeros((E, 2 * N, K // 2), dtype=torch.uint8, device=DEV)
+        codes[:, :N, 0], codes[:, N:, 0] = {1: 0x02, 6: 0x07}[times], 0x20  # (entry 0 of gate rows, entry 1 of up rows)
+        scales = torch.full((E, 2 * N, K // 32), 127, dtype=torch.uint8, device=DEV)
+        x = torch.zeros((S, K), dtype=torch.bfloat16, device=DEV)
+        x[:len(part), 0], x[:, 1] = part, 1
+        off = torch.linspace(0, S, E + 1, device=DEV).round().to(torch.int32)
+        y = taken(kernel, lambda: bm.mx4_product(codes, scales, x, offsets=off, glu=True, dtype=torch.float32))
+        assert torch.equal(y.nan_to_num(7.0), y[:, :1].expand_as(y).nan_to_num(7.0))
+        out.append(y[:len(part), 0].clone())
+    return torch.cat(out)
+
+
+@pytest.mark.parametrize("kernel", ["mx4_rows", "mx4_few", "mx4_tile"])
+def test_silu_of_exact_gates(kernel):
+    """2^-21 of itself: an ulp (2^-23) each of exponential and reciprocal, half of one of their operands' rounding and
+    of the product.  Without the exponent's rounding put back it is |v| 2^-24, 2^-18 at 64."""
+    v = torch.cat((torch.linspace(-86, 86, 500), torch.linspace(-8, 8, 200), torch.tensor([0.0, -0.0, 3e38, 1e-38, -200.0])))
+    v = v.to(DEV).to(torch.bfloat16)
+    want = v.double() / (1 + torch.exp(-v.double()))
+    within(gated(kernel, v), want, want.abs() * 2.0 ** -21 + 2.0 ** -126, kernel)
+    got = gated(kernel, torch.tensor([1e38, -1e38, torch.nan], device=DEV).to(torch.bfloat16), times=6)
+    assert got[0] == torch.inf and got[1:].isnan().all()  # (gates past fp32: silu(-inf) is inf / inf)
+
+
 # ----------------------------------------------------------------- router
 def grow_scratch():
     """A call of another operator that needs more of the library's scratch than any before."""
