@@ -65,12 +65,14 @@ struct Tile {
   int e, lo, hi, col;
 };
 __device__ __forceinline__ int slots_of(const int32_t* offsets, int E, int S, int e, int* lo) {
-  if (e > E) {
-    *lo = 0;
-    return offsets ? min(max(offsets[0], 0), S) : 0;
+  // (both loads at once whatever e is: a chain of two would lengthen every search)
+  const int first = offsets ? offsets[min(e, E)] : 0, end = offsets ? offsets[e < E ? e + 1 : 0] : 0;
+  if (!offsets) {
+    *lo = e == 1 ? S : 0;  // (E = 1)
+    return e == 0 ? S : 0;
   }
-  *lo = offsets ? min(max(offsets[e], 0), S) : (e == 0 ? 0 : S);
-  return (e < E && offsets ? min(max(offsets[e + 1], *lo), S) : S) - *lo;
+  *lo = e > E ? 0 : min(max(first, 0), S);
+  return (e == E ? S : min(max(end, *lo), S)) - *lo;
 }
 __device__ __forceinline__ bool find_tile(const int32_t* offsets, int E, int64_t S, int cols, int tile, Tile* out) {
   const int s = static_cast<int>(S), lane = threadIdx.x & 63;
