@@ -191,6 +191,112 @@ def test_more_tiles_than_a_launch_takes():
         within(got[lo:hi], want, d.abs() @ w[e].abs() * 24 * U + 2.0 ** -8 * want.abs(), ("gradient", lo))
 
 
+# Every way that a kernel stores and takes its slots: N a multiple of 256 (whole tiles, 16-byte stores) or not, K a
+# multiple of 512 (scales 16 bytes a row) or not.  form, kernel, E, N (2 N with glu), K, S
+STORED = [
+    ("bf16", "mx4_rows", 6, 256, 1056, 9), ("mx4", "mx4_rows", 6, 256, 1056, 9),
+    ("bf16", "mx4_few", 90, 1536, 1312, 300), ("mx4", "mx4_few", 90, 1536, 1312, 300),
+    ("bf16", "mx4_few", 40, 1536, 2080, 800), ("mx4", "mx4_few", 200, 2048, 96, 3500),
+    ("bf16", "mx4_tile", 5, 2048, 288, 9000), ("bf16", "mx4_tile", 4, 2048, 512, 9000),
+    ("bf16", "mx4_tile", 3, 1794, 1536, 9001), ("mx4", "mx4_tile", 5, 2048, 288, 9000),
+    ("mx4", "mx4_tile", 4, 2048, 1024, 9000), ("mx4", "mx4_tile", 4, 2050, 1024, 9000),
+    ("bf16", "mx4_tile", 130, 1024, 800, 9000), ("mx4", "mx4_tile", 130, 1024, 1024, 9000),
+]
+
+
+@pytest.mark.parametrize("glu", [False, True])
+@pytest.mark.parametrize("case", STORED)
+def test_every_store_of_the_products(case, glu):
+    """bf16 and fp32 results, rows given (some do not exist) and not, strided tokens, lost blocks, a tail."""
+    form, kernel, E, N, K, S = case
+    g = np.random.default_rng([E, N, K, S, glu, 3])
+    codes, scales = weights(E, N, K, g, lost=1)
+    off = offsets_of(E, S, S // 40, g)
+    rows = g.integers(0, S // 2, S).astype(np.int32)
+    rows[::9], rows[4::13] = -5, S
+    wide = torch.randn(S, K + 64, device=DEV).to(torch.bfloat16)
+    tokens = wide[:, 32:32 + K]
+    for X, r in ((tokens, None), (tokens[:S // 2], torch.from_numpy(rows).to(DEV)), (tokens[::2], None)):
+        o = off if r is not None else np.minimum(off, len(X)).astype(np.int32)
+        kw = {"offsets": torch.from_numpy(o).to(DEV), "rows": r, "glu": glu}
+        n = len(X) if r is None else S
+        full = n == S  # (fewer slots may go to another kernel)
+        X = X.contiguous() if form == "mx4" else X
+        results = []
+        for dtype in DT.values():
+            call = lambda: product(form, codes, scales, X, dtype=dtype, **kw)  # noqa: E731
+            y, x = taken(kernel, call) if full else call()
+            results.append(y)
+        want, bound = exact(codes, scales, x, o, r, glu)
+        for y in results:
+            assert y.shape == want.shape
+            within(y, want, bound + (2.0 ** -8 * want.abs() if y.dtype == torch.bfloat16 else 0), (case, glu, y.dtype))
+
+
+@pytest.mark.parametrize("case", [
+    ("mx4_grad_few", 6, 256, 1024, 9), ("mx4_grad_few", 90, 1552, 512, 1300), ("mx4_grad_few", 40, 1552, 480, 300),
+    ("mx4_grad_tile", 5, 296, 2048, 9000), ("mx4_grad_tile", 2, 264, 4096, 9000), ("mx4_grad_tile", 130, 800, 1024, 9001),
+    ("mx4_grad_tile", 5, 296, 2112, 9000), ("mx4_grad_tile", 1, 160, 1056, 50000)])
+def test_every_store_of_the_gradient(case):
+    kernel, E, N, K, S = case
+    g = np.random.default_rng([E, N, K, S, 4])
+    codes, scales = weights(E, N, K, g, lost=1)
+    off = offsets_of(E, S, S // 40, g)
+    wide = torch.randn(S, N + 24, device=DEV).to(torch.bfloat16)
+    dY = wide[:, 8:8 + N]
+    for dtype in DT.values():
+        got = taken(kernel, lambda: bm.mx4_product_grad(codes, scales, dY, offsets=torch.from_numpy(off).to(DEV),
+                                                        dtype=dtype))
+        want, bound = exact(codes, scales, dY, off, grad=True)
+        within(got, want, bound + (2.0 ** -8 * want.abs() if dtype == torch.bfloat16 else 0), (case, dtype))
+
+
+@pytest.mark.parametrize("case", [("bf16", "mx4_rows", 256, 512, 9), ("bf16", "mx4_tile", 2048, 512, 6000),
+                                  ("mx4", "mx4_tile", 2048, 1024, 6000), ("mx4", "mx4_tile", 2048, 544, 9000)])
+def test_one_expert_without_offsets(case):
+    form, kernel, N, K, S = case
+    g = np.random.default_rng([N, K, S])
+    codes, scales = weights(1, N, K, g)
+    X = torch.randn(S, K, device=DEV).to(torch.bfloat16)
+    got, x = taken(kernel, lambda: product(form, codes, scales, X))
+    want, bound = exact(codes, scales, x, [0, S])
+    within(got, want, bound + 2.0 ** -8 * want.abs(), case)
+    if kernel == "mx4_tile":
+        d = torch.randn(S, N, device=DEV).to(torch.bfloat16)
+        back = taken("mx4_grad_tile", lambda: bm.mx4_product_grad(codes, scales, d))
+        want, bound = exact(codes, scales, d, [0, S], grad=True)
+        within(back, want, bound + 2.0 ** -8 * want.abs(), (case, "grad"))
+
+
+def test_large_tiles_past_32_bits():
+    """Codes of more than 2^32 bytes, tokens past 2^31 entries."""
+    E, N, K, S = 33, 16384, 16384, 3000
+    codes = torch.zeros((E, N, K // 2), dtype=torch.uint8, device=DEV)
+    scales = torch.full((E, N, K // 32), 120, dtype=torch.uint8, device=DEV)
+    codes[E - 1] = torch.randint(0, 256, (N, K // 2), dtype=torch.uint8, device=DEV)
+    assert codes.numel() > 1 << 32
+    T = (1 << 17) + 700
+    X = torch.zeros((T, K), dtype=torch.bfloat16, device=DEV)
+    X[-600:] = torch.randn(600, K, device=DEV).to(torch.bfloat16)
+    rows = torch.randint(T - 600, T, (S,), dtype=torch.int32, device=DEV)
+    off = torch.zeros(E + 1, dtype=torch.int32, device=DEV)
+    off[E] = S
+    w64, x = values(codes[E - 1], scales[E - 1]), X[-600:].double()
+    table, size = x @ w64.t().contiguous(), x.abs() @ w64.abs().t().contiguous() * (K + 16) * U
+    at = (rows - (T - 600)).long()
+    got = taken("mx4_tile", lambda: bm.mx4_product(codes, scales, X, offsets=off, rows=rows))
+    within(got, table[at], size[at] + 2.0 ** -8 * table[at].abs(), "far")
+    q = bm.mx4_quantize(X)
+    x = bm.mx4_dequantize(q[0][-600:].contiguous(), q[1][-600:].contiguous()).double()
+    table, size = x @ w64.t().contiguous(), x.abs() @ w64.abs().t().contiguous() * (K + 16) * U
+    got = taken("mx4_tile", lambda: bm.mx4_product_q(codes, scales, *q, offsets=off, rows=rows))
+    within(got, table[at], size[at] + 2.0 ** -8 * table[at].abs(), "far in MX4")
+    del table, size, q, X, x, got
+    d = torch.randn(S, N, device=DEV).to(torch.bfloat16)
+    back = taken("mx4_grad_tile", lambda: bm.mx4_product_grad(codes, scales, d, offsets=off, dtype=torch.float32))
+    within(back, d.double() @ w64, d.double().abs() @ w64.abs() * (N + 16) * U, "far gradient")
+
+
 def gated(kernel, tokens, times=1):
     """silu(times x) of every x of tokens as the product with glu gives it (times 1 or 6), in fp32."""
     E, N, K, S = {"mx4_rows": (6, 16, 1056, 9), "mx4_few": (90, 776, 1312, 300), "mx4_tile": (4, 1024, 1024, 9000)}[kernel]
@@ -407,3 +513,92 @@ def test_gradient_of_a_token_is_rounded_after_its_slots_are_summed():
     dy[0, 0], dy[0, 1] = 8, 2.0 ** -5  # (both weights are 1/2)
     dx, _ = pipeline.mx4_layer_grad(saved, ex, dy.to(torch.bfloat16))
     assert dx.dtype == torch.bfloat16 and dx[0, 0] == 1 and (dx[0, 1:] == 0).all()
+
+
+@pytest.mark.parametrize("T,E,k,N,K", [(60, 12, 3, 96, 160), (3000, 4, 2, 512, 1024)])
+@pytest.mark.parametrize("quantize", [False, True])
+@pytest.mark.parametrize("renorm", [False, True])
+def test_layer_stage_by_stage(T, E, k, N, K, quantize, renorm):
+    """Every stage of a short batch and of a long one (the large tiles, the router's three launches) in 64 bits from
+    what the stage before it gave; tokens in 4 bits as the oracle rounds them."""
+    g = torch.Generator(device=DEV).manual_seed(T + 2 * quantize + renorm)
+    randn = lambda *s: torch.randn(s, generator=g, device=DEV)  # noqa: E731
+    ex = pipeline.mx4_experts(randn(E, N, K) / K ** 0.5, randn(E, N, K) / K ** 0.5, randn(E, K, N) / N ** 0.5)
+    x, logits, dy = randn(T, K).to(torch.bfloat16), randn(T, E), randn(T, K).to(torch.bfloat16)
+    valid = torch.rand(T, generator=g, device=DEV) < 0.9
+    dl = torch.tensor([0.3, 0.1], device=DEV)
+
+    def seen(v):
+        if not quantize:
+            return v
+        return torch.from_numpy(omx4.dequantize(*omx4.quantize(v.double().cpu().numpy()))).to(DEV)
+
+    bf16 = lambda want, bound: bound + 2.0 ** -8 * want.abs()  # noqa: E731
+    y, r = pipeline.mx4_layer(x, logits, ex, k, valid=valid, renorm=renorm, quantize_tokens=quantize)
+    yt, rt, saved = pipeline.mx4_layer(x, logits, ex, k, valid=valid, renorm=renorm, quantize_tokens=quantize, train=True)
+    assert equal(r, rt)
+    off = r.offsets.cpu().numpy()
+    top = torch.sort(logits, dim=1, descending=True, stable=True).indices[:, :k]
+    assert torch.equal(r.experts.long(), torch.where(valid[:, None], top, -1))
+
+    def joined(z, zb, got, what):
+        """y of rows z [S][K], each known to zb."""
+        w = r.weights.double()[:, :, None]
+        at = r.slots.long()
+        want, size = (w * z[at]).sum(1), (w * zb[at]).sum(1) + (k + 2) * U * (w * z[at].abs()).sum(1)
+        within(got, want, size + 2.0 ** -8 * (want.abs() + size), what)
+
+    # serving: h is what the product gives by itself
+    call = {"offsets": r.offsets, "rows": r.rows, "glu": True}
+    h, _ = product("mx4" if quantize else "bf16", ex.up_codes, ex.up_scales, x, **call)
+    want, bound = exact(ex.up_codes, ex.up_scales, seen(x), off, r.rows, True)
+    within(h, want, bf16(want, bound), "h")
+    z, zb = exact(ex.down_codes, ex.down_scales, seen(h), off)
+    joined(z, bf16(z, zb), y, "y")
+    # training
+    want, bound = exact(ex.up_codes, ex.up_scales, seen(x), off, r.rows)
+    within(saved.up, want, bound, "gate and up")
+    gate, up = saved.up.chunk(2, dim=1)
+    h = (torch.nn.functional.silu(gate) * up).to(torch.bfloat16)
+    z, zb = exact(ex.down_codes, ex.down_scales, seen(h), off)
+    within(saved.z, z, bf16(z, zb), "z")
+    joined(saved.z.double(), torch.zeros_like(z), yt, "y in training")
+    dx, dlogits = pipeline.mx4_layer_grad(saved, ex, dy, dlosses=dl)
+    dz, dw = bm.combine_grad(saved.z, r.slots, r.weights, dy)
+    assert torch.equal(dlogits, bm.route_grad(logits, r, dweights=dw, dlosses=dl, renorm=renorm))
+    want = (dy.double()[:, None] * r.weights.double()[:, :, None]).flatten(0, 1)
+    within(dz[r.slots.flatten().long()], want, 2.0 ** -8 * want.abs() + 1e-38, "dz")
+    dh = exact(ex.down_codes, ex.down_scales, dz, off, grad=True)[0]
+    gate, up = gate.double(), up.double()
+    sig = torch.sigmoid(gate)
+    dup = torch.cat((dh * up * sig * (1 + gate * (1 - sig)), dh * gate * sig), 1)
+    part = exact(ex.up_codes, ex.up_scales, dup, off, grad=True)[0]
+    want = part[r.slots.long()].sum(1)
+    # two roundings to bf16 (of dup's entries, whose errors add up like the entries, and of the sum), 2^-9 each at most
+    assert (dx.double() - want).norm() < 2.0 ** -7 * want.norm()
+
+
+def test_layer_and_gradients_of_many_rows_in_a_graph():
+    T, E, k, N, K = 6000, 8, 4, 64, 96
+    g = torch.Generator(device=DEV).manual_seed(8)
+    randn = lambda *s: torch.randn(s, generator=g, device=DEV)  # noqa: E731
+    ex = pipeline.mx4_experts(randn(E, N, K) / 10, randn(E, N, K) / 10, randn(E, K, N) / 8)
+    x, logits, dy = randn(T, K).to(torch.bfloat16), randn(T, E), randn(T, K).to(torch.bfloat16)
+    dl = torch.tensor([0.3, 0.1], device=DEV)
+
+    def step():
+        y, r, saved = pipeline.mx4_layer(x, logits, ex, k, train=True)
+        return (y, *r, *pipeline.mx4_layer_grad(saved, ex, dy, dlosses=dl))
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for turn in range(4):
+        for t in (x, logits, dy):
+            t.copy_(randn(*t.shape))
+        graph.replay()
+        want = step()
+        torch.cuda.synchronize()
+        assert equal(out, want), turn
