@@ -98,6 +98,13 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v) {
   return row_reduce<LPT>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
 
+// LDS operations of this wave before it are done, for its other lanes too.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // The V logits first .. first + V - 1 of a row (experts past E: -inf).
 template <bool BF16, int V>
 __device__ __forceinline__ void load_logits(const void* row, int first, int E, bool wide, float* x) {
@@ -322,7 +329,7 @@ __global__ __launch_bounds__(NT) void route_rows_kernel(RouteArgs a) {
       }
     }
     // their weights, a slot a lane (the row's lanes are of one wave, which wrote what is read here)
-    __builtin_amdgcn_wave_barrier();
+    wave_fence();
     float total_w = 0.0f;
     for (int j = lane; j < a.k; j += LPT) {
       float p = exp_neg(chosen[grp * a.k + j] - m) * inv;
@@ -333,6 +340,7 @@ __global__ __launch_bounds__(NT) void route_rows_kernel(RouteArgs a) {
     total_w = row_sum<LPT>(total_w);
     const float scale = a.renorm && total_w != 0.0f ? 1.0f / total_w : 1.0f;
     for (int j = lane; j < a.k; j += LPT) a.weights[t * a.k + j] = chosen[grp * a.k + j] * scale;
+    wave_fence();  // (the next row's winners write where other lanes have read)
   }
 #pragma unroll
   for (int i = 0; i < V; ++i) probs[grp * LPT * V + first + i] = sum[i];
@@ -480,13 +488,6 @@ struct GradArgs {
   const float* dlosses;
   void* dlogits;
 };
-
-// LDS operations of this wave before it are done, for its other lanes too.
-__device__ __forceinline__ void wave_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
 
 // A row on LPT lanes as in the forward form; a row's slots lie on its lanes too, and
 // their gate terms reach the lanes of their experts through LDS (by shuffles and
