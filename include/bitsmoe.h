@@ -675,9 +675,10 @@ bitsmoe_status bitsmoe_mx4_dequantize(const uint8_t* codes_dev, const uint8_t* s
  *   offsets_dev  [E + 1] int32, or NULL with E = 1: all slots are expert 0's
  *   rows_dev     [S] int32, or NULL: slot s reads row s
  *   Y_dev        [S] rows of N entries of type yt, ldy entries apart
- * S may be 0.  Shape rules: K % 32 == 0, ldx >= K, ldx % 8 == 0, ldy >= N,
- * E <= 65535, N and K <= 2^24, S < 2^31 - 256; where S <= 8 E or x_rows = 0,
- * (S / 16 + E + 2) times the sixteens of N below 2^23.
+ * S may be 0, and so may x_rows (X_dev is then not read).  Shape rules: K % 32
+ * == 0, ldx >= K, ldx % 8 == 0, ldy >= N, E <= 65535, N and K <= 2^24, S < 2^31
+ * - 256; where S <= 8 E or x_rows = 0, (S / 16 + E + 2) times the sixteens of N
+ * below 2^23.
  */
 bitsmoe_status bitsmoe_mx4_product(const uint8_t* codes_dev, const uint8_t* scales_dev, int64_t E,
                                    int64_t N, int64_t K, const void* X_dev, bitsmoe_dtype xt,

@@ -1506,8 +1506,7 @@ bitsmoe_status tile_product(const MulArgs& a, hipStream_t s) {
 // slots an expert (their walk over the experts is long) or no row that they could read for a slot without one.
 bool large_instead(const MulArgs& a) { return a.S > 8 * static_cast<int64_t>(a.E) && a.x_rows > 0; }
 
-bitsmoe_status product(const char* who, const MulArgs& a, bool glu, hipStream_t s) {
-  const bool mx = a.xcodes != nullptr;
+bitsmoe_status product(const char* who, const MulArgs& a, bool mx, bool glu, hipStream_t s) {
   Kernel kernel = product_kernel(a, mx, glu);
   unsigned grid = 0;
   const bool fits = kernel == kLargeTiles ||
@@ -1564,7 +1563,7 @@ extern "C" bitsmoe_status bitsmoe_mx4_product(const uint8_t* codes_dev, const ui
     return fail(BITSMOE_ERR_SHAPE, "mx4_product: needs ldx >= K and ldx % 8 == 0");
   if (S == 0) return ok();
   if (x_rows > 0 && !X_dev) return fail(BITSMOE_ERR_ARG, "mx4_product: null pointer");
-  return product("mx4_product", a, glu != 0, static_cast<hipStream_t>(stream));
+  return product("mx4_product", a, false, glu != 0, static_cast<hipStream_t>(stream));
 }
 
 extern "C" bitsmoe_status bitsmoe_mx4_product_q(const uint8_t* codes_dev, const uint8_t* scales_dev, int64_t E,
@@ -1578,8 +1577,8 @@ extern "C" bitsmoe_status bitsmoe_mx4_product_q(const uint8_t* codes_dev, const 
             Y_dev, ldy, yt == BITSMOE_F32};
   if (bitsmoe_status st = check("mx4_product_q", a, yt, N)) return st;
   if (S == 0) return ok();
-  if (!xcodes_dev || !xscales_dev) return fail(BITSMOE_ERR_ARG, "mx4_product_q: null pointer");
-  return product("mx4_product_q", a, glu != 0, static_cast<hipStream_t>(stream));
+  if (x_rows > 0 && (!xcodes_dev || !xscales_dev)) return fail(BITSMOE_ERR_ARG, "mx4_product_q: null pointer");
+  return product("mx4_product_q", a, true, glu != 0, static_cast<hipStream_t>(stream));
 }
 
 extern "C" bitsmoe_status bitsmoe_mx4_product_grad(const uint8_t* codes_dev, const uint8_t* scales_dev, int64_t E,

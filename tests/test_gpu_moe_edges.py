@@ -161,6 +161,21 @@ def test_slots_before_the_first_expert_and_after_the_last(case):
     assert (got[:off[0]] == 0).all() and (got[off[-1]:] == 0).all()
 
 
+@pytest.mark.parametrize("glu", [False, True])
+@pytest.mark.parametrize("E,N,K,S", [(6, 250, 1056, 9), (90, 1550, 1312, 300), (4, 2048, 1024, 9000)])
+def test_slots_of_no_rows_at_all(E, N, K, S, glu):
+    """No token of these experts is here: zeros, in either form."""
+    g = np.random.default_rng([E, N, K, S])
+    codes, scales = weights(E, N, K, g, lost=2)
+    kw = {"offsets": torch.from_numpy(offsets_of(E, S, 3, g)).to(DEV), "glu": glu,
+          "rows": torch.full((S,), -1, dtype=torch.int32, device=DEV)}
+    none = torch.zeros(0, K, dtype=torch.bfloat16, device=DEV)
+    for form in ("bf16", "mx4"):
+        out = torch.full((S, N // 2 if glu else N), torch.nan, device=DEV)
+        got, _ = product(form, codes, scales, none, dtype=torch.float32, out=out, **kw)
+        assert (got == 0).all(), form
+
+
 def test_more_tiles_than_a_launch_takes():
     """The small tiles that cost least here would be more than 2^23 workgroups: the
     resident large ones take the call instead."""
