@@ -253,7 +253,7 @@ __device__ __forceinline__ void store32(const MulArgs& a, int64_t s, int64_t n, 
 // which one load fetches with their scale, and the same entries of slot l % 16.
 // For the fewest slots: bound by launch and one chain of loads (four segments in
 // flight a wave), so the sum is split and the workgroups are small and many.  One
-// token's 8 experts, 2 x 768 x 2048 with glu (13 MB): 9.0 us.
+// token's 8 experts, 2 x 768 x 2048 with glu (13 MB): 8.2 us.
 template <bool MX, bool GLU>
 __global__ __launch_bounds__(kThreads) void mx4_rows_kernel(MulArgs a) {
   constexpr int H = GLU ? 2 : 1;
@@ -338,7 +338,7 @@ __global__ __launch_bounds__(kThreads) void mx4_rows_kernel(MulArgs a) {
 // where these take 23.
 // 16-byte chunk c of a slot lies at c ^ (slot mod 16): the sixteen slots of a
 // fragment read in different banks.  Bound by the weights' bytes: 512 slots over
-// 128 experts, 2048 x 768 (110 MB), take 23 us, 4.8 TB/s.
+// 128 experts, 2048 x 768 (110 MB), take 22 us, 5.0 TB/s.
 template <bool MX, bool GLU, int TB>
 __global__ __launch_bounds__(kThreads, TB == 1 ? 4 : 3) void mx4_few_kernel(MulArgs a) {
   constexpr int R = 4, AHEAD = 2, KC = 1024, XB = MX ? KC / 2 : 2 * KC, XC = XB / 16, SL = 16 * TB;
@@ -1048,7 +1048,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void mx4_tile_kernel(MulArgs a) {
 // read takes fragments from.  Two such tiles: the next step's is made while this
 // one's is multiplied, and between the matrix-core ops go the reads of the next
 // sixteen rows' fragments and the conversions.  32768 slots over 128 experts, 2048
-// x 768: 168 us, 0.61 PFLOP/s (0.77 with what pads the tiles), bound by the matrix
+// x 768: 165 us, 0.62 PFLOP/s (0.78 with what pads the tiles), bound by the matrix
 // cores' clock and, at half of their time, by the LDS (fragments used twice).
 // ---------------------------------------------------------------------------
 struct GradShape {
@@ -1441,8 +1441,8 @@ bool grid_of(const MulArgs& a, int64_t tile, int64_t per, unsigned* grid) {
 // chain of steps counts) or fill the card (their number does).  The constants (us;
 // L entries of the sum) fit timings of all kernels at thirty shapes, E 1 .. 256,
 // 1/8 .. 4096 slots an expert, outputs 256 .. 14336, sums of 512 .. 14336 entries:
-// the choice is within 1.3 times the best of them (1 % on average), and the worst of
-// them is two to nine times that (one expert, 64 slots, 1024 x 4096: 50 us in large
+// the choice is within 1.25 times the best of them (1 % on average), and the worst of
+// them is mostly two to four times that, nine at most (one expert, 64 slots, 1024 x 4096: 50 us in large
 // tiles, 42 in few-slot ones, 9 by rows; 4096 slots, 4096 x 4096: 150, 266, 1340).
 enum Kernel { kByRows, kFewSlots, kLargeTiles };
 

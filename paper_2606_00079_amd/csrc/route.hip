@@ -20,7 +20,7 @@
 //
 // The largest calls are bound by the logits' bytes and a row's chain of lane
 // exchanges, the others by their launches: 16384 rows of 256 fp32 logits, k = 8
-// (17 MB), take 17 us (rows), 5 (sums), 6 (places) and 16 for the gradient (34 MB);
+// (17 MB), take 18 us (rows), 4 (sums), 7 (places) and 16 for the gradient (34 MB);
 // one row of 128, 7.8 us in its one launch, the chain of k rounds, barriers and
 // placement.
 #include <atomic>
@@ -256,7 +256,7 @@ __global__ __launch_bounds__(NT) void route_rows_kernel(RouteArgs a) {
   float* probs = reinterpret_cast<float*>(smem);                  // [G][LPT * V]
   int32_t* cnt = reinterpret_cast<int32_t*>(probs + NT * V);  // [E + 1]
   float* chosen = reinterpret_cast<float*>(cnt + a.E + 1);        // [G][k]
-  float* tmp = chosen + G * a.k;                                  // [kThreads]
+  float* tmp = chosen + G * a.k;                                  // [NT / 64]
   // one run only: the experts of its slots, and what place_slots takes
   int32_t* list = reinterpret_cast<int32_t*>(tmp + NT / 64);  // [run][k]
   int32_t* taken = list + a.run * a.k;                        // [run + 1]
