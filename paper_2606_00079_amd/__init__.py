@@ -629,19 +629,19 @@ def route(logits, k: int, valid=None, renorm: bool = True) -> Routing:
     vp = _in(valid, "valid", logits, torch.uint8, (T,))
     lp, ld = _rows(logits, "logits")
     n, w = max(T * k, 0), max(k, 0)
-    # one allocation for the whole numbers and one for the others, their parts 16 bytes aligned
+    # one allocation for the whole numbers and one for the others, their parts 16 bytes aligned; after the whole numbers
+    # a workspace of the call's own (of many rows an eighth of fp32 logits or less), so that calls may overlap and be
+    # captured
     n4, e4, t4 = (n + 3) // 4 * 4, (E + 4) // 4 * 4, (T + 3) // 4 * 4
-    ints = logits.new_empty((3 * n4 + 2 * e4,), dtype=torch.int32)
+    L = lib()
+    room = L.bitsmoe_route_workspace(T, E) if T > 16 else 0
+    ints = logits.new_empty((3 * n4 + 2 * e4 + (room + 3) // 4,), dtype=torch.int32)
     floats = logits.new_empty((n4 + t4 + 4,), dtype=torch.float32)
     ip, fp = ints.data_ptr(), floats.data_ptr()
     ex, co, of, ro, sl = ip, ip + 12 * n4, ip + 12 * n4 + 4 * e4, ip + 4 * n4, ip + 8 * n4
     we, ls, lo = fp, fp + 4 * n4, fp + 4 * (n4 + t4)
-    L = lib()
-    # (a workspace of the call's own: it may overlap with others, and a graph that it is captured in keeps it)
-    room = L.bitsmoe_route_workspace(T, E) if T > 16 else 0
-    work = logits.new_empty((room,), dtype=torch.uint8) if room else None
     _check(L.bitsmoe_route_ws(lp, _code(logits, "logits", torch), T, E, ld, k, vp, int(renorm), ex, we, co, of,
-                              ro, sl, ls, lo, work.data_ptr() if room else None, room, stream), "route")
+                              ro, sl, ls, lo, ip + 12 * n4 + 8 * e4 if room else None, room, stream), "route")
     return Routing(ints.as_strided((T, w), (w, 1), 0), floats.as_strided((T, w), (w, 1), 0),
                    ints.as_strided((E + 1,), (1,), 3 * n4), ints.as_strided((E + 1,), (1,), 3 * n4 + e4),
                    ints.as_strided((n,), (1,), n4), ints.as_strided((T, w), (w, 1), 2 * n4),
