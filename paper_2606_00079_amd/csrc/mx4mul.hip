@@ -1442,8 +1442,9 @@ bool grid_of(const MulArgs& a, int64_t tile, int64_t per, unsigned* grid) {
 // L entries of the sum) fit timings of all kernels at thirty shapes, E 1 .. 256,
 // 1/8 .. 4096 slots an expert, outputs 256 .. 14336, sums of 512 .. 14336 entries:
 // the choice is within 1.25 times the best of them (1 % on average), and the worst of
-// them is mostly two to four times that, nine at most (one expert, 64 slots, 1024 x 4096: 50 us in large
-// tiles, 42 in few-slot ones, 9 by rows; 4096 slots, 4096 x 4096: 150, 266, 1340).
+// them is mostly two to four times that, fourteen at most (one expert, 64 slots,
+// 1024 x 4096: 50 us in large tiles, 41 in few-slot ones, 9 by rows; 4096 slots,
+// 4096 x 4096: 150, 257, 1341).
 enum Kernel { kByRows, kFewSlots, kLargeTiles };
 
 double tiles_of(const MulArgs& a, int64_t m) {
