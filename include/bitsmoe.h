@@ -57,6 +57,18 @@
  *   bitsmoe_combine           y_t = sum_j w_tj z_{slot(t,j)}                (device)
  *   bitsmoe_combine_grad      its gradients                                 (device)
  *   bitsmoe_combine_grad_all  the same, with 0 in the rows of no slot       (device)
+ *
+ * A training step of such a layer with its experts in bf16, whose activations are
+ * kept in microscaled 8-bit floats (MX8) for the backward pass:
+ *   bitsmoe_rms_norm          residual added, rows normalized, and in MX8      (device)
+ *   bitsmoe_rms_norm_grad     its gradients                                   (device)
+ *   bitsmoe_mx8_quantize      rows to MX8, and bitsmoe_mx8_dequantize back     (device)
+ *   bitsmoe_glu_mx8           silu(g) u, [g; u] kept in MX8                    (device)
+ *   bitsmoe_glu_mx8_grad      its gradient from what was kept                 (device)
+ *   bitsmoe_expert_product    y_s = W_e(s) x_s, bf16 weights                   (device)
+ *   bitsmoe_expert_product_grad  dx_s = W_e(s)^T dy_s                          (device)
+ *   bitsmoe_expert_weight_grad   dW_e = sum_s dy_s x_s^T                       (device)
+ *   bitsmoe_expert_weight_grad_q the same with x in MX8                        (device)
  * None of these reads anything back to the host, and only bitsmoe_route uses the
  * library's scratch (and waits for the stream where that has to grow): the others
  * may overlap on streams of their own and be captured in graphs.
@@ -753,6 +765,148 @@ bitsmoe_status bitsmoe_combine_grad_all(const void* Z_dev, bitsmoe_dtype zt, int
                                         const void* dY_dev, int64_t T, int64_t k, int64_t d,
                                         void* dZ_dev, float* dweights_dev, int32_t* work_dev,
                                         void* stream);
+
+/*
+ * Rows to MX8, the 8-bit form of activations kept for the backward pass.  Each
+ * block of 32 consecutive entries of a row gets the scale 2^(s - 127), the smallest
+ * power of two (from 2^-127, s = 0, on) at which the block's largest magnitude does
+ * not pass 448, and each entry the nearest E4M3 float (1 sign, 4 exponent and 3
+ * fraction bits, largest 448; ties to even) of its quotient by the scale.  A block
+ * with a NaN or an infinity gets s = 255 and codes 0, and stands for NaN.
+ *   X_dev       rows of cols entries of type xt, ld entries apart
+ *   codes_dev   [rows][cols] bytes
+ *   scales_dev  [rows][cols/32] bytes
+ * rows may be 0.  Shape rules as bitsmoe_mx4_quantize.
+ */
+bitsmoe_status bitsmoe_mx8_quantize(const void* X_dev, bitsmoe_dtype xt, int64_t rows,
+                                    int64_t cols, int64_t ld, uint8_t* codes_dev,
+                                    uint8_t* scales_dev, void* stream);
+
+/* What MX8 rows stand for, rounded to Y's type (exact but for bf16 below 2^-126):
+ * Y_dev [rows][cols] of type yt. */
+bitsmoe_status bitsmoe_mx8_dequantize(const uint8_t* codes_dev, const uint8_t* scales_dev,
+                                      int64_t rows, int64_t cols, void* Y_dev, bitsmoe_dtype yt,
+                                      void* stream);
+
+/*
+ * Root-mean-square norm of rows, after the residual's addition:
+ *     v_t = x_t + r_t, rounded to type xt (without R_dev: x_t),
+ *     inv_t = 1 / sqrt(mean_i v_ti^2 + eps),  y_ti = v_ti inv_t w_i.
+ *   X_dev, R_dev  T rows of d entries of type xt, ldx and ldr entries apart
+ *   W_dev         [d] of type wt
+ *   Sum_dev       [T][d] of type xt: v (not written without R_dev)
+ *   Y_dev         [T][d] of type xt, or NULL: not wanted
+ *   codes_dev, scales_dev   y in MX8 (of its value before rounding), or both NULL
+ *   inv_dev       [T] fp32
+ * Sum_dev may be X_dev or R_dev where those rows are densely packed.  T may be 0.
+ * Shape rules: d % 8 == 0 (MX8: d % 32 == 0), d <= 32768, T d <= 2^40, rows a multiple of 16
+ * bytes apart; eps > 0.
+ */
+bitsmoe_status bitsmoe_rms_norm(const void* X_dev, bitsmoe_dtype xt, int64_t ldx,
+                                const void* R_dev, int64_t ldr, const void* W_dev,
+                                bitsmoe_dtype wt, int64_t T, int64_t d, double eps, void* Sum_dev,
+                                void* Y_dev, uint8_t* codes_dev, uint8_t* scales_dev,
+                                float* inv_dev, void* stream);
+
+/* Bytes of the workspace of bitsmoe_rms_norm_grad on the current device. */
+int64_t bitsmoe_rms_norm_grad_workspace(int64_t T, int64_t d);
+
+/*
+ * Gradients of bitsmoe_rms_norm: with g_ti = dy_ti w_i and n_ti = v_ti inv_t,
+ *     dx_ti = inv_t (g_ti - n_ti mean_j(g_tj n_tj)) + dsum_ti,  dw_i = sum_t dy_ti n_ti.
+ * dx is that of x and of r alike; dsum is the gradient that reaches v by itself.
+ *   Sum_dev   T rows of d entries of type xt, ldsum entries apart: v
+ *   inv_dev   as bitsmoe_rms_norm wrote it
+ *   dY_dev    T rows of type xt, lddy apart; dSum_dev likewise, or NULL: 0
+ *   dX_dev    [T][d] of type xt;  dW_dev [d] fp32, or NULL: not wanted
+ *   work_dev  work_bytes bytes, contents of no matter, in use until the call's work
+ *             on the stream is done (NULL where dW_dev is, or none are needed)
+ * Sums are fp32 in a fixed order.  dX_dev may be dY_dev or dSum_dev where those
+ * rows are densely packed.  T may be 0 (dw is 0).  Shape rules as bitsmoe_rms_norm.
+ */
+bitsmoe_status bitsmoe_rms_norm_grad(const void* Sum_dev, bitsmoe_dtype xt, int64_t ldsum,
+                                     const void* W_dev, bitsmoe_dtype wt, const float* inv_dev,
+                                     const void* dY_dev, int64_t lddy, const void* dSum_dev,
+                                     int64_t lddsum, int64_t T, int64_t d, void* dX_dev,
+                                     float* dW_dev, void* work_dev, int64_t work_bytes,
+                                     void* stream);
+
+/*
+ * h = silu(g) u of S rows [g; u], and the rows in MX8 for the gradient.
+ *   GU_dev      S rows of N gate and then N up values of type gut, ld entries apart
+ *   H_dev       [S][N] bf16
+ *   codes_dev   [S][2 N] bytes;  scales_dev [S][2 N / 32] bytes
+ * S may be 0.  Shape rules: N % 32 == 0, N <= 2^29, S N <= 2^40, ld >= 2 N, rows a
+ * multiple of 16 bytes apart.
+ */
+bitsmoe_status bitsmoe_glu_mx8(const void* GU_dev, bitsmoe_dtype gut, int64_t S, int64_t N,
+                               int64_t ld, void* H_dev, uint8_t* codes_dev, uint8_t* scales_dev,
+                               void* stream);
+
+/*
+ * Gradient of silu(g) u at the values g', u' that MX8 rows stand for, s = 1 / (1 +
+ * exp(-g')):  dg = dh u' s (1 + g' (1 - s)), du = dh g' s, and h' = g' s u' again for
+ * who needs it (H_dev may be NULL).
+ *   codes_dev, scales_dev   as bitsmoe_glu_mx8 wrote them
+ *   dH_dev      S rows of N entries of type dht, lddh entries apart
+ *   dGU_dev     [S][2 N] bf16;  H_dev [S][N] bf16
+ * Shape rules as bitsmoe_glu_mx8.
+ */
+bitsmoe_status bitsmoe_glu_mx8_grad(const uint8_t* codes_dev, const uint8_t* scales_dev,
+                                    const void* dH_dev, bitsmoe_dtype dht, int64_t S, int64_t N,
+                                    int64_t lddh, void* dGU_dev, void* H_dev, void* stream);
+
+/*
+ * bitsmoe_mx4_product with weights in bf16: y_s = W_e x_{rows[s]}, or with glu
+ * silu(W^g_e x) * (W^u_e x), for the S slots in expert order.
+ *   W_dev        [E][N] rows of K entries of type t (glu: [E][2 N]), which is bf16
+ *   X_dev        x_rows rows of K entries of type t, ldx entries apart
+ *   the others   as bitsmoe_mx4_product
+ * S may be 0, and so may x_rows (X_dev is then not read).  Shape rules: K % 8 == 0,
+ * ldx >= K, ldx % 8 == 0, ldy >= N, E <= 65535, N and K <= 2^24, S < 2^31 - 256.
+ */
+bitsmoe_status bitsmoe_expert_product(const void* W_dev, bitsmoe_dtype t, int64_t E, int64_t N,
+                                      int64_t K, const void* X_dev, int64_t x_rows, int64_t ldx,
+                                      const int32_t* offsets_dev, const int32_t* rows_dev,
+                                      int64_t S, int glu, void* Y_dev, bitsmoe_dtype yt,
+                                      int64_t ldy, void* stream);
+
+/*
+ * Gradient of the tokens, dx_s = W_e^T dy_s, as bitsmoe_mx4_product_grad.
+ *   dY_dev  [S] rows of N entries of type t, lddy entries apart
+ *   dX_dev  [S] rows of K entries of type xt, ldx entries apart
+ * Shape rules as bitsmoe_expert_product, and N % 8 == 0, lddy % 8 == 0.
+ */
+bitsmoe_status bitsmoe_expert_product_grad(const void* W_dev, bitsmoe_dtype t, int64_t E,
+                                           int64_t N, int64_t K, const void* dY_dev, int64_t lddy,
+                                           const int32_t* offsets_dev, int64_t S, void* dX_dev,
+                                           bitsmoe_dtype xt, int64_t ldx, void* stream);
+
+/*
+ * Gradient of the weights: dW_e = sum over e's slots s of dy_s x_{rows[s]}^T, 0 for
+ * an expert without slots.  Slots whose row is not in [0, x_rows) add nothing.
+ *   dY_dev       [S] rows of N entries of type t (bf16), lddy entries apart
+ *   X_dev        x_rows rows of K entries of type t, ldx entries apart
+ *   offsets_dev, rows_dev   as bitsmoe_mx4_product
+ *   dW_dev       [E][N][K] of type wt, every entry written (S = 0: zeros)
+ * Sums are fp32 in a fixed order.  Shape rules as bitsmoe_expert_product_grad.
+ */
+bitsmoe_status bitsmoe_expert_weight_grad(const void* dY_dev, bitsmoe_dtype t, int64_t lddy,
+                                          int64_t E, int64_t N, int64_t K, const void* X_dev,
+                                          int64_t x_rows, int64_t ldx, const int32_t* offsets_dev,
+                                          const int32_t* rows_dev, int64_t S, void* dW_dev,
+                                          bitsmoe_dtype wt, void* stream);
+
+/*
+ * The same with the tokens in MX8: xcodes_dev [x_rows][K], xscales_dev
+ * [x_rows][K/32]; K % 32 == 0.  They take part as bf16 (exact from 2^-126 on).
+ */
+bitsmoe_status bitsmoe_expert_weight_grad_q(const void* dY_dev, bitsmoe_dtype t, int64_t lddy,
+                                            int64_t E, int64_t N, int64_t K,
+                                            const uint8_t* xcodes_dev, const uint8_t* xscales_dev,
+                                            int64_t x_rows, const int32_t* offsets_dev,
+                                            const int32_t* rows_dev, int64_t S, void* dW_dev,
+                                            bitsmoe_dtype wt, void* stream);
 
 /* Path of a LAPACK shared library for bitsmoe_shared_basis (LP64 or ILP64
  * dsyevd; both plain and "64_"-suffixed symbol names are tried).  When never

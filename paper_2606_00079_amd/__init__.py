@@ -24,6 +24,16 @@ An MoE layer whose experts are held in microscaled 4-bit floats (MX4):
     z = mx4_product(codes, scales, x, offsets=r.offsets, rows=r.rows)
     y = combine(z, r.slots, r.weights)
     (route_grad, mx4_product_grad, combine_grad: the gradients)
+
+The same layer with its experts in bf16, trained from activations that are kept
+in microscaled 8-bit floats (MX8), and the norm before it:
+
+    n = rms_norm(x, weight, residual=r, mx8=True)  # y, inv, sum, codes, scales
+    gu = expert_product(W_up, n.y, offsets=r.offsets, rows=r.rows, dtype=torch.float32)
+    h, codes, scales = glu_mx8(gu)           # silu(gate) * up, and [gate, up] in MX8
+    dgu, h = glu_mx8_grad(codes, scales, dh)
+    dW = expert_weight_grad_q(dgu, n.codes, n.scales, offsets=r.offsets, rows=r.rows)
+    (rms_norm_grad, expert_product_grad, expert_weight_grad: the other gradients)
 """
 from __future__ import annotations
 
@@ -59,6 +69,10 @@ EXPORTS = [
     "bitsmoe_mx4_quantize", "bitsmoe_mx4_dequantize", "bitsmoe_mx4_product",
     "bitsmoe_mx4_product_q", "bitsmoe_mx4_product_grad", "bitsmoe_combine",
     "bitsmoe_combine_grad", "bitsmoe_combine_grad_all",
+    "bitsmoe_mx8_quantize", "bitsmoe_mx8_dequantize", "bitsmoe_rms_norm",
+    "bitsmoe_rms_norm_grad_workspace", "bitsmoe_rms_norm_grad", "bitsmoe_glu_mx8",
+    "bitsmoe_glu_mx8_grad", "bitsmoe_expert_product", "bitsmoe_expert_product_grad",
+    "bitsmoe_expert_weight_grad", "bitsmoe_expert_weight_grad_q",
 ]
 # Candidate widths of the surrogate table, in column order.
 SURROGATE_WIDTHS = (0, 1, 2, 3, 4, 6, 8, 16)
@@ -138,6 +152,17 @@ def lib() -> ctypes.CDLL:
     L.bitsmoe_combine.argtypes = [vp, i32, i64, vp, vp, i64, i64, i64, vp, vp]
     L.bitsmoe_combine_grad.argtypes = [vp, i32, i64, vp, vp, vp, i64, i64, i64, vp, vp, vp]
     L.bitsmoe_combine_grad_all.argtypes = [vp, i32, i64, vp, vp, vp, i64, i64, i64, vp, vp, vp, vp]
+    L.bitsmoe_mx8_quantize.argtypes = L.bitsmoe_mx4_quantize.argtypes
+    L.bitsmoe_mx8_dequantize.argtypes = L.bitsmoe_mx4_dequantize.argtypes
+    L.bitsmoe_rms_norm.argtypes = [vp, i32, i64, vp, i64, vp, i32, i64, i64, ctypes.c_double] + [vp] * 6
+    L.bitsmoe_rms_norm_grad_workspace.argtypes = [i64, i64]
+    L.bitsmoe_rms_norm_grad.argtypes = [vp, i32, i64, vp, i32, vp, vp, i64, vp, i64, i64, i64, vp, vp, vp, i64, vp]
+    L.bitsmoe_glu_mx8.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp]
+    L.bitsmoe_glu_mx8_grad.argtypes = [vp, vp, vp, i32, i64, i64, i64, vp, vp, vp]
+    L.bitsmoe_expert_product.argtypes = [vp, i32, i64, i64, i64, vp, i64, i64, vp, vp, i64, i32, vp, i32, i64, vp]
+    L.bitsmoe_expert_product_grad.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, vp, i32, i64, vp]
+    L.bitsmoe_expert_weight_grad.argtypes = [vp, i32, i64, i64, i64, i64, vp, i64, i64, vp, vp, i64, vp, i32, vp]
+    L.bitsmoe_expert_weight_grad_q.argtypes = [vp, i32, i64, i64, i64, i64, vp, vp, i64, vp, vp, i64, vp, i32, vp]
     L.bitsmoe_set_lapack.argtypes = [ctypes.c_char_p]
     L.bitsmoe_timing.argtypes = [i32]
     L.bitsmoe_timing_only.argtypes = [ctypes.c_char_p]
@@ -149,6 +174,7 @@ def lib() -> ctypes.CDLL:
             getattr(L, name).restype = ctypes.c_int
     L.bitsmoe_release.restype = None
     L.bitsmoe_route_workspace.restype = i64
+    L.bitsmoe_rms_norm_grad_workspace.restype = i64
     lp = _find_lapack()
     if lp and os.environ.get("BITSMOE_LAPACK") is None:
         L.bitsmoe_set_lapack(lp.encode())
@@ -803,6 +829,230 @@ def combine_grad(Z, slots, weights, dY):
                                           _in(dY, "dY", Z, Z.dtype, (T, d)), T, k, d, dZ.data_ptr(), dw.data_ptr(),
                                           None if work is None else work.data_ptr(), stream), "combine_grad")
     return dZ, dw
+
+
+# ---------------------------------------------------------------------------
+# a training step of an MoE block with bf16 experts, activations kept in MX8
+# ---------------------------------------------------------------------------
+def mx8_quantize(X):
+    """Rows of X [..][cols] (bf16 or fp32) to MX8: codes uint8 [..][cols] (the bytes
+    of E4M3 floats) and scales uint8 [..][cols/32]."""
+    torch, stream = _place(X, "X")
+    lead, cols = X.shape[:-1], X.shape[-1]
+    if cols % 32 != 0 or cols == 0:
+        raise ValueError("cols must be a multiple of 32")
+    xp, ld = _rows(X, "X")
+    codes = X.new_empty((*lead, cols), dtype=torch.uint8)
+    scales = X.new_empty((*lead, cols // 32), dtype=torch.uint8)
+    _check(lib().bitsmoe_mx8_quantize(xp, _code(X, "X", torch), X.numel() // cols, cols, ld,
+                                      codes.data_ptr(), scales.data_ptr(), stream), "mx8_quantize")
+    return codes, scales
+
+
+def _mx8(codes, scales, name: str, like, torch, dims: int = 0):
+    """Addresses of MX8 rows."""
+    if (dims and codes.dim() != dims) or codes.shape[:-1] != scales.shape[:-1] or \
+            codes.shape[-1] != 32 * scales.shape[-1]:
+        raise ValueError(f"{name}'s codes must be [..][K] and its scales [..][K/32]")
+    return (_in(codes, f"{name}'s codes", like, torch.uint8),
+            _in(scales, f"{name}'s scales", like, torch.uint8))
+
+
+def mx8_dequantize(codes, scales, dtype=None, out=None):
+    """What MX8 rows stand for -> [..][cols] (bf16 unless ``dtype`` says fp32)."""
+    torch, stream = _place(codes, "X's codes")
+    cp, sp = _mx8(codes, scales, "X", codes, torch)
+    cols = codes.shape[-1]
+    out = _out(out, codes.shape, dtype or torch.bfloat16, codes, torch)
+    _check(lib().bitsmoe_mx8_dequantize(cp, sp, codes.numel() // max(cols, 1), cols, out.data_ptr(),
+                                        _code(out, "out", torch), stream), "mx8_dequantize")
+    return out
+
+
+class Norm(NamedTuple):
+    """What ``rms_norm`` gives for T rows of d entries."""
+    y: object       # [T][d] of the rows' type (None: not wanted)
+    inv: object     # fp32 [T]: 1 / sqrt(mean of squares + eps)
+    sum: object     # [T][d] of the rows' type: x + residual (x itself without one)
+    codes: object   # uint8 [T][d] and
+    scales: object  # uint8 [T][d/32]: y in MX8 (None: not wanted)
+
+
+def _like(t, name: str, like, shape):
+    """(address, row stride) of rows of like's type and device."""
+    if t.dtype is not like.dtype:
+        raise TypeError(f"{name} must be {str(like.dtype).replace('torch.', '')}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}")
+    if t.get_device() != like.get_device():
+        raise TypeError(f"{name} must be on the same CUDA (HIP) device")
+    return _rows(t, name)
+
+
+def rms_norm(X, weight, residual=None, eps: float = 1e-6, rows: bool = True, mx8: bool = False) -> Norm:
+    """y = v / sqrt(mean(v^2) + eps) * weight for the rows v = X + residual (rounded
+    to X's type) of [T][d], bf16 or fp32; weight [d] bf16 or fp32.  mx8: y also
+    in MX8; rows: y itself."""
+    torch, stream = _place(X, "X")
+    if X.dim() != 2:
+        raise ValueError("X must be [T][d]")
+    T, d = X.shape
+    xp, ldx = _rows(X, "X")
+    rp, ldr = (None, 0) if residual is None else _like(residual, "residual", X, X.shape)
+    total = X if residual is None else X.new_empty((T, d))
+    y = X.new_empty((T, d)) if rows else None
+    inv = X.new_empty((T,), dtype=torch.float32)
+    codes = scales = None
+    if mx8:
+        if d % 32 != 0:
+            raise ValueError("MX8 needs d to be a multiple of 32")
+        codes = X.new_empty((T, d), dtype=torch.uint8)
+        scales = X.new_empty((T, d // 32), dtype=torch.uint8)
+    _check(lib().bitsmoe_rms_norm(xp, _code(X, "X", torch), ldx, rp, ldr, _in(weight, "weight", X, weight.dtype, (d,)),
+                                  _code(weight, "weight", torch), T, d, eps,
+                                  None if residual is None else total.data_ptr(), y.data_ptr() if rows else None,
+                                  codes.data_ptr() if mx8 else None, scales.data_ptr() if mx8 else None,
+                                  inv.data_ptr(), stream), "rms_norm")
+    return Norm(y, inv, total, codes, scales)
+
+
+def rms_norm_grad(sum, weight, inv, dY, dsum=None, dweight: bool = True):
+    """Gradients of ``rms_norm`` from that of y and (None: 0) of the sum -> (dX [T][d]
+    of the rows' type, for X and the residual alike, and dweight fp32 [d] or None)."""
+    torch, stream = _place(sum, "sum")
+    if sum.dim() != 2:
+        raise ValueError("sum must be [T][d]")
+    T, d = sum.shape
+    vp, ldv = _rows(sum, "sum")
+    yp, ldy = _like(dY, "dY", sum, sum.shape)
+    sp, lds = (None, 0) if dsum is None else _like(dsum, "dsum", sum, sum.shape)
+    dX = sum.new_empty((T, d))
+    L = lib()
+    room = L.bitsmoe_rms_norm_grad_workspace(T, d) if dweight else 0
+    dw = sum.new_empty((d,), dtype=torch.float32) if dweight else None
+    work = sum.new_empty((room // 4,), dtype=torch.float32) if room else None
+    _check(L.bitsmoe_rms_norm_grad(vp, _code(sum, "sum", torch), ldv, _in(weight, "weight", sum, weight.dtype, (d,)),
+                                   _code(weight, "weight", torch), _in(inv, "inv", sum, torch.float32, (T,)), yp, ldy,
+                                   sp, lds, T, d, dX.data_ptr(), dw.data_ptr() if dweight else None,
+                                   work.data_ptr() if room else None, room, stream), "rms_norm_grad")
+    return dX, dw
+
+
+def glu_mx8(GU):
+    """h = silu(g) * u of rows [g, u] of GU [S][2 N] (bf16 or fp32) -> (h bf16 [S][N],
+    and GU in MX8: codes uint8 [S][2 N], scales uint8 [S][2 N/32])."""
+    torch, stream = _place(GU, "GU")
+    if GU.dim() != 2 or GU.shape[1] == 0 or GU.shape[1] % 64 != 0:
+        raise ValueError("GU must be [S][2 N] with N a multiple of 32")
+    S, N = GU.shape[0], GU.shape[1] // 2
+    gp, ld = _rows(GU, "GU")
+    h = GU.new_empty((S, N), dtype=torch.bfloat16)
+    codes = GU.new_empty((S, 2 * N), dtype=torch.uint8)
+    scales = GU.new_empty((S, N // 16), dtype=torch.uint8)
+    _check(lib().bitsmoe_glu_mx8(gp, _code(GU, "GU", torch), S, N, ld, h.data_ptr(), codes.data_ptr(),
+                                 scales.data_ptr(), stream), "glu_mx8")
+    return h, codes, scales
+
+
+def glu_mx8_grad(codes, scales, dH, again: bool = True):
+    """Gradient of silu(g) * u at what MX8 rows [g, u] stand for, from dH [S][N]
+    (bf16 or fp32) -> (bf16 [S][2 N], and with ``again`` h of those values, bf16 [S][N])."""
+    torch, stream = _place(dH, "dH")
+    if dH.dim() != 2:
+        raise ValueError("dH must be [S][N]")
+    S, N = dH.shape
+    cp, sp = _mx8(codes, scales, "GU", dH, torch, 2)
+    if codes.shape != (S, 2 * N):
+        raise ValueError("GU must be [S][2 N] for dH [S][N]")
+    hp, ld = _rows(dH, "dH")
+    dgu = dH.new_empty((S, 2 * N), dtype=torch.bfloat16)
+    h = dH.new_empty((S, N), dtype=torch.bfloat16) if again else None
+    _check(lib().bitsmoe_glu_mx8_grad(cp, sp, hp, _code(dH, "dH", torch), S, N, ld, dgu.data_ptr(),
+                                      h.data_ptr() if again else None, stream), "glu_mx8_grad")
+    return dgu, h
+
+
+def expert_product(W, X, offsets=None, rows=None, glu: bool = False, dtype=None, out=None):
+    """y_s = W_e x_{rows[s]} for the slots in expert order, as ``mx4_product`` with W
+    bf16 [E][N][K]: X bf16 [rows][K] -> [S][N], bf16 unless ``dtype`` says fp32.
+    glu: W holds gate rows, then up rows, and y = silu(gate) * up -> [S][N/2]."""
+    torch, stream = _place(X, "X")
+    if X.dim() != 2 or W.dim() != 3:
+        raise ValueError("X must be [rows][K] and W [E][N][K]")
+    E, N, K = W.shape
+    if X.shape[1] != K:
+        raise ValueError("X and W disagree on K")
+    if glu:
+        if N % 2:
+            raise ValueError("glu takes as many gate as up rows")
+        N //= 2
+    S = X.shape[0] if rows is None else rows.shape[0]
+    xp, ldx = _rows(X, "X")
+    out = _out(out, (S, N), dtype or torch.bfloat16, X, torch)
+    _check(lib().bitsmoe_expert_product(_in(W, "W", X, X.dtype), _code(X, "X", torch), E, N, K, xp, X.shape[0], ldx,
+                                        _in(offsets, "offsets", X, torch.int32, (E + 1,)),
+                                        _in(rows, "rows", X, torch.int32, (S,)), S, int(glu), out.data_ptr(),
+                                        _code(out, "out", torch), N, stream), "expert_product")
+    return out
+
+
+def expert_product_grad(W, dY, offsets=None, dtype=None, out=None):
+    """dx_s = W_e^T dy_s for the slots in expert order: W bf16 [E][N][K], dY bf16
+    [S][N] -> [S][K], bf16 unless ``dtype`` says fp32."""
+    torch, stream = _place(dY, "dY")
+    if dY.dim() != 2 or W.dim() != 3:
+        raise ValueError("dY must be [S][N] and W [E][N][K]")
+    S, (E, N, K) = dY.shape[0], W.shape
+    if dY.shape[1] != N:
+        raise ValueError("dY and W disagree on N")
+    yp, ldy = _rows(dY, "dY")
+    out = _out(out, (S, K), dtype or torch.bfloat16, dY, torch)
+    _check(lib().bitsmoe_expert_product_grad(_in(W, "W", dY, dY.dtype), _code(dY, "dY", torch), E, N, K, yp, ldy,
+                                             _in(offsets, "offsets", dY, torch.int32, (E + 1,)), S, out.data_ptr(),
+                                             _code(out, "out", torch), K, stream), "expert_product_grad")
+    return out
+
+
+def _experts_of(offsets, rows, S: int, x_rows: int, like, torch):
+    """(E, address of offsets, address of rows) of a weights' gradient."""
+    E = 1 if offsets is None else offsets.shape[0] - 1
+    if rows is None and x_rows != S:
+        raise ValueError("X must have a row for every slot, or rows be given")
+    return (E, _in(offsets, "offsets", like, torch.int32, (E + 1,)), _in(rows, "rows", like, torch.int32, (S,)))
+
+
+def expert_weight_grad(dY, X, offsets=None, rows=None, dtype=None, out=None):
+    """dW_e = sum over e's slots of dy_s x_{rows[s]}^T: dY bf16 [S][N], X bf16
+    [rows][K] -> [E][N][K], bf16 unless ``dtype`` says fp32 (E from offsets; without
+    them 1)."""
+    torch, stream = _place(dY, "dY")
+    if dY.dim() != 2 or X.dim() != 2:
+        raise ValueError("dY must be [S][N] and X [rows][K]")
+    (S, N), K = dY.shape, X.shape[1]
+    E, op, rp = _experts_of(offsets, rows, S, X.shape[0], dY, torch)
+    yp, ldy = _rows(dY, "dY")
+    xp, ldx = _like(X, "X", dY, X.shape)
+    out = _out(out, (E, N, K), dtype or torch.bfloat16, dY, torch)
+    _check(lib().bitsmoe_expert_weight_grad(yp, _code(dY, "dY", torch), ldy, E, N, K, xp, X.shape[0], ldx, op, rp, S,
+                                            out.data_ptr(), _code(out, "out", torch), stream), "expert_weight_grad")
+    return out
+
+
+def expert_weight_grad_q(dY, xcodes, xscales, offsets=None, rows=None, dtype=None, out=None):
+    """expert_weight_grad with the tokens in MX8 (``mx8_quantize`` of X, or what
+    ``rms_norm`` kept)."""
+    torch, stream = _place(dY, "dY")
+    if dY.dim() != 2:
+        raise ValueError("dY must be [S][N]")
+    xcp, xsp = _mx8(xcodes, xscales, "X", dY, torch, 2)
+    (S, N), K = dY.shape, xcodes.shape[1]
+    E, op, rp = _experts_of(offsets, rows, S, xcodes.shape[0], dY, torch)
+    yp, ldy = _rows(dY, "dY")
+    out = _out(out, (E, N, K), dtype or torch.bfloat16, dY, torch)
+    _check(lib().bitsmoe_expert_weight_grad_q(yp, _code(dY, "dY", torch), ldy, E, N, K, xcp, xsp, xcodes.shape[0], op,
+                                              rp, S, out.data_ptr(), _code(out, "out", torch), stream),
+           "expert_weight_grad_q")
+    return out
 
 
 def timing(enable: bool, only: Optional[str] = None) -> None:

@@ -18,6 +18,9 @@ widths {0, 1, 2, 3, 4, 6, 8, 16} under the equivalent-bit budget.
 
 ``mx4_layer`` runs an MoE layer whose experts are held in MX4, from the
 router's logits to the layer's output, and ``mx4_layer_grad`` its gradients.
+``experts_layer`` and ``experts_layer_grad`` do the same with experts in bf16 and
+give their gradients too; ``moe_block`` puts the residual's addition, the norm and
+the router's product before it.  What these keep for the backward pass is in MX8.
 """
 from __future__ import annotations
 
@@ -27,9 +30,11 @@ from typing import Dict, List, Optional, Sequence
 
 import numpy as np
 
-from . import (SURROGATE_WIDTHS, Routing, allocate, basis_importance, combine, combine_grad, gram,
-               gram_experts, gram_experts_in, gram_routed, mx4_product, mx4_product_grad,
-               mx4_product_q, mx4_quantize, pack, pack_layout, project, project_in, route,
+from . import (SURROGATE_WIDTHS, Norm, Routing, allocate, basis_importance, combine, combine_grad,
+               expert_product, expert_product_grad, expert_weight_grad, expert_weight_grad_q,
+               glu_mx8, glu_mx8_grad, gram, gram_experts, gram_experts_in, gram_routed,
+               mx4_product, mx4_product_grad, mx4_product_q, mx4_quantize, mx8_dequantize,
+               mx8_quantize, pack, pack_layout, project, project_in, rms_norm, rms_norm_grad, route,
                route_grad, score, score_diag, score_routed, shared_basis, shared_basis_gpu,
                surrogate, surrogate_budget)
 
@@ -303,17 +308,18 @@ class Mx4Saved:
     """What the gradients of a layer read."""
     routing: Routing
     logits: object
-    up: object       # [S][2 N] fp32: the gate and up values, not rounded
+    up: object       # [S][2 N] fp32: the gate and up values, not rounded; or [codes, scales] of them in MX8
     z: object        # [S][K] bf16: the experts' outputs
     renorm: bool
 
 
 def mx4_layer(x, logits, experts: Mx4Experts, k: int, valid=None, renorm: bool = True,
-              quantize_tokens: bool = False, train: bool = False):
+              quantize_tokens: bool = False, train: bool = False, checkpoint: bool = False):
     """y_t = sum_j w_tj down_e(silu(gate_e x_t) * up_e x_t) for tokens x bf16
     [T][K] and the router's logits [T][E] -> (y bf16 [T][K], Routing), and with
     ``train`` also what ``mx4_layer_grad`` reads.  quantize_tokens: the products
-    take their tokens in MX4 as well."""
+    take their tokens in MX4 as well.  checkpoint: gate and up are kept in MX8, a
+    quarter of the bytes, and the gradients are taken at what that stands for."""
     import torch
     r = route(logits, k, valid=valid, renorm=renorm)
 
@@ -324,7 +330,9 @@ def mx4_layer(x, logits, experts: Mx4Experts, k: int, valid=None, renorm: bool =
 
     # (in training gate and up are kept, and stay fp32 up to silu(g) u as they do within the product with glu)
     up = product(experts.up_codes, experts.up_scales, x, r.rows, not train, torch.float32 if train else None)
-    if train:
+    if train and checkpoint:
+        h, *up = glu_mx8(up)
+    elif train:
         g, u = up.chunk(2, dim=1)
         h = (torch.nn.functional.silu(g) * u).to(torch.bfloat16)
     else:
@@ -343,11 +351,111 @@ def mx4_layer_grad(saved: Mx4Saved, experts: Mx4Experts, dy, dlosses=None):
     dz, dw = combine_grad(saved.z, r.slots, r.weights, dy)
     dh = mx4_product_grad(experts.down_codes, experts.down_scales, dz, offsets=r.offsets,
                           dtype=torch.float32)
-    g, u = saved.up.chunk(2, dim=1)
-    sig = torch.sigmoid(g)
-    # (bf16 is what the matrix cores take: dz and this are rounded once each, as their operands)
-    dup = torch.cat((dh * u * sig * (1 + g * (1 - sig)), dh * g * sig), 1).to(torch.bfloat16)
+    # (bf16 is what the matrix cores take: dz and the gate's and up's gradient are rounded once each, as their operands)
+    if isinstance(saved.up, list):
+        dup, _ = glu_mx8_grad(*saved.up, dh, again=False)
+    else:
+        g, u = saved.up.chunk(2, dim=1)
+        sig = torch.sigmoid(g)
+        dup = torch.cat((dh * u * sig * (1 + g * (1 - sig)), dh * g * sig), 1).to(torch.bfloat16)
     # (a token's slots are summed up before the one rounding)
     dx = combine(mx4_product_grad(experts.up_codes, experts.up_scales, dup, offsets=r.offsets,
                                   dtype=torch.float32), r.slots).to(torch.bfloat16)
     return dx, route_grad(saved.logits, r, dweights=dw, dlosses=dlosses, renorm=saved.renorm)
+
+
+# ---------------------------------------------------------------------------
+# a training step of an MoE block with its experts in bf16
+# ---------------------------------------------------------------------------
+@dataclasses.dataclass
+class Experts:
+    """The experts' weights in bf16: gate rows, then up rows, of every expert
+    [E][2 N][K], and its down rows [E][K][N]."""
+    up: object
+    down: object
+
+
+@dataclasses.dataclass
+class ExpertsSaved:
+    """What the gradients of a layer read: its activations in MX8, each as (codes, scales)."""
+    routing: Routing
+    logits: object
+    x: tuple   # [T][K]: the tokens
+    up: tuple  # [S][2 N]: the gate and up values
+    z: tuple   # [S][K]: the experts' outputs
+    renorm: bool
+
+
+def experts_layer(x, logits, experts: Experts, k: int, valid=None, renorm: bool = True, train: bool = False,
+                  kept=None):
+    """``mx4_layer`` with experts in bf16: y_t = sum_j w_tj down_e(silu(gate_e x_t) *
+    up_e x_t) for tokens x bf16 [T][K] and the router's logits [T][E] -> (y bf16
+    [T][K], Routing), and with ``train`` also what ``experts_layer_grad`` reads.
+    kept: x in MX8 as (codes, scales), where the caller has it (``rms_norm``)."""
+    import torch
+    r = route(logits, k, valid=valid, renorm=renorm)
+    if not train:
+        h = expert_product(experts.up, x, offsets=r.offsets, rows=r.rows, glu=True)
+        z = expert_product(experts.down, h, offsets=r.offsets)
+        return combine(z, r.slots, r.weights), r
+    # (gate and up stay fp32 up to silu(g) u, as within the product with glu)
+    h, *up = glu_mx8(expert_product(experts.up, x, offsets=r.offsets, rows=r.rows, dtype=torch.float32))
+    z = expert_product(experts.down, h, offsets=r.offsets)
+    y = combine(z, r.slots, r.weights)
+    return y, r, ExpertsSaved(r, logits, mx8_quantize(x) if kept is None else kept, tuple(up), mx8_quantize(z), renorm)
+
+
+def experts_layer_grad(saved: ExpertsSaved, experts: Experts, dy, dlosses=None, dtype=None):
+    """Gradients from that of y (bf16 [T][K]) and of the two losses (fp32 [2]): (dx
+    bf16 [T][K], dlogits, d_up [E][2 N][K], d_down [E][K][N]), the weights' in bf16
+    unless ``dtype`` says fp32."""
+    import torch
+    r = saved.routing
+    dz, dw = combine_grad(mx8_dequantize(*saved.z), r.slots, r.weights, dy)
+    dh = expert_product_grad(experts.down, dz, offsets=r.offsets, dtype=torch.float32)
+    dup, h = glu_mx8_grad(*saved.up, dh)
+    d_down = expert_weight_grad(dz, h, offsets=r.offsets, dtype=dtype)
+    d_up = expert_weight_grad_q(dup, *saved.x, offsets=r.offsets, rows=r.rows, dtype=dtype)
+    # (a token's slots are summed up before the one rounding)
+    dx = combine(expert_product_grad(experts.up, dup, offsets=r.offsets, dtype=torch.float32), r.slots)
+    dlogits = route_grad(saved.logits, r, dweights=dw, dlosses=dlosses, renorm=saved.renorm)
+    return dx.to(torch.bfloat16), dlogits, d_up, d_down
+
+
+@dataclasses.dataclass
+class BlockSaved:
+    """What the gradients of a block read beside its weights."""
+    sum: object  # bf16 [T][K]: the residual stream, which the caller has too
+    inv: object  # fp32 [T]
+    layer: ExpertsSaved
+
+
+def moe_block(x, residual, weight, router, experts: Experts, k: int, eps: float = 1e-6, valid=None,
+              renorm: bool = True, train: bool = False):
+    """The second half of a transformer's block: the residual's addition, the norm
+    (weight [K]), the router's product (bf16 [E][K]; E a multiple of 8 for its
+    gradient) and the experts.  x and residual bf16 [T][K] (residual may be None) ->
+    (y, the sum that the next block adds y to, Routing), and with ``train`` also
+    what ``moe_block_grad`` reads."""
+    import torch
+    n: Norm = rms_norm(x, weight, residual=residual, eps=eps, mx8=train)
+    logits = expert_product(router.unsqueeze(0), n.y, dtype=torch.float32)
+    if not train:
+        y, r = experts_layer(n.y, logits, experts, k, valid=valid, renorm=renorm)
+        return y, n.sum, r
+    y, r, saved = experts_layer(n.y, logits, experts, k, valid=valid, renorm=renorm, train=True,
+                                kept=(n.codes, n.scales))
+    return y, n.sum, r, BlockSaved(n.sum, n.inv, saved)
+
+
+def moe_block_grad(saved: BlockSaved, weight, router, experts: Experts, dy, dsum=None, dlosses=None, dtype=None):
+    """Gradients of ``moe_block`` from those of y and of the sum (bf16 [T][K]) and of
+    the two losses: (dx, which is the residual's too, dweight fp32 [K], d_router,
+    d_up, d_down), the last three in bf16 unless ``dtype`` says fp32."""
+    import torch
+    dn, dlogits, d_up, d_down = experts_layer_grad(saved.layer, experts, dy, dlosses, dtype)
+    dl = dlogits.to(torch.bfloat16)
+    d_router = expert_weight_grad_q(dl, *saved.layer.x, dtype=dtype).squeeze(0)
+    dn = dn + expert_product_grad(router.unsqueeze(0), dl)
+    dx, dweight = rms_norm_grad(saved.sum, weight, saved.inv, dn, dsum=dsum)
+    return dx, dweight, d_router, d_up, d_down

@@ -1,0 +1,628 @@
+"""GPU parity of the operators of an MoE block's training step (norm, MX8, gated
+activation, products with bf16 experts and their gradients) against the fp64
+oracle.
+
+Bounds: MX8 codes and scales are equal.  A sum of n fp32 terms in any order is
+within n 2^-24 of the sum of their magnitudes; 2^-23 is allowed, as a matrix core
+may cut instead of round.  A result is rounded once, by half a step of its type at
+most: bf16 2^-8 of it, E4M3 2^-4.  exp and reciprocals are taken to be within 2^-21
+each, 2^-20 for a sigmoid, whose value below 2^-126 may be 0.
+"""
+import numpy as np
+import pytest
+
+from conftest import gpu_available
+from oracle import block, mx4, mx8
+
+pytestmark = pytest.mark.gpu
+
+if not gpu_available():  # pragma: no cover
+    pytest.skip("no GPU", allow_module_level=True)
+
+import torch  # noqa: E402
+
+import paper_2606_00079_amd as bm  # noqa: E402
+from paper_2606_00079_amd import pipeline  # noqa: E402
+
+DEV = "cuda:0"
+U = 2.0 ** -23
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+
+
+def np64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def dev(a, dtype=None):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV, dtype)
+
+
+def randn(g, *shape, dtype="bf16", scale=1.0):
+    return dev((g.standard_normal(shape) * scale).astype(np.float32)).to(DT[dtype])
+
+
+def within(got, want, bound, what):
+    got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
+    assert got.shape == want.shape, what
+    want = np.where(np.abs(want) >= 2.0 ** 128, np.copysign(np.inf, want), want)  # past fp32 and bf16
+    assert (np.isnan(got) == np.isnan(want)).all(), what
+    inf = np.isinf(want)
+    assert (got[inf] == want[inf]).all(), what
+    ok = np.isfinite(want)
+    off = np.abs(got[ok] - want[ok]) - np.broadcast_to(bound, want.shape)[ok]
+    assert not (off > 0).any(), (what, float(off.max()), int((off > 0).sum()))
+
+
+def apart(t, extra=8):
+    """The same matrix with rows further apart."""
+    wide = torch.full((t.shape[0], t.shape[1] + extra), float("nan"), dtype=t.dtype, device=t.device)
+    wide[:, :t.shape[1]] = t
+    return wide[:, :t.shape[1]]
+
+
+# ------------------------------------------------------------------- MX8
+def rows_for(kind, rows, cols, g):
+    x = g.standard_normal((rows, cols)) * np.exp(2 * g.standard_normal((rows, 1)))
+    if kind == "edges":  # every value of the format and the points half way, both signs, over many scales
+        pts = np.concatenate((mx8.GRID, (mx8.GRID[1:] + mx8.GRID[:-1]) / 2, [449, 464, 479]))
+        x = g.choice(pts, (rows, cols)) * g.choice([-1, 1], (rows, cols))
+        x *= 2.0 ** g.integers(-133, 118, (rows, cols // 32)).repeat(32, 1)
+    elif kind == "special":
+        at = g.random((rows, cols))
+        x[at < 0.01], x[(at > 0.01) & (at < 0.015)], x[(at > 0.015) & (at < 0.02)] = np.nan, np.inf, -np.inf
+        x[:, :32] = 0.0
+        x[rows // 2] = -0.0
+        x[0, 32:] = 1e-42
+        x[-1] = 3e38
+    return x
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["normal", "edges", "special"])
+@pytest.mark.parametrize("rows,cols", [(1, 32), (1, 2048), (3, 96), (257, 160), (64, 1024)])
+def test_mx8_is_exact(dtype, kind, rows, cols):
+    g = np.random.default_rng([rows, cols, len(kind)])
+    X = dev(rows_for(kind, rows, cols, g).astype(np.float32)).to(DT[dtype])
+    for x in (X, apart(X)):
+        codes, scales = bm.mx8_quantize(x)
+        want = mx8.quantize(np64(X))
+        assert (scales.cpu().numpy() == want[1]).all()
+        assert (codes.cpu().numpy() == want[0]).all()
+    values = mx8.dequantize(*want)
+    within(np64(bm.mx8_dequantize(codes, scales, dtype=torch.float32)), values, 0.0, "f32")
+    # (bf16 ends at 2^-133)
+    within(np64(bm.mx8_dequantize(codes, scales)), values, np.where(np.abs(values) < 2.0 ** -126, 2.0 ** -134, 0), "bf16")
+
+
+def test_every_mx8_code_with_every_scale():
+    codes = torch.arange(256, dtype=torch.uint8, device=DEV).repeat(256, 1)
+    scales = torch.arange(256, dtype=torch.uint8, device=DEV)[:, None].repeat(1, 8)
+    want = mx8.dequantize(codes.cpu().numpy(), scales.cpu().numpy())
+    within(np64(bm.mx8_dequantize(codes, scales, dtype=torch.float32)), want, 0.0, "f32")
+    within(np64(bm.mx8_dequantize(codes, scales)), want, np.where(np.abs(want) < 2.0 ** -126, 2.0 ** -134, 0), "bf16")
+
+
+def test_mx8_of_no_rows():
+    codes, scales = bm.mx8_quantize(torch.empty((0, 64), device=DEV))
+    assert codes.shape == (0, 64) and scales.shape == (0, 2) and bm.mx8_dequantize(codes, scales).shape == (0, 64)
+
+
+# ------------------------------------------------------------------- norm
+def check_norm(X, R, w, eps, what, mx8_too=True, dsum_too=True, rows=True):
+    T, d = X.shape
+    g = np.random.default_rng([T, d])
+    n = bm.rms_norm(X, w, residual=R, eps=eps, mx8=mx8_too, rows=rows)
+    dt = X.dtype
+    if R is None:
+        assert n.sum is X
+    else:
+        assert torch.equal(n.sum, (X.float() + R.float()).to(dt)) and n.sum.is_contiguous(), what
+    v, w64 = np64(n.sum), np64(w)
+    y, inv = block.rms_norm(v, w64, np.float64(np.float32(eps)))
+    rel = (d + 16) * U
+    within(np64(n.inv), inv, inv * rel, (what, "inv"))
+    if rows:
+        assert n.y.dtype == dt
+        within(np64(n.y), y, np.abs(y) * (rel + 3 * U + HALF[dt]), (what, "y"))
+    else:
+        assert n.y is None
+    if mx8_too:
+        got = np64(bm.mx8_dequantize(n.codes, n.scales, dtype=torch.float32))
+        top = np.abs(y).reshape(T, d // 32, 32).max(-1).repeat(32, 1)  # (a scale is below 1/224 of it)
+        within(got, y, np.abs(y) * (rel + 3 * U + 2.0 ** -4) + top * (2.0 ** -10 / 224 * 1.01), (what, "mx8"))
+    else:
+        assert n.codes is None and n.scales is None
+    dY = dev(g.standard_normal((T, d)).astype(np.float32)).to(dt)
+    dsum = dev(g.standard_normal((T, d)).astype(np.float32)).to(dt) if dsum_too else None
+    dX, dw = bm.rms_norm_grad(n.sum, w, n.inv, dY, dsum=dsum)
+    assert dX.dtype == dt and dw.dtype == torch.float32
+    i64, dy = np64(n.inv), np64(dY)
+    want, want_w = block.rms_norm_grad(v, w64, i64, dy, None if dsum is None else np64(dsum))
+    nh, gr = np.abs(v * i64[:, None]), np.abs(dy * w64)
+    along = (nh * gr).mean(1, keepdims=True)
+    bound = i64[:, None] * (nh * along * (d + 12) * U + 4 * U * gr)
+    if dsum is not None:
+        bound = bound + U * np.abs(np64(dsum))
+    within(np64(dX), want, bound + (np.abs(want) + bound) * HALF[dt], (what, "dx"))
+    within(np64(dw), want_w, (T + 8) * U * (np.abs(dy) * nh).sum(0), (what, "dw"))
+    again = bm.rms_norm_grad(n.sum, w, n.inv, dY, dsum=dsum)
+    assert torch.equal(again[0], dX) and torch.equal(again[1], dw)
+    only, none = bm.rms_norm_grad(n.sum, w, n.inv, dY, dsum=dsum, dweight=False)
+    assert none is None and torch.equal(only, dX)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d", [(1, 32), (1, 2048), (3, 512), (5, 544), (130, 64), (67, 1024), (33, 1056), (9, 2080),
+                                 (6, 4096), (5, 4128), (601, 7168), (3, 8224), (2, 16384), (3, 16416), (2, 32768)])
+def test_norm(dtype, T, d):
+    g = np.random.default_rng([T, d, 7])
+    X, R = randn(g, T, d, dtype=dtype, scale=3), randn(g, T, d, dtype=dtype)
+    w = dev((1 + 0.3 * g.standard_normal(d)).astype(np.float32))
+    check_norm(X, R, w, 1e-6, (T, d))
+    check_norm(X, None, w.bfloat16(), 1e-5, (T, d, "no residual"), dsum_too=False, rows=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [8, 40, 1000, 4104])
+def test_norm_of_rows_without_blocks(dtype, d):
+    g = np.random.default_rng(d)
+    X = randn(g, 19, d, dtype=dtype)
+    check_norm(X, randn(g, 19, d, dtype=dtype), randn(g, d, dtype="f32"), 1e-3, d, mx8_too=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norm_strides_and_gradients_in_place_of_columns(dtype):
+    g = np.random.default_rng(3)
+    X, R, w = (randn(g, 21, 96, dtype=dtype) for _ in range(3))
+    a, b = bm.rms_norm(X, w[0], residual=R, mx8=True), bm.rms_norm(apart(X), w[0], residual=apart(R, 16), mx8=True)
+    for x, y in zip(a, b):
+        assert torch.equal(x, y)
+    dY, ds = randn(g, 21, 96, dtype=dtype), randn(g, 21, 96, dtype=dtype)
+    a = bm.rms_norm_grad(a.sum, w[0], a.inv, dY, dsum=ds)
+    b = bm.rms_norm_grad(apart(b.sum), w[0], b.inv, apart(dY, 24), dsum=apart(ds))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_norm_of_no_rows():
+    w = torch.ones(64, device=DEV)
+    n = bm.rms_norm(torch.empty((0, 64), device=DEV), w, residual=torch.empty((0, 64), device=DEV), mx8=True)
+    assert n.y.shape == (0, 64) and n.codes.shape == (0, 64) and n.inv.shape == (0,)
+    dX, dw = bm.rms_norm_grad(n.sum, w, n.inv, n.y)
+    assert dX.shape == (0, 64) and torch.equal(dw, torch.zeros(64, device=DEV))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norm_of_extreme_rows(dtype):
+    """Zeros, rows whose squares pass fp32's range either way, an infinity, a NaN."""
+    g = np.random.default_rng(4)
+    X = g.standard_normal((8, 64))
+    X[0] = 0
+    X[1] *= 1e30
+    X[2] = 3.3e38
+    X[3] *= 1e-30
+    X[4] *= 2e19
+    X[5, 3] = np.inf
+    X[6, 5] = np.nan
+    X = dev(X.astype(np.float32)).to(DT[dtype])
+    w = torch.ones(64, device=DEV)
+    n = bm.rms_norm(X, w, eps=1e-6, mx8=True)
+    keep = [0, 1, 2, 3, 4, 7]
+    y, inv = block.rms_norm(np64(X)[keep], 1.0, np.float64(np.float32(1e-6)))
+    # (1 / 3.3e38 is below 2^-126: a step of 2^-149 there)
+    within(np64(n.inv)[keep], inv, inv * 80 * U + 2.0 ** -149, "inv")
+    within(np64(n.y)[keep], y, np.abs(y) * (84 * U + 2.0 ** -21 + HALF[dtype]) + 2.0 ** -134, "y")
+    got = np64(n.y)
+    assert np.isnan(got[5, 3]) and (np.delete(got[5], 3) == 0).all() and np.isnan(got[6]).all()
+    assert (n.scales[6] == 255).all() and n.scales[5].tolist() == [255, 0]
+    s = n.scales.cpu().numpy()
+    assert (s[0] == 0).all() and (s[1] < 255).all()
+
+
+def test_norm_refuses():
+    X, w = torch.zeros((4, 64), device=DEV), torch.ones(64, device=DEV)
+    for bad, error in [
+            (lambda: bm.rms_norm(X, w, residual=X.bfloat16()), TypeError),
+            (lambda: bm.rms_norm(X, w, residual=X[:3]), ValueError),
+            (lambda: bm.rms_norm(X, w[:32]), ValueError), (lambda: bm.rms_norm(X, w.half()), TypeError),
+            (lambda: bm.rms_norm(X.half(), w), TypeError), (lambda: bm.rms_norm(X.cpu(), w), TypeError),
+            (lambda: bm.rms_norm(X, w.cpu()), TypeError), (lambda: bm.rms_norm(X[0], w), ValueError),
+            (lambda: bm.rms_norm(X.t(), w[:4]), ValueError),
+            (lambda: bm.rms_norm(X[:, :40].contiguous(), w[:40].clone(), mx8=True), ValueError),
+            (lambda: bm.rms_norm(X, w, eps=0.0), bm.BitsmoeError),
+            (lambda: bm.rms_norm(X[:, 1:33], w[:32]), bm.BitsmoeError),
+            (lambda: bm.rms_norm_grad(X, w, w[:4], X.bfloat16()), TypeError),
+            (lambda: bm.rms_norm_grad(X, w, w[:4], X, dsum=X[:2]), ValueError),
+            (lambda: bm.rms_norm_grad(X, w, w[:3], X), ValueError)]:
+        with pytest.raises(error):
+            bad()
+
+
+# ------------------------------------------------------- gated activation
+def check_glu(GU, dH, what):
+    S, N = dH.shape
+    h, codes, scales = bm.glu_mx8(GU)
+    assert h.dtype == torch.bfloat16 and h.shape == (S, N)
+    gu = np64(GU)
+    want = mx8.quantize(gu)
+    assert (codes.cpu().numpy() == want[0]).all() and (scales.cpu().numpy() == want[1]).all(), what
+    with np.errstate(invalid="ignore"):
+        y = mx8.glu(gu)
+        tiny = 2.0 ** -125 * (1 + np.abs(gu[:, :N])) * (1 + np.abs(gu[:, N:]))
+        within(np64(h), y, np.abs(y) * (2.0 ** -8 + 2.0 ** -19) + tiny, (what, "h"))
+        dgu, again = bm.glu_mx8_grad(codes, scales, dH)
+        kept, dh = mx8.dequantize(*want), np64(dH)
+        y = mx8.glu(kept)
+        g, u = kept[:, :N], kept[:, N:]
+        tiny = 2.0 ** -125 * (1 + np.abs(g)) * (1 + np.abs(u))
+        within(np64(again), y, np.abs(y) * (2.0 ** -8 + 2.0 ** -19) + tiny, (what, "h again"))
+        s = 1 / (1 + np.exp(-np.maximum(g, -700)))
+        grad = mx8.glu_grad(kept, dh)
+        # each of the two terms of the gate's slope with a sigmoid's error, and 1 - s to 2^-20
+        mag = np.concatenate((np.abs(dh * u) * (s + np.abs(g) * s * (1 - s + 2.0 ** -3)), np.abs(dh * g * s)), 1)
+        rest = np.tile(tiny * (1 + np.abs(dh)), 2)
+        within(np64(dgu), grad, mag * 2.0 ** -17 + np.abs(grad) * 2.0 ** -8 + rest, (what, "dgu"))
+    only, none = bm.glu_mx8_grad(codes, scales, dH, again=False)
+    assert none is None and (only.view(torch.int16) == dgu.view(torch.int16)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("grad", ["bf16", "f32"])
+@pytest.mark.parametrize("S,N", [(1, 32), (184, 768), (7, 96), (1, 4096), (333, 160)])
+def test_glu(dtype, grad, S, N):
+    g = np.random.default_rng([S, N])
+    GU = randn(g, S, 2 * N, dtype=dtype, scale=3)
+    dH = randn(g, S, N, dtype=grad)
+    check_glu(GU, dH, (S, N))
+    a, b = bm.glu_mx8(GU), bm.glu_mx8(apart(GU))
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    a, b = bm.glu_mx8_grad(*a[1:], dH), bm.glu_mx8_grad(*a[1:], apart(dH))
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_glu_of_extreme_rows(dtype):
+    g = np.random.default_rng(5)
+    GU = g.standard_normal((6, 128))
+    GU[0], GU[1] = 0, 200 * GU[1]
+    GU[2, :64] = -90
+    GU[3, 64:] *= 1e30
+    GU[4, 3], GU[5, 70] = np.nan, np.nan
+    GU = dev(GU.astype(np.float32)).to(DT[dtype])
+    check_glu(GU, randn(g, 6, 64, dtype="f32"), "extreme")
+
+
+def test_glu_of_none_and_refusals():
+    h, codes, scales = bm.glu_mx8(torch.empty((0, 128), device=DEV))
+    assert h.shape == (0, 64) and codes.shape == (0, 128) and scales.shape == (0, 4)
+    assert bm.glu_mx8_grad(codes, scales, h)[0].shape == (0, 128)
+    GU = torch.zeros((4, 128), device=DEV)
+    _, codes, scales = bm.glu_mx8(GU)
+    for bad, error in [(lambda: bm.glu_mx8(GU[:, :96]), ValueError), (lambda: bm.glu_mx8(GU[0]), ValueError),
+                       (lambda: bm.glu_mx8(GU.half()), TypeError),
+                       (lambda: bm.glu_mx8_grad(codes, scales, GU[:, :32]), ValueError),
+                       (lambda: bm.glu_mx8_grad(codes, scales, GU[:3, :64]), ValueError),
+                       (lambda: bm.glu_mx8_grad(codes.float(), scales, GU[:, :64]), TypeError),
+                       (lambda: bm.glu_mx8_grad(codes, scales[:, :2], GU[:, :64]), ValueError)]:
+        with pytest.raises(error):
+            bad()
+
+
+# ------------------------------------------------------- experts' products
+def slots_for(g, S, E, head=0, tail=0, empty=()):
+    """offsets of E experts over S slots: `head` before the first one's and `tail` behind the last one's."""
+    left = S - head - tail
+    cuts = np.sort(g.integers(0, left + 1, E - 1))
+    counts = np.diff(np.r_[0, cuts, left])
+    for e in empty:
+        counts[(e + 1) % E] += counts[e]
+        counts[e] = 0
+    return np.r_[0, np.cumsum(counts)].astype(np.int32) + np.int32(head)
+
+
+def glu_bound(Wg, Wu, A, X, offsets, rows, L):
+    """Bound of silu(g) u before its rounding, from those of g and u."""
+    eg = (L + 8) * U * mx4.product(np.abs(Wg), A, offsets, rows)
+    eu = (L + 8) * U * mx4.product(np.abs(Wu), A, offsets, rows)
+    gate, up = mx4.product(Wg, X, offsets, rows), mx4.product(Wu, X, offsets, rows)
+    return 1.1 * eg * (np.abs(up) + eu) + np.abs(mx4.silu(gate)) * (eu + 2.0 ** -18 * np.abs(up))
+
+
+def check_products(g, E, N, K, offsets, rows, x_rows, S, glu=False, out="bf16", what=""):
+    W = randn(g, E, (2 if glu else 1) * N, K, scale=K ** -0.5)
+    X = randn(g, x_rows, K)
+    o, r = dev(offsets), None if rows is None else dev(rows)
+    got = bm.expert_product(W, X, offsets=o, rows=r, glu=glu, dtype=DT[out])
+    w64, x64 = np64(W), np64(X)
+    want = mx4.product(w64, x64, offsets, rows, glu=glu)
+    if glu:
+        bound = glu_bound(w64[:, :N], w64[:, N:], np.abs(x64), x64, offsets, rows, K)
+    else:
+        bound = (K + 8) * U * mx4.product(np.abs(w64), np.abs(x64), offsets, rows)
+    within(np64(got), want, bound + (np.abs(want) + bound) * HALF[out], (what, "product"))
+    assert torch.equal(got, bm.expert_product(W, apart(X), offsets=o, rows=r, glu=glu, dtype=DT[out]))
+    if glu or N % 8:
+        return
+    dY = randn(g, S, N)
+    got = bm.expert_product_grad(W, dY, offsets=o, dtype=DT[out])
+    y64 = np64(dY)
+    want = mx4.product_grad(w64, y64, offsets)
+    bound = (N + 8) * U * mx4.product_grad(np.abs(w64), np.abs(y64), offsets)
+    within(np64(got), want, bound + (np.abs(want) + bound) * HALF[out], (what, "grad"))
+    assert torch.equal(got, bm.expert_product_grad(W, apart(dY), offsets=o, dtype=DT[out]))
+    check_weights(g, dY, X, E, offsets, rows, out, what)
+
+
+def check_weights(g, dY, X, E, offsets, rows, out, what):
+    o, r = None if offsets is None else dev(offsets), None if rows is None else dev(rows)
+    counts = np.array([len(dY)]) if offsets is None else np.diff(np.clip(offsets, 0, len(dY)))
+    y64 = np64(dY)
+    forms = [("bf16", bm.expert_weight_grad(dY, X, offsets=o, rows=r, dtype=DT[out]), np64(X)),
+             ("apart", bm.expert_weight_grad(apart(dY), apart(X), offsets=o, rows=r, dtype=DT[out]), np64(X))]
+    if X.shape[1] % 32 == 0:
+        kept = bm.mx8_quantize(X)
+        forms.append(("mx8", bm.expert_weight_grad_q(dY, *kept, offsets=o, rows=r, dtype=DT[out]),
+                      np64(bm.mx8_dequantize(*kept))))
+    for form, got, x64 in forms:
+        want = block.weight_grad(y64, x64, E, offsets, rows)
+        bound = (counts + 8)[:, None, None] * U * block.weight_grad(np.abs(y64), np.abs(x64), E, offsets, rows)
+        within(np64(got), want, bound + (np.abs(want) + bound) * HALF[out], (what, "weights", form))
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("E,N,K,S", [(1, 8, 8, 1), (4, 64, 96, 37), (3, 72, 136, 130), (8, 128, 64, 3), (5, 200, 320, 700),
+                                     (64, 96, 128, 90), (2, 512, 512, 600), (1, 264, 1032, 65), (130, 64, 64, 1000)])
+def test_products(E, N, K, S, out):
+    g = np.random.default_rng([E, N, K, S])
+    x_rows = max(1, S // 2)
+    rows = g.integers(0, x_rows, S).astype(np.int32)
+    offsets = slots_for(g, S, E, empty=(0,) if E > 2 else ())
+    check_products(g, E, N, K, offsets, rows, x_rows, S, out=out, what="rows")
+    check_products(g, E, N, K, offsets, None, S, S, out=out, what="slots")
+    check_products(g, E, N, K, offsets, rows, x_rows, S, glu=True, out=out, what="glu")
+
+
+@pytest.mark.parametrize("N", [1, 3, 50, 257])
+def test_products_of_odd_outputs(N):
+    g = np.random.default_rng(N)
+    offsets = slots_for(g, 45, 4)
+    for glu in (False, True):
+        check_products(g, 4, N, 72, offsets, None, 45, 45, glu=glu, what=glu)
+        check_products(g, 4, N, 72, offsets, None, 45, 45, glu=glu, out="f32", what=glu)
+
+
+@pytest.mark.parametrize("S,head,tail", [(40, 3, 5), (300, 40, 130), (20, 20, 0), (20, 0, 20), (1000, 300, 1)])
+def test_slots_of_no_expert_and_rows_that_do_not_exist(S, head, tail):
+    g = np.random.default_rng([S, head])
+    E, N, K = 4, 72, 96
+    offsets = slots_for(g, S, E, head, tail)
+    rows = g.integers(-2, 14, S).astype(np.int32)
+    check_products(g, E, N, K, offsets, rows, 12, S, what="rows")
+    check_products(g, E, N, K, offsets, rows, 12, S, glu=True, out="f32", what="glu")
+    # whatever the weights hold, those slots are zeros
+    W = torch.full((E, N, K), float("nan"), dtype=torch.bfloat16, device=DEV)
+    X, o, r = randn(g, 12, K), dev(offsets), dev(rows)
+    there = ((np.arange(S) >= head) & (np.arange(S) < S - tail))
+    y = np64(bm.expert_product(W, X, offsets=o, rows=r))
+    has = there & (rows >= 0) & (rows < 12)
+    assert (y[~has] == 0).all() and np.isnan(y[has]).all()
+    y = np64(bm.expert_product_grad(W, randn(g, S, N), offsets=o))
+    assert (y[~there] == 0).all() and np.isnan(y[there]).all()
+    # and what slots of no expert or row hold does not reach the weights' gradient
+    dY = randn(g, S, N)
+    dY[dev(~has)] = float("nan")
+    clean = np.where(has[:, None], np64(dY), 0)
+    for x, got in ((X, bm.expert_weight_grad(dY, X, offsets=o, rows=r, dtype=torch.float32)),
+                   (bm.mx8_dequantize(*bm.mx8_quantize(X)),
+                    bm.expert_weight_grad_q(dY, *bm.mx8_quantize(X), offsets=o, rows=r, dtype=torch.float32))):
+        want = block.weight_grad(clean, np64(x), E, offsets, rows)
+        bound = (S + 8) * U * block.weight_grad(np.abs(clean), np.abs(np64(x)), E, offsets, rows)
+        within(np64(got), want, bound, "weights")
+
+
+def test_products_of_nothing():
+    g = np.random.default_rng(1)
+    W, o = randn(g, 3, 16, 32), torch.zeros(4, dtype=torch.int32, device=DEV)
+    none = torch.empty((0, 32), dtype=torch.bfloat16, device=DEV)
+    assert bm.expert_product(W, none, offsets=o).shape == (0, 16)
+    assert bm.expert_product_grad(W, none[:, :16], offsets=o).shape == (0, 32)
+    out = torch.full((3, 16, 32), float("nan"), device=DEV)
+    bm.expert_weight_grad(none[:, :16].contiguous(), none, offsets=o, dtype=torch.float32, out=out)
+    assert (out == 0).all()
+    out.fill_(float("nan"))
+    codes, scales = bm.mx8_quantize(none)
+    bm.expert_weight_grad_q(none[:, :16].contiguous(), codes, scales, offsets=o, dtype=torch.float32, out=out)
+    assert (out == 0).all()
+    # slots whose rows cannot exist
+    rows = torch.zeros(5, dtype=torch.int32, device=DEV)
+    o = torch.tensor([0, 2, 2, 5], dtype=torch.int32, device=DEV)
+    assert (bm.expert_product(W, none, offsets=o, rows=rows) == 0).all()
+    assert (bm.expert_weight_grad(randn(g, 5, 16), none, offsets=o, rows=rows) == 0).all()
+    assert (bm.expert_weight_grad_q(randn(g, 5, 16), codes, scales, offsets=o, rows=rows) == 0).all()
+
+
+def test_products_of_one_expert():
+    g = np.random.default_rng(2)
+    W, X = randn(g, 1, 60, 64, scale=0.125), randn(g, 33, 64)
+    want = np64(X) @ np64(W)[0].T
+    bound = 72 * U * (np.abs(np64(X)) @ np.abs(np64(W)[0]).T)
+    within(np64(bm.expert_product(W, X, dtype=torch.float32)), want, bound + np.abs(want) * 2.0 ** -24, "no offsets")
+    check_weights(g, randn(g, 33, 72), X, 1, None, None, "f32", "no offsets")
+
+
+def test_nan_and_infinite_tokens_stay_in_their_slots():
+    g = np.random.default_rng(8)
+    W, X = randn(g, 2, 64, 64), randn(g, 40, 64)
+    X[7, 3], X[21, 5] = float("nan"), float("inf")
+    o = torch.tensor([0, 20, 40], dtype=torch.int32, device=DEV)
+    y = bm.expert_product(W, X, offsets=o)
+    fine = torch.isfinite(y).all(1).cpu().numpy()
+    assert fine.sum() == 38 and not fine[7] and not fine[21]
+    dW = bm.expert_weight_grad(randn(g, 40, 64), X, offsets=o)
+    bad = ~torch.isfinite(dW)
+    assert bad[0, :, 3].all() and bad[1, :, 5].all() and bad.sum() == 128
+
+
+def test_products_refuse():
+    W, X = torch.zeros((2, 16, 32), dtype=torch.bfloat16, device=DEV), torch.zeros((4, 32), dtype=torch.bfloat16, device=DEV)
+    o = torch.tensor([0, 2, 4], dtype=torch.int32, device=DEV)
+    dY = X[:, :16].contiguous()
+    for bad, error in [
+            (lambda: bm.expert_product(W.float(), X, offsets=o), TypeError),
+            (lambda: bm.expert_product(W.float(), X.float(), offsets=o), bm.BitsmoeError),
+            (lambda: bm.expert_product(W, X[:, :16], offsets=o), ValueError),
+            (lambda: bm.expert_product(W, X, offsets=o[:2]), ValueError),
+            (lambda: bm.expert_product(W, X, offsets=o.long()), TypeError),
+            (lambda: bm.expert_product(W, X), bm.BitsmoeError),
+            (lambda: bm.expert_product(W[:, :15].contiguous(), X, offsets=o, glu=True), ValueError),
+            (lambda: bm.expert_product(W[:, :, :20].contiguous(), X[:, :20].contiguous(), offsets=o), bm.BitsmoeError),
+            (lambda: bm.expert_product(W.transpose(1, 2), dY, offsets=o), ValueError),
+            (lambda: bm.expert_product_grad(W, X, offsets=o), ValueError),
+            (lambda: bm.expert_product_grad(W[:, :12].contiguous(), dY[:, :12].contiguous(), offsets=o), bm.BitsmoeError),
+            (lambda: bm.expert_weight_grad(dY, X[:3], offsets=o), ValueError),
+            (lambda: bm.expert_weight_grad(dY, X.float(), offsets=o), TypeError),
+            (lambda: bm.expert_weight_grad(dY, X, offsets=o, out=torch.zeros((2, 16, 32), device=DEV)), TypeError),
+            (lambda: bm.expert_weight_grad_q(dY, X.view(torch.uint8), o, offsets=o), ValueError)]:
+        with pytest.raises(error):
+            bad()
+
+
+# ------------------------------------------------------- used together
+def test_layers_and_block_are_their_operators():
+    """The pipeline's functions give what their operators give one after another, to the bit."""
+    g = np.random.default_rng(11)
+    T, E, k, N, K = 37, 8, 2, 64, 96
+    ex = pipeline.Experts(randn(g, E, 2 * N, K, scale=0.1), randn(g, E, K, N, scale=0.1))
+    x, res, dy, ds = (randn(g, T, K) for _ in range(4))
+    w, router = dev((1 + 0.1 * g.standard_normal(K)).astype(np.float32)), randn(g, E, K, scale=0.1)
+    dl = torch.tensor([0.01, 0.001], device=DEV)
+    valid = dev(g.random(T) < 0.9)
+    y, total, r, saved = pipeline.moe_block(x, res, w, router, ex, k, valid=valid, train=True)
+    grads = pipeline.moe_block_grad(saved, w, router, ex, dy, dsum=ds, dlosses=dl, dtype=torch.float32)
+
+    f32 = torch.float32
+    n = bm.rms_norm(x, w, residual=res, mx8=True)
+    logits = bm.expert_product(router[None], n.y, dtype=f32)
+    q = bm.route(logits, k, valid=valid)
+    assert torch.equal(q.experts, r.experts) and torch.equal(total, n.sum)
+    gu = bm.expert_product(ex.up, n.y, offsets=q.offsets, rows=q.rows, dtype=f32)
+    h, codes, scales = bm.glu_mx8(gu)
+    z = bm.expert_product(ex.down, h, offsets=q.offsets)
+    assert torch.equal(y, bm.combine(z, q.slots, q.weights))
+    dz, dw = bm.combine_grad(bm.mx8_dequantize(*bm.mx8_quantize(z)), q.slots, q.weights, dy)
+    dgu, h = bm.glu_mx8_grad(codes, scales, bm.expert_product_grad(ex.down, dz, offsets=q.offsets, dtype=f32))
+    dx = bm.combine(bm.expert_product_grad(ex.up, dgu, offsets=q.offsets, dtype=f32), q.slots).bfloat16()
+    dlog = bm.route_grad(logits, q, dweights=dw, dlosses=dl).bfloat16()
+    dn = dx + bm.expert_product_grad(router[None], dlog)
+    want = (*bm.rms_norm_grad(n.sum, w, n.inv, dn, dsum=ds),
+            bm.expert_weight_grad_q(dlog, n.codes, n.scales, dtype=f32)[0],
+            bm.expert_weight_grad_q(dgu, n.codes, n.scales, offsets=q.offsets, rows=q.rows, dtype=f32),
+            bm.expert_weight_grad(dz, h, offsets=q.offsets, dtype=f32))
+    for name, a, b in zip(("dx", "dweight", "d_router", "d_up", "d_down"), grads, want):
+        assert a.dtype == b.dtype and torch.equal(a, b), name
+    # serving: the same but for the product with glu, which rounds silu(g) u once more and keeps nothing
+    y2, total2, r2 = pipeline.moe_block(x, res, w, router, ex, k, valid=valid)
+    assert torch.equal(total2, total) and torch.equal(r2.experts, r.experts)
+    off = (y2.double() - y.double()).norm() / y.double().norm()
+    assert off < 2.0 ** -6, off  # (two roundings of h and z to bf16 that may differ by a step, and y's)
+
+
+def test_block_gradient_is_that_of_the_block():
+    """Against the gradient of the whole block by autograd in fp64.  What is kept in 8 bits is off by 2^-4 at most, 2^-5
+    in the mean, twice in the gate's and once in the others' gradients; the six roundings to bf16 on the longest
+    way add up to 6 * 2^-8: below 0.125 in norm."""
+    g = np.random.default_rng(12)
+    T, E, k, N, K = 64, 8, 2, 96, 128
+    ex = pipeline.Experts(randn(g, E, 2 * N, K, scale=0.15), randn(g, E, K, N, scale=0.15))
+    x, res, dy, ds = (randn(g, T, K) for _ in range(4))
+    w, router = dev((1 + 0.1 * g.standard_normal(K)).astype(np.float32)), randn(g, E, K, scale=0.3)
+    dl = torch.tensor([0.01, 0.001], device=DEV)
+    y, total, r, saved = pipeline.moe_block(x, res, w, router, ex, k, train=True)
+    grads = pipeline.moe_block_grad(saved, w, router, ex, dy, dsum=ds, dlosses=dl, dtype=torch.float32)
+    leaves = [t.detach().double().cpu().requires_grad_() for t in (total, w, router, ex.up, ex.down)]
+    v, w64, rt, up, down = leaves
+    n = v / torch.sqrt((v * v).mean(1, keepdim=True) + 1e-6) * w64
+    logits = n @ rt.T
+    p = torch.softmax(logits, 1)
+    chosen = r.experts.long().cpu()
+    pw = p.gather(1, chosen)
+    pw = pw / pw.sum(1, keepdim=True)
+    out = torch.zeros_like(v)
+    for j in range(k):
+        gu = torch.bmm(up[chosen[:, j]], n.unsqueeze(2)).squeeze(2)
+        h = torch.nn.functional.silu(gu[:, :N]) * gu[:, N:]
+        out = out + pw[:, j:j + 1] * torch.bmm(down[chosen[:, j]], h.unsqueeze(2)).squeeze(2)
+    counts = torch.bincount(chosen.flatten(), minlength=E).double()
+    balance = E / (k * T * T) * (counts * p.sum(0)).sum()
+    zloss = torch.logsumexp(logits, 1).square().mean()
+    d64 = dl.double().cpu()
+    ((out * dy.double().cpu()).sum() + (v * ds.double().cpu()).sum() + d64[0] * balance + d64[1] * zloss).backward()
+    assert (out - y.double().cpu()).norm() / out.norm() < 6 * 2.0 ** -8
+    for name, got, leaf in zip(("dx", "dweight", "d_router", "d_up", "d_down"), grads, leaves):
+        off = (got.double().cpu() - leaf.grad).norm() / leaf.grad.norm()
+        assert off < 0.125, (name, float(off))
+
+
+@pytest.mark.parametrize("quantize_tokens", [False, True])
+def test_mx4_layer_keeps_gate_and_up_in_8_bits(quantize_tokens):
+    g = np.random.default_rng(13)
+    T, E, k, N, K = 37, 8, 2, 64, 96
+    ex = pipeline.mx4_experts(randn(g, E, N, K, scale=0.1), randn(g, E, N, K, scale=0.1), randn(g, E, K, N, scale=0.1))
+    x, logits, dy = randn(g, T, K), randn(g, T, E, dtype="f32"), randn(g, T, K)
+    y, r, saved = pipeline.mx4_layer(x, logits, ex, k, train=True, quantize_tokens=quantize_tokens)
+    y8, r8, saved8 = pipeline.mx4_layer(x, logits, ex, k, train=True, quantize_tokens=quantize_tokens, checkpoint=True)
+    codes, scales = bm.mx8_quantize(saved.up)
+    assert torch.equal(saved8.up[0], codes) and torch.equal(saved8.up[1], scales)
+    off = (y8.double() - y.double()).norm() / y.double().norm()
+    assert off < 2.0 ** -6, off  # (h by another silu: two roundings to bf16 that may differ by a step, or MX4's; and y's)
+    dx, dlogits = pipeline.mx4_layer_grad(saved8, ex, dy)
+    dz, dw = bm.combine_grad(saved8.z, r.slots, r.weights, dy)
+    dh = bm.mx4_product_grad(ex.down_codes, ex.down_scales, dz, offsets=r.offsets, dtype=torch.float32)
+    dup, _ = bm.glu_mx8_grad(codes, scales, dh)
+    want = bm.combine(bm.mx4_product_grad(ex.up_codes, ex.up_scales, dup, offsets=r.offsets, dtype=torch.float32), r.slots)
+    assert torch.equal(dx, want.bfloat16()) and torch.equal(dlogits, bm.route_grad(logits, r8, dweights=dw))
+
+
+def test_other_streams_and_captured_steps():
+    """A step captured into a graph and replayed with new inputs gives what the eager step gives, with eager work
+    between the replays; two of them side by side on their own streams do, too."""
+    g = np.random.default_rng(14)
+    T, E, k, N, K = 150, 8, 2, 64, 96
+    ex = pipeline.Experts(randn(g, E, 2 * N, K, scale=0.1), randn(g, E, K, N, scale=0.1))
+    w, router = dev((1 + 0.1 * g.standard_normal(K)).astype(np.float32)), randn(g, E, K, scale=0.1)
+
+    def step(x, res, dy, ds):
+        y, total, r, saved = pipeline.moe_block(x, res, w, router, ex, k, train=True)
+        return (y, total, *pipeline.moe_block_grad(saved, w, router, ex, dy, dsum=ds))
+
+    def inputs():
+        return [randn(g, T, K) for _ in range(4)]
+
+    graphs = []
+    for _ in range(2):
+        held = inputs()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            step(*held)
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = step(*held)
+        graphs.append((held, graph, out))
+    for _ in range(4):
+        new = [inputs() for _ in graphs]
+        want = [step(*i) for i in new]
+        torch.cuda.synchronize()
+        streams = [torch.cuda.Stream() for _ in graphs]
+        for (held, graph, out), i, s in zip(graphs, new, streams):
+            for a, b in zip(held, i):
+                a.copy_(b)
+        torch.cuda.synchronize()
+        for (held, graph, out), s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        for (held, graph, out), ref in zip(graphs, want):
+            for a, b in zip(out, ref):
+                assert torch.equal(a, b)
