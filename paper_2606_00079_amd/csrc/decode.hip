@@ -590,11 +590,11 @@ __device__ __forceinline__ half8 codes8_merged(const uint32_t (&lo)[4], const ui
 // the LDS address; nothing else in the kernel uses M0.
 __device__ __forceinline__ void lds_dma16(const void* g, const void* lds) {
   const uint32_t l = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds)));
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(g), "s"(l) : "memory");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(g), "s"(l) : "memory");
 }
 __device__ __forceinline__ void lds_dma4(const void* g, const void* lds) {
   const uint32_t l = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds)));
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" : : "v"(g), "s"(l) : "memory");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(g), "s"(l) : "memory");
 }
 // s_waitcnt vmcnt(N) alone, in the gfx9 encoding (vmcnt[3:0] in bits 3:0,
 // vmcnt[5:4] in bits 15:14).
