@@ -882,6 +882,10 @@ bitsmoe_status bitsmoe_expert_product_grad(const void* W_dev, bitsmoe_dtype t, i
                                            const int32_t* offsets_dev, int64_t S, void* dX_dev,
                                            bitsmoe_dtype xt, int64_t ldx, void* stream);
 
+/* Bytes of the workspace of the two calls below on the current device: 0 but for few and
+ * small experts of many slots, whose sums are then cut into parts. */
+int64_t bitsmoe_expert_weight_grad_workspace(int64_t E, int64_t N, int64_t K, int64_t S);
+
 /*
  * Gradient of the weights: dW_e = sum over e's slots s of dy_s x_{rows[s]}^T, 0 for
  * an expert without slots.  Slots whose row is not in [0, x_rows) add nothing.
@@ -889,13 +893,16 @@ bitsmoe_status bitsmoe_expert_product_grad(const void* W_dev, bitsmoe_dtype t, i
  *   X_dev        x_rows rows of K entries of type t, ldx entries apart
  *   offsets_dev, rows_dev   as bitsmoe_mx4_product
  *   dW_dev       [E][N][K] of type wt, every entry written (S = 0: zeros)
- * Sums are fp32 in a fixed order.  Shape rules as bitsmoe_expert_product_grad.
+ *   work_dev     work_bytes bytes, contents of no matter, in use until the call's work
+ *                on the stream is done; NULL: the sums are not cut, which may take longer
+ * Sums are fp32 in a fixed order (another one with the workspace).  Shape rules as bitsmoe_expert_product_grad.
  */
 bitsmoe_status bitsmoe_expert_weight_grad(const void* dY_dev, bitsmoe_dtype t, int64_t lddy,
                                           int64_t E, int64_t N, int64_t K, const void* X_dev,
                                           int64_t x_rows, int64_t ldx, const int32_t* offsets_dev,
                                           const int32_t* rows_dev, int64_t S, void* dW_dev,
-                                          bitsmoe_dtype wt, void* stream);
+                                          bitsmoe_dtype wt, void* work_dev, int64_t work_bytes,
+                                          void* stream);
 
 /*
  * The same with the tokens in MX8: xcodes_dev [x_rows][K], xscales_dev
@@ -906,7 +913,8 @@ bitsmoe_status bitsmoe_expert_weight_grad_q(const void* dY_dev, bitsmoe_dtype t,
                                             const uint8_t* xcodes_dev, const uint8_t* xscales_dev,
                                             int64_t x_rows, const int32_t* offsets_dev,
                                             const int32_t* rows_dev, int64_t S, void* dW_dev,
-                                            bitsmoe_dtype wt, void* stream);
+                                            bitsmoe_dtype wt, void* work_dev, int64_t work_bytes,
+                                            void* stream);
 
 /* Path of a LAPACK shared library for bitsmoe_shared_basis (LP64 or ILP64
  * dsyevd; both plain and "64_"-suffixed symbol names are tried).  When never
@@ -917,7 +925,9 @@ bitsmoe_status bitsmoe_set_lapack(const char* path);
  * pair of HIP events on its stream around each of its main kernels, under
  * the names "gram", "gram_experts", "project", "score_dgen", "score_gemm",
  * "pack", and for the experts' products in MX4, by the kernel that took the
- * call, "mx4_rows", "mx4_few", "mx4_tile", "mx4_grad_few" and "mx4_grad_tile".
+ * call, "mx4_rows", "mx4_few", "mx4_tile", "mx4_grad_few" and "mx4_grad_tile"; for
+ * those in bf16 "expert_rows", "expert_split", "expert_tile_32", "expert_tile_128",
+ * "expert_tile_256" and "expert_weights".
  * bitsmoe_kernel_time waits for the recorded events of `name`,
  * returns their summed duration in ms and the number of launches, and
  * forgets them.  Enabling costs two event records per kernel and no

@@ -73,6 +73,7 @@ EXPORTS = [
     "bitsmoe_rms_norm_grad_workspace", "bitsmoe_rms_norm_grad", "bitsmoe_glu_mx8",
     "bitsmoe_glu_mx8_grad", "bitsmoe_expert_product", "bitsmoe_expert_product_grad",
     "bitsmoe_expert_weight_grad", "bitsmoe_expert_weight_grad_q",
+    "bitsmoe_expert_weight_grad_workspace",
 ]
 # Candidate widths of the surrogate table, in column order.
 SURROGATE_WIDTHS = (0, 1, 2, 3, 4, 6, 8, 16)
@@ -161,8 +162,9 @@ def lib() -> ctypes.CDLL:
     L.bitsmoe_glu_mx8_grad.argtypes = [vp, vp, vp, i32, i64, i64, i64, vp, vp, vp]
     L.bitsmoe_expert_product.argtypes = [vp, i32, i64, i64, i64, vp, i64, i64, vp, vp, i64, i32, vp, i32, i64, vp]
     L.bitsmoe_expert_product_grad.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, vp, i32, i64, vp]
-    L.bitsmoe_expert_weight_grad.argtypes = [vp, i32, i64, i64, i64, i64, vp, i64, i64, vp, vp, i64, vp, i32, vp]
-    L.bitsmoe_expert_weight_grad_q.argtypes = [vp, i32, i64, i64, i64, i64, vp, vp, i64, vp, vp, i64, vp, i32, vp]
+    L.bitsmoe_expert_weight_grad.argtypes = [vp, i32, i64, i64, i64, i64, vp, i64, i64, vp, vp, i64, vp, i32, vp, i64, vp]
+    L.bitsmoe_expert_weight_grad_q.argtypes = [vp, i32, i64, i64, i64, i64, vp, vp, i64, vp, vp, i64, vp, i32, vp, i64, vp]
+    L.bitsmoe_expert_weight_grad_workspace.argtypes = [i64] * 4
     L.bitsmoe_set_lapack.argtypes = [ctypes.c_char_p]
     L.bitsmoe_timing.argtypes = [i32]
     L.bitsmoe_timing_only.argtypes = [ctypes.c_char_p]
@@ -175,6 +177,7 @@ def lib() -> ctypes.CDLL:
     L.bitsmoe_release.restype = None
     L.bitsmoe_route_workspace.restype = i64
     L.bitsmoe_rms_norm_grad_workspace.restype = i64
+    L.bitsmoe_expert_weight_grad_workspace.restype = i64
     lp = _find_lapack()
     if lp and os.environ.get("BITSMOE_LAPACK") is None:
         L.bitsmoe_set_lapack(lp.encode())
@@ -1021,6 +1024,15 @@ def _experts_of(offsets, rows, S: int, x_rows: int, like, torch):
     return (E, _in(offsets, "offsets", like, torch.int32, (E + 1,)), _in(rows, "rows", like, torch.int32, (S,)))
 
 
+def _parts_room(E: int, N: int, K: int, S: int, like, torch):
+    """The workspace of a weights' gradient: (tensor or None, address, bytes)."""
+    room = lib().bitsmoe_expert_weight_grad_workspace(E, N, K, S)
+    if not room:
+        return None, None, 0
+    work = like.new_empty((room,), dtype=torch.uint8)
+    return work, work.data_ptr(), room
+
+
 def expert_weight_grad(dY, X, offsets=None, rows=None, dtype=None, out=None):
     """dW_e = sum over e's slots of dy_s x_{rows[s]}^T: dY bf16 [S][N], X bf16
     [rows][K] -> [E][N][K], bf16 unless ``dtype`` says fp32 (E from offsets; without
@@ -1033,8 +1045,10 @@ def expert_weight_grad(dY, X, offsets=None, rows=None, dtype=None, out=None):
     yp, ldy = _rows(dY, "dY")
     xp, ldx = _like(X, "X", dY, X.shape)
     out = _out(out, (E, N, K), dtype or torch.bfloat16, dY, torch)
+    work, wp, room = _parts_room(E, N, K, S, dY, torch)
     _check(lib().bitsmoe_expert_weight_grad(yp, _code(dY, "dY", torch), ldy, E, N, K, xp, X.shape[0], ldx, op, rp, S,
-                                            out.data_ptr(), _code(out, "out", torch), stream), "expert_weight_grad")
+                                            out.data_ptr(), _code(out, "out", torch), wp, room, stream),
+           "expert_weight_grad")
     return out
 
 
@@ -1049,8 +1063,9 @@ def expert_weight_grad_q(dY, xcodes, xscales, offsets=None, rows=None, dtype=Non
     E, op, rp = _experts_of(offsets, rows, S, xcodes.shape[0], dY, torch)
     yp, ldy = _rows(dY, "dY")
     out = _out(out, (E, N, K), dtype or torch.bfloat16, dY, torch)
+    work, wp, room = _parts_room(E, N, K, S, dY, torch)
     _check(lib().bitsmoe_expert_weight_grad_q(yp, _code(dY, "dY", torch), ldy, E, N, K, xcp, xsp, xcodes.shape[0], op,
-                                              rp, S, out.data_ptr(), _code(out, "out", torch), stream),
+                                              rp, S, out.data_ptr(), _code(out, "out", torch), wp, room, stream),
            "expert_weight_grad_q")
     return out
 

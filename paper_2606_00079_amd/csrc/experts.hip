@@ -7,11 +7,16 @@
 //
 // for S slots, expert e's being offsets[e] .. offsets[e+1].  Sums are fp32 and
 // results are rounded once.
+#include <atomic>
+#include <cmath>
 #include <cstdint>
 #include <string>
+#include <type_traits>
+#include <utility>
 
 #include "internal.hpp"
 #include "mx8.hpp"
+#include "rows.hpp"
 #include "slots.hpp"
 
 namespace bitsmoe {
@@ -35,114 +40,858 @@ struct ExpertArgs {
   void* y;
   int64_t ldy;
   int yf32;
+  int parts;  // (weights' gradient) the sum is cut into, each with results of its own in y
 };
 
 enum Form { kForward, kTokens, kWeights };
 
-// 64 x 64 results a workgroup, the sum 32 entries at a time through LDS.
-template <Form FORM, bool MX, bool GLU>
-__global__ __launch_bounds__(kThreads) void expert_simple_kernel(ExpertArgs a) {
-  constexpr int H = GLU ? 2 : 1, LD = 40;
-  __shared__ __align__(16) uint16_t p[64 * LD], q[H][64 * LD];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int e, lo = 0, hi = 0;
-  int64_t m0, n0;  // of the results
-  if constexpr (FORM == kWeights) {
-    const int64_t nt = (a.N + 63) / 64, kt = (a.K + 63) / 64;
-    e = static_cast<int>(blockIdx.x / (nt * kt));
-    const int64_t in = blockIdx.x % (nt * kt);
-    m0 = in / kt * 64;
-    n0 = in % kt * 64;
-    const int count = slots_of(a.offsets, a.E, static_cast<int>(a.S), e, &lo);
-    hi = lo + count;
-  } else {
-    const int64_t cols = FORM == kForward ? a.N : a.K;
-    Tile t;
-    if (!find_tile(a.offsets, a.E, a.S, static_cast<int>((cols + 63) / 64), 64, &t)) return;
-    e = t.e;
-    m0 = lo = t.lo;
-    hi = t.hi;
-    n0 = static_cast<int64_t>(t.col) * 64;
+// 16 outputs x 16 slots a workgroup.  Its eight waves share out K in segments of
+// 64 entries, a cache line of a row: lane l holds chunks l / 16 and 4 + l / 16 of row
+// l % 16, and of slot l % 16.  For the fewest slots: bound by launch and one chain of
+// loads, so the sum is split and the workgroups are small and many.
+constexpr int kRowWaves = 8;
+template <bool GLU>
+__global__ __launch_bounds__(64 * kRowWaves) void expert_rows_kernel(ExpertArgs a) {
+  constexpr int H = GLU ? 2 : 1, AHEAD = 4;
+  __shared__ f32x4 part[kRowWaves][H][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
+  Tile t;
+  if (!find_tile(a.offsets, a.E, a.S, static_cast<int>((a.N + 15) / 16), 16, &t)) return;
+  const int64_t n0 = static_cast<int64_t>(t.col) * 16;
+  f32x4 acc[H];
+#pragma unroll
+  for (int h = 0; h < H; ++h) acc[h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  bool have = false;  // the row of this lane's slot exists
+  if (t.e < a.E) {
+    const int64_t slot = t.lo + r;
+    const int64_t row = slot < t.hi ? (a.rows ? static_cast<int64_t>(a.rows[slot]) : slot) : -1;
+    have = row >= 0 && row < a.x_rows;
+    const uint16_t* w[H];
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+      w[h] = a.w + ((static_cast<int64_t>(t.e) * H + h) * a.N + min(n0 + r, a.N - 1)) * a.K;
+    const uint16_t* x = a.x + row * a.ldx;
+    const int segments = static_cast<int>((a.K + 63) / 64);
+    for (int s0 = wave; s0 < segments; s0 += kRowWaves * AHEAD) {
+      uint4 wv[AHEAD][H][2], xv[AHEAD][2];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int64_t k = static_cast<int64_t>(s0 + u * kRowWaves) * 64 + 32 * c + 8 * q;
+          const bool in = k < a.K;
+#pragma unroll
+          for (int h = 0; h < H; ++h)
+            wv[u][h][c] = in ? *reinterpret_cast<const uint4*>(w[h] + k) : make_uint4(0, 0, 0, 0);
+          xv[u][c] = in && have ? *reinterpret_cast<const uint4*>(x + k) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int h = 0; h < H; ++h)
+            acc[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wv[u][h][c]),
+                                                             __builtin_bit_cast(bf16x8, xv[u][c]), acc[h], 0, 0, 0);
+    }
   }
-  const int64_t L = FORM == kForward ? a.K : FORM == kTokens ? a.N : hi - lo;  // of the sum
-  const int64_t mend = FORM == kWeights ? a.N : hi, nend = FORM == kForward ? a.N : a.K;
-  f32x4 acc[H][4];
+#pragma unroll
+  for (int h = 0; h < H; ++h) part[wave][h][lane] = acc[h];
+  __syncthreads();
+  if (wave != 0) return;
 #pragma unroll
   for (int h = 0; h < H; ++h)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[h][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  auto token = [&](int64_t s) {  // the row of slot s; -1: none
-    const int64_t r = a.rows ? a.rows[s] : s;
-    return r >= 0 && r < a.x_rows ? r : -1;
+    for (int i = 1; i < kRowWaves; ++i) acc[h] += part[i][h][lane];
+  if constexpr (GLU) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[0][i] = silu(acc[0][i]) * acc[1][i];
+  }
+  if (!have) acc[0] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};  // (zeros times weights that are no numbers are NaN)
+  const int64_t slot = t.lo + r, n = n0 + 4 * q;      // (a lane holds four outputs of one slot)
+  if (slot < t.hi && n < a.N) store4(a, slot, n, a.N, a.ldy % 4 == 0, acc[0]);
+}
+
+// ---------------------------------------------------------------------------
+// Tiles: MT x 256 results a workgroup, which stays and takes tile after tile.
+//
+// Two operands go into a matrix-core op: Q, whose 256 rows are results that lie
+// side by side in memory, on its row side, so that a lane holds runs of four of
+// them; and P, the MT others (slots; for the weights' gradient outputs).  Either
+// comes as its rows' entries of the sum lie, or, where the sum runs over the rows
+// of a matrix (W for the tokens' gradient, dy and x for the weights'), as those rows
+// do, and is then read through the transposing LDS read.
+//
+// Direct global->LDS loads fill a ring of stages of 64 entries of the sum, whole
+// cache lines of 128 bytes; a step that finds its stage read by every wave refills
+// it at once, across the end of a tile too.
+//
+// Tokens in MX8 (the weights' gradient) are widened to bf16 on their way: every
+// wave loads the codes of eight slots of a stage for itself, and in the step before
+// that stage's writes what they stand for into one of two tiles, between the ops.
+// ---------------------------------------------------------------------------
+template <Form FORM, int MT_, bool MX = false>
+struct Shape {
+  static constexpr int MT = MT_, QT = 256, KS = 64;
+  static constexpr int WM = MT == 32 ? 1 : 2, WN = 4, kWaves = WM * WN, kThreads = 64 * kWaves;
+  static constexpr int MB = MT / WM / 32, NB = 2;
+  static constexpr bool kPCols = FORM == kWeights, kQCols = FORM != kForward;  // operands whose sum runs over rows
+  static constexpr int kPStage = MT * KS * 2, kQStage = QT * KS * 2, kStage = kPStage + (MX ? 0 : kQStage);
+  static constexpr int NX = MT == 32 ? 4 : MT == 128 ? 3 : 2;
+  static constexpr int kRows = MT < 64 ? 64 : MT;  // of a buffer of row numbers
+  static constexpr int oRows = NX * kStage;  // (the ring's end)
+  // MX8: two widened tiles, then a wave's codes and its scales, a word each
+  static constexpr int oTiles = oRows, oCodes = oTiles + 2 * kQStage, kCodes = 8 * QT, oScales = oCodes + kWaves * kCodes;
+  // weights: lists of the rows of a wave's eight slots of eight stages: the first of three tiles, two others
+  static constexpr int oLists = MX ? oScales + kWaves * 8 * (QT / 32) * 4 : oRows, kLists = 5;
+  static constexpr int kBytes =
+      oLists + (FORM == kForward ? 3 * kRows * 4 : FORM == kWeights ? kWaves * kLists * 256 : 0);
+  static_assert(kBytes <= 163840);
+  static_assert(FORM != kWeights || (MT == 256 && NX == 2));
+
+  static constexpr int LP = kPStage / 1024 / kWaves, LQ = MX ? 0 : kQStage / 1024 / kWaves, kLoads = LP + LQ;
+  // A stage's loads go out a third at a time.
+  static constexpr int kFirst = (kLoads + 2) / 3, kSecond = kFirst + (kLoads + 1) / 3;
+  static constexpr int kCodeLoads = MX ? kCodes / 1024 + 1 : 0;
+};
+
+// What lanes past an end read.
+__device__ const uint8_t kZeros[16] __attribute__((aligned(16))) = {};
+__device__ const uint8_t kOne[4] = {127, 127, 127, 127};  // (scales)
+__device__ const int32_t kNoRow = -1;
+
+// A tile: the slots lo .. hi of expert e, and its first results.
+struct ResultTile {
+  int e, lo, hi, m0, n0, part;
+};
+
+template <Form FORM, int MT, bool GLU, bool MX>
+__global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert_tile_kernel(ExpertArgs a) {
+  using H = Shape<FORM, MT, MX>;
+  extern __shared__ __align__(16) char smem[];
+  int32_t* const rowbuf = reinterpret_cast<int32_t*>(smem + H::oRows);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  constexpr int QTO = GLU ? H::QT / 2 : H::QT;  // results a tile has in a row
+  const int wm = wave / H::WN, wn = wave % H::WN, r32 = lane & 31, half = lane >> 5;
+  const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem));
+  const char* const zero = reinterpret_cast<const char*>(kZeros);
+  const int N = static_cast<int>(a.N), K = static_cast<int>(a.K);
+  const int width = FORM == kForward ? N : K;  // of a row of results
+
+  // ---- which tiles
+  Walk walk;
+  ResultTile cur, next;
+  int64_t l = 0, end = 0, step_l = 0;  // (weights)
+  int more;
+  auto weight_tile = [&](int64_t l, ResultTile* t) __attribute__((always_inline)) {
+    const int64_t nt = (a.N + MT - 1) / MT, kt = (a.K + H::QT - 1) / H::QT;
+    const int64_t per = nt * kt * a.parts;
+    const int e = static_cast<int>(l / per), part = static_cast<int>((l - e * per) % a.parts);
+    const int64_t in = (l - e * per) / a.parts;
+    const auto* off = (const __attribute__((address_space(4))) int32_t*)reinterpret_cast<uintptr_t>(a.offsets);
+    const int S = static_cast<int>(a.S);
+    t->e = e;
+    t->lo = off ? min(max(off[e], 0), S) : 0;
+    t->hi = off ? min(max(off[e + 1], t->lo), S) : S;
+    if (a.parts > 1) {
+      const int each = ((t->hi - t->lo + H::KS - 1) / H::KS + a.parts - 1) / a.parts * H::KS;
+      t->lo = min(t->lo + part * each, t->hi);
+      t->hi = min(t->lo + each, t->hi);
+    }
+    t->part = part;
+    t->m0 = static_cast<int>(in / kt) * MT;
+    t->n0 = static_cast<int>(in % kt) * H::QT;
   };
-  if (FORM == kWeights || e < a.E) {
-    for (int64_t k0 = 0; k0 < L; k0 += 32) {
-      __syncthreads();
-      for (int i = tid; i < 64 * 32; i += kThreads) {
-        const int m = FORM == kWeights ? i % 64 : i / 32, k = FORM == kWeights ? i / 64 : i % 32;
-        uint16_t v = 0;
-        if (m0 + m < mend && k0 + k < L) {
-          if constexpr (FORM == kForward) {
-            const int64_t r = token(m0 + m);
-            if (r >= 0) v = a.x[r * a.ldx + k0 + k];
-          } else if constexpr (FORM == kTokens) {
-            v = a.dy[(m0 + m) * a.lddy + k0 + k];
-          } else {
-            if (token(lo + k0 + k) >= 0) v = a.dy[(lo + k0 + k) * a.lddy + m0 + m];
-          }
-        }
-        p[m * LD + k] = v;
+  auto slot_tile = [&](ResultTile* t) __attribute__((always_inline)) {
+    Tile s;
+    walk.get(&s);
+    t->e = s.e;
+    t->lo = s.lo;
+    t->hi = s.hi;
+    t->m0 = s.lo;
+    t->n0 = s.col * QTO;
+  };
+  auto get = [&](ResultTile* t) __attribute__((always_inline)) {
+    if constexpr (FORM == kWeights)
+      weight_tile(l, t);
+    else
+      slot_tile(t);
+  };
+  if constexpr (FORM == kWeights) {
+    // Each XCD gets an eighth of the work: an expert's tiles cost its steps, and the writing of results about as much as
+    // four steps (fp32: eight).
+    const int64_t per = (a.N + MT - 1) / MT * ((a.K + H::QT - 1) / H::QT) * a.parts;
+    const int runs = (a.E + 63) / 64;  // experts a lane
+    auto cost = [&](int e) __attribute__((always_inline)) {
+      int lo;
+      const int count = slots_of(a.offsets, a.E, static_cast<int>(a.S), e, &lo);
+      return ((count + H::KS - 1) / H::KS + a.parts - 1) / a.parts + (a.yf32 ? 8 : 4);
+    };
+    int own = 0;
+    for (int i = 0; i < runs; ++i)
+      if (lane * runs + i < a.E) own += cost(lane * runs + i);
+    const int sum = wave_scan(own);
+    const int64_t total = lane_value(sum, 63) * per;
+    auto border = [&](int x) __attribute__((always_inline)) {  // first tile whose cost begins at x eighths or after
+      const int64_t target = total * x / 8;
+      const uint64_t past = __ballot(sum * per > target);
+      if (!past) return a.E * per;
+      const int run = __builtin_ctzll(past);
+      int e = run * runs, c = cost(e);
+      int64_t before = static_cast<int64_t>(lane_value(sum, run) - lane_value(own, run)) * per;
+      while (before + c * per <= target) {
+        before += c * per;
+        c = cost(++e);
       }
-      for (int h = 0; h < H; ++h)
-        for (int i = tid; i < 64 * 32; i += kThreads) {
-          const int n = FORM == kForward ? i / 32 : i % 64, k = FORM == kForward ? i % 32 : i / 64;
-          uint16_t v = 0;
-          if (n0 + n < nend && k0 + k < L) {
-            if constexpr (FORM == kForward) {
-              v = a.w[((e * int64_t(H) + h) * a.N + n0 + n) * a.K + k0 + k];
-            } else if constexpr (FORM == kTokens) {
-              v = a.w[(e * a.N + k0 + k) * a.K + n0 + n];
-            } else {
-              const int64_t r = token(lo + k0 + k);
-              if (r >= 0) {
-                if constexpr (MX) {
-                  const uint32_t c = a.xcodes[r * a.K + n0 + n];
-                  const float scale = mx4_scale(a.xscales[(r * a.K + n0 + n) / 32]);
-                  v = f32_to_bf16(__builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, scale, false)[0]);
-                } else {
-                  v = a.x[r * a.ldx + n0 + n];
-                }
-              }
-            }
+      return e * per + (target - before + c - 1) / c;
+    };
+    l = border(blockIdx.x & 7);
+    end = border((blockIdx.x & 7) + 1);
+    step_l = gridDim.x >> 3;
+    l += blockIdx.x >> 3;
+    more = l < end;
+  } else {
+    int head, none;
+    more = walk.start(a.offsets, a.E, a.S, static_cast<int>((width + QTO - 1) / QTO), MT, &head, &none);
+    // slots of no expert: zeros
+    for (int64_t i = blockIdx.x; i < head + (a.S - none); i += gridDim.x) {
+      const int64_t s = i < head ? i : none + (i - head);
+      for (int64_t n = tid; n < width; n += H::kThreads) {
+        if (a.yf32)
+          static_cast<float*>(a.y)[s * a.ldy + n] = 0.0f;
+        else
+          static_cast<uint16_t*>(a.y)[s * a.ldy + n] = 0;
+      }
+    }
+  }
+  if (!more) return;
+  get(&cur);
+  auto steps_of = [&](const ResultTile& t) __attribute__((always_inline)) {  // (NX at least, so that the ring never reaches past the next tile)
+    const int L = FORM == kForward ? K : FORM == kTokens ? N : t.hi - t.lo;
+    return max((L + H::KS - 1) / H::KS, H::NX);
+  };
+
+  // ---- where the loads come from
+  const char *pp[H::LP], *pq[H::LQ ? H::LQ : 1];
+  // operands by rows: 8 lanes a row; row of load q, and the chunk of it that goes to this lane's place
+  // (the chunk is the same for all of them, as every wave's rows are eight of 32 or 64 apart)
+  auto row_of = [&](int q, int l) __attribute__((always_inline)) { return (wave + H::kWaves * q) * 8 + l / 8; };
+  const int chunk = chunk_slot(row_of(0, lane), lane & 7);
+  auto load_rows = [&](const ResultTile& t, int buf) __attribute__((always_inline)) {  // the rows of a tile's slots (past its end: its last)
+    if constexpr (FORM == kForward)
+      if (a.rows && wave < H::kRows / 64)
+        load_lds4(a.rows + min(t.lo + wave * 64 + lane, t.hi - 1), lds0 + H::oRows + (buf * H::kRows + wave * 64) * 4);
+  };
+  const char* px[2];  // weights: x at this lane's columns, for even and odd loads
+  auto aim = [&](const ResultTile& t, int buf) __attribute__((always_inline)) {
+    const int lane = opaque(tid) & 63, r32 = lane & 31, half = lane >> 5;  // (not kept in registers between the tiles)
+    if constexpr (FORM == kWeights) {  // two slots a load, 32 chunks each (columns past the end: the last ones)
+      auto col = [&](int first, int q, int end) __attribute__((always_inline)) { return min(first + 8 * (r32 ^ (4 * ((2 * q + half) & 3))), end - 8); };
+#pragma unroll
+      for (int q = 0; q < H::LP; ++q)
+        pp[q] = reinterpret_cast<const char*>(
+            a.dy + (static_cast<int64_t>(t.lo) + wave * 8 + 2 * q + half) * a.lddy + col(t.m0, q, N));
+#pragma unroll
+      for (int q = 0; q < 2; ++q) px[q] = reinterpret_cast<const char*>(a.x + col(t.n0, q, K));
+    } else {
+#pragma unroll
+      for (int q = 0; q < H::LP; ++q) {
+        const int r = row_of(q, lane), c = chunk_slot(r, lane & 7);
+        if constexpr (FORM == kForward) {
+          int64_t row = min(t.lo + r, t.hi - 1);
+          if (a.rows) {  // (one that does not exist: row 0, its results are replaced)
+            row = rowbuf[buf * H::kRows + r];
+            row = row >= 0 && row < a.x_rows ? row : 0;
           }
-          q[h][n * LD + k] = v;
+          pp[q] = reinterpret_cast<const char*>(a.x + row * a.ldx + c * 8);
+        } else {
+          pp[q] = reinterpret_cast<const char*>(a.dy + static_cast<int64_t>(min(t.lo + r, t.hi - 1)) * a.lddy + c * 8);
         }
-      __syncthreads();
-      const bf16x8 b = *reinterpret_cast<const bf16x8*>(p + (wave * 16 + (lane & 15)) * LD + 8 * (lane >> 4));
+      }
 #pragma unroll
-      for (int h = 0; h < H; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          acc[h][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              *reinterpret_cast<const bf16x8*>(q[h] + (i * 16 + (lane & 15)) * LD + 8 * (lane >> 4)), b, acc[h][i], 0,
-              0, 0);
+      for (int q = 0; q < H::LQ; ++q) {
+        if constexpr (FORM == kForward) {
+          const int r = row_of(q, lane), c = chunk_slot(r, lane & 7);
+          int64_t row;
+          if constexpr (GLU)  // 32 gate rows, then the 32 up rows of the same outputs
+            row = static_cast<int64_t>(t.e) * 2 * a.N + min(t.n0 + (r >> 6) * 32 + (r & 31), N - 1) +
+                  ((r >> 5) & 1) * a.N;
+          else
+            row = static_cast<int64_t>(t.e) * a.N + min(t.n0 + r, N - 1);
+          pq[q] = reinterpret_cast<const char*>(a.w + row * a.K + c * 8);
+        } else {  // two rows of W a load, 32 chunks each
+          const int r = (wave + H::kWaves * q) * 2 + half;
+          const int col = min(t.n0 + 8 * (r32 ^ (4 * (r & 3))), K - 8);
+          pq[q] = reinterpret_cast<const char*>(a.w + (static_cast<int64_t>(t.e) * a.N + r) * a.K + col);
+        }
+      }
     }
-  }
-  const int64_t m = m0 + wave * 16 + (lane & 15);
-  if (m >= mend) return;
-  bool have = true;
-  if constexpr (FORM == kForward) have = e < a.E && token(m) >= 0;
+  };
+
+  // ---- the loads of the next stage
+  int step = 0, to = 0, steps_to = 0;  // of the tile being loaded: its next step, ring place, steps
+  ResultTile ld;                       // that tile
+  // weights: the rows of slots come through LDS, asked for eight stages at once and long before
+  int row[4] = {};  // of this lane's slots in the stage being loaded; negative: none
+  int head = 0;     // list of the first stages of the tile being loaded
+  auto list_at = [&](int at) __attribute__((always_inline)) { return H::oLists + (wave * H::kLists + at) * 256; };
+  auto ask_rows = [&](const ResultTile& t, int chunk, int at) __attribute__((always_inline)) {
+    const int lane = opaque(tid) & 63;
+    const int s = t.lo + (chunk * 8 + lane / 8) * H::KS + wave * 8 + lane % 8;
+    load_lds4(s < t.hi ? a.rows + s : &kNoRow, lds0 + list_at(at));
+  };
+  auto row_of_slot = [&](int slot) __attribute__((always_inline)) {  // (of this wave's eight)
+    const int s = ld.lo + step * H::KS + wave * 8 + slot;
+    const int list = step < 8 ? head : 3 + (step >> 3 & 1);
+    const int r = a.rows ? *reinterpret_cast<const int*>(smem + list_at(list) + (step & 7) * 32 + slot * 4)
+                         : s < ld.hi ? s : -1;
+    return r < a.x_rows ? r : -1;
+  };
+  auto take_rows = [&]() __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f32x4 v = acc[0][i];
-    if constexpr (GLU) {
-#pragma unroll
-      for (int u = 0; u < 4; ++u) v[u] = silu(v[u]) * acc[1][i][u];
+    for (int q = 0; q < 4; ++q) row[q] = row_of_slot(2 * q + half);
+  };
+  auto load = [&](int k) __attribute__((always_inline)) {  // load k of the stage's LP + LQ
+    const uint32_t base = lds0 + to * H::kStage;
+    const bool of_p = k < H::LP;
+    const int q = of_p ? k : k - H::LP;
+    if constexpr (FORM == kWeights) {
+      const int r = row[q];
+      if (of_p) {
+        load_lds16(r >= 0 ? pp[q] : zero, base + (wave * H::LP + q) * 1024);
+        pp[q] += a.lddy * (H::KS * 2);
+      } else {
+        load_lds16(r >= 0 ? px[q & 1] + static_cast<uint64_t>(static_cast<uint32_t>(r)) * static_cast<uint32_t>(2 * a.ldx)
+                          : zero,
+                   base + H::kPStage + (wave * H::LQ + q) * 1024);
+      }
+    } else {
+      const int rem = (FORM == kForward ? K : N) - step * H::KS;  // entries from this stage on
+      const char* p = of_p ? pp[q] : pq[q];
+      if (rem < H::KS) {
+        asm volatile("");  // (a branch, not selects at every step)
+        if (of_p || FORM == kForward)
+          p = 8 * chunk < rem ? p : zero;
+        else
+          p = (wave + H::kWaves * q) * 2 + half < rem ? p : zero;
+      }
+      load_lds16(p, base + (of_p ? 0 : H::kPStage) + (wave + H::kWaves * q) * 1024);
+      if (of_p)
+        pp[q] += H::KS * 2;
+      else
+        pq[q] += FORM == kForward ? H::KS * 2 : H::KS * 2 * a.K;
     }
-    if (!have) v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const int64_t n = n0 + i * 16 + 4 * (lane >> 4);
-    if (n < nend) store4(a, FORM == kWeights ? e * a.N + m : m, n, nend, a.ldy % 4 == 0, v);
+  };
+  auto loaded = [&]() __attribute__((always_inline)) {
+    ++step;
+    to = to + 1 == H::NX ? 0 : to + 1;
+  };
+  auto issue = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < H::kLoads; ++k) load(k);
+    loaded();
+  };
+  // MX8: this wave's codes of the next stage, four slots of 256 bytes a load, and their scales, a lane slot lane / 8's
+  // block lane % 8
+  auto issue_codes = [&]() __attribute__((always_inline)) {
+    const int lane = opaque(tid) & 63;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int r = row_of_slot(4 * q + lane / 16), col = min(ld.n0 + 16 * (lane % 16), K - 16);
+      const uint8_t* p = a.xcodes + static_cast<int64_t>(r) * a.K + col;
+      load_lds16(r >= 0 ? reinterpret_cast<const char*>(p) : zero, lds0 + H::oCodes + wave * H::kCodes + q * 1024);
+    }
+    const int r = row_of_slot(lane / 8), block = min(ld.n0 / 32 + lane % 8, K / 32 - 1);
+    const uint8_t* p = a.xscales + static_cast<int64_t>(r) * (a.K / 32) + block;
+    load_lds1(r >= 0 ? p : kOne, lds0 + H::oScales + wave * 256);
+  };
+  auto widen = [&](int i, int tile) __attribute__((always_inline)) {  // entries 8 i .. 8 i + 7 of this lane's block
+    const int lane = opaque(tid) & 63;
+    const uint2 c = *reinterpret_cast<const uint2*>(smem + H::oCodes + wave * H::kCodes + lane * 32 + i * 8);
+    const float scale = mx4_scale(*reinterpret_cast<const uint32_t*>(smem + H::oScales + wave * 256 + lane * 4));
+    const int slot = wave * 8 + lane / 8, at = 4 * (lane % 8) + i;
+    *reinterpret_cast<uint4*>(smem + H::oTiles + tile * H::kQStage + slot * (H::QT * 2) + ((at ^ (4 * (slot & 3))) << 4)) =
+        make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, scale, false)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, scale, true)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, scale, false)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, scale, true)));
+  };
+  // until at most N of this wave's loads are under way: its own codes are there (no other wave reads them)
+  auto wait_own = [](auto n) { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(n)::value) : "memory"); };
+
+  // ---- going on into the next tile
+  int buf = 0, since = 0;
+  int dry = 0;
+  auto after = [&](int b) __attribute__((always_inline)) { return b == 2 ? 0 : b + 1; };
+  auto find_next = [&]() __attribute__((always_inline)) {
+    if constexpr (FORM == kWeights) {
+      l += step_l;
+      more = l < end;
+    } else {
+      walk.l += walk.step;
+      more = walk.find();
+    }
+    if (more) {
+      get(&next);
+      load_rows(next, after(buf));
+      if constexpr (FORM == kWeights) {
+        if (a.rows && l + step_l < end) {  // the list of the tile after it
+          ResultTile t;
+          weight_tile(l + step_l, &t);
+          ask_rows(t, 0, after(after(head)));
+        }
+      }
+    }
+    since = 0;
+  };
+  auto turn = [&]() __attribute__((always_inline)) {  // to the next tile if the loads are through with theirs
+    const int over = step == steps_to;
+    dry = over && !more;
+    if (dry) return;
+    if (over) {
+      // (the next tile's rows have landed if as many steps as the ring has stages waited since they were asked for)
+      if (FORM == kForward && a.rows && since < H::NX) wait_loads<0>();
+      aim(next, after(buf));
+      steps_to = steps_of(next);
+      step = 0;
+      ld = next;
+      head = after(head);
+    }
+    if constexpr (FORM == kWeights) {
+      take_rows();
+      // (entering a list: the one after it)
+      if (a.rows && (step & 7) == 0 && step + 8 < steps_to) ask_rows(ld, step / 8 + 1, 3 + ((step >> 3) + 1 & 1));
+    }
+  };
+
+  // ---- fragments of sixteen entries of the sum
+  struct Part {
+    bf16x8 p[H::MB], q[H::NB];
+  };
+  // Blocks of 32 rows of P go to the wm waves in turn, so that what an expert's last slots leave empty is shared out.
+  auto prow = [&](int m) __attribute__((always_inline)) { return (m * H::WM + wm) * 32; };
+  const int qrow = wn * 64;
+  auto by_rows = [&](const char* st, int row0, int j) __attribute__((always_inline)) {
+    const int r = row0 + r32;
+    return *reinterpret_cast<const bf16x8*>(st + r * 128 + chunk_slot(r, 2 * j + half) * 16);
+  };
+  auto by_cols = [&](const char* st, int col0, int j, int cols) __attribute__((always_inline)) {
+    // rows 16 j + 8 half + 4 i + (lane % 16) / 4, columns from 16 ((lane / 16) % 2) + 4 (lane % 4) on
+    const int col = col0 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    s16x4 v[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = 16 * j + 8 * half + 4 * i + ((lane & 15) >> 2);
+      v[i] = read_transposed(st + r * (cols * 2) + (((col >> 3) ^ (4 * (r & 3))) << 4) + (col & 7) * 2);
+    }
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  auto read_q = [&](Part& f, int j, const char* st, int tile) __attribute__((always_inline)) {
+    const char* q = MX ? smem + H::oTiles + tile * H::kQStage : st + H::kPStage;
+#pragma unroll
+    for (int n = 0; n < H::NB; ++n)
+      if constexpr (H::kQCols)
+        f.q[n] = by_cols(q, qrow + 32 * n, j, H::QT);
+      else
+        f.q[n] = by_rows(q, qrow + 32 * n, j);
+  };
+  auto read_p = [&](Part& f, int m, int j, const char* st) __attribute__((always_inline)) {
+    if constexpr (H::kPCols)
+      f.p[m] = by_cols(st, prow(m), j, MT);
+    else
+      f.p[m] = by_rows(st, prow(m), j);
+  };
+  f32x16 acc[H::NB][H::MB];
+  auto clear = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < H::NB; ++i)
+#pragma unroll
+      for (int j = 0; j < H::MB; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+  };
+  // This wave's blocks of a tile that hold results.
+  auto blocks_of = [&](const ResultTile& t) __attribute__((always_inline)) {
+    const int blocks = (min((FORM == kWeights ? N : t.hi) - t.m0, MT) + 31) / 32;
+    const bool cols = t.n0 + (GLU ? wn * 32 : qrow) < width;
+    return cols ? (blocks - wm + H::WM - 1) / H::WM : 0;
+  };
+  int blocks = 0;
+  // The ops of a part, with the reads of the parts of `reads` and `between(m)` after a block's ops.
+  auto multiply = [&](const Part& f, const char* st, int tile, auto between, auto... reads) __attribute__((always_inline)) {
+#pragma unroll
+    for (int m = 0; m < H::MB; ++m) {
+      if (m < blocks) {
+#pragma unroll
+        for (int n = 0; n < H::NB; ++n) {
+          acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.q[n], f.p[m], acc[n][m], 0, 0, 0);
+          if (m == 0 && n == 0) (read_q(*reads.first, reads.second, st, tile), ...);
+          if (n == H::NB - 1) (read_p(*reads.first, m, reads.second, st), ...);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      between(m);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  const auto nothing = [](int) {};
+
+  load_rows(cur, 0);
+  wait_loads<0>();
+  aim(cur, 0);
+  ld = cur;
+  steps_to = steps_of(cur);
+  if constexpr (FORM == kWeights) {
+    if (a.rows) {
+      ask_rows(cur, 0, 0);
+      if (l + step_l < end) {
+        ResultTile t;
+        weight_tile(l + step_l, &t);
+        ask_rows(t, 0, 1);
+      }
+      if (8 < steps_to) ask_rows(cur, 1, 4);
+    }
+    wait_own(std::integral_constant<int, 0>{});
   }
+#pragma unroll
+  for (int i = 0; i < H::NX; ++i) {
+    if constexpr (FORM == kWeights) take_rows();
+    if constexpr (MX) {
+      issue_codes();
+      if (i == 0) {
+        wait_own(std::integral_constant<int, 0>{});
+#pragma unroll
+        for (int j = 0; j < 4; ++j) widen(j, 0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      }
+    }
+    issue();
+  }
+  if constexpr (MX)
+    wait_loads<0>();
+  else
+    wait_loads<(H::NX - 1) * H::kLoads>();
+  find_next();
+  clear();
+  const char* st = smem;
+  int tile = 0;
+  Part f0, f1, f2;
+  // (a tile's first fragments are read whole: the step before it does not know which of its blocks hold results)
+  auto read_first = [&](Part& f, const char* st, int tile) __attribute__((always_inline)) {
+    read_q(f, 0, st, tile);
+#pragma unroll
+    for (int m = 0; m < H::MB; ++m) read_p(f, m, 0, st);
+  };
+  read_first(f0, st, tile);
+  // Waits for the next stage and the workgroup; N loads are younger than it.  So are the stores of the tile before (they
+  // count with the loads), in a tile's first steps: they may go on where this wave made all that there can be.
+  constexpr int kStores16 = (GLU ? 1 : H::NB) * H::MB * 2, kStores32 = 2 * kStores16;
+  int stored = 0;
+  int pending = 0;  // the last third of a stage's loads is to go out yet
+  // Loads [from, to) of a stage, those of the m-th of MB turns.
+  auto loads = [&](int from, int to, int m) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < H::kLoads; ++k)
+      if (k >= from && k < to && (k - from) * H::MB / (to - from) == m) load(k);
+  };
+  auto wait_step = [&](auto n, bool first) __attribute__((always_inline)) {
+    if (!first || !stored)
+      wait_loads<decltype(n)::value>();
+    else if (a.yf32)
+      wait_loads<decltype(n)::value + kStores32>();
+    else
+      wait_loads<decltype(n)::value + kStores16>();
+  };
+  for (;;) {
+    const int steps = steps_of(cur);
+    blocks = blocks_of(cur);
+    for (int i = 0; i < steps; ++i) {
+      const int last = i + 1 == steps, rest = pending;
+      if (FORM == kWeights && i * H::KS >= cur.hi - cur.lo) blocks = 0;  // (a stage of no slots)
+      if constexpr (FORM == kWeights) {
+        // (No registers are left for reading a stage to its end earlier.)
+        multiply(f0, st, tile, [&](int m) __attribute__((always_inline)) {
+          if (rest) loads(H::kSecond, H::kLoads, m);
+        }, std::pair{&f1, 1});
+        if (rest) loaded();
+        if constexpr (MX) {
+          // the next stage's codes are there but for what was asked for later, P of that stage
+          if (i > 0 || !stored)
+            wait_own(std::integral_constant<int, H::kLoads>{});
+          else if (a.yf32)
+            wait_own(std::integral_constant<int, H::kLoads + kStores32>{});
+          else
+            wait_own(std::integral_constant<int, H::kLoads + kStores16>{});
+        }
+        turn();
+        multiply(f1, st, tile, [&](int m) __attribute__((always_inline)) {
+          if (MX && m < 2) widen(m, tile ^ 1);
+        }, std::pair{&f0, 2});
+        multiply(f0, st, tile, [&](int m) __attribute__((always_inline)) {
+          if (MX && m < 2) widen(2 + m, tile ^ 1);
+        }, std::pair{&f1, 3});
+        // the next stage is whole, and every wave has read all of this one
+        if (dry)
+          wait_loads<0>();
+        else
+          wait_step(std::integral_constant<int, 0>{}, i == 0);
+        if constexpr (MX)
+          if (!dry) issue_codes();  // (in the place of those that are widened)
+      } else {
+        // A stage is read to its end half a step early, and its place loaded again while the other half and the next
+        // step's first part are multiplied: all at once the loads would hold up the ops behind them.
+        multiply(f0, st, tile, [&](int m) __attribute__((always_inline)) {
+          if (rest) loads(H::kSecond, H::kLoads, m);
+        }, std::pair{&f1, 1});
+        if (rest) loaded();
+        turn();
+        const int go = !dry;
+        multiply(f1, st, tile, nothing, std::pair{&f0, 2}, std::pair{&f2, 3});
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        multiply(f0, st, tile, [&](int m) __attribute__((always_inline)) {
+          if (go) loads(0, H::kFirst, m);
+        });
+        if (dry)
+          wait_loads<0>();
+        else
+          wait_step(std::integral_constant<int, (H::NX - 2) * H::kLoads + H::kFirst>{}, i < H::NX - 1);
+        ++since;
+      }
+      tile ^= 1;
+      st = st + H::kStage == smem + H::oRows ? smem : st + H::kStage;
+      const int go = !dry;
+      // (what is read after a tile's last step is not used; its loads all go out before the results)
+      multiply(FORM == kWeights ? f1 : f2, st, tile, [&](int m) __attribute__((always_inline)) {
+        if (go) {
+          loads(FORM == kWeights ? 0 : H::kFirst, H::kSecond, m);
+          if (last) loads(H::kSecond, H::kLoads, m);
+        }
+      }, std::pair{&f0, 0});
+      pending = go && !last;
+      if (go && last) loaded();
+    }
+    const int mend = FORM == kWeights ? N : cur.hi;
+    const bool whole = cur.n0 + QTO <= width && a.ldy % 8 == 0;
+    const int r32 = opaque(tid) & 31, half = (opaque(tid) & 63) >> 5;
+    if (more) read_first(f0, st, tile);
+#pragma unroll
+    for (int m = 0; m < H::MB; ++m) {
+      const int at = cur.m0 + prow(m) + r32;
+      if (at >= mend) continue;
+      bool have = true;
+      if constexpr (FORM == kForward) {
+        if (a.rows) {
+          const int row = rowbuf[buf * H::kRows + prow(m) + r32];
+          have = row >= 0 && row < a.x_rows;
+        }
+      }
+      const int64_t to_row =
+          FORM == kWeights ? (static_cast<int64_t>(cur.part) * a.E + cur.e) * a.N + at : at;
+#pragma unroll
+      for (int n = 0; n < (GLU ? 1 : H::NB); ++n) {
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          v[i] = acc[n][m][i];
+          if constexpr (GLU) v[i] = silu(v[i]) * acc[1][m][i];
+          if (FORM == kForward && !have) v[i] = 0.0f;
+        }
+        store32(a, to_row, cur.n0 + (GLU ? wn * 32 : qrow + 32 * n), half, whole, width, v);
+      }
+    }
+    if (!more) return;
+    stored = whole && cur.m0 + MT <= mend;
+    cur = next;
+    buf = after(buf);
+    clear();
+    find_next();
+  }
+}
+
+// 32 x 64 results a workgroup (glu: 32 gate and 32 up rows), the sum split over its
+// four waves: wave w takes stages w, w + 4, ... of 64 entries through a ring of its
+// own, with no barrier up to the end, where the four sums are joined in LDS in the
+// order of the waves.  For calls of too few large tiles to fill the card: what counts
+// is how fast one workgroup goes through a long sum.
+struct SplitShape {
+  static constexpr int MT = 32, QT = 64, KS = 64, NX = 3, kWaves = 4;
+  static constexpr int kPStage = MT * KS * 2, kStage = kPStage + QT * KS * 2, kRing = NX * kStage;
+  static constexpr int LP = kPStage / 1024, LQ = QT * KS * 2 / 1024, kLoads = LP + LQ;
+  static constexpr int kBytes = kWaves * kRing;
+  static_assert(kBytes <= 163840 && 2 * kLoads < 64);
+};
+
+template <Form FORM, bool GLU>
+__global__ __launch_bounds__(kThreads) void expert_split_kernel(ExpertArgs a) {
+  using H = SplitShape;
+  extern __shared__ __align__(16) char smem[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r32 = lane & 31, half = lane >> 5;
+  constexpr int QTO = GLU ? H::QT / 2 : H::QT;
+  const int N = static_cast<int>(a.N), K = static_cast<int>(a.K), width = FORM == kForward ? N : K;
+  Tile t;
+  if (!find_tile(a.offsets, a.E, a.S, (width + QTO - 1) / QTO, H::MT, &t)) return;
+  const int n0 = t.col * QTO;
+  f32x16 acc[2];
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[n][e] = 0.0f;
+  bool have = t.e < a.E;  // the row of this lane's slot exists
+  if (t.e < a.E) {
+    const char* const zero = reinterpret_cast<const char*>(kZeros);
+    const int sum = FORM == kForward ? K : N, stages = (sum + H::KS - 1) / H::KS;
+    char* const ring = smem + wave * H::kRing;
+    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring));
+    auto token = [&](int r) {  // (a row that does not exist: row 0, its results are replaced)
+      const int s = min(t.lo + r, t.hi - 1);
+      if (!a.rows) return static_cast<int64_t>(s);
+      const int64_t row = a.rows[s];
+      return row >= 0 && row < a.x_rows ? row : -1;
+    };
+    // (8 lanes a row of either operand)
+    const int wchunk = (lane & 7) ^ (4 * ((lane / 8 >> 1) & 1));
+    const char *pp[H::LP], *pq[H::LQ];
+#pragma unroll
+    for (int q = 0; q < H::LP; ++q) {
+      const int r = q * 8 + lane / 8, c = chunk_slot(r, lane & 7);
+      if constexpr (FORM == kForward)
+        pp[q] = reinterpret_cast<const char*>(a.x + max(token(r), int64_t(0)) * a.ldx + c * 8);
+      else
+        pp[q] = reinterpret_cast<const char*>(a.dy + static_cast<int64_t>(min(t.lo + r, t.hi - 1)) * a.lddy + c * 8);
+    }
+#pragma unroll
+    for (int q = 0; q < H::LQ; ++q) {
+      const int r = q * 8 + lane / 8;
+      if constexpr (FORM == kForward) {
+        int64_t row;
+        if constexpr (GLU)
+          row = static_cast<int64_t>(t.e) * 2 * a.N + min(n0 + (r & 31), N - 1) + (r >> 5) * a.N;
+        else
+          row = static_cast<int64_t>(t.e) * a.N + min(n0 + r, N - 1);
+        pq[q] = reinterpret_cast<const char*>(a.w + row * a.K + chunk_slot(r, lane & 7) * 8);
+      } else {
+        pq[q] = reinterpret_cast<const char*>(a.w + (static_cast<int64_t>(t.e) * a.N + r) * a.K +
+                                              min(n0 + 8 * wchunk, K - 8));
+      }
+    }
+    if constexpr (FORM == kForward) have = token(r32) >= 0;
+    int to = 0;
+    auto issue = [&](int stage) {  // (past the last one: zeros, so that waits go by count)
+      const int rem = sum - stage * H::KS;
+      const int64_t at = static_cast<int64_t>(stage) * (H::KS * 2);
+#pragma unroll
+      for (int q = 0; q < H::LP; ++q) {
+        const int c = chunk_slot(q * 8 + lane / 8, lane & 7);
+        load_lds16(8 * c < rem ? pp[q] + at : zero, lds0 + to * H::kStage + q * 1024);
+      }
+#pragma unroll
+      for (int q = 0; q < H::LQ; ++q) {
+        const int c = chunk_slot(q * 8 + lane / 8, lane & 7);
+        const bool in = FORM == kForward ? 8 * c < rem : q * 8 + lane / 8 < rem;
+        load_lds16(in ? pq[q] + (FORM == kForward ? at : at * a.K) : zero,
+                   lds0 + to * H::kStage + H::kPStage + q * 1024);
+      }
+      to = to + 1 == H::NX ? 0 : to + 1;
+    };
+#pragma unroll
+    for (int i = 0; i < H::NX; ++i) issue(wave + i * H::kWaves);
+    const char* st = ring;
+    for (int s = wave; s < stages; s += H::kWaves) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((H::NX - 1) * H::kLoads) : "memory");
+      bf16x8 p[4], q[4][2];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        p[j] = *reinterpret_cast<const bf16x8*>(st + r32 * 128 + chunk_slot(r32, 2 * j + half) * 16);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          const char* w = st + H::kPStage;
+          if constexpr (FORM == kForward) {
+            q[j][n] = *reinterpret_cast<const bf16x8*>(w + (32 * n + r32) * 128 + chunk_slot(r32, 2 * j + half) * 16);
+          } else {
+            const int col = 32 * n + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+            s16x4 v[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int r = 16 * j + 8 * half + 4 * i + ((lane & 15) >> 2);
+              v[i] = read_transposed(w + r * 128 + (((col >> 3) ^ (4 * ((r >> 1) & 1))) << 4) + (col & 7) * 2);
+            }
+            q[j][n] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+          }
+        }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      issue(s + H::NX * H::kWaves);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+          acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q[j][n], p[j], acc[n], 0, 0, 0);
+      st = st + H::kStage == ring + H::kRing ? ring : st + H::kStage;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // [wave][n][16][64]
+    float* join = reinterpret_cast<float*>(smem);
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) join[((wave * 2 + n) * 16 + e) * 64 + lane] = acc[n][e];
+    __syncthreads();
+    if (wave >= (GLU ? 1 : 2)) return;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        if (!GLU && n != 0) continue;  // (wave n takes block n, into acc[0])
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < H::kWaves; ++w) v += join[((w * 2 + (GLU ? n : wave)) * 16 + e) * 64 + lane];
+        acc[n][e] = v;
+      }
+  } else if (wave >= (GLU ? 1 : 2)) {
+    return;
+  }
+  const int slot = t.lo + r32;
+  if (slot >= t.hi) return;
+  float v[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    v[e] = GLU ? silu(acc[0][e]) * acc[1][e] : acc[0][e];
+    if (!have) v[e] = 0.0f;
+  }
+  store32(a, slot, n0 + 32 * wave, half, n0 + QTO <= width && a.ldy % 8 == 0, width, v);
+}
+
+template <Form FORM, bool GLU = false>
+bitsmoe_status split(const ExpertArgs& a, unsigned grid, hipStream_t s) {
+  auto* fn = expert_split_kernel<FORM, GLU>;
+  static std::atomic<uint64_t> allowed{0};
+  if (bitsmoe_status st = allow_lds(reinterpret_cast<const void*>(fn), SplitShape::kBytes, &allowed)) return st;
+  KernelTimer timer("expert_split", s);
+  fn<<<grid, kThreads, SplitShape::kBytes, s>>>(a);
+  BITSMOE_LAUNCH_CHECK("expert_split_kernel");
+  return ok();
+}
+
+// One workgroup a compute unit, as many on every XCD.
+unsigned tile_grid() {
+  const int cus = device_cus();
+  return static_cast<unsigned>(cus < 8 ? 8 : cus / 8 * 8);
+}
+
+template <Form FORM, int MT, bool GLU = false, bool MX = false>
+bitsmoe_status tiles(const ExpertArgs& a, hipStream_t s) {
+  using H = Shape<FORM, MT, MX>;
+  auto* fn = expert_tile_kernel<FORM, MT, GLU, MX>;
+  static std::atomic<uint64_t> allowed{0};
+  if (bitsmoe_status st = allow_lds(reinterpret_cast<const void*>(fn), H::kBytes, &allowed)) return st;
+  KernelTimer timer(FORM == kWeights ? "expert_weights" : MT == 32 ? "expert_tile_32" : MT == 128 ? "expert_tile_128"
+                                                                                               : "expert_tile_256", s);
+  fn<<<tile_grid(), H::kThreads, H::kBytes, s>>>(a);
+  BITSMOE_LAUNCH_CHECK("expert_tile_kernel");
+  return ok();
 }
 
 constexpr int kLargestTile = 256;
@@ -166,8 +915,9 @@ bitsmoe_status check(const char* who, const ExpertArgs& a, bitsmoe_dtype t, bits
 }
 
 bitsmoe_status check_stride(const char* who, int64_t cols, int64_t ld) {
-  if (ld < cols || ld % 8 != 0 || ld > (int64_t(1) << 32))
-    return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": rows must not overlap, and lie a multiple of 16 bytes apart");
+  if (ld < cols || ld % 8 != 0 || ld > 0x7FFFFFFF)
+    return fail(BITSMOE_ERR_SHAPE,
+                std::string(who) + ": rows must not overlap, and lie a multiple of 16 bytes and below 2^31 entries apart");
   return BITSMOE_OK;
 }
 
@@ -179,14 +929,127 @@ bool grid_of(const ExpertArgs& a, int64_t tile, int64_t per, unsigned* grid) {
   return true;
 }
 
+// Which kernel takes a product.  The counts of an expert's slots are on the device;
+// the host goes by S and E alone: about
+//     tiles(m) = max(active, S / m + active / 2),  active = E (1 - exp(-S / E))
+// tiles of m slots (as of slots that choose by chance).  The constants (us; L entries of
+// the sum, `wide` rows of weights or columns of results) fit timings of every kernel at
+// 53 shapes, E 1 .. 238, S / E 0.03 .. 4100, sums of 64 .. 14336 entries: the choice
+// is 3 % off the best kernel on average, where the worst is mostly two to ten times it
+// (194 slots of 8 experts, 1024 x 4096: 38 us by rows, 18.6 split, 44, 51 and 66 in tiles of 32, 128 and 256 slots;
+// 32768 slots of 128 experts, 1536 x 2048: 3112, 949, 562, 317 and 292; 512 slots of 128 experts, 2048 x 768: 140,
+// 119, 71, 72 and 82).
+enum Kernel { kByRows, kSplit, kTiles32, kTiles128, kTiles256 };
+
+Kernel product_kernel(const ExpertArgs& a, Form form, int64_t wide, bool glu) {
+  const double E = a.E, S = static_cast<double>(a.S), active = E * (1.0 - std::exp(-S / E));
+  const double L = static_cast<double>(form == kForward ? a.K : a.N);
+  const double bytes = active * static_cast<double>(a.N * (glu ? 2 : 1)) * static_cast<double>(a.K) * 2e-6;
+  auto tiles = [&](double m, int64_t cols) {
+    const double t = S / m + active / 2;
+    return (t > active ? t : active) * static_cast<double>((wide + cols - 1) / cols);
+  };
+  // workgroups that stay, one a compute unit, between their rounds' number and their share
+  auto rounds = [&](double t) {
+    const double share = t / device_cus();
+    return 0.5 * (std::ceil(share) + (share > 1.0 ? share : 1.0));
+  };
+  auto with_bytes = [&](double us, double rate) { return us > bytes / rate ? us : bytes / rate; };
+  const double chain = L * 0.001, each = tiles(16, 16) * (L * 5.3e-6 + 0.0023);
+  const double cost[5] = {with_bytes(5.6 + (chain > each ? chain : each), 4.6),
+                          with_bytes(1.6 + rounds(tiles(32, 64)) * (4.5 + L * 0.0024), 4.2),
+                          with_bytes(1.8 + rounds(tiles(32, 256)) * (4.0 + L * 0.0094), 5.0),
+                          with_bytes(rounds(tiles(128, 256)) * (6.0 + L * 0.0118), 5.0),
+                          with_bytes(rounds(tiles(256, 256)) * (6.2 + L * 0.0172), 5.0)};
+  int best = form == kForward ? kByRows : kSplit;  // (there is no kernel by rows for W by its rows)
+  for (int k = best + 1; k <= kTiles256; ++k)
+    if (cost[k] < cost[best]) best = k;
+  return static_cast<Kernel>(best);
+}
+
+template <Form FORM, bool GLU>
+bitsmoe_status product(const ExpertArgs& a, hipStream_t s) {
+  constexpr int kPer = GLU ? 2 : 1;
+  const int64_t results = FORM == kForward ? a.N : a.K;
+  Kernel kernel = product_kernel(a, FORM, results * kPer, GLU);
+  unsigned grid = 0;
+  // (a call of more tiles than a launch takes goes to workgroups that stay)
+  if ((kernel == kByRows && !grid_of(a, 16, (results + 15) / 16, &grid)) ||
+      (kernel == kSplit && !grid_of(a, SplitShape::MT, (results * kPer + SplitShape::QT - 1) / SplitShape::QT, &grid)))
+    kernel = kTiles32;
+  if constexpr (FORM == kForward) {
+    if (kernel == kByRows) {
+      KernelTimer timer("expert_rows", s);
+      expert_rows_kernel<GLU><<<grid, 64 * kRowWaves, 0, s>>>(a);
+      BITSMOE_LAUNCH_CHECK("expert_rows_kernel");
+      return ok();
+    }
+  }
+  switch (kernel) {
+    case kSplit:
+      return split<FORM, GLU>(a, grid, s);
+    case kTiles32:
+      return tiles<FORM, 32, GLU>(a, s);
+    case kTiles128:
+      return tiles<FORM, 128, GLU>(a, s);
+    default:
+      return tiles<FORM, 256, GLU>(a, s);
+  }
+}
+
 int clip(int64_t E) { return static_cast<int>(E < 0x7FFFFFFF ? E : 0x7FFFFFFF); }
 
-bitsmoe_status weight_grad(const char* who, const ExpertArgs& a, hipStream_t s) {
-  const int64_t tiles = (a.N + 63) / 64 * ((a.K + 63) / 64);
-  if (tiles > ((int64_t(1) << 23) - 1) / a.E) return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": too many weights");
-  auto* fn = a.xcodes ? expert_simple_kernel<kWeights, true, false> : expert_simple_kernel<kWeights, false, false>;
-  fn<<<static_cast<unsigned>(tiles * a.E), kThreads, 0, s>>>(a);
-  BITSMOE_LAUNCH_CHECK("expert_simple_kernel");
+// The weights' gradient from its parts' sums, in their order.
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void expert_join_kernel(const float* part, int parts, int64_t n, void* y) {
+  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < n; i += int64_t(gridDim.x) * kThreads) {
+    Eight<BF16> sum;
+    Eight<false> v;
+    v.load(part, i);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) sum.v[q] = v.v[q];
+    for (int p = 1; p < parts; ++p) {
+      v.load(part + p * n * 8, i);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) sum.v[q] += v.v[q];
+    }
+    sum.store(y, i);
+  }
+}
+
+// Parts of the weights' gradient's sum: where its tiles are too few to fill the card, as many as do, but of four
+// stages at least, and with at most 64 MB of sums.
+int weight_parts(int64_t E, int64_t N, int64_t K, int64_t S) {
+  const int64_t tiles = E * ((N + 255) / 256) * ((K + 255) / 256), cus = device_cus();
+  if (tiles * 2 > cus) return 1;
+  const int64_t fill = cus / tiles, stages = S / (64 * E) / 4, room = (int64_t(64) << 20) / (E * N * K * 4);
+  const int64_t parts = fill < stages ? fill : stages;
+  return static_cast<int>(parts < room ? (parts < 1 ? 1 : parts) : room < 1 ? 1 : room);
+}
+
+bitsmoe_status weight_grad(const char* who, ExpertArgs a, void* work, int64_t work_bytes, hipStream_t s) {
+  const int64_t tiles_ = (a.N + 255) / 256 * ((a.K + 255) / 256);
+  if (tiles_ > (int64_t(1) << 40) / a.E) return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": too many weights");
+  if (!aligned16({work}))
+    return fail(BITSMOE_ERR_ARG, std::string(who) + ": device pointers must be 16-byte aligned");
+  const int parts = work ? weight_parts(a.E, a.N, a.K, a.S) : 1;
+  void* const y = a.y;
+  const bool bf16 = !a.yf32;
+  if (parts > 1) {
+    if (work_bytes < parts * a.E * a.N * a.K * 4)
+      return fail(BITSMOE_ERR_ARG, std::string(who) + ": the workspace is too small");
+    a.parts = parts;
+    a.y = work;
+    a.yf32 = 1;
+  }
+  if (bitsmoe_status st = a.xcodes ? tiles<kWeights, 256, false, true>(a, s) : tiles<kWeights, 256>(a, s)) return st;
+  if (parts > 1) {
+    const int64_t n = a.E * a.N * a.K / 8, blocks = (n + kThreads - 1) / kThreads;
+    auto* fn = bf16 ? expert_join_kernel<true> : expert_join_kernel<false>;
+    fn<<<static_cast<unsigned>(blocks < 4096 ? blocks : 4096), kThreads, 0, s>>>(static_cast<const float*>(work), parts, n,
+                                                                                 y);
+    BITSMOE_LAUNCH_CHECK("expert_join_kernel");
+  }
   return ok();
 }
 
@@ -199,20 +1062,19 @@ extern "C" bitsmoe_status bitsmoe_expert_product(const void* W_dev, bitsmoe_dtyp
                                                  const void* X_dev, int64_t x_rows, int64_t ldx,
                                                  const int32_t* offsets_dev, const int32_t* rows_dev, int64_t S,
                                                  int glu, void* Y_dev, bitsmoe_dtype yt, int64_t ldy, void* stream) {
-  const ExpertArgs a{static_cast<const uint16_t*>(W_dev), clip(E), N, K, static_cast<const uint16_t*>(X_dev),
+  ExpertArgs a{static_cast<const uint16_t*>(W_dev), clip(E), N, K, static_cast<const uint16_t*>(X_dev),
                      nullptr, nullptr, x_rows, ldx, nullptr, 0, offsets_dev, rows_dev, S, Y_dev, ldy,
-                     yt == BITSMOE_F32};
+                     yt == BITSMOE_F32, 1};
   if (bitsmoe_status st = check("expert_product", a, t, yt, N)) return st;
   if (bitsmoe_status st = check_stride("expert_product", K, ldx)) return st;
   if (S == 0) return ok();
   if (!W_dev || !Y_dev || (x_rows > 0 && !X_dev)) return fail(BITSMOE_ERR_ARG, "expert_product: null pointer");
-  unsigned grid;
-  if (!grid_of(a, 64, (N + 63) / 64, &grid))
-    return fail(BITSMOE_ERR_SHAPE, "expert_product: too many slots and outputs for one call");
-  auto* fn = glu ? expert_simple_kernel<kForward, false, true> : expert_simple_kernel<kForward, false, false>;
-  fn<<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
-  BITSMOE_LAUNCH_CHECK("expert_simple_kernel");
-  return ok();
+  if (x_rows == 0) {  // (the kernels read a first row for slots whose own does not exist, and give them 0)
+    a.x = a.w;
+    a.ldx = 0;
+  }
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  return glu ? product<kForward, true>(a, s) : product<kForward, false>(a, s);
 }
 
 extern "C" bitsmoe_status bitsmoe_expert_product_grad(const void* W_dev, bitsmoe_dtype t, int64_t E, int64_t N,
@@ -221,49 +1083,52 @@ extern "C" bitsmoe_status bitsmoe_expert_product_grad(const void* W_dev, bitsmoe
                                                       bitsmoe_dtype xt, int64_t ldx, void* stream) {
   const ExpertArgs a{static_cast<const uint16_t*>(W_dev), clip(E), N, K, nullptr, nullptr, nullptr, S, 0,
                      static_cast<const uint16_t*>(dY_dev), lddy, offsets_dev, nullptr, S, dX_dev, ldx,
-                     xt == BITSMOE_F32};
+                     xt == BITSMOE_F32, 1};
   if (bitsmoe_status st = check("expert_product_grad", a, t, xt, K)) return st;
   if (N % 8 != 0) return fail(BITSMOE_ERR_SHAPE, "expert_product_grad: needs N % 8 == 0");
   if (bitsmoe_status st = check_stride("expert_product_grad", N, lddy)) return st;
   if (S == 0) return ok();
   if (!W_dev || !dY_dev || !dX_dev) return fail(BITSMOE_ERR_ARG, "expert_product_grad: null pointer");
-  unsigned grid;
-  if (!grid_of(a, 64, (K + 63) / 64, &grid))
-    return fail(BITSMOE_ERR_SHAPE, "expert_product_grad: too many slots and columns for one call");
-  expert_simple_kernel<kTokens, false, false><<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(a);
-  BITSMOE_LAUNCH_CHECK("expert_simple_kernel");
-  return ok();
+  return product<kTokens, false>(a, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int64_t bitsmoe_expert_weight_grad_workspace(int64_t E, int64_t N, int64_t K, int64_t S) {
+  if (E <= 0 || N <= 0 || K <= 0 || S <= 0 || E > 65535 || N > (1 << 24) || K > (1 << 24)) return 0;
+  const int parts = weight_parts(E, N, K, S);
+  return parts > 1 ? parts * E * N * K * 4 : 0;
 }
 
 extern "C" bitsmoe_status bitsmoe_expert_weight_grad(const void* dY_dev, bitsmoe_dtype t, int64_t lddy, int64_t E,
                                                      int64_t N, int64_t K, const void* X_dev, int64_t x_rows,
                                                      int64_t ldx, const int32_t* offsets_dev, const int32_t* rows_dev,
-                                                     int64_t S, void* dW_dev, bitsmoe_dtype wt, void* stream) {
+                                                     int64_t S, void* dW_dev, bitsmoe_dtype wt, void* work_dev,
+                                                     int64_t work_bytes, void* stream) {
   const ExpertArgs a{nullptr, clip(E), N, K, static_cast<const uint16_t*>(X_dev), nullptr, nullptr, x_rows, ldx,
                      static_cast<const uint16_t*>(dY_dev), lddy, offsets_dev, rows_dev, S, dW_dev, K,
-                     wt == BITSMOE_F32};
+                     wt == BITSMOE_F32, 1};
   if (bitsmoe_status st = check("expert_weight_grad", a, t, wt, K)) return st;
   if (N % 8 != 0) return fail(BITSMOE_ERR_SHAPE, "expert_weight_grad: needs N % 8 == 0");
   if (bitsmoe_status st = check_stride("expert_weight_grad", N, lddy)) return st;
   if (bitsmoe_status st = check_stride("expert_weight_grad", K, ldx)) return st;
   if (!dW_dev || (S > 0 && (!dY_dev || (x_rows > 0 && !X_dev))))
     return fail(BITSMOE_ERR_ARG, "expert_weight_grad: null pointer");
-  return weight_grad("expert_weight_grad", a, static_cast<hipStream_t>(stream));
+  return weight_grad("expert_weight_grad", a, work_dev, work_bytes, static_cast<hipStream_t>(stream));
 }
 
 extern "C" bitsmoe_status bitsmoe_expert_weight_grad_q(const void* dY_dev, bitsmoe_dtype t, int64_t lddy, int64_t E,
                                                        int64_t N, int64_t K, const uint8_t* xcodes_dev,
                                                        const uint8_t* xscales_dev, int64_t x_rows,
                                                        const int32_t* offsets_dev, const int32_t* rows_dev, int64_t S,
-                                                       void* dW_dev, bitsmoe_dtype wt, void* stream) {
+                                                       void* dW_dev, bitsmoe_dtype wt, void* work_dev, int64_t work_bytes,
+                                                       void* stream) {
   const ExpertArgs a{nullptr, clip(E), N, K, nullptr, xcodes_dev, xscales_dev, x_rows, K,
                      static_cast<const uint16_t*>(dY_dev), lddy, offsets_dev, rows_dev, S, dW_dev, K,
-                     wt == BITSMOE_F32};
+                     wt == BITSMOE_F32, 1};
   if (bitsmoe_status st = check("expert_weight_grad_q", a, t, wt, K)) return st;
   if (N % 8 != 0 || K % kMx8Block != 0)
     return fail(BITSMOE_ERR_SHAPE, "expert_weight_grad_q: needs N % 8 == 0 and K % 32 == 0");
   if (bitsmoe_status st = check_stride("expert_weight_grad_q", N, lddy)) return st;
   if (!dW_dev || (S > 0 && (!dY_dev || (x_rows > 0 && (!xcodes_dev || !xscales_dev)))))
     return fail(BITSMOE_ERR_ARG, "expert_weight_grad_q: null pointer");
-  return weight_grad("expert_weight_grad_q", a, static_cast<hipStream_t>(stream));
+  return weight_grad("expert_weight_grad_q", a, work_dev, work_bytes, static_cast<hipStream_t>(stream));
 }

@@ -131,12 +131,13 @@ def test_expert_product_grad(lib, status, change):
 
 
 WEIGHT = dict(dY=P, t=BF16, lddy=16, E=2, N=16, K=64, X=P, x_rows=4, ldx=64, offsets=P, rows=P, S=8, dW=P, wt=F32,
-              stream=None)
+              work=None, work_bytes=0, stream=None)
 WEIGHT_Q = dict(dY=P, t=BF16, lddy=16, E=2, N=16, K=64, xcodes=P, xscales=P, x_rows=4, offsets=P, rows=P, S=8, dW=P,
-                wt=F32, stream=None)
+                wt=F32, work=None, work_bytes=0, stream=None)
 OURS = [b for b in BOTH if "W" not in b[1]] + [
     (ARG, {"dY": None}), (ARG, {"dW": None}), (ARG, {"dW": None, "S": 0}), (ARG, {"rows": BAD}), (DTYPE, {"wt": 4}),
-    (SHAPE, {"N": 12}), (SHAPE, {"lddy": 8}), (SHAPE, {"rows": None}),
+    (SHAPE, {"N": 12}), (SHAPE, {"lddy": 8}), (SHAPE, {"rows": None}), (SHAPE, {"lddy": 1 << 31}),
+    (ARG, {"S": 4096, "E": 1, "work": P, "work_bytes": 4096}), (ARG, {"work": BAD, "work_bytes": 1 << 40}),
 ]
 
 
@@ -148,6 +149,13 @@ def test_expert_weight_grad(lib, status, change):
 @pytest.mark.parametrize("status,change", OURS + [(ARG, {"xcodes": None}), (ARG, {"xscales": BAD}), (SHAPE, {"K": 40})])
 def test_expert_weight_grad_q(lib, status, change):
     refused(lib, status, "bitsmoe_expert_weight_grad_q", *{**WEIGHT_Q, **change}.values())
+
+
+def test_expert_weight_grad_workspace(lib):
+    size = lib.bitsmoe_expert_weight_grad_workspace
+    assert size(128, 1536, 2048, 32768) == size(1, 128, 2048, 0) == size(0, 8, 8, 8) == size(1, 8, 8, 100) == 0
+    assert size(1, 128, 2048, 4096) % (128 * 2048 * 4) == 0 and size(1, 128, 2048, 4096) > 128 * 2048 * 4
+    assert size(1, 128, 2048, 1 << 30) <= 64 << 20
 
 
 def test_nothing_to_do(lib):

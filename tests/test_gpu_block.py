@@ -463,6 +463,25 @@ def test_nan_and_infinite_tokens_stay_in_their_slots():
     assert bad[0, :, 3].all() and bad[1, :, 5].all() and bad.sum() == 128
 
 
+def test_weights_gradient_of_mx8_rows_of_any_scale():
+    """Rows of scales 2^-100 .. 2^100, zeros, and blocks that stand for NaN."""
+    g = np.random.default_rng(9)
+    E, N, K, S = 3, 64, 320, 150
+    x = g.standard_normal((S, K)) * 2.0 ** g.integers(-100, 100, (S, 1))
+    x[5], x[60, 64:96], x[100, 3] = 0, 0, np.inf
+    kept = bm.mx8_quantize(dev(x.astype(np.float32)))
+    dY, offsets = randn(g, S, N), np.array([0, 50, 50, 150], np.int32)
+    got = np64(bm.expert_weight_grad_q(dY, *kept, offsets=dev(offsets), dtype=torch.float32))
+    x64 = np64(bm.mx8_dequantize(*kept, dtype=torch.float32))
+    assert np.isnan(got[2][:, :32]).all() and np.isnan(x64[100, :32]).all()
+    x64[100, :32] = 0
+    want = block.weight_grad(np64(dY), x64, E, offsets)
+    bound = 158 * U * block.weight_grad(np.abs(np64(dY)), np.abs(x64), E, offsets)
+    ok = np.ones(got.shape, bool)
+    ok[2][:, :32] = False
+    within(got[ok], want[ok], bound[ok], "weights")
+
+
 def test_products_refuse():
     W, X = torch.zeros((2, 16, 32), dtype=torch.bfloat16, device=DEV), torch.zeros((4, 32), dtype=torch.bfloat16, device=DEV)
     o = torch.tensor([0, 2, 4], dtype=torch.int32, device=DEV)
@@ -626,3 +645,97 @@ def test_other_streams_and_captured_steps():
         for (held, graph, out), ref in zip(graphs, want):
             for a, b in zip(out, ref):
                 assert torch.equal(a, b)
+
+
+# ------------------------------------------------------- every kernel of the products
+def by_experts(f, offsets, S):
+    """f(e, slots) for every expert's slots, joined in their order (fp64 on the device)."""
+    o = np.clip(offsets, 0, S)
+    return [f(e, slice(int(o[e]), int(o[e + 1]))) for e in range(len(o) - 1)]
+
+
+@pytest.mark.parametrize("kernel,form,E,N,K,S", [
+    ("expert_rows", "product", 16, 72, 520, 9), ("expert_rows", "glu", 5, 300, 1032, 30),
+    ("expert_split", "product", 2, 1032, 4104, 150), ("expert_split", "glu", 2, 520, 4104, 150),
+    ("expert_split", "grad", 3, 264, 776, 100), ("expert_tile_32", "product", 1, 6568, 136, 276),
+    ("expert_tile_32", "glu", 1, 3304, 136, 276), ("expert_tile_32", "grad", 8, 1032, 4104, 200),
+    ("expert_tile_128", "product", 5, 104, 328, 20000), ("expert_tile_128", "glu", 5, 56, 328, 20000),
+    ("expert_tile_128", "grad", 3, 648, 1832, 3000), ("expert_tile_256", "product", 12, 840, 840, 33000),
+    ("expert_tile_256", "glu", 12, 424, 840, 33000), ("expert_tile_256", "grad", 55, 152, 104, 39000),
+    ("expert_weights", "weights", 5, 520, 776, 3000), ("expert_weights", "mx8", 5, 520, 800, 3000),
+    ("expert_weights", "weights", 300, 264, 328, 2000), ("expert_weights", "mx8", 300, 264, 320, 2000),
+    ("expert_weights", "weights", 1, 136, 520, 5000), ("expert_weights", "mx8", 1, 136, 544, 5000),
+])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_every_kernel(kernel, form, E, N, K, S, out):
+    """Sizes that each kernel takes, with several tiles a workgroup, tiles that end inside, empty experts, slots of
+    no expert and rows that do not exist."""
+    g = np.random.default_rng([E, N, K, S])
+    head, tail = (3, 5) if S > 100 else (0, 1)
+    offsets = slots_for(g, S, E, head, tail, empty=(1,) if E > 2 else ())
+    x_rows = S // 2 + 1
+    rows = g.integers(0, x_rows, S).astype(np.int32)
+    rows[::37] = x_rows + 5
+    o, r = dev(offsets), dev(rows)
+    there = torch.from_numpy((rows < x_rows)).to(DEV)
+    wide = 2 * N if form == "glu" else N
+    W = (torch.randn((E, wide, K), generator=torch.Generator(DEV).manual_seed(S), device=DEV) / K ** 0.5).bfloat16()
+    X, dY = randn(g, x_rows, K), randn(g, S, N)
+    x64 = X.double()[r.long().clamp(max=x_rows - 1)] * there[:, None]
+    codes, scales = bm.mx8_quantize(X) if form == "mx8" else (None, None)
+    dt, half = DT[out], HALF[out]
+    bm.timing(True, kernel)
+    if form in ("product", "glu"):
+        got = bm.expert_product(W, X, offsets=o, rows=r, glu=form == "glu", dtype=dt)
+    elif form == "grad":
+        got = bm.expert_product_grad(W, dY, offsets=o, dtype=dt)
+    elif form == "weights":
+        got = bm.expert_weight_grad(dY, X, offsets=o, rows=r, dtype=dt)
+    else:
+        got = bm.expert_weight_grad_q(dY, codes, scales, offsets=o, rows=r, dtype=dt)
+    bm.timing(False)
+    assert bm.kernel_time(kernel)[1] == 1
+    w64, y64 = W.double(), dY.double()
+    if form in ("product", "glu"):
+        a, b, L = x64, w64.transpose(1, 2), K
+    elif form == "grad":
+        a, b, L = y64, w64, N
+    if form in ("weights", "mx8"):
+        if form == "mx8":
+            x64 = bm.mx8_dequantize(codes, scales, dtype=torch.float32).double()[r.long().clamp(max=x_rows - 1)] * there[:, None]
+        y64 = y64 * there[:, None]
+        want = torch.stack(by_experts(lambda e, s: y64[s].T @ x64[s], offsets, S))
+        mag = torch.stack(by_experts(lambda e, s: y64[s].abs().T @ x64[s].abs(), offsets, S))
+        counts = torch.from_numpy(np.diff(np.clip(offsets, 0, S)) + 8).to(DEV)[:, None, None]
+        bound = counts * U * mag
+    else:
+        want = torch.zeros((S, b.shape[2]), dtype=torch.float64, device=DEV)
+        mag = torch.zeros_like(want)
+        want[head:S - tail] = torch.cat(by_experts(lambda e, s: a[s] @ b[e], offsets, S))
+        mag[head:S - tail] = torch.cat(by_experts(lambda e, s: a[s].abs() @ b[e].abs(), offsets, S))
+        bound = (L + 8) * U * mag
+        if form == "glu":
+            gate, up, eg, eu = want[:, :N], want[:, N:], bound[:, :N], bound[:, N:]
+            sg = gate * torch.sigmoid(gate)
+            want, bound = sg * up, 1.1 * eg * (up.abs() + eu) + sg.abs() * (eu + 2.0 ** -18 * up.abs())
+    off = (got.double() - want).abs() - (bound + (want.abs() + bound) * half)
+    assert got.dtype == dt and not (off > 0).any(), (float(off.max()), int((off > 0).sum()))
+
+
+@pytest.mark.parametrize("E,N,K,S", [(1, 264, 1032, 33), (2, 256, 1024, 100), (40, 512, 512, 4000)])
+def test_products_give_the_same_every_time(E, N, K, S):
+    """Whatever the timing of the loads: each call after the card has gone idle, and in a row."""
+    g = np.random.default_rng(S)
+    W, X, dY, o = randn(g, E, N, K), randn(g, S, K), randn(g, S, N), dev(slots_for(g, S, E))
+    q = bm.mx8_quantize(X) if K % 32 == 0 else None
+
+    def all_of_them():
+        return [bm.expert_product(W, X, offsets=o), bm.expert_product_grad(W, dY, offsets=o),
+                bm.expert_weight_grad(dY, X, offsets=o)] + ([bm.expert_weight_grad_q(dY, *q, offsets=o)] if q else [])
+
+    first = all_of_them()
+    for i in range(150):
+        if i % 2:
+            torch.cuda.synchronize()
+        for a, b in zip(all_of_them(), first):
+            assert torch.equal(a, b)
