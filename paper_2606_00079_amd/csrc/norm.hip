@@ -132,36 +132,53 @@ struct NormGradArgs {
 };
 
 // A row on L threads as above; each workgroup takes every gridDim.x-th (group of)
-// row and keeps its columns' sums of dw in registers.
+// row and keeps its columns' sums of dw in registers.  The next row is on its way while
+// this one is summed.
 template <bool XB, bool WB, int L, int PER>
 __global__ __launch_bounds__(L > kThreads ? L : kThreads) void norm_grad_kernel(NormGradArgs a) {
   constexpr int kRows = L == 64 ? kThreads / 64 : 1;
-  __shared__ float part[L / 64];
+  __shared__ float part[2][L / 64];
   const int t = L == 64 ? threadIdx.x & 63 : threadIdx.x;
   float dw[PER][8];
 #pragma unroll
   for (int i = 0; i < PER; ++i)
 #pragma unroll
     for (int q = 0; q < 8; ++q) dw[i][q] = 0.0f;
-  for (int64_t row = int64_t(blockIdx.x) * kRows + (L == 64 ? threadIdx.x >> 6 : 0); row < a.T;
-       row += int64_t(gridDim.x) * kRows) {
-    Eight<XB> v[PER], g[PER];
+  struct Row {
+    RawEight<XB> v[PER], g[PER], s[PER];
+    float inv;
+  };
+  auto load = [&](Row& r, int64_t row) {
     const char* vp = static_cast<const char*>(a.v) + row * a.ldv * Eight<XB>::kBytes;
     const char* gp = static_cast<const char*>(a.dy) + row * a.lddy * Eight<XB>::kBytes;
     const char* sp = static_cast<const char*>(a.dsum) + row * a.ldds * Eight<XB>::kBytes;
-    const float inv = a.inv[row];
-    float dot = 0.0f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int c = i * L + t;
+      r.s[i].clear();
       if (c < a.pieces) {
-        v[i].load(vp, c);
-        g[i].load(gp, c);
+        r.v[i].load(vp, c);
+        r.g[i].load(gp, c);
+        if (a.dsum) r.s[i].load(sp, c);
       } else {
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v[i].v[q] = g[i].v[q] = 0.0f;
+        r.v[i].clear();
+        r.g[i].clear();
       }
     }
+    r.inv = a.inv[row];
+  };
+  constexpr bool kAhead = L < 1024;  // (of the longest rows registers hold but one)
+  const int64_t step = int64_t(gridDim.x) * kRows;
+  int64_t row = int64_t(blockIdx.x) * kRows + (L == 64 ? threadIdx.x >> 6 : 0);
+  Row cur, next;
+  if (kAhead && row < a.T) load(cur, row);
+  for (int turn = 0; row < a.T; row += step, turn ^= 1) {
+    if constexpr (kAhead) {
+      if (row + step < a.T) load(next, row + step);
+    } else {
+      load(cur, row);
+    }
+    float dot = 0.0f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int c = i * L + t;
@@ -170,27 +187,35 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void norm_grad_kernel(
       w.load(a.w, c);
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        v[i].v[q] *= inv;
-        dw[i][q] = fmaf(g[i].v[q], v[i].v[q], dw[i][q]);
-        g[i].v[q] *= w.v[q];
-        dot = fmaf(g[i].v[q], v[i].v[q], dot);
+        const float n = cur.v[i].value(q) * cur.inv, g = cur.g[i].value(q);
+        dw[i][q] = fmaf(g, n, dw[i][q]);
+        dot = fmaf(g * w.v[q], n, dot);
       }
     }
-    dot = row_sum<L>(dot, part) / a.d;
+    dot = wave_sum(dot);
+    if constexpr (L > 64) {
+      if ((threadIdx.x & 63) == 0) part[turn][threadIdx.x >> 6] = dot;
+      __syncthreads();  // (one a row: the row after next writes where this one's was)
+      dot = 0.0f;
+#pragma unroll
+      for (int i = 0; i < L / 64; ++i) dot += part[turn][i];
+    }
+    dot /= a.d;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int c = i * L + t;
       if (c >= a.pieces) continue;
+      Eight<WB> w;
+      w.load(a.w, c);
+      Eight<XB> dx;
 #pragma unroll
-      for (int q = 0; q < 8; ++q) g[i].v[q] = inv * (g[i].v[q] - v[i].v[q] * dot);
-      if (a.dsum) {
-        Eight<XB> s;
-        s.load(sp, c);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) g[i].v[q] += s.v[q];
+      for (int q = 0; q < 8; ++q) {
+        const float n = cur.v[i].value(q) * cur.inv;
+        dx.v[q] = cur.inv * (cur.g[i].value(q) * w.v[q] - n * dot) + cur.s[i].value(q);
       }
-      g[i].store(a.dx, row * a.pieces + c);
+      dx.store(a.dx, row * a.pieces + c);
     }
+    if constexpr (kAhead) cur = next;
   }
   if (!a.dw) return;
   if constexpr (L == 64) {  // the four waves' sums, in the order of the waves
@@ -231,7 +256,13 @@ __global__ __launch_bounds__(64 * kJoin) void norm_join_kernel(const float* part
   const int64_t c = int64_t(blockIdx.x) * 64 + lane;
   float s = 0.0f;
   if (c < d)
-    for (int r = wave; r < rows; r += kJoin) s += part[r * d + c];
+    for (int r = wave; r < rows; r += 8 * kJoin) {  // eight loads under way
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = r + u * kJoin < rows ? part[(r + u * kJoin) * d + c] : 0.0f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += v[u];
+    }
   sums[wave][lane] = s;
   __syncthreads();
   if (wave > 0 || c >= d) return;
@@ -254,7 +285,7 @@ void by_length(int pieces, F f) {
   else if (pieces <= 1024)
     f.template operator()<256, 4>();
   else if (pieces <= 2048)
-    f.template operator()<1024, 2>();
+    f.template operator()<512, 4>();
   else
     f.template operator()<1024, 4>();
 }

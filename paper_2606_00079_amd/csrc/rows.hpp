@@ -48,4 +48,28 @@ struct Eight {
   }
 };
 
+// The same as they lie in memory: what is on its way for the next row takes half the
+// registers in bf16.
+template <bool BF16>
+struct RawEight {
+  uint4 u[BF16 ? 1 : 2];
+  __device__ __forceinline__ void load(const void* row, int64_t i) {
+#pragma unroll
+    for (int q = 0; q < (BF16 ? 1 : 2); ++q) u[q] = static_cast<const uint4*>(row)[i * (BF16 ? 1 : 2) + q];
+  }
+  __device__ __forceinline__ float value(int q) const {
+    if constexpr (BF16) {
+      const uint32_t d = q < 2 ? u[0].x : q < 4 ? u[0].y : q < 6 ? u[0].z : u[0].w;
+      return __uint_as_float(q & 1 ? d & 0xFFFF0000u : d << 16);
+    } else {
+      const uint4 w = u[q >> 2];
+      return __uint_as_float((q & 3) == 0 ? w.x : (q & 3) == 1 ? w.y : (q & 3) == 2 ? w.z : w.w);
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int q = 0; q < (BF16 ? 1 : 2); ++q) u[q] = make_uint4(0, 0, 0, 0);
+  }
+};
+
 }  // namespace bitsmoe
