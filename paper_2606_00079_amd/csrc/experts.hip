@@ -366,22 +366,23 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
                    base + H::kPStage + (wave * H::LQ + q) * 1024);
       }
     } else {
-      const int rem = (FORM == kForward ? K : N) - step * H::KS;  // entries from this stage on
-      const char* p = of_p ? pp[q] : pq[q];
-      if (rem < H::KS) {
-        asm volatile("");  // (a branch, not selects at every step)
-        if (of_p || FORM == kForward)
-          p = 8 * chunk < rem ? p : zero;
-        else
-          p = (wave + H::kWaves * q) * 2 + half < rem ? p : zero;
-      }
-      load_lds16(p, base + (of_p ? 0 : H::kPStage) + (wave + H::kWaves * q) * 1024);
+      load_lds16(of_p ? pp[q] : pq[q], base + (of_p ? 0 : H::kPStage) + (wave + H::kWaves * q) * 1024);
       if (of_p)
         pp[q] += H::KS * 2;
       else
         pq[q] += FORM == kForward ? H::KS * 2 : H::KS * 2 * a.K;
     }
   };
+  // Before the loads of a stage in which the sum ends, or past its end: zeros from there on.
+  auto cut = [&](int rem) __attribute__((always_inline)) {
+    if (FORM == kWeights || rem >= H::KS) return;
+#pragma unroll
+    for (int q = 0; q < H::LP; ++q) pp[q] = 8 * chunk < rem ? pp[q] : zero;
+#pragma unroll
+    for (int q = 0; q < H::LQ; ++q)
+      pq[q] = (FORM == kForward ? 8 * chunk : (wave + H::kWaves * q) * 2 + half) < rem ? pq[q] : zero;
+  };
+  auto entries_left = [&]() __attribute__((always_inline)) { return (FORM == kForward ? K : N) - step * H::KS; };
   auto loaded = [&]() __attribute__((always_inline)) {
     ++step;
     to = to + 1 == H::NX ? 0 : to + 1;
@@ -446,8 +447,15 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
   };
   auto turn = [&]() __attribute__((always_inline)) {  // to the next tile if the loads are through with theirs
     const int over = step == steps_to;
-    dry = over && !more;
-    if (dry) return;
+    dry |= over && !more;
+    if (dry) {  // (zeros: so waits go by count to the end)
+      if constexpr (FORM == kWeights) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) row[q] = -1;
+      }
+      cut(0);
+      return;
+    }
     if (over) {
       // (the next tile's rows have landed if as many steps as the ring has stages waited since they were asked for)
       if (FORM == kForward && a.rows && since < H::NX) wait_loads<0>();
@@ -457,6 +465,7 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
       ld = next;
       head = after(head);
     }
+    cut(entries_left());
     if constexpr (FORM == kWeights) {
       take_rows();
       // (entering a list: the one after it)
@@ -468,8 +477,7 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
   struct Part {
     bf16x8 p[H::MB], q[H::NB];
   };
-  // Blocks of 32 rows of P go to the wm waves in turn, so that what an expert's last slots leave empty is shared out.
-  auto prow = [&](int m) __attribute__((always_inline)) { return (m * H::WM + wm) * 32; };
+  auto prow = [&](int m) __attribute__((always_inline)) { return (wm * H::MB + m) * 32; };
   const int qrow = wn * 64;
   auto by_rows = [&](const char* st, int row0, int j) __attribute__((always_inline)) {
     const int r = row0 + r32;
@@ -510,25 +518,18 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
   };
-  // This wave's blocks of a tile that hold results.
-  auto blocks_of = [&](const ResultTile& t) __attribute__((always_inline)) {
-    const int blocks = (min((FORM == kWeights ? N : t.hi) - t.m0, MT) + 31) / 32;
-    const bool cols = t.n0 + (GLU ? wn * 32 : qrow) < width;
-    return cols ? (blocks - wm + H::WM - 1) / H::WM : 0;
-  };
-  int blocks = 0;
   // The ops of a part, with the reads of the parts of `reads` and `between(m)` after a block's ops.
+  // (What an expert's last slots leave of a tile empty is multiplied all the same: a branch around each block's ops
+  // took a tenth of a full tile's time, and gave 2 % where half of the tiles are part empty.)
   auto multiply = [&](const Part& f, const char* st, int tile, auto between, auto... reads) __attribute__((always_inline)) {
 #pragma unroll
     for (int m = 0; m < H::MB; ++m) {
-      if (m < blocks) {
 #pragma unroll
-        for (int n = 0; n < H::NB; ++n) {
-          acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.q[n], f.p[m], acc[n][m], 0, 0, 0);
-          if (m == 0 && n == 0) (read_q(*reads.first, reads.second, st, tile), ...);
-          if (n == H::NB - 1) (read_p(*reads.first, m, reads.second, st), ...);
-          __builtin_amdgcn_sched_barrier(0);
-        }
+      for (int n = 0; n < H::NB; ++n) {
+        acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.q[n], f.p[m], acc[n][m], 0, 0, 0);
+        if (m == 0 && n == 0) (read_q(*reads.first, reads.second, st, tile), ...);
+        if (n == H::NB - 1) (read_p(*reads.first, m, reads.second, st), ...);
+        __builtin_amdgcn_sched_barrier(0);
       }
       between(m);
       __builtin_amdgcn_sched_barrier(0);
@@ -555,6 +556,7 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
   }
 #pragma unroll
   for (int i = 0; i < H::NX; ++i) {
+    cut(entries_left());
     if constexpr (FORM == kWeights) take_rows();
     if constexpr (MX) {
       issue_codes();
@@ -604,71 +606,46 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
   };
   for (;;) {
     const int steps = steps_of(cur);
-    blocks = blocks_of(cur);
     for (int i = 0; i < steps; ++i) {
       const int last = i + 1 == steps, rest = pending;
-      if (FORM == kWeights && i * H::KS >= cur.hi - cur.lo) blocks = 0;  // (a stage of no slots)
-      if constexpr (FORM == kWeights) {
-        // (No registers are left for reading a stage to its end earlier.)
-        multiply(f0, st, tile, [&](int m) __attribute__((always_inline)) {
-          if (rest) loads(H::kSecond, H::kLoads, m);
-        }, std::pair{&f1, 1});
-        if (rest) loaded();
-        if constexpr (MX) {
-          // the next stage's codes are there but for what was asked for later, P of that stage
-          if (i > 0 || !stored)
-            wait_own(std::integral_constant<int, H::kLoads>{});
-          else if (a.yf32)
-            wait_own(std::integral_constant<int, H::kLoads + kStores32>{});
-          else
-            wait_own(std::integral_constant<int, H::kLoads + kStores16>{});
-        }
-        turn();
-        multiply(f1, st, tile, [&](int m) __attribute__((always_inline)) {
-          if (MX && m < 2) widen(m, tile ^ 1);
-        }, std::pair{&f0, 2});
-        multiply(f0, st, tile, [&](int m) __attribute__((always_inline)) {
-          if (MX && m < 2) widen(2 + m, tile ^ 1);
-        }, std::pair{&f1, 3});
-        // the next stage is whole, and every wave has read all of this one
-        if (dry)
-          wait_loads<0>();
+      // A stage is read to its end half a step early, and its place loaded again while the other half and the next
+      // step's first part are multiplied: all at once the loads would hold up the ops behind them.
+      multiply(f0, st, tile, [&](int m) __attribute__((always_inline)) {
+        if (rest) loads(H::kSecond, H::kLoads, m);
+      }, std::pair{&f1, 1});
+      if (rest) loaded();
+      if constexpr (MX) {
+        // the next stage's codes are there but for what was asked for later, two thirds of P of that stage
+        constexpr int kLater = H::kLoads - H::kFirst;
+        if (i > 0 || !stored)
+          wait_own(std::integral_constant<int, kLater>{});
+        else if (a.yf32)
+          wait_own(std::integral_constant<int, kLater + kStores32>{});
         else
-          wait_step(std::integral_constant<int, 0>{}, i == 0);
-        if constexpr (MX)
-          if (!dry) issue_codes();  // (in the place of those that are widened)
-      } else {
-        // A stage is read to its end half a step early, and its place loaded again while the other half and the next
-        // step's first part are multiplied: all at once the loads would hold up the ops behind them.
-        multiply(f0, st, tile, [&](int m) __attribute__((always_inline)) {
-          if (rest) loads(H::kSecond, H::kLoads, m);
-        }, std::pair{&f1, 1});
-        if (rest) loaded();
-        turn();
-        const int go = !dry;
-        multiply(f1, st, tile, nothing, std::pair{&f0, 2}, std::pair{&f2, 3});
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        multiply(f0, st, tile, [&](int m) __attribute__((always_inline)) {
-          if (go) loads(0, H::kFirst, m);
-        });
-        if (dry)
-          wait_loads<0>();
-        else
-          wait_step(std::integral_constant<int, (H::NX - 2) * H::kLoads + H::kFirst>{}, i < H::NX - 1);
-        ++since;
+          wait_own(std::integral_constant<int, kLater + kStores16>{});
       }
+      turn();
+      multiply(f1, st, tile, [&](int m) __attribute__((always_inline)) {
+        if (MX && m < 2) widen(m, tile ^ 1);
+      }, std::pair{&f0, 2}, std::pair{&f2, 3});
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      multiply(f0, st, tile, [&](int m) __attribute__((always_inline)) {
+        if (MX && m < 2) widen(2 + m, tile ^ 1);
+        loads(0, H::kFirst, m);
+      });
+      // the next stage is whole (but for what was asked for later)
+      wait_step(std::integral_constant<int, (H::NX - 2) * H::kLoads + H::kFirst>{}, i < H::NX - 1);
+      ++since;
+      if constexpr (MX) issue_codes();  // (in the place of those that are widened)
       tile ^= 1;
       st = st + H::kStage == smem + H::oRows ? smem : st + H::kStage;
-      const int go = !dry;
       // (what is read after a tile's last step is not used; its loads all go out before the results)
-      multiply(FORM == kWeights ? f1 : f2, st, tile, [&](int m) __attribute__((always_inline)) {
-        if (go) {
-          loads(FORM == kWeights ? 0 : H::kFirst, H::kSecond, m);
-          if (last) loads(H::kSecond, H::kLoads, m);
-        }
+      multiply(f2, st, tile, [&](int m) __attribute__((always_inline)) {
+        loads(H::kFirst, H::kSecond, m);
+        if (last) loads(H::kSecond, H::kLoads, m);
       }, std::pair{&f0, 0});
-      pending = go && !last;
-      if (go && last) loaded();
+      pending = !last;
+      if (last) loaded();
     }
     const int mend = FORM == kWeights ? N : cur.hi;
     const bool whole = cur.n0 + QTO <= width && a.ldy % 8 == 0;
@@ -699,7 +676,10 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
         store32(a, to_row, cur.n0 + (GLU ? wn * 32 : qrow + 32 * n), half, whole, width, v);
       }
     }
-    if (!more) return;
+    if (!more) {
+      wait_loads<0>();  // (LDS must not be written after the end)
+      return;
+    }
     stored = whole && cur.m0 + MT <= mend;
     cur = next;
     buf = after(buf);
