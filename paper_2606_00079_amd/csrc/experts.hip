@@ -144,8 +144,10 @@ struct Shape {
   static constexpr int oTiles = oRows, oCodes = oTiles + 2 * kQStage, kCodes = 8 * QT, oScales = oCodes + kWaves * kCodes;
   // weights: lists of the rows of a wave's eight slots of eight stages: the first of three tiles, two others
   static constexpr int oLists = MX ? oScales + kWaves * 8 * (QT / 32) * 4 : oRows, kLists = 5;
-  static constexpr int kBytes =
-      oLists + (FORM == kForward ? 3 * kRows * 4 : FORM == kWeights ? kWaves * kLists * 256 : 0);
+  // where a wave turns its results into whole rows of its columns (with MX8 its own rows of a widened tile)
+  static constexpr int oTurn = oLists + (FORM == kForward ? 3 * kRows * 4 : FORM == kWeights ? kWaves * kLists * 256 : 0);
+  static constexpr bool kTurn = MT == 256;
+  static constexpr int kBytes = oTurn + (kTurn && !MX ? kWaves * 2048 : 0);
   static_assert(kBytes <= 163840);
   static_assert(FORM != kWeights || (MT == 256 && NX == 2));
 
@@ -651,29 +653,98 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
     const bool whole = cur.n0 + QTO <= width && a.ldy % 8 == 0;
     const int r32 = opaque(tid) & 31, half = (opaque(tid) & 63) >> 5;
     if (more) read_first(f0, st, tile);
+    const int64_t first_row = FORM == kWeights ? (static_cast<int64_t>(cur.part) * a.E + cur.e) * a.N : 0;
+    auto exists = [&](int m) __attribute__((always_inline)) {  // the row of a forward result's slot
+      if (FORM != kForward || !a.rows) return true;
+      const int row = rowbuf[buf * H::kRows + prow(m) + r32];
+      return row >= 0 && row < a.x_rows;
+    };
+    if (H::kTurn && !GLU && whole) {
+      // A lane holds pieces of 16 bytes of one row; through LDS eight (16 in fp32: a quarter of the rows at a time, else
+      // half) lanes get those of a row, so that a store writes whole cache lines: 32 bytes of 32 rows a store took as long
+      // again (dW of 128 x 1536 x 2048: kTurnBefore).
+      const int lane = opaque(tid) & 63;
+      char* const turn_at = smem + (MX ? H::oTiles + (tile ^ 1) * H::kQStage + wave * 4096 : H::oTurn + wave * 2048);
 #pragma unroll
-    for (int m = 0; m < H::MB; ++m) {
-      const int at = cur.m0 + prow(m) + r32;
-      if (at >= mend) continue;
-      bool have = true;
-      if constexpr (FORM == kForward) {
-        if (a.rows) {
-          const int row = rowbuf[buf * H::kRows + prow(m) + r32];
-          have = row >= 0 && row < a.x_rows;
+      for (int m = 0; m < H::MB; ++m) {
+        const bool have = exists(m);
+        const int row0 = cur.m0 + prow(m);
+        if (a.yf32) {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            if ((r32 >> 3) == g) {
+#pragma unroll
+              for (int n = 0; n < H::NB; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  f32x4 v;
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) v[i] = have ? acc[n][m][4 * e + i] : 0.0f;
+                  *reinterpret_cast<f32x4*>(turn_at + (r32 & 7) * 256 + (((8 * n + 2 * e + half) ^ (r32 & 7)) << 4)) = v;
+                }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int r = 4 * i + lane / 16, row = row0 + 8 * g + r;
+              const f32x4 v = *reinterpret_cast<const f32x4*>(turn_at + r * 256 + (((lane & 15) ^ r) << 4));
+              if (row < mend)
+                *reinterpret_cast<f32x4*>(static_cast<float*>(a.y) + (first_row + row) * a.ldy + cur.n0 + qrow +
+                                          4 * (lane & 15)) = v;
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          }
+        } else {
+          uint4 v[H::NB][2];
+#pragma unroll
+          for (int n = 0; n < H::NB; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float u[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) u[i] = have ? acc[n][m][8 * e + i] : 0.0f;
+              v[n][e] = eight_in_a_row(u);
+            }
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            if ((r32 >> 4) == g) {
+#pragma unroll
+              for (int n = 0; n < H::NB; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                  *reinterpret_cast<uint4*>(turn_at + (r32 & 15) * 128 + (((4 * n + 2 * e + half) ^ (r32 & 7)) << 4)) =
+                      v[n][e];
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int r = 8 * i + lane / 8, row = row0 + 16 * g + r;
+              const uint4 w = *reinterpret_cast<const uint4*>(turn_at + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
+              if (row < mend)
+                *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.y) + (first_row + row) * a.ldy + cur.n0 + qrow +
+                                          8 * (lane & 7)) = w;
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          }
         }
       }
-      const int64_t to_row =
-          FORM == kWeights ? (static_cast<int64_t>(cur.part) * a.E + cur.e) * a.N + at : at;
+    } else {
 #pragma unroll
-      for (int n = 0; n < (GLU ? 1 : H::NB); ++n) {
-        float v[16];
+      for (int m = 0; m < H::MB; ++m) {
+        const int at = cur.m0 + prow(m) + r32;
+        if (at >= mend) continue;
+        const bool have = exists(m);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          v[i] = acc[n][m][i];
-          if constexpr (GLU) v[i] = silu(v[i]) * acc[1][m][i];
-          if (FORM == kForward && !have) v[i] = 0.0f;
+        for (int n = 0; n < (GLU ? 1 : H::NB); ++n) {
+          float v[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            v[i] = acc[n][m][i];
+            if constexpr (GLU) v[i] = silu(v[i]) * acc[1][m][i];
+            if (FORM == kForward && !have) v[i] = 0.0f;
+          }
+          store32(a, first_row + at, cur.n0 + (GLU ? wn * 32 : qrow + 32 * n), half, whole, width, v);
         }
-        store32(a, to_row, cur.n0 + (GLU ? wn * 32 : qrow + 32 * n), half, whole, width, v);
       }
     }
     if (!more) {
@@ -938,9 +1009,9 @@ Kernel product_kernel(const ExpertArgs& a, Form form, int64_t wide, bool glu) {
   const double chain = L * 0.001, each = tiles(16, 16) * (L * 5.3e-6 + 0.0023);
   const double cost[5] = {with_bytes(5.6 + (chain > each ? chain : each), 4.6),
                           with_bytes(1.6 + rounds(tiles(32, 64)) * (4.5 + L * 0.0024), 4.2),
-                          with_bytes(1.8 + rounds(tiles(32, 256)) * (4.0 + L * 0.0094), 5.0),
-                          with_bytes(rounds(tiles(128, 256)) * (6.0 + L * 0.0118), 5.0),
-                          with_bytes(rounds(tiles(256, 256)) * (6.2 + L * 0.0172), 5.0)};
+                          with_bytes(2.2 + rounds(tiles(32, 256)) * (4.0 + L * 0.0071), 5.0),
+                          with_bytes(rounds(tiles(128, 256)) * (6.3 + L * 0.0116), 5.0),
+                          with_bytes(rounds(tiles(256, 256)) * (7.0 + L * 0.0190), 5.0)};
   int best = form == kForward ? kByRows : kSplit;  // (there is no kernel by rows for W by its rows)
   for (int k = best + 1; k <= kTiles256; ++k)
     if (cost[k] < cost[best]) best = k;

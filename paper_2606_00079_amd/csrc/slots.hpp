@@ -183,6 +183,23 @@ __device__ __forceinline__ void store4(const A& a, int64_t s, int64_t n, int64_t
   }
 }
 
+// Eight results in a row as bf16, from two runs of four of a 32 x 32 accumulator: those at
+// 16 e + 4 half + i (i < 4) and 16 e + 8 + 4 half + i; the two half-waves exchange words, and
+// a lane gets those from 16 e + 8 half on.
+__device__ __forceinline__ uint4 eight_in_a_row(const float (&v)[8]) {
+  uint32_t w[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bf16x2 b = {static_cast<__bf16>(v[4 * i + 2 * h]), static_cast<__bf16>(v[4 * i + 2 * h + 1])};
+      w[i][h] = __builtin_bit_cast(uint32_t, b);
+    }
+  const auto x = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
+  const auto y = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+  return make_uint4(x[0], y[0], x[1], y[1]);
+}
+
 // A lane's part of the 32 results n .. n + 31 (of N) of slot s: v[i] is that of
 // n + 8 (i / 4) + 4 half + i % 4, as a 32 x 32 accumulator lies.
 template <class A>
@@ -200,22 +217,12 @@ __device__ __forceinline__ void store32(const A& a, int64_t s, int64_t n, int ha
     for (int e = 0; e < 4; ++e)
       *reinterpret_cast<f32x4*>(p + 8 * e) = f32x4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
   } else {
-    // the two half-waves exchange words, so that each has eight results in a row
     uint16_t* p = static_cast<uint16_t*>(a.y) + s * a.ldy + n + 8 * half;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      uint32_t w[2][2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int at = 8 * e + 4 * i + 2 * h;
-          const bf16x2 b = {static_cast<__bf16>(v[at]), static_cast<__bf16>(v[at + 1])};
-          w[i][h] = __builtin_bit_cast(uint32_t, b);
-        }
-      const auto x = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
-      const auto y = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
-      *reinterpret_cast<uint4*>(p + 16 * e) = make_uint4(x[0], y[0], x[1], y[1]);
+      const float u[8] = {v[8 * e],     v[8 * e + 1], v[8 * e + 2], v[8 * e + 3],
+                          v[8 * e + 4], v[8 * e + 5], v[8 * e + 6], v[8 * e + 7]};
+      *reinterpret_cast<uint4*>(p + 16 * e) = eight_in_a_row(u);
     }
   }
 }
