@@ -800,7 +800,7 @@ bitsmoe_status bitsmoe_mx8_dequantize(const uint8_t* codes_dev, const uint8_t* s
  *   inv_dev       [T] fp32
  * Sum_dev may be X_dev or R_dev where those rows are densely packed.  T may be 0.
  * Shape rules: d % 8 == 0 (MX8: d % 32 == 0), d <= 32768, T d <= 2^40, rows a multiple of 16
- * bytes apart; eps > 0.
+ * bytes apart; eps > 0 (in fp32 too).
  */
 bitsmoe_status bitsmoe_rms_norm(const void* X_dev, bitsmoe_dtype xt, int64_t ldx,
                                 const void* R_dev, int64_t ldr, const void* W_dev,
@@ -818,6 +818,8 @@ int64_t bitsmoe_rms_norm_grad_workspace(int64_t T, int64_t d);
  *   Sum_dev   T rows of d entries of type xt, ldsum entries apart: v
  *   inv_dev   as bitsmoe_rms_norm wrote it
  *   dY_dev    T rows of type xt, lddy apart; dSum_dev likewise, or NULL: 0
+ *   valid_dev [T], or NULL: all rows count.  Of a row whose byte is 0 v, inv and dy are not
+ *             read: its dx is dsum, and it adds nothing to dw
  *   dX_dev    [T][d] of type xt;  dW_dev [d] fp32, or NULL: not wanted
  *   work_dev  work_bytes bytes, contents of no matter, in use until the call's work
  *             on the stream is done (NULL where dW_dev is, or none are needed)
@@ -827,9 +829,9 @@ int64_t bitsmoe_rms_norm_grad_workspace(int64_t T, int64_t d);
 bitsmoe_status bitsmoe_rms_norm_grad(const void* Sum_dev, bitsmoe_dtype xt, int64_t ldsum,
                                      const void* W_dev, bitsmoe_dtype wt, const float* inv_dev,
                                      const void* dY_dev, int64_t lddy, const void* dSum_dev,
-                                     int64_t lddsum, int64_t T, int64_t d, void* dX_dev,
-                                     float* dW_dev, void* work_dev, int64_t work_bytes,
-                                     void* stream);
+                                     int64_t lddsum, const uint8_t* valid_dev, int64_t T,
+                                     int64_t d, void* dX_dev, float* dW_dev, void* work_dev,
+                                     int64_t work_bytes, void* stream);
 
 /*
  * h = silu(g) u of S rows [g; u], and the rows in MX8 for the gradient.
@@ -863,7 +865,8 @@ bitsmoe_status bitsmoe_glu_mx8_grad(const uint8_t* codes_dev, const uint8_t* sca
  *   X_dev        x_rows rows of K entries of type t, ldx entries apart
  *   the others   as bitsmoe_mx4_product
  * S may be 0, and so may x_rows (X_dev is then not read).  Shape rules: K % 8 == 0,
- * ldx >= K, ldx % 8 == 0, ldy >= N, E <= 65535, N and K <= 2^24, S < 2^31 - 256.
+ * ldx >= K, ldx % 8 == 0, ldx < 2^31, ldy >= N, ldy <= 2^32, E <= 65535, N and K <= 2^24,
+ * S < 2^31 - 256, x_rows < 2^31.
  */
 bitsmoe_status bitsmoe_expert_product(const void* W_dev, bitsmoe_dtype t, int64_t E, int64_t N,
                                       int64_t K, const void* X_dev, int64_t x_rows, int64_t ldx,
@@ -875,7 +878,7 @@ bitsmoe_status bitsmoe_expert_product(const void* W_dev, bitsmoe_dtype t, int64_
  * Gradient of the tokens, dx_s = W_e^T dy_s, as bitsmoe_mx4_product_grad.
  *   dY_dev  [S] rows of N entries of type t, lddy entries apart
  *   dX_dev  [S] rows of K entries of type xt, ldx entries apart
- * Shape rules as bitsmoe_expert_product, and N % 8 == 0, lddy % 8 == 0.
+ * Shape rules as bitsmoe_expert_product, and N % 8 == 0, lddy % 8 == 0, lddy < 2^31.
  */
 bitsmoe_status bitsmoe_expert_product_grad(const void* W_dev, bitsmoe_dtype t, int64_t E,
                                            int64_t N, int64_t K, const void* dY_dev, int64_t lddy,

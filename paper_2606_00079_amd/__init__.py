@@ -157,7 +157,7 @@ def lib() -> ctypes.CDLL:
     L.bitsmoe_mx8_dequantize.argtypes = L.bitsmoe_mx4_dequantize.argtypes
     L.bitsmoe_rms_norm.argtypes = [vp, i32, i64, vp, i64, vp, i32, i64, i64, ctypes.c_double] + [vp] * 6
     L.bitsmoe_rms_norm_grad_workspace.argtypes = [i64, i64]
-    L.bitsmoe_rms_norm_grad.argtypes = [vp, i32, i64, vp, i32, vp, vp, i64, vp, i64, i64, i64, vp, vp, vp, i64, vp]
+    L.bitsmoe_rms_norm_grad.argtypes = [vp, i32, i64, vp, i32, vp, vp, i64, vp, i64, vp, i64, i64, vp, vp, vp, i64, vp]
     L.bitsmoe_glu_mx8.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp]
     L.bitsmoe_glu_mx8_grad.argtypes = [vp, vp, vp, i32, i64, i64, i64, vp, vp, vp]
     L.bitsmoe_expert_product.argtypes = [vp, i32, i64, i64, i64, vp, i64, i64, vp, vp, i64, i32, vp, i32, i64, vp]
@@ -919,9 +919,10 @@ def rms_norm(X, weight, residual=None, eps: float = 1e-6, rows: bool = True, mx8
     return Norm(y, inv, total, codes, scales)
 
 
-def rms_norm_grad(sum, weight, inv, dY, dsum=None, dweight: bool = True):
+def rms_norm_grad(sum, weight, inv, dY, dsum=None, dweight: bool = True, valid=None):
     """Gradients of ``rms_norm`` from that of y and (None: 0) of the sum -> (dX [T][d]
-    of the rows' type, for X and the residual alike, and dweight fp32 [d] or None)."""
+    of the rows' type, for X and the residual alike, and dweight fp32 [d] or None).
+    Rows with valid[t] = 0 (bool or uint8) do not count, whatever they hold."""
     torch, stream = _place(sum, "sum")
     if sum.dim() != 2:
         raise ValueError("sum must be [T][d]")
@@ -929,6 +930,9 @@ def rms_norm_grad(sum, weight, inv, dY, dsum=None, dweight: bool = True):
     vp, ldv = _rows(sum, "sum")
     yp, ldy = _like(dY, "dY", sum, sum.shape)
     sp, lds = (None, 0) if dsum is None else _like(dsum, "dsum", sum, sum.shape)
+    if valid is not None and valid.dtype is torch.bool:
+        valid = valid.view(torch.uint8)
+    vap = _in(valid, "valid", sum, torch.uint8, (T,))
     dX = sum.new_empty((T, d))
     L = lib()
     room = L.bitsmoe_rms_norm_grad_workspace(T, d) if dweight else 0
@@ -936,7 +940,7 @@ def rms_norm_grad(sum, weight, inv, dY, dsum=None, dweight: bool = True):
     work = sum.new_empty((room // 4,), dtype=torch.float32) if room else None
     _check(L.bitsmoe_rms_norm_grad(vp, _code(sum, "sum", torch), ldv, _in(weight, "weight", sum, weight.dtype, (d,)),
                                    _code(weight, "weight", torch), _in(inv, "inv", sum, torch.float32, (T,)), yp, ldy,
-                                   sp, lds, T, d, dX.data_ptr(), dw.data_ptr() if dweight else None,
+                                   sp, lds, vap, T, d, dX.data_ptr(), dw.data_ptr() if dweight else None,
                                    work.data_ptr() if room else None, room, stream), "rms_norm_grad")
     return dX, dw
 

@@ -123,6 +123,7 @@ struct NormGradArgs {
   const float* inv;
   const void* dy;
   const void* dsum;  // or null
+  const uint8_t* valid;  // of the rows, or null: all are
   int64_t T, ldv, lddy, ldds;
   int pieces;
   float d;
@@ -152,20 +153,21 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void norm_grad_kernel(
     const char* vp = static_cast<const char*>(a.v) + row * a.ldv * Eight<XB>::kBytes;
     const char* gp = static_cast<const char*>(a.dy) + row * a.lddy * Eight<XB>::kBytes;
     const char* sp = static_cast<const char*>(a.dsum) + row * a.ldds * Eight<XB>::kBytes;
+    const int pieces = a.valid && !a.valid[row] ? 0 : a.pieces;  // (nothing of a row that is not is read but dsum)
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int c = i * L + t;
       r.s[i].clear();
-      if (c < a.pieces) {
+      if (a.dsum && c < a.pieces) r.s[i].load(sp, c);
+      if (c < pieces) {
         r.v[i].load(vp, c);
         r.g[i].load(gp, c);
-        if (a.dsum) r.s[i].load(sp, c);
       } else {
         r.v[i].clear();
         r.g[i].clear();
       }
     }
-    r.inv = a.inv[row];
+    r.inv = pieces ? a.inv[row] : 0.0f;
   };
   constexpr bool kAhead = L < 1024;  // (of the longest rows registers hold but one)
   const int64_t step = int64_t(gridDim.x) * kRows;
@@ -342,7 +344,8 @@ extern "C" bitsmoe_status bitsmoe_rms_norm(const void* X_dev, bitsmoe_dtype xt, 
                                            double eps, void* Sum_dev, void* Y_dev, uint8_t* codes_dev,
                                            uint8_t* scales_dev, float* inv_dev, void* stream) {
   if (bitsmoe_status st = check("rms_norm", xt, wt, T, d)) return st;
-  if (!(eps > 0 && eps < 1e30)) return fail(BITSMOE_ERR_ARG, "rms_norm: eps must be positive");
+  if (!(static_cast<float>(eps) > 0.0f && eps < 1e30))
+    return fail(BITSMOE_ERR_ARG, "rms_norm: eps must be positive, and in fp32 too");
   if (codes_dev && d % kMx8Block != 0) return fail(BITSMOE_ERR_SHAPE, "rms_norm: MX8 needs d % 32 == 0");
   if (bitsmoe_status st = check_stride("rms_norm", xt, d, ldx)) return st;
   if (R_dev)
@@ -371,8 +374,8 @@ extern "C" int64_t bitsmoe_rms_norm_grad_workspace(int64_t T, int64_t d) {
 extern "C" bitsmoe_status bitsmoe_rms_norm_grad(const void* Sum_dev, bitsmoe_dtype xt, int64_t ldsum,
                                                 const void* W_dev, bitsmoe_dtype wt, const float* inv_dev,
                                                 const void* dY_dev, int64_t lddy, const void* dSum_dev,
-                                                int64_t lddsum, int64_t T, int64_t d, void* dX_dev, float* dW_dev,
-                                                void* work_dev, int64_t work_bytes, void* stream) {
+                                                int64_t lddsum, const uint8_t* valid_dev, int64_t T, int64_t d,
+                                                void* dX_dev, float* dW_dev, void* work_dev, int64_t work_bytes, void* stream) {
   if (bitsmoe_status st = check("rms_norm_grad", xt, wt, T, d)) return st;
   if (bitsmoe_status st = check_stride("rms_norm_grad", xt, d, ldsum)) return st;
   if (bitsmoe_status st = check_stride("rms_norm_grad", xt, d, lddy)) return st;
@@ -393,7 +396,7 @@ extern "C" bitsmoe_status bitsmoe_rms_norm_grad(const void* Sum_dev, bitsmoe_dty
   const int groups = grad_groups(T, d);
   if (dW_dev && groups > 1 && (!work_dev || work_bytes < groups * d * 4))
     return fail(BITSMOE_ERR_ARG, "rms_norm_grad: the workspace is missing or too small");
-  const NormGradArgs a{Sum_dev, W_dev, inv_dev, dY_dev, dSum_dev, T, ldsum, lddy, lddsum, static_cast<int>(d / 8),
+  const NormGradArgs a{Sum_dev, W_dev, inv_dev, dY_dev, dSum_dev, valid_dev, T, ldsum, lddy, lddsum, static_cast<int>(d / 8),
                        static_cast<float>(d), dX_dev, dW_dev, groups > 1 ? static_cast<float*>(work_dev) : dW_dev};
   const bool xb = xt == BITSMOE_BF16, wb = wt == BITSMOE_BF16;
   xb ? (wb ? launch_grad<true, true>(a, groups, s) : launch_grad<true, false>(a, groups, s))

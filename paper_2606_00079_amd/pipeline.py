@@ -428,6 +428,7 @@ class BlockSaved:
     sum: object  # bf16 [T][K]: the residual stream, which the caller has too
     inv: object  # fp32 [T]
     layer: ExpertsSaved
+    valid: object = None
 
 
 def moe_block(x, residual, weight, router, experts: Experts, k: int, eps: float = 1e-6, valid=None,
@@ -436,7 +437,8 @@ def moe_block(x, residual, weight, router, experts: Experts, k: int, eps: float 
     (weight [K]), the router's product (bf16 [E][K]; E a multiple of 8 for its
     gradient) and the experts.  x and residual bf16 [T][K] (residual may be None) ->
     (y, the sum that the next block adds y to, Routing), and with ``train`` also
-    what ``moe_block_grad`` reads."""
+    what ``moe_block_grad`` reads.  Rows with valid[t] = 0 do not count, whatever
+    they hold: their y is 0, and no weight's gradient sees them."""
     import torch
     n: Norm = rms_norm(x, weight, residual=residual, eps=eps, mx8=train)
     logits = expert_product(router.unsqueeze(0), n.y, dtype=torch.float32)
@@ -445,7 +447,7 @@ def moe_block(x, residual, weight, router, experts: Experts, k: int, eps: float 
         return y, n.sum, r
     y, r, saved = experts_layer(n.y, logits, experts, k, valid=valid, renorm=renorm, train=True,
                                 kept=(n.codes, n.scales))
-    return y, n.sum, r, BlockSaved(n.sum, n.inv, saved)
+    return y, n.sum, r, BlockSaved(n.sum, n.inv, saved, valid)
 
 
 def moe_block_grad(saved: BlockSaved, weight, router, experts: Experts, dy, dsum=None, dlosses=None, dtype=None):
@@ -455,7 +457,11 @@ def moe_block_grad(saved: BlockSaved, weight, router, experts: Experts, dy, dsum
     import torch
     dn, dlogits, d_up, d_down = experts_layer_grad(saved.layer, experts, dy, dlosses, dtype)
     dl = dlogits.to(torch.bfloat16)
-    d_router = expert_weight_grad_q(dl, *saved.layer.x, dtype=dtype).squeeze(0)
+    rows = None
+    if saved.valid is not None:  # (a row of zeros times one that holds no numbers is none)
+        rows = torch.arange(dl.shape[0], dtype=torch.int32, device=dl.device)
+        rows = torch.where(saved.valid.bool(), rows, -1)
+    d_router = expert_weight_grad_q(dl, *saved.layer.x, rows=rows, dtype=dtype).squeeze(0)
     dn = dn + expert_product_grad(router.unsqueeze(0), dl)
-    dx, dweight = rms_norm_grad(saved.sum, weight, saved.inv, dn, dsum=dsum)
+    dx, dweight = rms_norm_grad(saved.sum, weight, saved.inv, dn, dsum=dsum, valid=saved.valid)
     return dx, dweight, d_router, d_up, d_down

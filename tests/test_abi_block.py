@@ -50,7 +50,7 @@ NORM = dict(X=P, xt=BF16, ldx=64, R=P, ldr=64, W=P, wt=F32, T=4, d=64, eps=1e-6,
 @pytest.mark.parametrize("status,change", [
     (ARG, {"X": None}), (ARG, {"W": None}), (ARG, {"inv": None}), (ARG, {"Sum": None}), (ARG, {"codes": None}),
     (ARG, {"scales": None}), (ARG, {"Y": BAD}), (ARG, {"R": BAD}), (ARG, {"T": -1}), (ARG, {"d": 0}),
-    (ARG, {"eps": 0.0}), (ARG, {"eps": -1.0}), (ARG, {"eps": float("nan")}), (ARG, {"eps": float("inf")}),
+    (ARG, {"eps": 0.0}), (ARG, {"eps": 1e-60}), (ARG, {"eps": -1.0}), (ARG, {"eps": float("nan")}), (ARG, {"eps": float("inf")}),
     (DTYPE, {"xt": 2}), (DTYPE, {"wt": -1}), (SHAPE, {"d": 60, "ldx": 64, "ldr": 64}),
     (SHAPE, {"d": 40}), (SHAPE, {"d": 32800, "ldx": 32800, "ldr": 32800}), (SHAPE, {"ldx": 56}), (SHAPE, {"ldr": 68}),
     (SHAPE, {"T": 1 << 36}),
@@ -59,7 +59,7 @@ def test_rms_norm(lib, status, change):
     refused(lib, status, "bitsmoe_rms_norm", *{**NORM, **change}.values())
 
 
-NORM_GRAD = dict(Sum=P, xt=BF16, ldsum=64, W=P, wt=F32, inv=P, dY=P, lddy=64, dSum=P, lddsum=64, T=40, d=64, dX=P, dW=P,
+NORM_GRAD = dict(Sum=P, xt=BF16, ldsum=64, W=P, wt=F32, inv=P, dY=P, lddy=64, dSum=P, lddsum=64, valid=None, T=40, d=64, dX=P, dW=P,
                  work=P, work_bytes=1 << 30, stream=None)
 
 

@@ -739,3 +739,126 @@ def test_products_give_the_same_every_time(E, N, K, S):
             torch.cuda.synchronize()
         for a, b in zip(all_of_them(), first):
             assert torch.equal(a, b)
+
+
+# ------------------------------------------------------- rows that do not count
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d", [(1, 64), (6, 64), (40, 1032), (9, 4096), (1100, 512), (5, 16416)])
+def test_norm_gradient_of_rows_that_do_not_count(dtype, T, d):
+    """The others' gradients are those of a call with zeros there, whatever the rows hold."""
+    g = np.random.default_rng([T, d, 21])
+    v, dY, ds = (randn(g, T, d, dtype=dtype) for _ in range(3))
+    w, valid = randn(g, d, dtype="f32"), dev(g.random(T) < 0.6)
+    valid[0] = False
+    inv = bm.rms_norm(v, w).inv
+    v0, inv0, dY0 = (torch.where(valid.view(T, *[1] * (t.dim() - 1)), t, 0) for t in (v, inv, dY))
+    bad = [torch.where(valid.view(T, *[1] * (t.dim() - 1)), t, float("nan")) for t in (v, inv, dY)]
+    dX, dw = bm.rms_norm_grad(bad[0], w, bad[1], bad[2], dsum=ds, valid=valid)
+    want, want_w = bm.rms_norm_grad(v0, w, inv0, dY0, dsum=ds)
+    assert torch.equal(dX, want) and torch.equal(dw, want_w) and torch.equal(dX[~valid], ds[~valid])
+    dX, dw = bm.rms_norm_grad(bad[0], w, bad[1], bad[2], valid=valid.view(torch.uint8))
+    assert torch.isfinite(dX).all() and not dX[~valid].any() and torch.equal(dw, want_w)
+
+
+def test_norm_gradient_refuses_other_masks():
+    X, w = torch.zeros((4, 64), device=DEV), torch.ones(64, device=DEV)
+    for mask, error in [(torch.ones(3, dtype=torch.bool, device=DEV), ValueError), (torch.ones(4, device=DEV), TypeError),
+                        (torch.ones(4, dtype=torch.bool), TypeError)]:
+        with pytest.raises(error):
+            bm.rms_norm_grad(X, w, w[:4], X, valid=mask)
+
+
+def test_block_of_a_padded_batch():
+    """NaN in the rows behind the sequences reaches nothing but those rows' sum."""
+    g = np.random.default_rng(15)
+    T, E, k, N, K = 70, 8, 2, 64, 96
+    ex = pipeline.Experts(randn(g, E, 2 * N, K, scale=0.1), randn(g, E, K, N, scale=0.1))
+    x, res, dy, ds = (randn(g, T, K) for _ in range(4))
+    w, router = dev((1 + 0.1 * g.standard_normal(K)).astype(np.float32)), randn(g, E, K, scale=0.1)
+    dl = torch.tensor([0.01, 0.001], device=DEV)
+    valid = dev(np.arange(T) % 35 < 22)
+    out = []
+    for fill in (0.0, float("nan")):
+        xs, rs = (torch.where(valid[:, None], t, fill) for t in (x, res))
+        y, total, r, saved = pipeline.moe_block(xs, rs, w, router, ex, k, valid=valid, train=True)
+        dys = torch.where(valid[:, None], dy, fill)
+        out.append((y, total[valid], r.losses, *pipeline.moe_block_grad(saved, w, router, ex, dys, dsum=ds, dlosses=dl)))
+        y2, _, _ = pipeline.moe_block(xs, rs, w, router, ex, k, valid=valid)
+        out[-1] += (y2,)
+    for a, b in zip(*out):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
+    assert not out[0][0][~valid].any()
+
+
+# ------------------------------------------------------- offsets past 32 bits
+def test_rows_past_32_bits():
+    """Norm, MX8 and gated activation of more than 2^32 bytes and 2^31 entries give the last rows what a call of
+    those rows alone gives."""
+    d, T = 32768, (1 << 17) + 5
+    g = np.random.default_rng(16)
+    tail = randn(g, 7, d)
+    X = torch.zeros((T, d), dtype=torch.bfloat16, device=DEV)
+    X[-7:] = tail
+    w = torch.ones(d, device=DEV)
+    n, m = bm.rms_norm(X, w, residual=X, mx8=True), bm.rms_norm(tail, w, residual=tail, mx8=True)
+    for a, b in zip(n, m):
+        assert torch.equal(a[-7:], b)
+    a, b = (bm.rms_norm_grad(i.sum, w, i.inv, i.y, dsum=i.sum) for i in (n, m))
+    # (the rows before are zeros: their share of dw is 0, the others' is summed in another order)
+    assert torch.equal(a[0][-7:], b[0]) and (a[1] - b[1]).abs().max() <= 16 * U * (m.y.float() ** 2).sum(0).max()
+    del n, a
+    (codes, scales), (c, s) = bm.mx8_quantize(X), bm.mx8_quantize(tail)
+    assert torch.equal(codes[-7:], c) and torch.equal(scales[-7:], s)
+    assert torch.equal(bm.mx8_dequantize(codes, scales)[-7:], bm.mx8_dequantize(c, s))
+    del codes, scales
+    a, b = bm.glu_mx8(X), bm.glu_mx8(tail)
+    for p, q in zip(a, b):
+        assert torch.equal(p[-7:], q)
+    a, b = (bm.glu_mx8_grad(i[1], i[2], i[0]) for i in (a, b))
+    for p, q in zip(a, b):
+        assert torch.equal(p[-7:], q)
+
+
+@pytest.mark.parametrize("S", [3, 150, 600])
+def test_experts_past_32_bits(S):
+    """Weights of more than 2^32 entries: the last expert's results and gradient are those of that expert alone."""
+    E, N, K = 129, 4096, 8192
+    g = np.random.default_rng([17, S])
+    W = torch.zeros((E, N, K), dtype=torch.bfloat16, device=DEV)
+    W[-1] = torch.randn(N, K, device=DEV, generator=torch.Generator(DEV).manual_seed(S)) * 0.02
+    x, dy = randn(g, S, K), randn(g, S, N)
+    off = torch.zeros(E + 1, dtype=torch.int32, device=DEV)
+    off[-1] = S
+    f32 = torch.float32
+    want = x.float() @ W[-1].float().T
+    tol = (K + 8) * U * float(x.float().norm(dim=1).max() * W[-1].float().norm(dim=1).max())
+    assert (bm.expert_product(W, x, offsets=off, dtype=f32) - want).abs().max() <= 2 * tol  # (the library's sum is off too)
+    want = dy.float() @ W[-1].float()
+    tol = (N + 8) * U * float(dy.float().norm(dim=1).max() * W[-1].float().norm(dim=0).max())
+    assert (bm.expert_product_grad(W, dy, offsets=off, dtype=f32) - want).abs().max() <= 2 * tol
+    del W
+    codes, scales = bm.mx8_quantize(x)
+    for got, t in [(bm.expert_weight_grad(dy, x, offsets=off), x),
+                   (bm.expert_weight_grad_q(dy, codes, scales, offsets=off), bm.mx8_dequantize(codes, scales))]:
+        want = (dy.float().T @ t.float())
+        tol = 2 * (S + 8) * U * float(dy.float().norm(dim=0).max() * t.float().norm(dim=0).max())
+        assert ((got[-1].float() - want).abs() <= tol + HALF["bf16"] * (want.abs() + tol)).all()
+        assert not got[:-1].any()
+        del got
+
+
+@pytest.mark.parametrize("S,E", [(2, 2), (90, 1), (1500, 1)])
+def test_token_rows_past_32_bits(S, E):
+    """Rows of tokens nearly 2^31 entries apart: those of a call with the same rows packed."""
+    g = np.random.default_rng([18, S])
+    N, K, ld = 256, 64, (1 << 31) - 8
+    flat = torch.zeros(2 * ld + K, dtype=torch.bfloat16, device=DEV)
+    X = flat.as_strided((3, K), (ld, 1))
+    packed = randn(g, 3, K)
+    X.copy_(packed)
+    W, dy = randn(g, E, N, K, scale=0.1), randn(g, S, N)
+    rows = dev(g.integers(0, 3, S).astype(np.int32))
+    off = dev(np.linspace(0, S, E + 1).astype(np.int32))
+    assert torch.equal(bm.expert_product(W, X, offsets=off, rows=rows), bm.expert_product(W, packed, offsets=off, rows=rows))
+    assert torch.equal(bm.expert_weight_grad(dy, X, offsets=off, rows=rows),
+                       bm.expert_weight_grad(dy, packed, offsets=off, rows=rows))
