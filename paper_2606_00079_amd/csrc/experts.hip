@@ -6,7 +6,11 @@
 //     dW_e = sum over e's slots of dy_s x_row(s)^T     (expert_weight_grad; _q: x in MX8)
 //
 // for S slots, expert e's being offsets[e] .. offsets[e+1].  Sums are fp32 and
-// results are rounded once.
+// results are rounded once; with glu silu(g) u is taken of the fp32 sums.
+//
+// Few slots an expert: bound by the weights' bytes (every byte of W is used S / E times);
+// many: by the matrix cores, whose clock gives way under real data (8192^3 by the
+// library 1.37 to 1.39 PFLOP/s, 1.40 GHz).  Between the two lie a factor of about 270 slots an expert.
 #include <atomic>
 #include <cmath>
 #include <cstdint>
@@ -48,7 +52,10 @@ enum Form { kForward, kTokens, kWeights };
 // 16 outputs x 16 slots a workgroup.  Its eight waves share out K in segments of
 // 64 entries, a cache line of a row: lane l holds chunks l / 16 and 4 + l / 16 of row
 // l % 16, and of slot l % 16.  For the fewest slots: bound by launch and one chain of
-// loads, so the sum is split and the workgroups are small and many.
+// loads, so the sum is split and the workgroups are small and many (8 slots of 128
+// experts, 1536 x 2048: 11.8 us, 50 MB at 4.3 TB/s; 2 slots of 8 experts, 1024 x 4096: 7.6 us,
+// where the large tiles below take 30 to 72).  More slots an expert read the
+// weights again for every 16, which tiles do for every 32 to 256.
 constexpr int kRowWaves = 8;
 template <bool GLU>
 __global__ __launch_bounds__(64 * kRowWaves) void expert_rows_kernel(ExpertArgs a) {
@@ -126,9 +133,24 @@ __global__ __launch_bounds__(64 * kRowWaves) void expert_rows_kernel(ExpertArgs 
 // cache lines of 128 bytes; a step that finds its stage read by every wave refills
 // it at once, across the end of a tile too.
 //
+// 256 x 256 results take 8 waves of 64 x 128, two a SIMD: each fragment of 16 entries
+// that is read feeds two or four ops (a step of 64 entries: 32 ops a wave, beside
+// 24 KB read and 8 KB loaded by it).  Four waves of 128 x 128 read a third less but
+// stood still at every wait, and were slower.  What there is of branches around the
+// ops costs most: without any 8192^3 went from 939 to 827 us (1.33 PFLOP/s; the library
+// 683 to 718 us with the sum along both operands' rows), W^T dy to 832 (785 to 845), dy x^T to 1010 (900
+// to 980).  32 and 128 slots a tile are for experts with fewer (512 slots of 128 experts,
+// 2048 x 768: 71 us in tiles of 32 slots, 403 MB at 5.7 TB/s; 74 and 93 in larger ones).
+//
 // Tokens in MX8 (the weights' gradient) are widened to bf16 on their way: every
 // wave loads the codes of eight slots of a stage for itself, and in the step before
-// that stage's writes what they stand for into one of two tiles, between the ops.
+// that stage's writes what they stand for into one of two tiles, between the ops
+// (8192^3: 1225 to 1290 us, where bf16 tokens take 1010; the MX8 form reads half the bytes, and spares
+// who kept MX8 the 2 bytes an entry that widened tokens would take: 128 experts of 1536 x 2048, 32768 slots 440 us).
+//
+// The weights' gradient has short sums and much to write (there 256 entries and 805 MB of
+// results a call): it is bound by that writing, which does not overlap with the next tile's
+// ops, as loads and stores of a wave are waited for in their order.
 // ---------------------------------------------------------------------------
 template <Form FORM, int MT_, bool MX = false>
 struct Shape {
@@ -152,9 +174,9 @@ struct Shape {
   static_assert(FORM != kWeights || (MT == 256 && NX == 2));
 
   static constexpr int LP = kPStage / 1024 / kWaves, LQ = MX ? 0 : kQStage / 1024 / kWaves, kLoads = LP + LQ;
-  // A stage's loads go out a third at a time.
+  // Loads 0 .. kFirst, .. kSecond and .. kLoads of a stage go out in the third and fourth part of the step that frees
+  // its place and in the first of the next.
   static constexpr int kFirst = (kLoads + 2) / 3, kSecond = kFirst + (kLoads + 1) / 3;
-  static constexpr int kCodeLoads = MX ? kCodes / 1024 + 1 : 0;
 };
 
 // What lanes past an end read.
@@ -268,7 +290,8 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
   }
   if (!more) return;
   get(&cur);
-  auto steps_of = [&](const ResultTile& t) __attribute__((always_inline)) {  // (NX at least, so that the ring never reaches past the next tile)
+  // (NX at least, so that the ring never reaches past the next tile)
+  auto steps_of = [&](const ResultTile& t) __attribute__((always_inline)) {
     const int L = FORM == kForward ? K : FORM == kTokens ? N : t.hi - t.lo;
     return max((L + H::KS - 1) / H::KS, H::NX);
   };
@@ -279,7 +302,8 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
   // (the chunk is the same for all of them, as every wave's rows are eight of 32 or 64 apart)
   auto row_of = [&](int q, int l) __attribute__((always_inline)) { return (wave + H::kWaves * q) * 8 + l / 8; };
   const int chunk = chunk_slot(row_of(0, lane), lane & 7);
-  auto load_rows = [&](const ResultTile& t, int buf) __attribute__((always_inline)) {  // the rows of a tile's slots (past its end: its last)
+  // the rows of a tile's slots (past its end: its last)
+  auto load_rows = [&](const ResultTile& t, int buf) __attribute__((always_inline)) {
     if constexpr (FORM == kForward)
       if (a.rows && wave < H::kRows / 64)
         load_lds4(a.rows + min(t.lo + wave * 64 + lane, t.hi - 1), lds0 + H::oRows + (buf * H::kRows + wave * 64) * 4);
@@ -288,7 +312,9 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
   auto aim = [&](const ResultTile& t, int buf) __attribute__((always_inline)) {
     const int lane = opaque(tid) & 63, r32 = lane & 31, half = lane >> 5;  // (not kept in registers between the tiles)
     if constexpr (FORM == kWeights) {  // two slots a load, 32 chunks each (columns past the end: the last ones)
-      auto col = [&](int first, int q, int end) __attribute__((always_inline)) { return min(first + 8 * (r32 ^ (4 * ((2 * q + half) & 3))), end - 8); };
+      auto col = [&](int first, int q, int end) __attribute__((always_inline)) {
+        return min(first + 8 * (r32 ^ (4 * ((2 * q + half) & 3))), end - 8);
+      };
 #pragma unroll
       for (int q = 0; q < H::LP; ++q)
         pp[q] = reinterpret_cast<const char*>(
@@ -661,8 +687,9 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
     };
     if (H::kTurn && !GLU && whole) {
       // A lane holds pieces of 16 bytes of one row; through LDS eight (16 in fp32: a quarter of the rows at a time, else
-      // half) lanes get those of a row, so that a store writes whole cache lines: 32 bytes of 32 rows a store took as long
-      // again (dW of 128 x 1536 x 2048: kTurnBefore).
+      // half) lanes get those of a row, so that a store writes whole cache lines, not 32 bytes of 32 rows (dW of 128
+      // experts, 1536 x 2048, 32768 slots: 392 to 382 us; 2048 x 768 and 512 slots: 118 to 110).  Stores that pass the
+      // caches by took 1.5 to 3 times as long.
       const int lane = opaque(tid) & 63;
       char* const turn_at = smem + (MX ? H::oTiles + (tile ^ 1) * H::kQStage + wave * 4096 : H::oTurn + wave * 2048);
 #pragma unroll
@@ -763,7 +790,8 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
 // four waves: wave w takes stages w, w + 4, ... of 64 entries through a ring of its
 // own, with no barrier up to the end, where the four sums are joined in LDS in the
 // order of the waves.  For calls of too few large tiles to fill the card: what counts
-// is how fast one workgroup goes through a long sum.
+// is how fast one workgroup goes through a long sum (194 slots of 8 experts, 1024 x 4096: 18.6 us for
+// 67 MB, where the tiles above take 39 to 74; 8 slots of 128 experts, 1536 x 2048, with glu: 12.7).
 struct SplitShape {
   static constexpr int MT = 32, QT = 64, KS = 64, NX = 3, kWaves = 4;
   static constexpr int kPStage = MT * KS * 2, kStage = kPStage + QT * KS * 2, kRing = NX * kStage;
@@ -985,11 +1013,11 @@ bool grid_of(const ExpertArgs& a, int64_t tile, int64_t per, unsigned* grid) {
 //     tiles(m) = max(active, S / m + active / 2),  active = E (1 - exp(-S / E))
 // tiles of m slots (as of slots that choose by chance).  The constants (us; L entries of
 // the sum, `wide` rows of weights or columns of results) fit timings of every kernel at
-// 53 shapes, E 1 .. 238, S / E 0.03 .. 4100, sums of 64 .. 14336 entries: the choice
-// is 3 % off the best kernel on average, where the worst is mostly two to ten times it
-// (194 slots of 8 experts, 1024 x 4096: 38 us by rows, 18.6 split, 44, 51 and 66 in tiles of 32, 128 and 256 slots;
-// 32768 slots of 128 experts, 1536 x 2048: 3112, 949, 562, 317 and 292; 512 slots of 128 experts, 2048 x 768: 140,
-// 119, 71, 72 and 82).
+// 53 shapes in three forms, E 1 .. 238, S / E 0.03 .. 4100, sums of 64 .. 14336 entries: the choice
+// is 3 % off the best kernel on average and 1.76 times it at worst, where the worst kernel is 3.5 times it on average
+// (194 slots of 8 experts, 1024 x 4096: 38 us by rows, 18.6 split, 39, 50 and 74 in tiles of 32, 128 and 256 slots;
+// 32768 slots of 128 experts, 1536 x 2048: 3124, 952, 507, 294 and 287; 512 slots of 128 experts, 2048 x 768: 141,
+// 119, 71, 74 and 93).
 enum Kernel { kByRows, kSplit, kTiles32, kTiles128, kTiles256 };
 
 Kernel product_kernel(const ExpertArgs& a, Form form, int64_t wide, bool glu) {
@@ -1050,7 +1078,7 @@ bitsmoe_status product(const ExpertArgs& a, hipStream_t s) {
 
 int clip(int64_t E) { return static_cast<int>(E < 0x7FFFFFFF ? E : 0x7FFFFFFF); }
 
-// The weights' gradient from its parts' sums, in their order.
+// The weights' gradient from its parts' sums, in their order (bound by bytes: 64 MB of sums 12 us).
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void expert_join_kernel(const float* part, int parts, int64_t n, void* y) {
   for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < n; i += int64_t(gridDim.x) * kThreads) {
@@ -1069,7 +1097,9 @@ __global__ __launch_bounds__(kThreads) void expert_join_kernel(const float* part
 }
 
 // Parts of the weights' gradient's sum: where its tiles are too few to fill the card, as many as do, but of four
-// stages at least, and with at most 64 MB of sums.
+// stages at least, and with at most 64 MB of sums, whose join takes 12 us.  (128 x 2048 of 4096 tokens, a router's:
+// 97 us in one part, 29 in 16; of 32768: 713 and 58; 1024 x 2048 of 16384: 367 and 94; 8 experts of 256 x 512, 8192
+// slots: 31 and 30 in 4.)
 int weight_parts(int64_t E, int64_t N, int64_t K, int64_t S) {
   const int64_t tiles = E * ((N + 255) / 256) * ((K + 255) / 256), cus = device_cus();
   if (tiles * 2 > cus) return 1;

@@ -6,7 +6,9 @@
 // v is rounded to the rows' type before the norm is taken: that is what the next
 // block adds to and what the gradient reads, so the gradient is that of the
 // values used.  A row stays in registers between its reading and its writing, so
-// both directions are bound by memory.
+// both directions are bound by memory.  8192 x 7168 bf16 with the residual: the norm with its
+// MX8 form 97 us (two rows read; sum, y and 1 byte an entry written: 531 MB at 5.4 TB/s), the
+// gradient 118 (three rows read, one written: 470 MB at 4.0) and its join 5; one row of 2048 3.6.
 #include <cstdint>
 #include <string>
 
@@ -49,7 +51,8 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
   return v;
 }
 
-// A row on L threads, PER pieces each.
+// A row on L threads, PER pieces each: a wave where that is enough (1003 x 2048 fp32:
+// 6.2 us), as sums within it need no barrier; else a workgroup.
 template <bool XB, bool WB, int L, int PER>
 __global__ __launch_bounds__(L > kThreads ? L : kThreads) void norm_kernel(NormArgs a) {
   constexpr int kRows = L == 64 ? kThreads / 64 : 1;
@@ -133,8 +136,10 @@ struct NormGradArgs {
 };
 
 // A row on L threads as above; each workgroup takes every gridDim.x-th (group of)
-// row and keeps its columns' sums of dw in registers.  The next row is on its way while
-// this one is summed.
+// row and keeps its columns' sums of dw in registers, so that dy and v are read once for
+// both gradients, in an order that does not change.  The next row is on its way while this one is summed, as a
+// workgroup's rows come one after another (8192 x 7168 bf16, forward and back: 290 to 245 us by that, one barrier a row
+// and the join's loads).
 template <bool XB, bool WB, int L, int PER>
 __global__ __launch_bounds__(L > kThreads ? L : kThreads) void norm_grad_kernel(NormGradArgs a) {
   constexpr int kRows = L == 64 ? kThreads / 64 : 1;
@@ -250,7 +255,8 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void norm_grad_kernel(
 }
 
 // dw from the workgroups' sums: 64 columns a workgroup of sixteen waves, which take
-// every sixteenth row of them.
+// every sixteenth row of them, eight loads at a time (512 rows of 7168: 15 MB, 5 us; there
+// are too few columns to fill the card, so that what counts is one chain of loads).
 constexpr int kJoin = 16;
 __global__ __launch_bounds__(64 * kJoin) void norm_join_kernel(const float* part, int rows, int64_t d, float* dw) {
   __shared__ float sums[kJoin][64];
