@@ -16,7 +16,6 @@
 #include <cstdint>
 #include <string>
 #include <type_traits>
-#include <utility>
 
 #include "internal.hpp"
 #include "mx8.hpp"
@@ -169,6 +168,7 @@ struct Shape {
   // where a wave turns its results into whole rows of its columns (with MX8 its own rows of a widened tile)
   static constexpr int oTurn = oLists + (FORM == kForward ? 3 * kRows * 4 : FORM == kWeights ? kWaves * kLists * 256 : 0);
   static constexpr bool kTurn = MT == 256;
+  static constexpr bool kShort = FORM != kWeights && MT >= 128;
   static constexpr int kBytes = oTurn + (kTurn && !MX ? kWaves * 2048 : 0);
   static_assert(kBytes <= 163840);
   static_assert(FORM != kWeights || (MT == 256 && NX == 2));
@@ -505,7 +505,18 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
   struct Part {
     bf16x8 p[H::MB], q[H::NB];
   };
-  auto prow = [&](int m) __attribute__((always_inline)) { return (wm * H::MB + m) * 32; };
+  struct Ahead {  // a part to be read: the j-th of its stage
+    Part* part;
+    int j;
+  };
+  // A tile of at most MT / 2 slots (an expert's last) goes through steps of its own, in which every wave has half as
+  // many of them: 32768 slots of 128 experts, 1536 x 2048, 277 to 269 us; 16384 219 to 205; 5184 of 223, 360 x 448, 33
+  // to 27; full tiles as before, where a branch around each block's ops took a tenth of their time.  (Each has its sums
+  // to itself: where the two forms' steps met before the results, sums were copied and spilled.)
+  auto is_short = [&](const ResultTile& t) __attribute__((always_inline)) { return H::kShort && t.hi - t.m0 <= MT / 2; };
+  int prow0 = 0;  // this wave's first
+  auto prow = [&](int m) __attribute__((always_inline)) { return prow0 + m * 32; };
+  auto set_rows = [&](const ResultTile& t) __attribute__((always_inline)) { prow0 = wm * (is_short(t) ? H::MB / 2 : H::MB) * 32; };
   const int qrow = wn * 64;
   auto by_rows = [&](const char* st, int row0, int j) __attribute__((always_inline)) {
     const int r = row0 + r32;
@@ -547,16 +558,15 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
         for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
   };
   // The ops of a part, with the reads of the parts of `reads` and `between(m)` after a block's ops.
-  // (What an expert's last slots leave of a tile empty is multiplied all the same: a branch around each block's ops
-  // took a tenth of a full tile's time, and gave 2 % where half of the tiles are part empty.)
-  auto multiply = [&](const Part& f, const char* st, int tile, auto between, auto... reads) __attribute__((always_inline)) {
+  // (Blocks of 32 slots that lie past a tile's end are multiplied all the same.)
+  auto multiply = [&](auto blocks, const Part& f, const char* st, int tile, auto between, auto... reads) __attribute__((always_inline)) {
 #pragma unroll
-    for (int m = 0; m < H::MB; ++m) {
+    for (int m = 0; m < decltype(blocks)::value; ++m) {
 #pragma unroll
       for (int n = 0; n < H::NB; ++n) {
         acc[n][m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.q[n], f.p[m], acc[n][m], 0, 0, 0);
-        if (m == 0 && n == 0) (read_q(*reads.first, reads.second, st, tile), ...);
-        if (n == H::NB - 1) (read_p(*reads.first, m, reads.second, st), ...);
+        if (m == 0 && n == 0) (read_q(*reads.part, reads.j, st, tile), ...);
+        if (n == H::NB - 1) (read_p(*reads.part, m, reads.j, st), ...);
         __builtin_amdgcn_sched_barrier(0);
       }
       between(m);
@@ -602,27 +612,25 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
   else
     wait_loads<(H::NX - 1) * H::kLoads>();
   find_next();
-  clear();
   const char* st = smem;
   int tile = 0;
-  Part f0, f1, f2;
-  // (a tile's first fragments are read whole: the step before it does not know which of its blocks hold results)
+  // (a tile's first fragments: those that the step before it read may be of other rows)
   auto read_first = [&](Part& f, const char* st, int tile) __attribute__((always_inline)) {
     read_q(f, 0, st, tile);
 #pragma unroll
     for (int m = 0; m < H::MB; ++m) read_p(f, m, 0, st);
   };
-  read_first(f0, st, tile);
+  set_rows(cur);
   // Waits for the next stage and the workgroup; N loads are younger than it.  So are the stores of the tile before (they
   // count with the loads), in a tile's first steps: they may go on where this wave made all that there can be.
   constexpr int kStores16 = (GLU ? 1 : H::NB) * H::MB * 2, kStores32 = 2 * kStores16;
   int stored = 0;
   int pending = 0;  // the last third of a stage's loads is to go out yet
-  // Loads [from, to) of a stage, those of the m-th of MB turns.
-  auto loads = [&](int from, int to, int m) __attribute__((always_inline)) {
+  // Loads [from, to) of a stage, those of the m-th of `turns`.
+  auto loads = [&](int from, int to, int m, int turns) __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < H::kLoads; ++k)
-      if (k >= from && k < to && (k - from) * H::MB / (to - from) == m) load(k);
+      if (k >= from && k < to && (k - from) * turns / (to - from) == m) load(k);
   };
   auto wait_step = [&](auto n, bool first) __attribute__((always_inline)) {
     if (!first || !stored)
@@ -632,15 +640,20 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
     else
       wait_loads<decltype(n)::value + kStores16>();
   };
-  for (;;) {
+  // A tile of `blocks` blocks of slots a wave.
+  auto run = [&](auto blocks) __attribute__((always_inline)) {
+    constexpr int kTurns = decltype(blocks)::value;
     const int steps = steps_of(cur);
+    Part f0, f1, f2;
+    clear();
+    read_first(f0, st, tile);
     for (int i = 0; i < steps; ++i) {
       const int last = i + 1 == steps, rest = pending;
       // A stage is read to its end half a step early, and its place loaded again while the other half and the next
       // step's first part are multiplied: all at once the loads would hold up the ops behind them.
-      multiply(f0, st, tile, [&](int m) __attribute__((always_inline)) {
-        if (rest) loads(H::kSecond, H::kLoads, m);
-      }, std::pair{&f1, 1});
+      multiply(blocks, f0, st, tile, [&](int m) __attribute__((always_inline)) {
+        if (rest) loads(H::kSecond, H::kLoads, m, kTurns);
+      }, Ahead{&f1, 1});
       if (rest) loaded();
       if constexpr (MX) {
         // the next stage's codes are there but for what was asked for later, two thirds of P of that stage
@@ -653,13 +666,13 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
           wait_own(std::integral_constant<int, kLater + kStores16>{});
       }
       turn();
-      multiply(f1, st, tile, [&](int m) __attribute__((always_inline)) {
+      multiply(blocks, f1, st, tile, [&](int m) __attribute__((always_inline)) {
         if (MX && m < 2) widen(m, tile ^ 1);
-      }, std::pair{&f0, 2}, std::pair{&f2, 3});
+      }, Ahead{&f0, 2}, Ahead{&f2, 3});
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      multiply(f0, st, tile, [&](int m) __attribute__((always_inline)) {
+      multiply(blocks, f0, st, tile, [&](int m) __attribute__((always_inline)) {
         if (MX && m < 2) widen(2 + m, tile ^ 1);
-        loads(0, H::kFirst, m);
+        loads(0, H::kFirst, m, kTurns);
       });
       // the next stage is whole (but for what was asked for later)
       wait_step(std::integral_constant<int, (H::NX - 2) * H::kLoads + H::kFirst>{}, i < H::NX - 1);
@@ -668,17 +681,17 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
       tile ^= 1;
       st = st + H::kStage == smem + H::oRows ? smem : st + H::kStage;
       // (what is read after a tile's last step is not used; its loads all go out before the results)
-      multiply(f2, st, tile, [&](int m) __attribute__((always_inline)) {
-        loads(H::kFirst, H::kSecond, m);
-        if (last) loads(H::kSecond, H::kLoads, m);
-      }, std::pair{&f0, 0});
+      multiply(blocks, f2, st, tile, [&](int m) __attribute__((always_inline)) {
+        loads(H::kFirst, H::kSecond, m, kTurns);
+        if (last) loads(H::kSecond, H::kLoads, m, kTurns);
+      }, Ahead{&f0, 0});
       pending = !last;
       if (last) loaded();
     }
     const int mend = FORM == kWeights ? N : cur.hi;
     const bool whole = cur.n0 + QTO <= width && a.ldy % 8 == 0;
     const int r32 = opaque(tid) & 31, half = (opaque(tid) & 63) >> 5;
-    if (more) read_first(f0, st, tile);
+    stored = whole && cur.m0 + MT <= mend;
     const int64_t first_row = FORM == kWeights ? (static_cast<int64_t>(cur.part) * a.E + cur.e) * a.N : 0;
     auto exists = [&](int m) __attribute__((always_inline)) {  // the row of a forward result's slot
       if (FORM != kForward || !a.rows) return true;
@@ -693,7 +706,7 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
       const int lane = opaque(tid) & 63;
       char* const turn_at = smem + (MX ? H::oTiles + (tile ^ 1) * H::kQStage + wave * 4096 : H::oTurn + wave * 2048);
 #pragma unroll
-      for (int m = 0; m < H::MB; ++m) {
+      for (int m = 0; m < kTurns; ++m) {
         const bool have = exists(m);
         const int row0 = cur.m0 + prow(m);
         if (a.yf32) {
@@ -757,7 +770,7 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
       }
     } else {
 #pragma unroll
-      for (int m = 0; m < H::MB; ++m) {
+      for (int m = 0; m < kTurns; ++m) {
         const int at = cur.m0 + prow(m) + r32;
         if (at >= mend) continue;
         const bool have = exists(m);
@@ -774,14 +787,23 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
         }
       }
     }
+  };
+  for (;;) {
+    if constexpr (H::kShort) {
+      if (is_short(cur))
+        run(std::integral_constant<int, H::MB / 2>{});
+      else
+        run(std::integral_constant<int, H::MB>{});
+    } else {
+      run(std::integral_constant<int, H::MB>{});
+    }
     if (!more) {
       wait_loads<0>();  // (LDS must not be written after the end)
       return;
     }
-    stored = whole && cur.m0 + MT <= mend;
     cur = next;
+    if (H::kShort) set_rows(cur);
     buf = after(buf);
-    clear();
     find_next();
   }
 }

@@ -862,3 +862,45 @@ def test_token_rows_past_32_bits(S, E):
     assert torch.equal(bm.expert_product(W, X, offsets=off, rows=rows), bm.expert_product(W, packed, offsets=off, rows=rows))
     assert torch.equal(bm.expert_weight_grad(dy, X, offsets=off, rows=rows),
                        bm.expert_weight_grad(dy, packed, offsets=off, rows=rows))
+
+
+# ------------------------------------------------------- tiles that are part empty
+@pytest.mark.parametrize("form", ["product", "glu", "grad"])
+@pytest.mark.parametrize("kernel,wide,L", [("expert_tile_128", 520, 712), ("expert_tile_256", 2056, 136)])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_last_tiles_of_every_length(kernel, wide, L, form, out):
+    """Experts whose slots end right before, at and right behind each part of a tile, full and short tiles in turn."""
+    g = np.random.default_rng([19, wide])
+    counts = np.tile([0, 1, 31, 32, 33, 64, 127, 128, 129, 160, 255, 256, 257, 383, 384, 385, 512, 700, 96, 2], 4)
+    counts[20:] = g.permutation(counts[20:])
+    E, S, head = len(counts), int(counts.sum()) + 5, 3
+    offsets = np.r_[0, np.cumsum(counts)].astype(np.int32) + np.int32(head)
+    rows = g.integers(0, 500, S).astype(np.int32)
+    rows[::41] = 500
+    there = torch.from_numpy(rows < 500).to(DEV)[:, None]
+    o, r = dev(offsets), dev(rows)
+    rand = torch.Generator(DEV).manual_seed(wide)
+    shape = (E, wide, L) if form != "grad" else (E, L, wide)
+    W = (torch.randn(shape, generator=rand, device=DEV) / L ** 0.5).bfloat16()
+    X = torch.randn((S if form == "grad" else 500, L), generator=rand, device=DEV).bfloat16()
+    bm.timing(True, kernel)
+    if form == "grad":
+        got = bm.expert_product_grad(W, X, offsets=o, dtype=DT[out])
+    else:
+        got = bm.expert_product(W, X, offsets=o, rows=r, glu=form == "glu", dtype=DT[out])
+    bm.timing(False)
+    assert bm.kernel_time(kernel)[1] == 1
+    a = X.double() if form == "grad" else X.double()[r.long().clamp(max=499)] * there
+    b = W.double() if form == "grad" else W.double().transpose(1, 2)
+    want = torch.zeros((S, wide), dtype=torch.float64, device=DEV)
+    mag = torch.zeros_like(want)
+    want[head:S - 2] = torch.cat(by_experts(lambda e, s: a[s] @ b[e], offsets, S))
+    mag[head:S - 2] = torch.cat(by_experts(lambda e, s: a[s].abs() @ b[e].abs(), offsets, S))
+    bound = (L + 8) * U * mag
+    if form == "glu":
+        N = wide // 2
+        gate, up, eg, eu = want[:, :N], want[:, N:], bound[:, :N], bound[:, N:]
+        sg = gate * torch.sigmoid(gate)
+        want, bound = sg * up, 1.1 * eg * (up.abs() + eu) + sg.abs() * (eu + 2.0 ** -18 * up.abs())
+    off = (got.double() - want).abs() - (bound + (want.abs() + bound) * HALF[out])
+    assert not (off > 0).any(), (float(off.max()), int((off > 0).sum()))
