@@ -1033,13 +1033,14 @@ bool grid_of(const ExpertArgs& a, int64_t tile, int64_t per, unsigned* grid) {
 // Which kernel takes a product.  The counts of an expert's slots are on the device;
 // the host goes by S and E alone: about
 //     tiles(m) = max(active, S / m + active / 2),  active = E (1 - exp(-S / E))
-// tiles of m slots (as of slots that choose by chance).  The constants (us; L entries of
+// tiles of m slots (as of slots that choose by chance), of which active / 2 hold at most half their slots (all of
+// them do where active experts have as few) and take three tenths less.  The constants (us; L entries of
 // the sum, `wide` rows of weights or columns of results) fit timings of every kernel at
 // 53 shapes in three forms, E 1 .. 238, S / E 0.03 .. 4100, sums of 64 .. 14336 entries: the choice
-// is 3 % off the best kernel on average and 1.76 times it at worst, where the worst kernel is 3.5 times it on average
-// (194 slots of 8 experts, 1024 x 4096: 38 us by rows, 18.6 split, 39, 50 and 74 in tiles of 32, 128 and 256 slots;
-// 32768 slots of 128 experts, 1536 x 2048: 3124, 952, 507, 294 and 287; 512 slots of 128 experts, 2048 x 768: 141,
-// 119, 71, 74 and 93).
+// is 3 % off the best kernel on average and 1.72 times it at worst, where the worst kernel is 3.2 times it on average
+// (194 slots of 8 experts, 1024 x 4096: 38 us by rows, 18.6 split, 39, 41 and 62 in tiles of 32, 128 and 256 slots;
+// 32768 slots of 128 experts, 1536 x 2048: 3136, 953, 503, 280 and 274; 512 slots of 128 experts, 2048 x 768: 141,
+// 119, 71, 72 and 85).
 enum Kernel { kByRows, kSplit, kTiles32, kTiles128, kTiles256 };
 
 Kernel product_kernel(const ExpertArgs& a, Form form, int64_t wide, bool glu) {
@@ -1055,13 +1056,18 @@ Kernel product_kernel(const ExpertArgs& a, Form form, int64_t wide, bool glu) {
     const double share = t / device_cus();
     return 0.5 * (std::ceil(share) + (share > 1.0 ? share : 1.0));
   };
+  auto large = [&](double m, double most, double each) {  // tiles of m slots, some of them short
+    const double t = tiles(m, 256), all = t / static_cast<double>((wide + 255) / 256);
+    const double brief = S > active * m / 2 ? active / 2 / all : 1.0;
+    return rounds(t) * (most + L * each * (1.0 - 0.3 * brief));
+  };
   auto with_bytes = [&](double us, double rate) { return us > bytes / rate ? us : bytes / rate; };
   const double chain = L * 0.001, each = tiles(16, 16) * (L * 5.3e-6 + 0.0023);
   const double cost[5] = {with_bytes(5.6 + (chain > each ? chain : each), 4.6),
                           with_bytes(1.6 + rounds(tiles(32, 64)) * (4.5 + L * 0.0024), 4.2),
                           with_bytes(2.2 + rounds(tiles(32, 256)) * (4.0 + L * 0.0071), 5.0),
-                          with_bytes(rounds(tiles(128, 256)) * (6.3 + L * 0.0116), 5.0),
-                          with_bytes(rounds(tiles(256, 256)) * (7.0 + L * 0.0190), 5.0)};
+                          with_bytes(large(128, 6.3, 0.0116), 5.0),
+                          with_bytes(large(256, 7.0, 0.0190), 5.0)};
   int best = form == kForward ? kByRows : kSplit;  // (there is no kernel by rows for W by its rows)
   for (int k = best + 1; k <= kTiles256; ++k)
     if (cost[k] < cost[best]) best = k;
