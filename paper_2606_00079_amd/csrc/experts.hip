@@ -223,8 +223,11 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
       t->hi = min(t->lo + each, t->hi);
     }
     t->part = part;
-    t->m0 = static_cast<int>(in / kt) * MT;
-    t->n0 = static_cast<int>(in % kt) * H::QT;
+    // (in groups of up to eight rows of tiles, column by column: what an XCD works on at a time shares both operands)
+    const int group = static_cast<int>(in / (8 * kt)), rest = static_cast<int>(in - group * 8 * kt);
+    const int high = min(8, static_cast<int>(nt) - 8 * group);
+    t->m0 = (8 * group + rest % high) * MT;
+    t->n0 = rest / high * H::QT;
   };
   auto slot_tile = [&](ResultTile* t) __attribute__((always_inline)) {
     Tile s;
