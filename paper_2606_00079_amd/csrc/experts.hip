@@ -137,19 +137,21 @@ __global__ __launch_bounds__(64 * kRowWaves) void expert_rows_kernel(ExpertArgs 
 // 24 KB read and 8 KB loaded by it).  Four waves of 128 x 128 read a third less but
 // stood still at every wait, and were slower.  What there is of branches around the
 // ops costs most: without any 8192^3 went from 939 to 827 us (1.33 PFLOP/s; the library
-// 683 to 718 us with the sum along both operands' rows), W^T dy to 832 (785 to 845), dy x^T to 1010 (900
+// 683 to 718 us with the sum along both operands' rows), W^T dy to 832 (785 to 845); dy x^T takes 957 (900
 // to 980).  32 and 128 slots a tile are for experts with fewer (512 slots of 128 experts,
 // 2048 x 768: 71 us in tiles of 32 slots, 403 MB at 5.7 TB/s; 74 and 93 in larger ones).
 //
 // Tokens in MX8 (the weights' gradient) are widened to bf16 on their way: every
 // wave loads the codes of eight slots of a stage for itself, and in the step before
 // that stage's writes what they stand for into one of two tiles, between the ops
-// (8192^3: 1225 to 1290 us, where bf16 tokens take 1010; the MX8 form reads half the bytes, and spares
-// who kept MX8 the 2 bytes an entry that widened tokens would take: 128 experts of 1536 x 2048, 32768 slots 440 us).
+// (8192^3: 1220 us, where bf16 tokens take 957; the MX8 form reads half the bytes, and spares who
+// kept MX8 the 2 bytes an entry that widened tokens would take: 128 experts of 1536 x 2048, 32768 slots 409
+// and 372 us).
 //
 // The weights' gradient has short sums and much to write (there 256 entries and 805 MB of
 // results a call): it is bound by that writing, which does not overlap with the next tile's
-// ops, as loads and stores of a wave are waited for in their order.
+// ops, as loads and stores of a wave are waited for in their order.  (Two workgroups of 128 x 256 results a compute
+// unit with stages of 32 entries overlap them, but go through a sum a third slower: 470 us, 8192^3 1367.)
 // ---------------------------------------------------------------------------
 template <Form FORM, int MT_, bool MX = false>
 struct Shape {
@@ -223,7 +225,9 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
       t->hi = min(t->lo + each, t->hi);
     }
     t->part = part;
-    // (in groups of up to eight rows of tiles, column by column: what an XCD works on at a time shares both operands)
+    // In groups of up to eight rows of tiles, column by column, so that what an XCD works on at a time shares both
+    // operands (128 experts of 1536 x 2048, 32768 slots: 395 us row by row, 397, 382, 372 and 372 in groups of 2, 4, 8
+    // and 16 rows; 8192^3 1011, 982, 967, 957 and 975).
     const int group = static_cast<int>(in / (8 * kt)), rest = static_cast<int>(in - group * 8 * kt);
     const int high = min(8, static_cast<int>(nt) - 8 * group);
     t->m0 = (8 * group + rest % high) * MT;
