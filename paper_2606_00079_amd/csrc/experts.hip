@@ -209,11 +209,19 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
   ResultTile cur, next;
   int64_t l = 0, end = 0, step_l = 0;  // (weights)
   int more;
-  auto weight_tile = [&](int64_t l, ResultTile* t) __attribute__((always_inline)) {
-    const int64_t nt = (a.N + MT - 1) / MT, kt = (a.K + H::QT - 1) / H::QT;
-    const int64_t per = nt * kt * a.parts;
-    const int e = static_cast<int>(l / per), part = static_cast<int>((l - e * per) % a.parts);
-    const int64_t in = (l - e * per) / a.parts;
+  // (weights) a tile is the `in`th of expert e's; 64-bit divisions for every tile would take as long as one of its steps
+  const uint32_t kt = static_cast<uint32_t>((a.K + H::QT - 1) / H::QT), nt = static_cast<uint32_t>((a.N + MT - 1) / MT);
+  const uint32_t per = nt * kt * static_cast<uint32_t>(a.parts);  // (below 2^31)
+  int at_e = 0;
+  uint32_t at_in = 0;
+  auto weight_tile = [&](ResultTile* t) __attribute__((always_inline)) {
+    const int e = at_e;
+    uint32_t in = at_in;
+    int part = 0;
+    if (a.parts > 1) {
+      part = static_cast<int>(in % a.parts);
+      in /= a.parts;
+    }
     const auto* off = (const __attribute__((address_space(4))) int32_t*)reinterpret_cast<uintptr_t>(a.offsets);
     const int S = static_cast<int>(a.S);
     t->e = e;
@@ -228,10 +236,9 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
     // In groups of up to eight rows of tiles, column by column, so that what an XCD works on at a time shares both
     // operands (128 experts of 1536 x 2048, 32768 slots: 395 us row by row, 397, 382, 372 and 372 in groups of 2, 4, 8
     // and 16 rows; 8192^3 1011, 982, 967, 957 and 975).
-    const int group = static_cast<int>(in / (8 * kt)), rest = static_cast<int>(in - group * 8 * kt);
-    const int high = min(8, static_cast<int>(nt) - 8 * group);
-    t->m0 = (8 * group + rest % high) * MT;
-    t->n0 = rest / high * H::QT;
+    const uint32_t group = in / (8 * kt), rest = in - group * 8 * kt, high = min(8u, nt - 8 * group), col = rest / high;
+    t->m0 = static_cast<int>(8 * group + rest - col * high) * MT;
+    t->n0 = static_cast<int>(col) * H::QT;
   };
   auto slot_tile = [&](ResultTile* t) __attribute__((always_inline)) {
     Tile s;
@@ -242,16 +249,18 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
     t->m0 = s.lo;
     t->n0 = s.col * QTO;
   };
-  auto get = [&](ResultTile* t) __attribute__((always_inline)) {
-    if constexpr (FORM == kWeights)
-      weight_tile(l, t);
-    else
-      slot_tile(t);
+  ResultTile later;  // (weights) the one after next
+  auto find_later = [&]() __attribute__((always_inline)) {
+    at_in += static_cast<uint32_t>(step_l);
+    while (at_in >= per) {
+      at_in -= per;
+      ++at_e;
+    }
+    weight_tile(&later);
   };
   if constexpr (FORM == kWeights) {
     // Each XCD gets an eighth of the work: an expert's tiles cost its steps, and the writing of results about as much as
     // four steps (fp32: eight).
-    const int64_t per = (a.N + MT - 1) / MT * ((a.K + H::QT - 1) / H::QT) * a.parts;
     const int runs = (a.E + 63) / 64;  // experts a lane
     auto cost = [&](int e) __attribute__((always_inline)) {
       int lo;
@@ -262,25 +271,27 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
     for (int i = 0; i < runs; ++i)
       if (lane * runs + i < a.E) own += cost(lane * runs + i);
     const int sum = wave_scan(own);
-    const int64_t total = lane_value(sum, 63) * per;
+    const int64_t total = static_cast<int64_t>(lane_value(sum, 63)) * per;
     auto border = [&](int x) __attribute__((always_inline)) {  // first tile whose cost begins at x eighths or after
       const int64_t target = total * x / 8;
-      const uint64_t past = __ballot(sum * per > target);
-      if (!past) return a.E * per;
+      const uint64_t past = __ballot(static_cast<int64_t>(sum) * per > target);
+      if (!past) return static_cast<int64_t>(a.E) * per;
       const int run = __builtin_ctzll(past);
       int e = run * runs, c = cost(e);
       int64_t before = static_cast<int64_t>(lane_value(sum, run) - lane_value(own, run)) * per;
-      while (before + c * per <= target) {
-        before += c * per;
+      while (before + static_cast<int64_t>(c) * per <= target) {
+        before += static_cast<int64_t>(c) * per;
         c = cost(++e);
       }
-      return e * per + (target - before + c - 1) / c;
+      return static_cast<int64_t>(e) * per + (target - before + c - 1) / c;
     };
     l = border(blockIdx.x & 7);
     end = border((blockIdx.x & 7) + 1);
     step_l = gridDim.x >> 3;
     l += blockIdx.x >> 3;
     more = l < end;
+    at_e = static_cast<int>(l / per);
+    at_in = static_cast<uint32_t>(l - static_cast<int64_t>(at_e) * per);
   } else {
     int head, none;
     more = walk.start(a.offsets, a.E, a.S, static_cast<int>((width + QTO - 1) / QTO), MT, &head, &none);
@@ -296,7 +307,12 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
     }
   }
   if (!more) return;
-  get(&cur);
+  if constexpr (FORM == kWeights) {
+    weight_tile(&cur);
+    if (l + step_l < end) find_later();
+  } else {
+    slot_tile(&cur);
+  }
   // (NX at least, so that the ring never reaches past the next tile)
   auto steps_of = [&](const ResultTile& t) __attribute__((always_inline)) {
     const int L = FORM == kForward ? K : FORM == kTokens ? N : t.hi - t.lo;
@@ -468,14 +484,15 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
       more = walk.find();
     }
     if (more) {
-      get(&next);
-      load_rows(next, after(buf));
       if constexpr (FORM == kWeights) {
-        if (a.rows && l + step_l < end) {  // the list of the tile after it
-          ResultTile t;
-          weight_tile(l + step_l, &t);
-          ask_rows(t, 0, after(after(head)));
+        next = later;
+        if (l + step_l < end) {
+          find_later();
+          if (a.rows) ask_rows(later, 0, after(after(head)));
         }
+      } else {
+        slot_tile(&next);
+        load_rows(next, after(buf));
       }
     }
     since = 0;
@@ -590,11 +607,7 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
   if constexpr (FORM == kWeights) {
     if (a.rows) {
       ask_rows(cur, 0, 0);
-      if (l + step_l < end) {
-        ResultTile t;
-        weight_tile(l + step_l, &t);
-        ask_rows(t, 0, 1);
-      }
+      if (l + step_l < end) ask_rows(later, 0, 1);
       if (8 < steps_to) ask_rows(cur, 1, 4);
     }
     wait_own(std::integral_constant<int, 0>{});
@@ -1145,7 +1158,7 @@ int weight_parts(int64_t E, int64_t N, int64_t K, int64_t S) {
 
 bitsmoe_status weight_grad(const char* who, ExpertArgs a, void* work, int64_t work_bytes, hipStream_t s) {
   const int64_t tiles_ = (a.N + 255) / 256 * ((a.K + 255) / 256);
-  if (tiles_ > (int64_t(1) << 40) / a.E) return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": too many weights");
+  if (tiles_ > (int64_t(1) << 30) || tiles_ > (int64_t(1) << 40) / a.E) return fail(BITSMOE_ERR_SHAPE, std::string(who) + ": too many weights");
   if (!aligned16({work}))
     return fail(BITSMOE_ERR_ARG, std::string(who) + ": device pointers must be 16-byte aligned");
   const int parts = work ? weight_parts(a.E, a.N, a.K, a.S) : 1;

@@ -85,6 +85,11 @@ __device__ __forceinline__ bool find_tile(const int32_t* offsets, int E, int64_t
   }
 }
 
+// (A 64-bit division takes as long as a step of a tile's sum; only calls of more than 2^32 tiles need one.)
+__device__ __forceinline__ int64_t quotient(int64_t a, uint32_t b) {
+  return a >> 32 ? a / static_cast<int64_t>(b) : static_cast<int64_t>(static_cast<uint32_t>(a) / b);
+}
+
 // The same order of tiles for a workgroup that stays and takes one tile after
 // another (without those of no expert): it goes on from expert to expert with
 // scalar loads, which do not touch the count of its vector loads.
@@ -101,7 +106,7 @@ struct Walk {
   // to the expert of tile l; false if there is none
   __device__ __forceinline__ bool find() {
     if (l >= end) return false;
-    const int g = static_cast<int>(l / cols);
+    const int g = static_cast<int>(quotient(l, static_cast<uint32_t>(cols)));
     while (g >= before + tiles()) {
       before += tiles();
       ++e;
@@ -111,7 +116,7 @@ struct Walk {
   }
   __device__ __forceinline__ void get(Tile* out) const {
     const int64_t in = l - static_cast<int64_t>(before) * cols;
-    const int group = static_cast<int>(in / (8 * static_cast<int64_t>(cols)));
+    const int group = static_cast<int>(quotient(in, 8u * static_cast<uint32_t>(cols)));
     const int rest = static_cast<int>(in - group * 8 * static_cast<int64_t>(cols));
     const int high = min(8, tiles() - 8 * group), row = 8 * group + rest % high;
     out->e = e;
