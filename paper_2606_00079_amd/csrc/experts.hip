@@ -145,8 +145,8 @@ __global__ __launch_bounds__(64 * kRowWaves) void expert_rows_kernel(ExpertArgs 
 // wave loads the codes of eight slots of a stage for itself, and in the step before
 // that stage's writes what they stand for into one of two tiles, between the ops
 // (8192^3: 1220 us, where bf16 tokens take 957; the MX8 form reads half the bytes, and spares who
-// kept MX8 the 2 bytes an entry that widened tokens would take: 128 experts of 1536 x 2048, 32768 slots 409
-// and 372 us).
+// kept MX8 the 2 bytes an entry that widened tokens would take: 128 experts of 1536 x 2048, 32768 slots 399
+// and 342 us).
 //
 // The weights' gradient has short sums and much to write (there 256 entries and 805 MB of
 // results a call): it is bound by that writing, which does not overlap with the next tile's
