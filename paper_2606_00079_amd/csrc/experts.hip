@@ -20,6 +20,7 @@
 #include "internal.hpp"
 #include "mx8.hpp"
 #include "rows.hpp"
+#include "slot_range.hpp"
 #include "slots.hpp"
 
 namespace bitsmoe {
@@ -227,11 +228,7 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
     t->e = e;
     t->lo = off ? min(max(off[e], 0), S) : 0;
     t->hi = off ? min(max(off[e + 1], t->lo), S) : S;
-    if (a.parts > 1) {
-      const int each = ((t->hi - t->lo + H::KS - 1) / H::KS + a.parts - 1) / a.parts * H::KS;
-      t->lo = min(t->lo + part * each, t->hi);
-      t->hi = min(t->lo + each, t->hi);
-    }
+    if (a.parts > 1) take_part(&t->lo, &t->hi, part, a.parts, H::KS);
     t->part = part;
     // In groups of up to eight rows of tiles, column by column, so that what an XCD works on at a time shares both
     // operands (128 experts of 1536 x 2048, 32768 slots: 395 us row by row, 397, 382, 372 and 372 in groups of 2, 4, 8
