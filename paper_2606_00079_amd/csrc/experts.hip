@@ -385,8 +385,8 @@ __global__ __launch_bounds__(MT == 32 ? 256 : 512, MT == 32 ? 1 : 2) void expert
   auto list_at = [&](int at) __attribute__((always_inline)) { return H::oLists + (wave * H::kLists + at) * 256; };
   auto ask_rows = [&](const ResultTile& t, int chunk, int at) __attribute__((always_inline)) {
     const int lane = opaque(tid) & 63;
-    const int s = t.lo + (chunk * 8 + lane / 8) * H::KS + wave * 8 + lane % 8;
-    load_lds4(s < t.hi ? a.rows + s : &kNoRow, lds0 + list_at(at));
+    const int s = slot_ahead(t.lo, t.hi, static_cast<unsigned>(chunk * 8 + lane / 8) * H::KS + wave * 8 + lane % 8);
+    load_lds4(s >= 0 ? a.rows + s : &kNoRow, lds0 + list_at(at));
   };
   auto row_of_slot = [&](int slot) __attribute__((always_inline)) {  // (of this wave's eight)
     const int s = ld.lo + step * H::KS + wave * 8 + slot;
@@ -1019,7 +1019,7 @@ bitsmoe_status check(const char* who, const ExpertArgs& a, bitsmoe_dtype t, bits
   if (a.E <= 0 || a.N <= 0 || a.K <= 0 || a.S < 0 || a.x_rows < 0) return bad(BITSMOE_ERR_ARG, ": non-positive size");
   if (t != BITSMOE_BF16) return bad(BITSMOE_ERR_DTYPE, ": weights and rows must be bf16");
   if (yt != BITSMOE_F32 && yt != BITSMOE_BF16) return bad(BITSMOE_ERR_DTYPE, ": results are fp32 or bf16");
-  // (slots are ints, and the end of a tile that begins at one is too)
+  // (slots are ints, and so is what lies a tile behind one; farther ahead only slot_range.hpp's rules look)
   if (a.K % 8 != 0 || a.K > (1 << 24) || a.N > (1 << 24) || a.E > 65535 || a.S > 0x7FFFFFFF - kLargestTile ||
       a.x_rows > 0x7FFFFFFF)
     return bad(BITSMOE_ERR_SHAPE, ": needs K % 8 == 0, K and N <= 2^24, E <= 65535, S < 2^31 - 256 and rows < 2^31");

@@ -31,3 +31,13 @@ def check(tmp_path_factory):
 @pytest.mark.parametrize("parts", [1, 2, 3, 7, 32, 64, 100, 255, 256, 304])
 def test_parts_cover_an_experts_slots(check, lo, hi, parts):
     assert check(lo, hi, parts, 64) == ["1"]
+
+
+@pytest.mark.parametrize("lo,hi", [(0, 0), (0, 1), (7, 7), (3, 70), (1, 100001), (MOST, MOST), (MOST - 1, MOST),
+                                   (MOST - 700, MOST - 254), (12345, MOST), (0, MOST)])
+def test_slots_asked_for_ahead(check, lo, hi):
+    """Eight stages of 64 slots at once, from every eighth stage that has a slot on: the first and last of them, and
+    those around the expert's end."""
+    last = max(0, hi - lo - 1) // 512 * 512
+    for ahead in sorted({0, 1, 511, last, last + 1, last + 511, max(0, hi - lo - 1), hi - lo, min(hi - lo + 1, last + 511)}):
+        assert check(lo, hi, ahead) == [str(lo + ahead if lo + ahead < hi else -1)], ahead
