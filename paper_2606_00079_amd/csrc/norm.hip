@@ -153,6 +153,7 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void norm_grad_kernel(
   struct Row {
     RawEight<XB> v[PER], g[PER], s[PER];
     float inv;
+    bool counts;
   };
   auto load = [&](Row& r, int64_t row) {
     const char* vp = static_cast<const char*>(a.v) + row * a.ldv * Eight<XB>::kBytes;
@@ -172,7 +173,8 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void norm_grad_kernel(
         r.g[i].clear();
       }
     }
-    r.inv = pieces ? a.inv[row] : 0.0f;
+    r.counts = pieces != 0;
+    r.inv = r.counts ? a.inv[row] : 0.0f;
   };
   constexpr bool kAhead = L < 1024;  // (of the longest rows registers hold but one)
   const int64_t step = int64_t(gridDim.x) * kRows;
@@ -215,10 +217,13 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void norm_grad_kernel(
       Eight<WB> w;
       w.load(a.w, c);
       Eight<XB> dx;
+      // (a row that does not count is zeros here, and zeros times weights that are no numbers are NaN; the select costs 1
+      // to 3 % at 8192 x 7168 bf16, a branch in its place 17 %)
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        const float n = cur.v[i].value(q) * cur.inv;
-        dx.v[q] = cur.inv * (cur.g[i].value(q) * w.v[q] - n * dot) + cur.s[i].value(q);
+        const float n = cur.v[i].value(q) * cur.inv, ds = cur.s[i].value(q);
+        const float from_y = cur.inv * (cur.g[i].value(q) * w.v[q] - n * dot);
+        dx.v[q] = cur.counts ? from_y + ds : ds;
       }
       dx.store(a.dx, row * a.pieces + c);
     }
