@@ -393,6 +393,8 @@ def experts_layer(x, logits, experts: Experts, k: int, valid=None, renorm: bool 
     [T][K], Routing), and with ``train`` also what ``experts_layer_grad`` reads.
     kept: x in MX8 as (codes, scales), where the caller has it (``rms_norm``)."""
     import torch
+    if logits.shape[:1] != x.shape[:1]:
+        raise ValueError("x and logits disagree on T")
     if kept is not None and kept[0].shape != x.shape:
         raise ValueError("kept must be x in MX8: codes of x's shape")
     r = route(logits, k, valid=valid, renorm=renorm)

@@ -23,3 +23,11 @@ def test_kept_tokens_of_another_shape(rows, cols):
     kept = (torch.zeros((rows, cols), dtype=torch.uint8), torch.zeros((rows, cols // 32), dtype=torch.uint8))
     with pytest.raises(ValueError, match="kept"):
         layer(kept=kept)
+
+
+@pytest.mark.parametrize("train", [False, True])
+@pytest.mark.parametrize("x_rows,logit_rows", [(T, T - 1), (T, T + 1), (T, 0), (0, T)])
+def test_logits_of_other_rows(x_rows, logit_rows, train):
+    """Slots of rows that are not there would give zeros without a word."""
+    with pytest.raises(ValueError, match="logits"):
+        layer(x_rows, logit_rows, train=train)
