@@ -10,7 +10,7 @@
 //
 // Few slots an expert: bound by the weights' bytes (every byte of W is used S / E times);
 // many: by the matrix cores, whose clock gives way under real data (8192^3 by the
-// library 1.37 to 1.39 PFLOP/s, 1.40 GHz).  Between the two lie a factor of about 270 slots an expert.
+// library 1.53 to 1.61 PFLOP/s).  Between the two lie a factor of about 320 slots an expert.
 #include <atomic>
 #include <cmath>
 #include <cstdint>
@@ -138,16 +138,16 @@ __global__ __launch_bounds__(64 * kRowWaves) void expert_rows_kernel(ExpertArgs 
 // 24 KB read and 8 KB loaded by it).  Four waves of 128 x 128 read a third less but
 // stood still at every wait, and were slower.  What there is of branches around the
 // ops costs most: without any 8192^3 went from 939 to 827 us (1.33 PFLOP/s; the library
-// 683 to 718 us with the sum along both operands' rows), W^T dy to 832 (785 to 845); dy x^T takes 957 (900
+// 682 to 718 us with the sum along both operands' rows), W^T dy to 832 (785 to 845); dy x^T takes 938 to 957 (900
 // to 980).  32 and 128 slots a tile are for experts with fewer (512 slots of 128 experts,
 // 2048 x 768: 71 us in tiles of 32 slots, 403 MB at 5.7 TB/s; 74 and 93 in larger ones).
 //
 // Tokens in MX8 (the weights' gradient) are widened to bf16 on their way: every
 // wave loads the codes of eight slots of a stage for itself, and in the step before
 // that stage's writes what they stand for into one of two tiles, between the ops
-// (8192^3: 1220 us, where bf16 tokens take 957; the MX8 form reads half the bytes, and spares who
-// kept MX8 the 2 bytes an entry that widened tokens would take: 128 experts of 1536 x 2048, 32768 slots 399
-// and 342 us).
+// (8192^3: 1202 us, where bf16 tokens take 946; 128 experts of 1536 x 2048, 32768 slots 403 and 343).
+// An entry is widened again for every tile that reads it, so what this spares who kept MX8 is the 2 bytes an entry
+// that widened tokens would take, not time: mx8_dequantize and the bf16 form after it take 967 and 348 us there.
 //
 // The weights' gradient has short sums and much to write (there 256 entries and 805 MB of
 // results a call): it is bound by that writing, which does not overlap with the next tile's
@@ -1053,8 +1053,9 @@ bool grid_of(const ExpertArgs& a, int64_t tile, int64_t per, unsigned* grid) {
 // tiles of m slots (as of slots that choose by chance), of which active / 2 hold at most half their slots (all of
 // them do where active experts have as few) and take three tenths less.  The constants (us; L entries of
 // the sum, `wide` rows of weights or columns of results) fit timings of every kernel at
-// 53 shapes in three forms, E 1 .. 238, S / E 0.03 .. 4100, sums of 64 .. 14336 entries: the choice
-// is 3 % off the best kernel on average and 1.72 times it at worst, where the worst kernel is 3.2 times it on average
+// 53 shapes in three forms, E 1 .. 238, S / E 0.03 .. 4100, sums of 64 .. 14336 entries: there the choice
+// is 3 % off the best kernel on average and 1.72 times it at worst, where the worst kernel is 3.2 times it on average;
+// at 54 other shapes, timed afterwards, 2 % off and 1.41 times it at worst
 // (194 slots of 8 experts, 1024 x 4096: 38 us by rows, 18.6 split, 39, 41 and 62 in tiles of 32, 128 and 256 slots;
 // 32768 slots of 128 experts, 1536 x 2048: 3136, 953, 503, 280 and 274; 512 slots of 128 experts, 2048 x 768: 141,
 // 119, 71, 72 and 85).

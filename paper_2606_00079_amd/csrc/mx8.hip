@@ -5,13 +5,13 @@
 //     s = 1 / (1 + exp(-g')), of the values g', u' kept         (glu_mx8_grad)
 //
 // All are bound by memory: eight entries a lane (of g and of u), four lanes a
-// block, whose maximum takes two lane exchanges.  8192 x 7168 from MX8 to bf16: 29 us (6.2
-// TB/s; what a norm wrote just before is partly in the last-level cache).  4096 rows of 2 x
+// block, whose maximum takes two lane exchanges.  8192 x 7168 from bf16 to MX8 30 us (6.0 TB/s), 32768 x 2048 33 us, from
+// MX8 to bf16 29 us (6.2 TB/s; what was written just before is partly in the last-level cache).  4096 rows of 2 x
 // 14336, bf16: 93 us (473 MB at 5.1 TB/s), the gradient with h again 104 (592 MB at 5.7); 184
 // rows of 2 x 768 fp32: 3 us each way.
 //
 // The gradient takes g' and u' as kept, so that it is that of the function at values
-// that are off by 2^-4 at most; h' again costs one more store here, where keeping h
+// that are off by 2^-4 of themselves at most, or by 2^-10 of their block's scale; h' again costs one more store here, where keeping h
 // would cost 2 bytes an entry for the whole step.
 #include <cstdint>
 #include <string>

@@ -8,7 +8,7 @@
 // values used.  A row stays in registers between its reading and its writing, so
 // both directions are bound by memory.  8192 x 7168 bf16 with the residual: the norm with its
 // MX8 form 97 us (two rows read; sum, y and 1 byte an entry written: 531 MB at 5.4 TB/s), the
-// gradient 118 (three rows read, one written: 470 MB at 4.0) and its join 5; one row of 2048 3.6.
+// gradient 119 (three rows read, one written: 470 MB at 3.9) and its join 5; one row of 2048 3.9.
 #include <cstdint>
 #include <string>
 

@@ -457,7 +457,9 @@ def moe_block(x, residual, weight, router, experts: Experts, k: int, eps: float 
 def moe_block_grad(saved: BlockSaved, weight, router, experts: Experts, dy, dsum=None, dlosses=None, dtype=None):
     """Gradients of ``moe_block`` from those of y and of the sum (bf16 [T][K]) and of
     the two losses: (dx, which is the residual's too, dweight fp32 [K], d_router,
-    d_up, d_down), the last three in bf16 unless ``dtype`` says fp32."""
+    d_up, d_down), the last three in bf16 unless ``dtype`` says fp32.  (The norm's
+    gradient takes bf16 rows: the experts' and the router's part of the normed rows'
+    gradient are rounded to it each, and so is their sum.)"""
     import torch
     dn, dlogits, d_up, d_down = experts_layer_grad(saved.layer, experts, dy, dlosses, dtype)
     dl = dlogits.to(torch.bfloat16)
